@@ -460,6 +460,100 @@ int32_t treemodel_update(eck_trees *trees, const void *feat, int32_t feat_dtype,
                          const float *energy_measured, uint64_t n_pairs, int32_t n_rounds, float eta, float lambda,
                          float *snr_out, float *loss_out, void *ws, uint64_t ws_bytes, void *stream);
 
+/* --------------------------------------- operators of gated cost models
+ *
+ * What a deeper cost model over the same candidates is made of: residual
+ * blocks  x <- x + dropout(feedforward(layernorm(x)))  on rows of activations.
+ * A matrix of activations is row-major: row i of an [n][ld] array, ld >= width
+ * elements apart, is candidate i.  Elements are ECK_F32 or ECK_BF16; sums,
+ * statistics and products accumulate in fp32, results are rounded once.
+ * Pointers are aligned to their elements, nothing more is asked for (rows that
+ * start on 16 bytes are fastest); workspaces start on 256 bytes.  Nothing
+ * depends on the order of execution: equal calls give equal bits. */
+
+#define ECK_ROWS 0    /* x is an [n][ld] matrix of activations */
+#define ECK_COLUMNS 1 /* x is a [width][ld] matrix with a candidate per column, as features_compute writes it */
+
+#define ECK_ACT_SILU 0 /* a(g) = g / (1 + exp(-g)) */
+#define ECK_ACT_GELU 1 /* a(g) = g (1 + erf(g / sqrt 2)) / 2 */
+#define ECK_ACT_RELU 2 /* a(g) = max(g, 0); derivative 0 at g = 0 */
+
+/* Layer norm of every candidate's `width` values:
+ *   mean = sum x / width,  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps),
+ *   y = (x - mean) rstd gamma + beta.
+ *   x: device, of dtype, in x_order; gamma, beta: device float [width], NULL
+ *   reads as ones and zeros; y: device [n][ld_y] of dtype;
+ *   mean_out, rstd_out: device float [n], both or neither NULL (what
+ *   layernorm_backward wants to know).  In ROWS order y may be x.
+ * Errors: EINVAL (x or y NULL, one of mean_out / rstd_out alone, n or width 0,
+ * bad x_order or dtype, eps negative or not finite), ESHAPE (ld_x, ld_y too
+ * small), EUNSUPPORTED (COLUMNS with width > ECK_MAX_COLUMNS_WIDTH, n > 2^31,
+ * width > 2^24), EALIGN. */
+#define ECK_MAX_COLUMNS_WIDTH 256
+int32_t layernorm_forward(const void *x, int32_t x_order, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t width,
+                          const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y, float *mean_out,
+                          float *rstd_out, void *stream);
+
+/* Its backward pass, from dy = dL/dy ([n][ld_dy] of dtype, rows), the x of the
+ * forward call and its statistics.  With g = dy gamma and xh = (x - mean) rstd:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),
+ *   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy   (fp32).
+ *   dx_out: device, of dtype, in x_order (ld_dx), or NULL (features need none);
+ *   dgamma_out, dbeta_out: device float [width], overwritten; both or neither
+ *   NULL.  dx_out may be dy or x in ROWS order.  ws may be NULL where dgamma_out is.
+ * Errors: EINVAL (nulls; nothing to compute), ESHAPE, EUNSUPPORTED (as
+ * layernorm_forward), EWORKSPACE, EALIGN. */
+uint64_t layernorm_backward_workspace_bytes(uint64_t n, uint32_t width, int32_t dtype);
+int32_t layernorm_backward(const void *x, int32_t x_order, int32_t dtype, uint64_t ld_x, const void *dy, uint64_t ld_dy,
+                           uint64_t n, uint32_t width, const float *gamma, const float *mean, const float *rstd,
+                           void *dx_out, uint64_t ld_dx, float *dgamma_out, float *dbeta_out, void *ws,
+                           uint64_t ws_bytes, void *stream);
+
+/* Dropout from the counter-based generator that draws the candidates' genes:
+ * no mask is stored, the same (seed, round, row, column) gives the same one.
+ *   out = residual + (dropped ? 0 : x * 2^32 / (2^32 - p_drop_q32))
+ * Element (r, c) is dropped iff its 32-bit draw is below p_drop_q32 (the
+ * probability times 2^32): the low (even c) or high (odd c) half of output
+ * number (first_row + r) * ceil(width / 2) + c / 2 + 1 of a SplitMix64 generator
+ * whose state starts at mix(seed + gamma*(round+1)), as in candidate_enumerate.
+ * The backward pass is the same call on the gradient, without a residual.
+ * A dropped element is 0 whatever x holds there (NaN too).
+ *   x, residual (or NULL), out: device, [n][ld] of dtype; out may be x or
+ *   residual.  first_row: the number of row 0, for matrices handled in pieces.
+ * Errors: EINVAL (x or out NULL, n or width 0, bad dtype), ESHAPE (an ld <
+ * width), EUNSUPPORTED (n > 2^31, width > 2^24), EALIGN. */
+int32_t dropout_apply(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t width, uint32_t p_drop_q32,
+                      uint64_t seed, uint32_t round, uint64_t first_row, const void *residual, uint64_t ld_residual,
+                      void *out, uint64_t ld_out, void *stream);
+
+/* A gated feed-forward block:
+ *   [g | u] = x W_gate_up,   h = a(g) u,   y = h W_down.
+ *   x: device [n][ld_x]; w_gate_up: device [n_in][2*n_hidden] (gate columns,
+ *   then up columns), w_down: device [n_hidden][n_out], contiguous ([fan_in]
+ *   [fan_out] row-major, as in a model's state); y: device [n][ld_y]; all of
+ *   dtype.  act: ECK_ACT_*.  pre_out: device float [n][2*n_hidden], receives
+ *   [g | u] for gatedffn_backward, or NULL.
+ * h is rounded to dtype before the second product; y must not overlap inputs.
+ * Errors: EINVAL (nulls, a zero size, bad dtype or act), ESHAPE (an ld too
+ * small), EUNSUPPORTED (n > 2^31 or a width > 2^24, or more than 2^31 tiles),
+ * EWORKSPACE, EALIGN. */
+uint64_t gatedffn_forward_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_hidden, uint32_t n_out, int32_t dtype);
+int32_t gatedffn_forward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t n_in, uint32_t n_hidden,
+                         uint32_t n_out, const void *w_gate_up, const void *w_down, int32_t act, void *y,
+                         uint64_t ld_y, float *pre_out, void *ws, uint64_t ws_bytes, void *stream);
+
+/* Its backward pass, from dy = dL/dy ([n][ld_dy]) and the pre of the forward call:
+ *   dh = dy W_down^T,  du = dh a(g),  dg = dh u a'(g),
+ *   dx = [dg | du] W_gate_up^T,  dW_gate_up = x^T [dg | du],  dW_down = h^T dy.
+ * The gradients are of dtype and overwritten; each may be NULL, not all.
+ * dg, du and h are rounded to dtype before the products they enter.
+ * Errors: as gatedffn_forward. */
+uint64_t gatedffn_backward_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_hidden, uint32_t n_out, int32_t dtype);
+int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t n_in, uint32_t n_hidden,
+                          uint32_t n_out, const void *w_gate_up, const void *w_down, int32_t act, const float *pre,
+                          const void *dy, uint64_t ld_dy, void *dx_out, uint64_t ld_dx, void *dw_gate_up_out,
+                          void *dw_down_out, void *ws, uint64_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,7 +9,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBDIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIBDIR, "libeck.so")
-SOURCES = ["space.hip", "model.hip", "score_f32.hip", "topk.hip", "update.hip", "refit.hip", "refit_f32.hip", "trees.hip"]
+SOURCES = ["space.hip", "model.hip", "score_f32.hip", "topk.hip", "update.hip", "refit.hip", "refit_f32.hip", "trees.hip",
+           "layernorm.hip", "dropout.hip", "gatedffn.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     # compiler-generated packed fp32 math is switched off for device code

@@ -9,6 +9,7 @@
 #include <new>
 
 #include "eck_internal.h"
+#include "splitmix.h"
 #include "lanes.h"
 
 using namespace eck;
@@ -265,15 +266,6 @@ extern "C" int32_t eck_space_table(const eck_space *sp, int32_t gene, uint32_t *
 
 namespace {
 
-__device__ __forceinline__ uint64_t splitmix_finalise(uint64_t z)
-{
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    return z ^ (z >> 31);
-}
-
-constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
-
 // Kernel arguments of a batch: where each space's device copy lives, and the
 // SplitMix64 state its stream starts from.  Block row y works on space y, whose
 // candidates occupy columns [y*n, (y+1)*n) of the gene / feature matrices.
@@ -326,15 +318,6 @@ __global__ __launch_bounds__(256) void enumerate_kernel(SpaceBatch spaces, Strea
             genes[(uint64_t)g * ld + col] = (uint16_t)value;
         }
     }
-}
-
-// SplitMix64 state of stream (seed, round)
-uint64_t stream_state(uint64_t seed, uint32_t round)
-{
-    uint64_t z = seed + kGamma * ((uint64_t)round + 1);
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    return z ^ (z >> 31);
 }
 
 // The spaces of one launch must agree in what the kernels' template and loop bounds depend on.

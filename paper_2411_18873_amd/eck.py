@@ -22,6 +22,8 @@ SPACE_KNOB, SPACE_SPLIT, SPACE_SPLIT_XRED = 0, 1, 2
 MODE_EXHAUSTIVE, MODE_SAMPLE, MODE_MUTATE, MODE_CROSSOVER = 0, 1, 2, 3
 F32, BF16 = 0, 1
 SELECT_THRESHOLD, SELECT_RANK = 0, 1
+ROWS, COLUMNS = 0, 1
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
 MAX_K = 4096
 MAX_BATCH = 128
 
@@ -33,7 +35,9 @@ EXPORTS = ["eck_version", "eck_space_create", "eck_space_upload", "eck_space_des
            "topk_select_workspace_bytes", "topk_select_rank_workspace_bytes", "topk_select", "topk_select_static", "costmodel_update_workspace_bytes", "costmodel_update",
            "eck_trees_create", "eck_trees_destroy", "eck_trees_count", "eck_trees_set", "eck_trees_get",
            "treemodel_score", "treemodel_update_workspace_bytes", "treemodel_update", "eck_k_step", "eck_k_count",
-           "eck_candidates_dedup", "eck_candidates_dedup_workspace_bytes"]
+           "eck_candidates_dedup", "eck_candidates_dedup_workspace_bytes",
+           "layernorm_forward", "layernorm_backward_workspace_bytes", "layernorm_backward", "dropout_apply",
+           "gatedffn_forward_workspace_bytes", "gatedffn_forward", "gatedffn_backward_workspace_bytes", "gatedffn_backward"]
 
 
 class EckError(RuntimeError):
@@ -111,12 +115,24 @@ def lib():
         L.costmodel_update_workspace_bytes.argtypes = [vp, u64, i32]
         L.costmodel_update_workspace_bytes.restype = u64
         L.costmodel_update.argtypes = [vp, vp, i32, u64, vp, u64, i32, i32, f32, f32, f32, f32, vp, vp, vp, u64, vp]
+        L.layernorm_forward.argtypes = [vp, i32, i32, u64, u64, u32, vp, vp, f32, vp, u64, vp, vp, vp]
+        L.layernorm_backward_workspace_bytes.argtypes = [u64, u32, i32]
+        L.layernorm_backward_workspace_bytes.restype = u64
+        L.layernorm_backward.argtypes = [vp, i32, i32, u64, vp, u64, u64, u32, vp, vp, vp, vp, u64, vp, vp, vp, u64, vp]
+        L.dropout_apply.argtypes = [vp, i32, u64, u64, u32, u32, u64, u32, u64, vp, u64, vp, u64, vp]
+        L.gatedffn_forward_workspace_bytes.argtypes = [u64, u32, u32, u32, i32]
+        L.gatedffn_forward_workspace_bytes.restype = u64
+        L.gatedffn_forward.argtypes = [vp, i32, u64, u64, u32, u32, u32, vp, vp, i32, vp, u64, vp, vp, u64, vp]
+        L.gatedffn_backward_workspace_bytes.argtypes = [u64, u32, u32, u32, i32]
+        L.gatedffn_backward_workspace_bytes.restype = u64
+        L.gatedffn_backward.argtypes = [vp, i32, u64, u64, u32, u32, u32, vp, vp, i32, vp, vp, u64, vp, u64, vp, vp, vp, u64, vp]
         for name in EXPORTS:
             fn = getattr(L, name)
             if name not in ("eck_space_destroy", "eck_model_destroy", "topk_select_workspace_bytes",
                             "topk_select_rank_workspace_bytes", "eck_trees_destroy",
                             "eck_candidates_dedup_workspace_bytes", "treemodel_update_workspace_bytes",
-                            "costmodel_update_workspace_bytes"):
+                            "costmodel_update_workspace_bytes", "layernorm_backward_workspace_bytes",
+                            "gatedffn_forward_workspace_bytes", "gatedffn_backward_workspace_bytes"):
                 fn.restype = i32
         _lib = L
     return _lib
@@ -527,3 +543,125 @@ def candidates_dedup(genes, n, flags, overwrite=False, ws=None):
     _check("eck_candidates_dedup", lib().eck_candidates_dedup(
         _ptr(genes), genes.shape[1], n, genes.shape[0], _ptr(flags), 1 if overwrite else 0, _ptr(ws),
         ws.numel() * ws.element_size(), _stream()))
+
+
+# ------------------------------------------------------------------------------ operators of gated cost models
+
+
+def _rows(t, name, dtype, shape=None):
+    """a matrix of activations: CUDA, of dtype, values of a row side by side (rows may lie further apart); its row distance"""
+    if not (t.is_cuda and t.dtype is dtype and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise TypeError("%s must be a CUDA matrix of %s with adjacent columns" % (name, dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
+    # (torch says any distance for a single row, and a matrix of one column may be a view of any)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, name, width):
+    if t is not None:
+        _dev(t, torch.float32, name)
+        if t.numel() != width:
+            raise ValueError("%s must have %d elements" % (name, width))
+    return _ptr(t)
+
+
+def _ws(ws):
+    if ws is None:
+        return None, 0
+    if not (ws.is_cuda and ws.is_contiguous()):
+        raise TypeError("ws must be a contiguous CUDA tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _normed(x, order, n, width, dtype, name):
+    """the row distance of a layer norm's input (or its gradient) of n candidates, in its order"""
+    if order != COLUMNS:
+        return _rows(x, name, dtype, (n, width))
+    ld = _rows(x, name, dtype)
+    if x.shape[0] != width or x.shape[1] < n:
+        raise ValueError("%s must be of shape (%d, %d or more)" % (name, width, n))
+    return max(ld, n)
+
+
+def layernorm_forward(x, gamma, beta, y, mean_out=None, rstd_out=None, eps=1e-5, order=ROWS):
+    """y [n][width] = layer norm of x: [n][width] (ROWS), or a feature matrix [width][n or more] (COLUMNS)"""
+    n, width = y.shape
+    ld_y = _rows(y, "y", y.dtype)
+    ld_x = _normed(x, order, n, width, y.dtype, "x")
+    _check("layernorm_forward", lib().layernorm_forward(
+        x.data_ptr(), order, _FEAT_DTYPE[y.dtype], ld_x, n, width, _vector(gamma, "gamma", width), _vector(beta, "beta", width), eps,
+        y.data_ptr(), ld_y, _vector(mean_out, "mean_out", n), _vector(rstd_out, "rstd_out", n), _stream()))
+
+
+def layernorm_backward_workspace_bytes(n, width, dtype):
+    return int(lib().layernorm_backward_workspace_bytes(n, width, dtype))
+
+
+def layernorm_backward(x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, order=ROWS):
+    """dx (as x, or None), dgamma and dbeta (float [width], or both None) from dy [n][width] and the forward call's statistics"""
+    n, width = dy.shape
+    ld_dy = _rows(dy, "dy", dy.dtype)
+    ld_x = _normed(x, order, n, width, dy.dtype, "x")
+    ld_dx = 0 if dx is None else _normed(dx, order, n, width, dy.dtype, "dx")
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("layernorm_backward", lib().layernorm_backward(
+        x.data_ptr(), order, _FEAT_DTYPE[dy.dtype], ld_x, dy.data_ptr(), ld_dy, n, width, _vector(gamma, "gamma", width),
+        _vector(mean, "mean", n), _vector(rstd, "rstd", n), _ptr(dx), ld_dx, _vector(dgamma, "dgamma", width),
+        _vector(dbeta, "dbeta", width), ws_ptr, ws_bytes, _stream()))
+
+
+def dropout_apply(x, out, p_drop_q32, seed, round=0, first_row=0, residual=None):
+    """out = residual + dropout(x) with probability p_drop_q32 / 2^32; on a gradient (no residual) the backward pass"""
+    if not 0 <= p_drop_q32 < 1 << 32:
+        raise ValueError("p_drop_q32 must be the probability times 2^32, below 2^32")
+    n, width = out.shape
+    ld_out = _rows(out, "out", out.dtype)
+    ld_x = _rows(x, "x", out.dtype, out.shape)
+    ld_res = 0 if residual is None else _rows(residual, "residual", out.dtype, out.shape)
+    _check("dropout_apply", lib().dropout_apply(x.data_ptr(), _FEAT_DTYPE[out.dtype], ld_x, n, width, p_drop_q32, seed, round, first_row,
+                                                _ptr(residual), ld_res, out.data_ptr(), ld_out, _stream()))
+
+
+def _block(x, w_gate_up, w_down, dtype):
+    """sizes of a gated feed-forward block: n, n_in, n_hidden, n_out, x's row distance"""
+    _dev(w_gate_up, dtype, "w_gate_up")
+    _dev(w_down, dtype, "w_down")
+    (n, n_in), (n_hidden, n_out) = x.shape, w_down.shape
+    if w_gate_up.shape != (n_in, 2 * n_hidden):
+        raise ValueError("w_gate_up must be of shape (%d, %d)" % (n_in, 2 * n_hidden))
+    return n, n_in, n_hidden, n_out, _rows(x, "x", dtype)
+
+
+def gatedffn_forward_workspace_bytes(n, n_in, n_hidden, n_out, dtype):
+    return int(lib().gatedffn_forward_workspace_bytes(n, n_in, n_hidden, n_out, dtype))
+
+
+def gatedffn_backward_workspace_bytes(n, n_in, n_hidden, n_out, dtype):
+    return int(lib().gatedffn_backward_workspace_bytes(n, n_in, n_hidden, n_out, dtype))
+
+
+def gatedffn_forward(x, w_gate_up, w_down, y, ws, pre_out=None, act=ACT_SILU):
+    """y [n][n_out] = (a(g) u) w_down with [g | u] = x w_gate_up; pre_out: float [n][2 n_hidden] for the backward pass"""
+    n, n_in, n_hidden, n_out, ld_x = _block(x, w_gate_up, w_down, y.dtype)
+    ld_y = _rows(y, "y", y.dtype, (n, n_out))
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("gatedffn_forward", lib().gatedffn_forward(
+        x.data_ptr(), _FEAT_DTYPE[y.dtype], ld_x, n, n_in, n_hidden, n_out, w_gate_up.data_ptr(), w_down.data_ptr(), act, y.data_ptr(),
+        ld_y, _vector(pre_out, "pre_out", 2 * n * n_hidden), ws_ptr, ws_bytes, _stream()))
+
+
+def gatedffn_backward(x, w_gate_up, w_down, pre, dy, dx, dw_gate_up, dw_down, ws, act=ACT_SILU):
+    """gradients of gatedffn_forward from dy [n][n_out] and its pre_out; dx, dw_gate_up, dw_down may be None (not all)"""
+    n, n_in, n_hidden, n_out, ld_x = _block(x, w_gate_up, w_down, dy.dtype)
+    ld_dy = _rows(dy, "dy", dy.dtype, (n, n_out))
+    ld_dx = 0 if dx is None else _rows(dx, "dx", dy.dtype, (n, n_in))
+    for t, name, shape in ((dw_gate_up, "dw_gate_up", w_gate_up.shape), (dw_down, "dw_down", w_down.shape)):
+        _dev(t, dy.dtype, name)
+        if t is not None and t.shape != shape:
+            raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("gatedffn_backward", lib().gatedffn_backward(
+        x.data_ptr(), _FEAT_DTYPE[dy.dtype], ld_x, n, n_in, n_hidden, n_out, w_gate_up.data_ptr(), w_down.data_ptr(), act,
+        _vector(pre, "pre", 2 * n * n_hidden), dy.data_ptr(), ld_dy, _ptr(dx), ld_dx, _ptr(dw_gate_up), _ptr(dw_down), ws_ptr, ws_bytes,
+        _stream()))
