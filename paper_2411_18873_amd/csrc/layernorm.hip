@@ -18,30 +18,47 @@ namespace {
 
 constexpr int BLOCK = 256;
 
-// sum over groups of TPR neighbouring lanes, or over the block, in every thread; all threads have to call it
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float *scratch)
+// Sums over groups of TPR neighbouring lanes, or over the block, in every thread; all threads have to call it.  Loads stay on their
+// way across its barrier.  Two calls in a row use different halves of scratch (turn: 0 and 1), so that one barrier each will do.
+template <int TPR, int COUNT>
+__device__ __forceinline__ void row_sums(float (&v)[COUNT], float (*scratch)[COUNT][BLOCK / 64], int turn)
 {
 #pragma unroll
-    for (uint32_t stride = 1; stride < 64 && stride < TPR; stride <<= 1)
-        v += __uint_as_float(lane_exchange(__float_as_uint(v), stride));
-    if (TPR > 64) {
-        __syncthreads(); // (the sum before this one has been read)
-        if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = scratch[0];
+    for (int i = 0; i < COUNT; ++i)
 #pragma unroll
-        for (int w = 1; w < TPR / 64; ++w) v += scratch[w];
+        for (uint32_t stride = 1; stride < 64 && stride < TPR; stride <<= 1) v[i] += __uint_as_float(lane_exchange(__float_as_uint(v[i]), stride));
+    if (TPR <= 64) return;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) scratch[turn][i][threadIdx.x >> 6] = v[i];
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        v[i] = scratch[turn][i][0];
+#pragma unroll
+        for (int w = 1; w < BLOCK / 64; ++w) v[i] += scratch[turn][i][w];
     }
-    return v;
 }
 
-// a thread's parameters: elements at .. at + N - 1 of gamma and beta, as ones and zeros where there are none
+// the sum over the block
+__device__ __forceinline__ float block_sum(float v, float (*scratch)[1][BLOCK / 64], int turn)
+{
+    float one[1] = {v};
+    row_sums<BLOCK, 1>(one, scratch, turn);
+    return one[0];
+}
+
+// a thread's parameters: elements at .. at + N - 1 of gamma or beta, ones or zeros where there are none
 template <int N>
 __device__ __forceinline__ void load_vector(const float *p, uint32_t at, uint32_t width, float none, float (&v)[N])
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = p && at + i < width ? p[at + i] : none;
+    for (int i = 0; i < N; i += 4) {
+        float some[4] = {none, none, none, none};
+        if (p) load_chunk(p, at + i, width, some, none);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i + j] = some[j];
+    }
 }
 
 template <class T, int TPR, int ITEMS>
@@ -49,9 +66,17 @@ __global__ __launch_bounds__(BLOCK) void forward_kernel(const T *x, uint64_t ld_
                                                         const float *beta, float eps, T *y, uint64_t ld_y, float *mean_out, float *rstd_out)
 {
     constexpr int N = Chunk<T>::N, ROWS = BLOCK / TPR;
-    __shared__ float scratch[BLOCK / 64];
+    __shared__ float scratch[2][1][BLOCK / 64];
     const uint32_t lane = threadIdx.x % TPR;
     const float share = 1.0f / (float)width;
+    Chunk<T> raw[ITEMS];
+    const auto fetch = [&](uint64_t r) {
+        const T *row = x + (r < n ? r : n - 1) * ld_x; // (all lanes stay, for the sums)
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) raw[k] = fetch_chunk(row, (k * TPR + lane) * N, width);
+    };
+    uint64_t r = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    fetch(r);
     float ga[ITEMS][N], be[ITEMS][N];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
@@ -59,35 +84,38 @@ __global__ __launch_bounds__(BLOCK) void forward_kernel(const T *x, uint64_t ld_
         load_vector(beta, (k * TPR + lane) * N, width, 0.0f, be[k]);
     }
     for (uint64_t r0 = (uint64_t)blockIdx.x * ROWS; r0 < n; r0 += (uint64_t)gridDim.x * ROWS) {
-        const uint64_t r = r0 + threadIdx.x / TPR;
-        const T *row = x + (r < n ? r : n - 1) * ld_x; // (all lanes stay, for the sums)
-        float v[ITEMS][N], sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) load_chunk(row, (k * TPR + lane) * N, width, v[k]);
+        float v[ITEMS][N], sum[1] = {0.0f}, squares[1] = {0.0f};
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum += v[k][i];
-        const float mean = row_sum<TPR>(sum, scratch) * share;
-        float squares = 0.0f;
+            for (int i = 0; i < N; ++i) {
+                v[k][i] = (float)raw[k].v[i];
+                sum[0] += v[k][i];
+            }
+        const uint64_t here = r;
+        r += (uint64_t)gridDim.x * ROWS;
+        if (r0 + (uint64_t)gridDim.x * ROWS < n) fetch(r); // on its way while this row is worked out
+        row_sums<TPR>(sum, scratch, 0);
+        const float mean = sum[0] * share;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[k][i] -= mean;
-                squares += (k * TPR + lane) * N + i < width ? v[k][i] * v[k][i] : 0.0f;
+                squares[0] += (k * TPR + lane) * N + i < width ? v[k][i] * v[k][i] : 0.0f;
             }
-        const float rstd = 1.0f / sqrtf(row_sum<TPR>(squares, scratch) * share + eps);
-        if (r >= n) continue;
+        row_sums<TPR>(squares, scratch, 1);
+        const float rstd = 1.0f / sqrtf(squares[0] * share + eps);
+        if (here >= n) continue;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[k][i] = v[k][i] * rstd * ga[k][i] + be[k][i];
-            store_chunk(y + r * ld_y, (k * TPR + lane) * N, width, v[k]);
+            store_chunk(y + here * ld_y, (k * TPR + lane) * N, width, v[k]);
         }
         if (mean_out && lane == 0) {
-            mean_out[r] = mean;
-            rstd_out[r] = rstd;
+            mean_out[here] = mean;
+            rstd_out[here] = rstd;
         }
     }
 }
@@ -99,7 +127,7 @@ __global__ __launch_bounds__(BLOCK) void forward_long_kernel(const T *x, uint64_
                                                              float *rstd_out)
 {
     constexpr int N = Chunk<T>::N;
-    __shared__ float scratch[BLOCK / 64];
+    __shared__ float scratch[2][1][BLOCK / 64];
     const float share = 1.0f / (float)width;
     for (uint64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const T *row = x + r * ld_x;
@@ -109,13 +137,13 @@ __global__ __launch_bounds__(BLOCK) void forward_long_kernel(const T *x, uint64_
 #pragma unroll
             for (int i = 0; i < N; ++i) sum += v[i];
         }
-        const float mean = row_sum<BLOCK>(sum, scratch) * share;
+        const float mean = block_sum(sum, scratch, 0) * share;
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
             load_chunk(row, at, width, v, mean);
 #pragma unroll
             for (int i = 0; i < N; ++i) squares += (v[i] - mean) * (v[i] - mean);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<BLOCK>(squares, scratch) * share + eps);
+        const float rstd = 1.0f / sqrtf(block_sum(squares, scratch, 1) * share + eps);
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
             float ga[N], be[N];
             load_chunk(row, at, width, v);
@@ -139,10 +167,24 @@ __global__ __launch_bounds__(BLOCK) void backward_kernel(const T *x, uint64_t ld
                                                          uint64_t ld_dx, float *partial)
 {
     constexpr int N = Chunk<T>::N, ROWS = BLOCK / TPR, WAVES = BLOCK / 64;
-    __shared__ float scratch[WAVES];
+    __shared__ float scratch[2][2][WAVES];
     __shared__ float joined[TPR > 64 ? 1 : WAVES * TPR * N];
     const uint32_t lane = threadIdx.x % TPR;
     const float share = 1.0f / (float)width;
+    Chunk<T> raw_x[ITEMS], raw_d[ITEMS];
+    float m, s;
+    const auto fetch = [&](uint64_t r) {
+        const uint64_t from = r < n ? r : n - 1;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            raw_x[k] = fetch_chunk(x + from * ld_x, (k * TPR + lane) * N, width);
+            raw_d[k] = fetch_chunk(dy + from * ld_dy, (k * TPR + lane) * N, width);
+        }
+        m = mean[from];
+        s = rstd[from];
+    };
+    uint64_t r = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    fetch(r);
     float ga[ITEMS][N], dgamma[ITEMS][N], dbeta[ITEMS][N];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
@@ -150,36 +192,35 @@ __global__ __launch_bounds__(BLOCK) void backward_kernel(const T *x, uint64_t ld
 #pragma unroll
         for (int i = 0; i < N; ++i) dgamma[k][i] = dbeta[k][i] = 0.0f;
     }
-    for (uint64_t r0 = (uint64_t)blockIdx.x * ROWS; r0 < n; r0 += (uint64_t)gridDim.x * ROWS) {
-        const uint64_t r = r0 + threadIdx.x / TPR, from = r < n ? r : n - 1;
+    int turn = 0;
+    for (uint64_t r0 = (uint64_t)blockIdx.x * ROWS; r0 < n; r0 += (uint64_t)gridDim.x * ROWS, turn ^= 1) {
         const bool counts = r < n;
-        float xh[ITEMS][N], d[ITEMS][N], sum = 0.0f, dot = 0.0f;
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            load_chunk(x + from * ld_x, (k * TPR + lane) * N, width, xh[k]);
-            load_chunk(dy + from * ld_dy, (k * TPR + lane) * N, width, d[k]); // zeros past the end
-        }
-        const float m = mean[from], s = rstd[from];
+        float xh[ITEMS][N], d[ITEMS][N], sums[2] = {0.0f, 0.0f}; // of g and of g xh
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                xh[k][i] = (k * TPR + lane) * N + i < width ? (xh[k][i] - m) * s : 0.0f;
+                xh[k][i] = (k * TPR + lane) * N + i < width ? ((float)raw_x[k].v[i] - m) * s : 0.0f;
+                d[k][i] = (float)raw_d[k].v[i];
                 dgamma[k][i] += counts ? d[k][i] * xh[k][i] : 0.0f;
                 dbeta[k][i] += counts ? d[k][i] : 0.0f;
                 d[k][i] *= ga[k][i];
-                sum += d[k][i];
-                dot += d[k][i] * xh[k][i];
+                sums[0] += d[k][i];
+                sums[1] += d[k][i] * xh[k][i];
             }
-        if (!dx) continue; // (for all threads)
-        sum = row_sum<TPR>(sum, scratch) * share;
-        dot = row_sum<TPR>(dot, scratch) * share;
+        const uint64_t here = r;
+        const float scale = s;
+        r += (uint64_t)gridDim.x * ROWS;
+        if (r0 + (uint64_t)gridDim.x * ROWS < n) fetch(r); // on its way while this row is worked out
+        if (!dx) continue;                                 // (for all threads)
+        row_sums<TPR>(sums, scratch, turn);
+        const float from_g = sums[0] * share, from_dot = sums[1] * share;
         if (!counts) continue;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) d[k][i] = s * (d[k][i] - sum - xh[k][i] * dot);
-            store_chunk(dx + r * ld_dx, (k * TPR + lane) * N, width, d[k]);
+            for (int i = 0; i < N; ++i) d[k][i] = scale * (d[k][i] - from_g - xh[k][i] * from_dot);
+            store_chunk(dx + here * ld_dx, (k * TPR + lane) * N, width, d[k]);
         }
     }
     if (!partial) return;
@@ -190,9 +231,7 @@ __global__ __launch_bounds__(BLOCK) void backward_kernel(const T *x, uint64_t ld
         for (int k = 0; k < ITEMS; ++k) {
             float(&v)[N] = which ? dbeta[k] : dgamma[k];
             if (TPR > 64) {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if ((k * TPR + lane) * N + i < width) mine[which * width + (k * TPR + lane) * N + i] = v[i];
+                store_chunk(mine + which * width, (k * TPR + lane) * N, width, v);
                 continue;
             }
             // the rows of a wavefront, then of the block
@@ -221,7 +260,7 @@ __global__ __launch_bounds__(BLOCK) void backward_long_kernel(const T *x, uint64
                                                               T *dx, uint64_t ld_dx)
 {
     constexpr int N = Chunk<T>::N;
-    __shared__ float scratch[BLOCK / 64];
+    __shared__ float scratch[2][1][BLOCK / 64];
     const float share = 1.0f / (float)width;
     for (uint64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const float m = mean[r], s = rstd[r];
@@ -236,8 +275,8 @@ __global__ __launch_bounds__(BLOCK) void backward_long_kernel(const T *x, uint64
                 dot += d[i] * ga[i] * ((xh[i] - m) * s);
             }
         }
-        sum = row_sum<BLOCK>(sum, scratch) * share;
-        dot = row_sum<BLOCK>(dot, scratch) * share;
+        sum = block_sum(sum, scratch, 0) * share;
+        dot = block_sum(dot, scratch, 1) * share;
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
             load_chunk(x + r * ld_x, at, width, xh);
             load_chunk(dy + r * ld_dy, at, width, d);
@@ -266,51 +305,66 @@ __global__ __launch_bounds__(BLOCK) void columns_long_kernel(const T *x, uint64_
     partial[(uint64_t)blockIdx.y * 2 * width + width + c] = dbeta;
 }
 
-// dgamma and dbeta: the blocks' partial sums, sixteen wavefronts a block of 64 columns
+// dgamma and dbeta: the blocks' partial sums; sixteen columns a block, 64 threads each
 __global__ __launch_bounds__(1024) void join_kernel(const float *partial, uint32_t parts, uint32_t width, float *dgamma, float *dbeta)
 {
-    __shared__ float sums[16][64];
-    const uint64_t columns = 2ull * width, c = (uint64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    __shared__ float sums[64][17];
+    const uint64_t columns = 2ull * width, c = (uint64_t)blockIdx.x * 16 + threadIdx.x % 16;
+    const uint32_t slice = threadIdx.x / 16;
     float sum = 0.0f;
-    if (c < columns)
-        for (uint32_t p = threadIdx.x >> 6; p < parts; p += 16) sum += partial[p * columns + c];
-    sums[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+    if (c < columns) {
+#pragma unroll 4
+        for (uint32_t p = slice; p < parts; p += 64) sum += partial[p * columns + c];
+    }
+    sums[slice][threadIdx.x % 16] = sum;
     __syncthreads();
-    if (threadIdx.x >= 64 || c >= columns) return;
+    if (threadIdx.x >= 256) return;
+    // sixteen lanes a column: lane j adds rows j, j + 16, ..., then the lanes each other
+    const uint32_t column = threadIdx.x / 16, j = threadIdx.x % 16;
+    sum = (sums[j][column] + sums[j + 16][column]) + (sums[j + 32][column] + sums[j + 48][column]);
 #pragma unroll
-    for (int w = 1; w < 16; ++w) sum += sums[w][threadIdx.x];
-    if (c < width) dgamma[c] = sum;
-    else dbeta[c - width] = sum;
+    for (uint32_t stride = 1; stride < 16; stride <<= 1) sum += __uint_as_float(lane_exchange(__float_as_uint(sum), stride));
+    const uint64_t at = (uint64_t)blockIdx.x * 16 + column;
+    if (j != 0 || at >= columns) return;
+    if (at < width) dgamma[at] = sum;
+    else dbeta[at - width] = sum;
 }
 
 // ------------------------------------------------------------------------------------------------ features
 //
-// A block takes 64 candidates.  Thread (group, chunk) holds sixteen bytes of candidates of every GROUPS-th feature; rows go
-// through the LDS, because a candidate's features lie ld elements apart on one side and next to each other on the other.
+// A block takes tiles of four times CHUNKS candidates.  Thread (group, chunk) holds four candidates of four neighbouring features at
+// a time; rows go through the LDS, because a candidate's features lie ld elements apart on one side and next to each other on the
+// other.  In a row, sixteen bytes are stored in place p ^ chunk % 8, or all chunks would write to the same banks.  The next tile is
+// on its way while one is worked out: blocks of one tile each were bound by the rate at which blocks start (2^20 candidates of 64
+// bf16 features: 91 us).
 
-constexpr int TILE = 64;
-template <class T>
+template <class T, int CHUNKS_>
 struct Columns {
-    static constexpr int N = Chunk<T>::N, CHUNKS = TILE / N, GROUPS = BLOCK / CHUNKS; // bf16: 8 chunks, 32 groups; fp32: 16, 16
-    // elements of a candidate's row in the LDS: a word more than the width, so that neighbouring candidates start on other banks
-    static __host__ __device__ uint32_t pitch(uint32_t width) { return (width + 1) / 2 * 2 + 4 / sizeof(T); }
+    static constexpr int N = 4, CHUNKS = CHUNKS_, GROUPS = BLOCK / CHUNKS, TILE = CHUNKS * N, FEATURES = 4 * GROUPS;
+    static constexpr int VECTOR = 16 / sizeof(T), LINE = 128 / sizeof(T); // rows are whole 128 bytes
+    typedef T Granule __attribute__((ext_vector_type(4)));
+    typedef T Whole __attribute__((ext_vector_type(VECTOR)));
+    static __host__ __device__ uint32_t pitch(uint32_t width) { return (width + LINE - 1) / LINE * LINE; }
+    // where features from f on (four from a multiple of four, or sixteen bytes from a multiple of VECTOR) of candidate c lie
+    static __device__ __forceinline__ T *at(T *rows, uint32_t pitch, uint32_t c, uint32_t f)
+    {
+        return rows + c * pitch + (f ^ (c / N % 8 * VECTOR));
+    }
 };
 
-// sum over the features of each of a thread's N candidates, in all threads with that chunk
-template <class T>
-__device__ __forceinline__ void candidate_sums(float (&v)[Chunk<T>::N], float (*scratch)[TILE])
+// sums over the features of each of a thread's N candidates, in all threads with that chunk
+template <class C>
+__device__ __forceinline__ void candidate_sums(float (&v)[C::N], float (*scratch)[C::TILE])
 {
-    using C = Columns<T>;
     const uint32_t chunk = threadIdx.x % C::CHUNKS;
 #pragma unroll
     for (int i = 0; i < C::N; ++i)
 #pragma unroll
         for (uint32_t stride = C::CHUNKS; stride < 64; stride <<= 1) v[i] += __uint_as_float(lane_exchange(__float_as_uint(v[i]), stride));
-    __syncthreads();
     if ((threadIdx.x & 63) < C::CHUNKS)
 #pragma unroll
         for (int i = 0; i < C::N; ++i) scratch[threadIdx.x >> 6][chunk * C::N + i] = v[i];
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < C::N; ++i) {
         v[i] = scratch[0][chunk * C::N + i];
@@ -319,55 +373,98 @@ __device__ __forceinline__ void candidate_sums(float (&v)[Chunk<T>::N], float (*
     }
 }
 
-template <class T, int ITEMS>
+// a thread's features of the tile from candidate `first` on, zeros past the matrix
+template <class C, class T, int ITEMS>
+__device__ __forceinline__ void fetch_features(const T *x, uint64_t ld_x, uint32_t width, uint64_t first, uint64_t n,
+                                               Chunk<T, C::N> (&raw)[ITEMS][4])
+{
+    const uint32_t f0 = threadIdx.x / C::CHUNKS * 4;
+    const uint64_t c = first + threadIdx.x % C::CHUNKS * C::N;
+    if (first + C::TILE <= n) { // (the same for the block)
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t f = k * C::FEATURES + f0 + j;
+                raw[k][j] = {};
+                if (f < width) raw[k][j] = *reinterpret_cast<const Chunk<T, C::N> *>(x + f * ld_x + c);
+            }
+    } else {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < C::N; ++i) {
+                    const uint32_t f = k * C::FEATURES + f0 + j;
+                    raw[k][j].v[i] = (T)0.0f;
+                    if (f < width && c + i < n) raw[k][j].v[i] = x[f * ld_x + c + i];
+                }
+    }
+}
+
+template <class T, int CHUNKS, int ITEMS>
 __global__ __launch_bounds__(BLOCK) void forward_columns_kernel(const T *x, uint64_t ld_x, uint64_t n, uint32_t width, const float *gamma,
                                                                 const float *beta, float eps, T *y, uint64_t ld_y, float *mean_out,
                                                                 float *rstd_out)
 {
-    using C = Columns<T>;
-    constexpr int N = C::N;
+    using C = Columns<T, CHUNKS>;
+    constexpr int N = C::N, TILE = C::TILE;
     extern __shared__ __attribute__((aligned(16))) unsigned char dynamic[];
     T *rows = reinterpret_cast<T *>(dynamic);
-    __shared__ float scratch[BLOCK / 64][TILE];
-    const uint32_t chunk = threadIdx.x % C::CHUNKS, group = threadIdx.x / C::CHUNKS, pitch = C::pitch(width);
+    __shared__ float scratch[2][BLOCK / 64][TILE];
+    const uint32_t chunk = threadIdx.x % C::CHUNKS, group = threadIdx.x / C::CHUNKS, pitch = C::pitch(width), chunks = (width + C::VECTOR - 1) / C::VECTOR;
     const float share = 1.0f / (float)width;
+    Chunk<T, N> raw[ITEMS][4];
+    fetch_features<C, T, ITEMS>(x, ld_x, width, (uint64_t)blockIdx.x * TILE, n, raw);
     for (uint64_t first = (uint64_t)blockIdx.x * TILE; first < n; first += (uint64_t)gridDim.x * TILE) {
         const uint32_t here = (uint32_t)(n - first < TILE ? n - first : TILE);
-        float v[ITEMS][N], mean[N], rstd[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) mean[i] = rstd[i] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t f = k * C::GROUPS + group;
-            if (f < width) load_chunk(x + f * ld_x + first, chunk * N, here, v[k]);
-            else
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[k][i] = 0.0f;
-        }
+        float v[ITEMS][4][N], mean[N], rstd[N];
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) mean[i] += v[k][i];
-        candidate_sums<T>(mean, scratch);
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[k][j][i] = (float)raw[k][j].v[i];
+        // the next tile is on its way while this one is worked out
+        fetch_features<C, T, ITEMS>(x, ld_x, width, first + (uint64_t)gridDim.x * TILE, n, raw);
+#pragma unroll
+        for (int i = 0; i < N; ++i) mean[i] = rstd[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) mean[i] += v[k][j][i];
+        candidate_sums<C>(mean, scratch[0]);
 #pragma unroll
         for (int i = 0; i < N; ++i) mean[i] *= share;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[k][i] -= mean[i];
-                rstd[i] += k * C::GROUPS + group < width ? v[k][i] * v[k][i] : 0.0f;
-            }
-        candidate_sums<T>(rstd, scratch);
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    v[k][j][i] -= mean[i];
+                    rstd[i] += k * C::FEATURES + 4 * group + j < width ? v[k][j][i] * v[k][j][i] : 0.0f;
+                }
+        candidate_sums<C>(rstd, scratch[1]);
 #pragma unroll
         for (int i = 0; i < N; ++i) rstd[i] = 1.0f / sqrtf(rstd[i] * share + eps);
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t f = k * C::GROUPS + group;
-            if (f >= width) continue;
-            const float ga = gamma ? gamma[f] : 1.0f, be = beta ? beta[f] : 0.0f;
+            const uint32_t f = k * C::FEATURES + 4 * group;
+            if (f >= pitch) continue;
+            float ga[4], be[4];
+            load_vector(gamma, f, width, 1.0f, ga);
+            load_vector(beta, f, width, 0.0f, be);
 #pragma unroll
-            for (int i = 0; i < N; ++i) rows[(chunk * N + i) * pitch + f] = (T)(v[k][i] * rstd[i] * ga + be);
+            for (int i = 0; i < N; ++i) {
+                typename C::Granule out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[j] = (T)(v[k][j][i] * rstd[i] * ga[j] + be[j]);
+                *reinterpret_cast<typename C::Granule *>(C::at(rows, pitch, chunk * N + i, f)) = out;
+            }
         }
         if (mean_out && group == 0)
 #pragma unroll
@@ -376,43 +473,45 @@ __global__ __launch_bounds__(BLOCK) void forward_columns_kernel(const T *x, uint
                     mean_out[first + chunk * N + i] = mean[i];
                     rstd_out[first + chunk * N + i] = rstd[i];
                 }
-        __syncthreads();
-        const uint32_t chunks = (width + N - 1) / N;
+        lds_barrier();
         for (uint32_t j = threadIdx.x; j < here * chunks; j += BLOCK) {
-            const uint32_t c = j / chunks, at = j % chunks * N;
-            float out[N];
-            load_chunk(rows + c * pitch, at, width, out);
+            const uint32_t c = j / chunks, at = j % chunks * C::VECTOR;
+            const typename C::Whole whole = *reinterpret_cast<const typename C::Whole *>(C::at(rows, pitch, c, at));
+            float out[C::VECTOR];
+#pragma unroll
+            for (int i = 0; i < C::VECTOR; ++i) out[i] = (float)whole[i];
             store_chunk(y + (first + c) * ld_y, at, width, out);
         }
-        __syncthreads();
+        lds_barrier();
     }
 }
 
-template <class T, int ITEMS>
+template <class T, int CHUNKS, int ITEMS>
 __global__ __launch_bounds__(BLOCK) void backward_columns_kernel(const T *x, uint64_t ld_x, const T *dy, uint64_t ld_dy, uint64_t n,
                                                                  uint32_t width, const float *gamma, const float *mean, const float *rstd,
                                                                  T *dx, uint64_t ld_dx, float *partial)
 {
-    using C = Columns<T>;
-    constexpr int N = C::N;
+    using C = Columns<T, CHUNKS>;
+    constexpr int N = C::N, TILE = C::TILE;
     extern __shared__ __attribute__((aligned(16))) unsigned char dynamic[];
     T *rows = reinterpret_cast<T *>(dynamic);
-    __shared__ float scratch[BLOCK / 64][TILE];
-    const uint32_t chunk = threadIdx.x % C::CHUNKS, group = threadIdx.x / C::CHUNKS, pitch = C::pitch(width);
+    __shared__ float scratch[2][BLOCK / 64][TILE];
+    const uint32_t chunk = threadIdx.x % C::CHUNKS, group = threadIdx.x / C::CHUNKS, pitch = C::pitch(width), chunks = (width + C::VECTOR - 1) / C::VECTOR;
     const float share = 1.0f / (float)width;
-    float dgamma[ITEMS], dbeta[ITEMS];
+    float dgamma[ITEMS][4], dbeta[ITEMS][4];
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) dgamma[k] = dbeta[k] = 0.0f;
+    for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dgamma[k][j] = dbeta[k][j] = 0.0f;
+    Chunk<T, N> raw[ITEMS][4];
+    fetch_features<C, T, ITEMS>(x, ld_x, width, (uint64_t)blockIdx.x * TILE, n, raw);
     for (uint64_t first = (uint64_t)blockIdx.x * TILE; first < n; first += (uint64_t)gridDim.x * TILE) {
-        const uint32_t here = (uint32_t)(n - first < TILE ? n - first : TILE), chunks = (width + N - 1) / N;
+        const uint32_t here = (uint32_t)(n - first < TILE ? n - first : TILE);
         for (uint32_t j = threadIdx.x; j < here * chunks; j += BLOCK) {
-            const uint32_t c = j / chunks, at = j % chunks * N;
-            float in[N];
-            load_chunk(dy + (first + c) * ld_dy, at, width, in);
-            store_chunk(rows + c * pitch, at, width, in);
+            const uint32_t c = j / chunks, at = j % chunks * C::VECTOR;
+            *reinterpret_cast<typename C::Whole *>(C::at(rows, pitch, c, at)) = fetch_chunk(dy + (first + c) * ld_dy, at, width).v;
         }
-        __syncthreads();
-        float xh[ITEMS][N], d[ITEMS][N], m[N], s[N], sum[N], dot[N];
+        float m[N], s[N], sum[N], dot[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const bool counts = chunk * N + i < here;
@@ -420,65 +519,79 @@ __global__ __launch_bounds__(BLOCK) void backward_columns_kernel(const T *x, uin
             s[i] = counts ? rstd[first + chunk * N + i] : 0.0f;
             sum[i] = dot[i] = 0.0f;
         }
+        lds_barrier();
+        float xh[ITEMS][4][N], d[ITEMS][4][N];
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const uint32_t f = k * C::GROUPS + group;
-            if (f < width) load_chunk(x + f * ld_x + first, chunk * N, here, xh[k]);
+            const uint32_t f = k * C::FEATURES + 4 * group;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) xh[k][j][i] = (float)raw[k][j].v[i];
+            float ga[4];
+            load_vector(gamma, f, width, 1.0f, ga);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const bool counts = f < width && chunk * N + i < here;
-                xh[k][i] = counts ? (xh[k][i] - m[i]) * s[i] : 0.0f;
-                d[k][i] = counts ? (float)rows[(chunk * N + i) * pitch + f] : 0.0f;
-                dgamma[k] += d[k][i] * xh[k][i];
-                dbeta[k] += d[k][i];
-            }
-            const float ga = gamma && f < width ? gamma[f] : 1.0f;
+                typename C::Granule in = {};
+                if (f < pitch) in = *reinterpret_cast<const typename C::Granule *>(C::at(rows, pitch, chunk * N + i, f));
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                d[k][i] *= ga;
-                sum[i] += d[k][i];
-                dot[i] += d[k][i] * xh[k][i];
+                for (int j = 0; j < 4; ++j) {
+                    const bool counts = f + j < width && chunk * N + i < here;
+                    xh[k][j][i] = counts ? (xh[k][j][i] - m[i]) * s[i] : 0.0f;
+                    d[k][j][i] = counts ? (float)in[j] : 0.0f;
+                    dgamma[k][j] += d[k][j][i] * xh[k][j][i];
+                    dbeta[k][j] += d[k][j][i];
+                    d[k][j][i] *= ga[j];
+                    sum[i] += d[k][j][i];
+                    dot[i] += d[k][j][i] * xh[k][j][i];
+                }
             }
         }
+        fetch_features<C, T, ITEMS>(x, ld_x, width, first + (uint64_t)gridDim.x * TILE, n, raw);
         if (dx) {
-            candidate_sums<T>(sum, scratch);
-            candidate_sums<T>(dot, scratch);
+            candidate_sums<C>(sum, scratch[0]);
+            candidate_sums<C>(dot, scratch[1]);
 #pragma unroll
-            for (int k = 0; k < ITEMS; ++k) {
-                const uint32_t f = k * C::GROUPS + group;
-                if (f >= width) continue;
+            for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-                for (int i = 0; i < N; ++i) d[k][i] = s[i] * (d[k][i] - sum[i] * share - xh[k][i] * (dot[i] * share));
-                store_chunk(dx + f * ld_dx + first, chunk * N, here, d[k]);
-            }
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t f = k * C::FEATURES + 4 * group + j;
+                    if (f >= width) continue;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) d[k][j][i] = s[i] * (d[k][j][i] - sum[i] * share - xh[k][j][i] * (dot[i] * share));
+                    store_chunk(dx + f * ld_dx + first, chunk * N, here, d[k][j]);
+                }
         }
-        __syncthreads();
+        lds_barrier();
     }
     if (!partial) return;
     float *mine = partial + (uint64_t)blockIdx.x * 2 * width;
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
+    for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-        for (uint32_t stride = 1; stride < C::CHUNKS; stride <<= 1) {
-            dgamma[k] += __uint_as_float(lane_exchange(__float_as_uint(dgamma[k]), stride));
-            dbeta[k] += __uint_as_float(lane_exchange(__float_as_uint(dbeta[k]), stride));
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (uint32_t stride = 1; stride < C::CHUNKS; stride <<= 1) {
+                dgamma[k][j] += __uint_as_float(lane_exchange(__float_as_uint(dgamma[k][j]), stride));
+                dbeta[k][j] += __uint_as_float(lane_exchange(__float_as_uint(dbeta[k][j]), stride));
+            }
+            const uint32_t f = k * C::FEATURES + 4 * group + j;
+            if (chunk == 0 && f < width) {
+                mine[f] = dgamma[k][j];
+                mine[width + f] = dbeta[k][j];
+            }
         }
-        const uint32_t f = k * C::GROUPS + group;
-        if (chunk == 0 && f < width) {
-            mine[f] = dgamma[k];
-            mine[width + f] = dbeta[k];
-        }
-    }
 }
 
 // ------------------------------------------------------------------------------------------------ launches
 
 // Calls f with the number of threads a row and the chunks a thread that hold a row of `width`; false if none does.  (A power of
-// two below 64 lanes wastes less than half of them on short rows; a wavefront holds four chunks a lane, then a block takes over.)
-template <class T, class F>
+// two below 64 lanes wastes less than half of them on short rows; a wavefront holds two chunks a lane, or four in the backward
+// pass, then a block takes over.  16384 rows of 2000 bf16: forward 28.5 us by blocks, 30.8 by wavefronts; backward 57.3 and 48.2.)
+template <class T, int WAVE_ITEMS, class F>
 bool with_row_shape(uint32_t width, F &&f)
 {
-    constexpr uint32_t N = Chunk<T>::N;
+    constexpr uint32_t N = 16 / sizeof(T);
 #define ECK_ROW_SHAPE(tpr, items)                                                                  \
     if (width <= (tpr) * (items) * N) {                                                            \
         f(std::integral_constant<int, tpr>{}, std::integral_constant<int, items>{});               \
@@ -489,41 +602,44 @@ bool with_row_shape(uint32_t width, F &&f)
     ECK_ROW_SHAPE(32, 1)
     ECK_ROW_SHAPE(64, 1)
     ECK_ROW_SHAPE(64, 2)
-    ECK_ROW_SHAPE(256, 1)
+    if constexpr (WAVE_ITEMS == 4) { ECK_ROW_SHAPE(64, 4) }
+    else { ECK_ROW_SHAPE(256, 1) }
     ECK_ROW_SHAPE(256, 2)
     ECK_ROW_SHAPE(256, 4)
 #undef ECK_ROW_SHAPE
     return false;
 }
 
-// the same for the chunks of features a thread
+// the same for the chunks of a tile and the fours of features a thread: as many candidates as 32 features a thread allow, 256 bytes
+// of each feature at most
 template <class T, class F>
 void with_columns_shape(uint32_t width, F &&f)
 {
-    constexpr uint32_t G = Columns<T>::GROUPS;
-    if (width <= G) f(std::integral_constant<int, 1>{});
-    else if (width <= 2 * G) f(std::integral_constant<int, 2>{});
-    else if (width <= 4 * G) f(std::integral_constant<int, 4>{});
-    else if (width <= 8 * G) f(std::integral_constant<int, 8>{});
-    else f(std::integral_constant<int, 16>{});
+    static_assert(ECK_MAX_COLUMNS_WIDTH == 256, "no width is left out");
+    constexpr int MOST = 64 / sizeof(T);
+    if (width <= 1024 / MOST) f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 1>{});
+    else if (width <= 64) f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 2>{});
+    else if (width <= 128) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
 }
 
 uint32_t at_most(uint64_t blocks, uint32_t most) { return (uint32_t)(blocks < most ? blocks : most); }
 
-// Blocks of the backward pass, each of which leaves a partial sum per column.  Four a compute unit keep the memory busy; fewer where
-// their partial sums (8 bytes a column, written and read) would be more than an eighth of what the rows move.
+// Blocks of the backward pass, each of which leaves a partial sum per column: what keeps 32 KB on their way to a compute unit, one
+// to four a unit, two at least of blocks that work on several rows at once.  (us by 1, 2, 3 and 4 a unit: 8192 rows of 4096 bf16
+// 52.9, 49.0, 54.7, 67.9; of fp32 81.6, 86.2, 93.9, 93.8; 32768 of 1024 bf16 39.8, 37.6, 38.7, 46.0; 50003 of 250 fp32 66.8, 44.3,
+// 37.0, 33.7; 16384 of 2000 bf16 57.4, 48.2.)
 uint32_t backward_blocks(uint64_t n, uint32_t width, int32_t dtype, int32_t order)
 {
-    const uint64_t vector = 16 / element_bytes(dtype), chunks = (width + vector - 1) / vector;
+    if (order == ECK_COLUMNS) return at_most((n + 31) / 32, 1024); // (32 candidates: the smallest tile)
+    const uint64_t size = element_bytes(dtype), vector = 16 / size, chunks = (width + vector - 1) / vector;
     uint64_t rows = 1; // a block's at a time
-    if (order == ECK_COLUMNS) rows = TILE;
-    else
-        for (uint64_t tpr = 8; tpr <= 64; tpr *= 2)
-            if (chunks <= tpr * (tpr == 64 ? 2 : 1)) {
-                rows = BLOCK / tpr;
-                break;
-            }
-    return at_most((n + rows - 1) / rows, 1024);
+    for (uint64_t tpr = 8; tpr <= 64 && rows == 1; tpr *= 2)
+        if (chunks <= tpr * (tpr == 64 ? 4 : 1)) rows = BLOCK / tpr;
+    uint64_t a_unit = 32768 / (2 * rows * width * size);
+    a_unit = a_unit > 4 ? 4 : a_unit < 1 ? 1 : a_unit;
+    if (rows > 1 && a_unit < 2) a_unit = 2;
+    return at_most((n + rows - 1) / rows, (uint32_t)(256 * a_unit));
 }
 constexpr uint32_t LONG_PARTS = 64;
 
@@ -532,12 +648,13 @@ int32_t forward(const void *x, int32_t order, uint64_t ld_x, uint64_t n, uint32_
                 void *y, uint64_t ld_y, float *mean, float *rstd, hipStream_t st)
 {
     if (order == ECK_COLUMNS) {
-        const size_t lds = (size_t)TILE * Columns<T>::pitch(width) * sizeof(T);
-        with_columns_shape<T>(width, [&](auto items) {
-            hipLaunchKernelGGL((forward_columns_kernel<T, decltype(items)::value>), dim3(at_most((n + TILE - 1) / TILE, 1 << 20)), dim3(BLOCK),
-                               lds, st, (const T *)x, ld_x, n, width, gamma, beta, eps, (T *)y, ld_y, mean, rstd);
+        with_columns_shape<T>(width, [&](auto chunks, auto items) {
+            using C = Columns<T, decltype(chunks)::value>;
+            hipLaunchKernelGGL((forward_columns_kernel<T, C::CHUNKS, decltype(items)::value>), dim3(at_most((n + C::TILE - 1) / C::TILE, 2048)),
+                               dim3(BLOCK), C::TILE * C::pitch(width) * sizeof(T), st, (const T *)x, ld_x, n, width, gamma, beta, eps, (T *)y, ld_y,
+                               mean, rstd);
         });
-    } else if (!with_row_shape<T>(width, [&](auto tpr, auto items) {
+    } else if (!with_row_shape<T, 2>(width, [&](auto tpr, auto items) {
                    constexpr int TPR = decltype(tpr)::value, ROWS = BLOCK / TPR;
                    hipLaunchKernelGGL((forward_kernel<T, TPR, decltype(items)::value>), dim3(at_most((n + ROWS - 1) / ROWS, 2048)), dim3(BLOCK), 0,
                                       st, (const T *)x, ld_x, n, width, gamma, beta, eps, (T *)y, ld_y, mean, rstd);
@@ -559,12 +676,12 @@ int32_t backward(const void *x_, int32_t order, uint64_t ld_x, const void *dy_, 
     uint32_t parts = backward_blocks(n, width, code_of<T>, order);
     if (!dgamma) partial = nullptr;
     if (order == ECK_COLUMNS) {
-        const size_t lds = (size_t)TILE * Columns<T>::pitch(width) * sizeof(T);
-        with_columns_shape<T>(width, [&](auto items) {
-            hipLaunchKernelGGL((backward_columns_kernel<T, decltype(items)::value>), dim3(parts), dim3(BLOCK), lds, st, x, ld_x, dy, ld_dy, n,
-                               width, gamma, mean, rstd, dx, ld_dx, partial);
+        with_columns_shape<T>(width, [&](auto chunks, auto items) {
+            using C = Columns<T, decltype(chunks)::value>;
+            hipLaunchKernelGGL((backward_columns_kernel<T, C::CHUNKS, decltype(items)::value>), dim3(parts), dim3(BLOCK),
+                               C::TILE * C::pitch(width) * sizeof(T), st, x, ld_x, dy, ld_dy, n, width, gamma, mean, rstd, dx, ld_dx, partial);
         });
-    } else if (!with_row_shape<T>(width, [&](auto tpr, auto items) {
+    } else if (!with_row_shape<T, 4>(width, [&](auto tpr, auto items) {
                    hipLaunchKernelGGL((backward_kernel<T, decltype(tpr)::value, decltype(items)::value>), dim3(parts), dim3(BLOCK), 0, st, x,
                                       ld_x, dy, ld_dy, n, width, gamma, mean, rstd, dx, ld_dx, partial);
                })) {
@@ -578,7 +695,7 @@ int32_t backward(const void *x_, int32_t order, uint64_t ld_x, const void *dy_, 
                                rstd, dx, ld_dx);
     }
     if (partial)
-        hipLaunchKernelGGL(join_kernel, dim3((2 * width + 63) / 64), dim3(1024), 0, st, partial, parts, width, dgamma, dbeta);
+        hipLaunchKernelGGL(join_kernel, dim3((2 * width + 15) / 16), dim3(1024), 0, st, partial, parts, width, dgamma, dbeta);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
