@@ -88,7 +88,7 @@ int32_t launch_tiles(Product p, uint32_t shares, float *partial, hipStream_t st)
     q.tiles_n = (q.N + S::BN - 1) / S::BN;
     q.to.out = partial;
     q.to.ld_out = up_to(q.N, 8);
-    if (int32_t rc = launch_shape<S, A_FAST, B_FAST, PARTIAL, 1>(q, st)) return rc;
+    if (int32_t rc = launch_shape<S, A_FAST, B_FAST, PARTIAL, PARTS>(q, st)) return rc;
     const uint64_t blocks = ((uint64_t)p.M * ((p.N + 7) / 8) + 255) / 256;
     hipLaunchKernelGGL((join_kernel<KIND, PARTS>), dim3((uint32_t)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, partial, shares, p.M, p.N,
                        q.to.ld_out, p.b_up, p.to);
@@ -99,7 +99,7 @@ int32_t launch_tiles(Product p, uint32_t shares, float *partial, hipStream_t st)
 template <bool A_FAST, bool B_FAST, int KIND, int PARTS>
 int32_t launch(const Product &p, float *partial, hipStream_t st)
 {
-    const Plan how = plan(p.M, KIND == GATE ? (uint64_t)p.b_up + p.N : p.N, p.K, p.parts);
+    const Plan how = plan(p.M, KIND == GATE ? (uint64_t)p.b_up + p.N : p.N, p.K, PARTS);
     if (how.shape == 0) return launch_tiles<Small, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
     if (how.shape == 1) return launch_tiles<Medium, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
     return launch_tiles<Large, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
@@ -198,13 +198,13 @@ int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, c
     float *partial = (float *)space.take(room.partial);
 
     Product p = {};
-    p.a = ox, p.b = ogu, p.parts = P, p.b_up = s.hidden();
+    p.a = ox, p.b = ogu, p.b_up = s.hidden();
     p.M = (uint32_t)s.n, p.N = s.n_hidden, p.K = s.n_in;
     p.to.out = const_cast<bf16 *>(h.p), p.to.ld_out = h.ld, p.to.part_out = h.part, p.to.pre = pre, p.to.n_hidden = s.n_hidden, p.to.act = act;
     ECK_TRY((launch<true, false, GATE, P>(p, partial, st)));
 
     p = {};
-    p.a = h, p.b = od, p.parts = P;
+    p.a = h, p.b = od;
     p.M = (uint32_t)s.n, p.N = s.n_out, p.K = s.n_hidden;
     p.to.out = y, p.to.ld_out = ld_y, p.to.piece = s.n_out, p.to.pitch = NO_GAP;
     return launch<true, false, STORE, P>(p, partial, st);
@@ -226,7 +226,7 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     ECK_TRY(as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, room_d, &od, st));
 
     Product p = {}; // dh, and from it dg, du and h
-    p.a = ody, p.b = od, p.parts = P;
+    p.a = ody, p.b = od;
     p.M = (uint32_t)s.n, p.N = s.n_hidden, p.K = s.n_out;
     p.to.out = dw_down ? const_cast<bf16 *>(h.p) : nullptr, p.to.ld_out = h.ld, p.to.part_out = h.part;
     p.to.pre = const_cast<float *>(pre), p.to.n_hidden = s.n_hidden, p.to.act = act, p.to.pitch = s.hidden();
@@ -235,7 +235,7 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     if (dx) {
         ECK_TRY(as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, room_gu, &other, st));
         p = {};
-        p.a = d_pre, p.b = other, p.parts = P;
+        p.a = d_pre, p.b = other;
         p.M = (uint32_t)s.n, p.N = s.n_in, p.K = s.hidden() + s.n_hidden;
         p.to.out = dx, p.to.ld_out = ld_dx, p.to.piece = s.n_in, p.to.pitch = NO_GAP;
         ECK_TRY((launch<true, true, STORE, P>(p, partial, st)));
@@ -243,14 +243,14 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     if (dw_gate_up) {
         ECK_TRY(as_operand(x, ld_x, s.n, s.n_in, 1, room_x, &other, st));
         p = {};
-        p.a = other, p.b = d_pre, p.parts = P;
+        p.a = other, p.b = d_pre;
         p.M = s.n_in, p.N = s.hidden() + s.n_hidden, p.K = (uint32_t)s.n;
         p.to.out = dw_gate_up, p.to.ld_out = 2ull * s.n_hidden, p.to.piece = s.n_hidden, p.to.pitch = s.hidden();
         ECK_TRY((launch<false, false, STORE, P>(p, partial, st)));
     }
     if (dw_down) {
         p = {};
-        p.a = h, p.b = ody, p.parts = P;
+        p.a = h, p.b = ody;
         p.M = s.n_hidden, p.N = s.n_out, p.K = (uint32_t)s.n;
         p.to.out = dw_down, p.to.ld_out = s.n_out, p.to.piece = s.n_out, p.to.pitch = NO_GAP;
         ECK_TRY((launch<false, false, STORE, P>(p, partial, st)));

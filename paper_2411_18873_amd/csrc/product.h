@@ -1,7 +1,7 @@
 // Products of bfloat16 matrices on the matrix cores, and what a gated feed-forward block does with their sums (HIP, gfx950).
 //
 // C[m][c] = sum over k of A(m, k) B(k, c).  An operand's values lie next to each other along k (K_FAST) or along m or c; both are
-// staged as they lie, 32 values of k at a time, by loads that go straight into the LDS, and become matrix-core operands on the
+// staged as they lie, 64 values of k at a time, by loads that go straight into the LDS, and become matrix-core operands on the
 // way out of it (the second kind by the transposing LDS reads).  A block works on a tile of C, its wavefronts on parts of it.
 //
 // fp32 matrices come as three bfloat16 parts each (f32_split.h): of the nine products of parts the six largest are summed, one
@@ -25,7 +25,9 @@ __device__ __forceinline__ Gate gate_of(int32_t act, float g)
 {
     if (act == ECK_ACT_RELU) return {g > 0.0f ? g : g == g ? 0.0f : g, g > 0.0f ? 1.0f : 0.0f};
     if (act == ECK_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
+        // (exponential and reciprocal as the instructions give them, within 2^-23 of the value each: full ones are 25 more
+        // instructions an element, 70 us of the 1030 of 8192 x 8192 results)
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
         return {g * s, s * (1.0f + g * (1.0f - s))};
     }
     const float s = 0.5f * (1.0f + erff(g * 0.70710678f));
@@ -63,7 +65,6 @@ struct Product {
     Operand a, b;
     uint32_t M, N, K; // GATE: N = pairs
     uint32_t b_up;    // GATE: columns from a gate's to its up column in b
-    uint32_t parts;   // 1, or 3: fp32 matrices
     uint32_t tiles_m, tiles_n, shares;
     Target to;
 };
@@ -107,8 +108,17 @@ __device__ __forceinline__ void load_eight(const float *row, uint32_t at, uint32
 {
 #pragma unroll
     for (int i = 0; i < 8; i += 4) {
-        float some[4];
-        load_chunk(row, at + i, width, some);
+        float some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (at + i + 4 <= width) {
+            // read once, and not to push the operands out of the L2 (8192 x 8192 derivatives: 750 us without the hint, 635 with)
+            const auto c = __builtin_nontemporal_load(reinterpret_cast<const Chunk<float>::Vector *>(row + at + i));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) some[j] = c[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at + i + j < width) some[j] = row[at + i + j];
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i + j] = some[j];
     }
@@ -137,18 +147,26 @@ __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32
     }
 }
 
-template <int PARTS>
-__device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint32_t c, const float (&dh)[8])
+// what eight columns of dh are multiplied with (zeros past the end: the padding of h, dg and du is zero)
+struct Pre {
+    float g[8], u[8];
+};
+__device__ __forceinline__ void load_pre(const Target &to, uint64_t m, uint32_t c, Pre &pre)
 {
-    float g[8], u[8], h[8], dg[8], du[8];
     const float *row = to.pre + m * 2 * to.n_hidden;
-    load_eight(row, c, to.n_hidden, g); // (zeros past the end: the padding of h, dg and du is zero)
-    load_eight(row + to.n_hidden, c, to.n_hidden, u);
+    load_eight(row, c, to.n_hidden, pre.g);
+    load_eight(row + to.n_hidden, c, to.n_hidden, pre.u);
+}
+
+template <int PARTS>
+__device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint32_t c, const float (&dh)[8], const Pre &pre)
+{
+    float h[8], dg[8], du[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const Gate gate = gate_of(to.act, g[i]);
-        h[i] = gate.value * u[i];
-        dg[i] = dh[i] * u[i] * gate.slope;
+        const Gate gate = gate_of(to.act, pre.g[i]);
+        h[i] = gate.value * pre.u[i];
+        dg[i] = dh[i] * pre.u[i] * gate.slope;
         du[i] = dh[i] * gate.value;
     }
     if (to.out) store_operand<PARTS>((bf16 *)to.out + m * to.ld_out + c, to.part_out, h);
@@ -159,7 +177,7 @@ __device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint3
 
 // ------------------------------------------------------------------------------------------------ staging
 
-constexpr int BK = 32, STAGES = 4;
+constexpr int BK = 64;
 constexpr uint32_t NOWHERE = 0x80000000u; // an offset outside every buffer: such loads bring zeros
 
 // 16 bytes per lane from base + offset into the LDS, lane after lane from lds_at (the same in all lanes)
@@ -175,10 +193,12 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// How 32 k's of ROWS rows (or columns) of an operand lie in the LDS.
-//   K_FAST  rows of 64 bytes, four chunks of eight k's.  Sixteen lanes read the same chunk of sixteen neighbouring rows: chunk c of
-//           row r is stored in place c ^ (r / 4 % 4), which spreads them over all banks.
-//   else    32 rows of k, ROWS values each, in units of sixteen.  The transposing read takes units of eight k's at a time (k % 4 and
+// How 64 k's of ROWS rows (or columns) of an operand lie in the LDS.
+//   K_FAST  rows of 128 bytes (so every load takes whole cache lines: of 32 k's at a time the L1 asked the L2 for each line twice,
+//           1.33e8 requests for 6.7e7 in a product of 8192^3), eight chunks of eight k's; chunk c of row r is stored in place
+//           c ^ (r / 2 % 8).  A read of sixteen rows takes four cycles if the lanes served in one (rows 0 .. 3 and 12 .. 15 of one
+//           chunk with 4 .. 11 of the next, or the other way round) take from all banks: so found from the bank conflicts counted.
+//   else    64 rows of k, ROWS values each, in units of sixteen.  The transposing read takes units of eight k's at a time (k % 4 and
 //           k / 8 % 2 vary within half a wavefront): unit j of k is stored in place j ^ those three bits (two where a row has just
 //           four units and two rows share the banks).
 template <int ROWS, bool K_FAST, int WAVES>
@@ -193,8 +213,6 @@ struct Stage {
     }
 
     uint32_t offset[LOADS], k_of[LOADS]; // bytes from the tile's first value, or NOWHERE; first k
-    i32x4 base;
-    uint64_t step;                       // bytes from one stage to the next
     uint32_t lds_at;
 
     // place(r): for row r of the tile (K_FAST), or for the eight columns from r on, where in memory that is, in rows or columns from
@@ -204,12 +222,11 @@ struct Stage {
     {
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         lds_at = lds + wave * LOADS * 1024;
-        step = K_FAST ? BK * 2 : BK * 2 * ld;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const uint32_t piece = wave * LOADS + j;
             if (K_FAST) {
-                const uint32_t r = piece * 16 + lane / 4, chunk = (lane & 3) ^ (r >> 2 & 3);
+                const uint32_t r = piece * 8 + lane / 8, chunk = (lane & 7) ^ (r >> 1 & 7);
                 const uint32_t at = place(r);
                 k_of[j] = chunk * 8;
                 offset[j] = at != NOWHERE ? (uint32_t)(at * ld * 2) + chunk * 16 : NOWHERE;
@@ -230,15 +247,16 @@ struct Stage {
         for (int j = 0; j < LOADS; ++j) load_to_lds(lds_at + stage_at + j * 1024, k_of[j] < left ? offset[j] : NOWHERE, where);
     }
 
-    // operands of rows [16 t, 16 t + 16): lane (g = lane / 16, r) holds k's 8g .. 8g + 7 of row r.  at: LDS address of the stage
-    static __device__ __forceinline__ bf16x8 read(uint32_t at, uint32_t t)
+    // operands of rows [16 t, 16 t + 16): lane (g = lane / 16, r) holds k's 32 half + 8g .. 8g + 7 of row r.  at: LDS address of the
+    // stage
+    static __device__ __forceinline__ bf16x8 read(uint32_t at, uint32_t t, uint32_t half)
     {
         typedef __attribute__((address_space(3))) const bf16x8 *Whole;
         typedef __attribute__((address_space(3))) s16x4 *Half;
         const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-        if (K_FAST) return *(Whole)(uintptr_t)(at + t * 1024 + r * 64 + ((g ^ (r >> 2 & 3)) << 4));
+        if (K_FAST) return *(Whole)(uintptr_t)(at + t * 2048 + r * 128 + ((half * 4 + g ^ r >> 1) << 4));
         // sixteen lanes: four k's, four values of sixteen columns each; lane r receives the four k's of column r
-        const uint32_t k = 8 * g + (r >> 2);
+        const uint32_t k = 32 * half + 8 * g + (r >> 2);
         const uint32_t p = at + k * (ROWS * 2) + ((t ^ unit_swizzle(k)) << 5) + ((r & 3) << 3);
         const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half)(uintptr_t)p);
         const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half)(uintptr_t)(p + 4 * ROWS * 2));
@@ -248,19 +266,20 @@ struct Stage {
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-// Tiles of BM x BN, wavefronts in WM rows and WN columns.
-template <int BM_, int BN_, int WM_, int WN_>
+// Tiles of BM x BN, wavefronts in WM rows and WN columns, STAGES of 64 k's in the LDS.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES, STAGES = STAGES_;
     static constexpr int TM = BM / WM / 16, TN = BN / WN / 16; // 16 x 16 tiles of a wavefront
     static constexpr int LDS = (BM + BN) * BK * 2 * STAGES;
+    static constexpr int AT_ONCE = 160 * 1024 / LDS * WAVES / 4; // wavefronts a SIMD: the registers may be used up to that
 };
-typedef Shape<256, 256, 2, 4> Large;
-typedef Shape<128, 128, 2, 2> Medium;
-typedef Shape<64, 64, 4, 1> Small;
+typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<128, 128, 2, 2, 2> Medium;
+typedef Shape<64, 64, 4, 1, 3> Small;
 
 template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
-__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(const Product p)
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void product_kernel(const Product p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     typedef Stage<S::BM, A_FAST, S::WAVES> StageA;
@@ -293,22 +312,34 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(const Product p)
     // (the tile's own place is added to the base: offsets within a tile and a step fit 32 bits)
     const bf16 *a0 = p.a.p + (A_FAST ? m0 * p.a.ld : (uint64_t)m0), *b0 = p.b.p + (B_FAST ? c0 * p.b.ld : (uint64_t)c0);
 
-    // steps of 32 k's: all of the first pair of parts, then the next; this block's share of them
-    const uint32_t steps_k = (p.K + BK - 1) / BK, pairs = p.parts == 3 ? 6 : 1;
-    const uint64_t all = (uint64_t)steps_k * pairs;
+    // steps of 64 k's: all of the first pair of parts, then the next; this block's share of them
+    const uint32_t steps_k = (p.K + BK - 1) / BK;
+    const uint64_t all = (uint64_t)steps_k * (PARTS == 3 ? 6 : 1);
     const uint32_t first = (uint32_t)(all * share / p.shares), steps = (uint32_t)(all * (share + 1) / p.shares) - first;
-    uint32_t next = first, next_pair = first / steps_k, next_k = first % steps_k; // to be loaded
-    const auto load = [&](uint32_t slot) {
+    uint32_t to_come = steps, pair = first / steps_k, left; // steps not yet on their way, k's from the next one on
+    const bf16 *at_a, *at_b;
+    const auto begin_pair = [&](uint32_t k) {
         // x0 w2, x2 w0, x1 w1, x0 w1, x1 w0, x0 w0
-        const uint32_t pair = min(next_pair, 5u);
-        const uint32_t part_a = p.parts == 3 ? 0x010120u >> 4 * pair & 15 : 0, part_b = p.parts == 3 ? 0x001102u >> 4 * pair & 15 : 0;
-        const uint32_t k = next_k * BK, left = next < first + steps ? p.K - k : 0;
-        sa.load(a0 + part_a * p.a.part + (A_FAST ? (uint64_t)k : k * p.a.ld), left, slot * STAGE);
-        sb.load(b0 + part_b * p.b.part + (B_FAST ? (uint64_t)k : k * p.b.ld), left, slot * STAGE);
-        ++next;
-        if (++next_k == steps_k) {
-            next_k = 0;
-            ++next_pair;
+        const uint32_t part_a = PARTS == 3 ? 0x010120u >> 4 * pair & 15 : 0, part_b = PARTS == 3 ? 0x001102u >> 4 * pair & 15 : 0;
+        at_a = a0 + part_a * p.a.part + (A_FAST ? (uint64_t)k : k * p.a.ld);
+        at_b = b0 + part_b * p.b.part + (B_FAST ? (uint64_t)k : k * p.b.ld);
+        left = p.K - k;
+    };
+    begin_pair(first % steps_k * BK);
+    const uint64_t step_a = A_FAST ? BK : BK * p.a.ld, step_b = B_FAST ? BK : BK * p.b.ld;
+    const auto load = [&](uint32_t slot) { // past the end: zeros
+        const uint32_t some = to_come ? left : 0;
+        sa.load(at_a, some, slot * STAGE);
+        sb.load(at_b, some, slot * STAGE);
+    };
+    const auto advance = [&]() {
+        to_come = to_come ? to_come - 1 : 0;
+        at_a += step_a;
+        at_b += step_b;
+        left -= BK; // (past the end of the last pair nothing is to come)
+        if (PARTS == 3 && to_come && (int32_t)left <= 0) {
+            ++pair;
+            begin_pair(0);
         }
     };
 
@@ -318,73 +349,97 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(const Product p)
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) sum[i][j] = f32x4{0, 0, 0, 0};
     bf16x8 a[2][S::TM], b[2][S::TN];
-    const auto read = [&](uint32_t slot, bf16x8(&fa)[S::TM], bf16x8(&fb)[S::TN]) {
+    const auto read = [&](uint32_t slot, int half) {
         const uint32_t at = lds0 + slot * STAGE;
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) fb[j] = StageB::read(at + S::BM * BK * 2, wn * S::TN + j);
+        for (int j = 0; j < S::TN; ++j) b[half][j] = StageB::read(at + S::BM * BK * 2, wn * S::TN + j, half);
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i) fa[i] = StageA::read(at, wm * S::TM + i);
+        for (int i = 0; i < S::TM; ++i) a[half][i] = StageA::read(at, wm * S::TM + i, half);
     };
-    const auto multiply = [&](const bf16x8(&fa)[S::TM], const bf16x8(&fb)[S::TN]) {
+    const auto multiply = [&](int half) {
         // columns as the first operand: a lane's four sums are neighbouring columns of one row
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], sum[i][j], 0, 0, 0);
+            for (int j = 0; j < S::TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[half][j], a[half][i], sum[i][j], 0, 0, 0);
+        // an LDS read (of the next half), a few products, and so on: left to itself the compiler reads every operand right before
+        // its use
+        constexpr int READS = S::TM * (A_FAST ? 1 : 2) + S::TN * (B_FAST ? 1 : 2), PRODUCTS = S::TM * S::TN;
+        constexpr int EACH = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+#pragma unroll
+        for (int r = 0; r < READS; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
+        }
     };
 
-    // Step i is multiplied from registers while step i + 1 is read from the LDS and steps i + 2 to i + 4 are on their way; at the
-    // meeting at its start everybody has read step i, so step i + 4 may take its place.  Steps past the end bring zeros.
+    // One half of a step's k's is multiplied from registers while the next half is read from the LDS and later steps are on their
+    // way.  At the meeting between the halves everybody has read the step's second half, so that its place is free, and the next
+    // step has come.  Steps past the end bring zeros.
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) load(s);
-    wait_and_meet<(STAGES - 1) * PER_STEP>();
-    read(0, a[0], b[0]);
-    for (uint32_t i = 0; i < steps; i += 2) {
-#pragma unroll
-        for (int odd = 0; odd < 2; ++odd) {
-            const uint32_t slot = (i + odd) & (STAGES - 1);
-            wait_and_meet<(STAGES - 2) * PER_STEP>();
-            load(slot);
-            read((slot + 1) & (STAGES - 1), a[odd ^ 1], b[odd ^ 1]);
-            multiply(a[odd], b[odd]);
-        }
+    for (int s = 0; s < S::STAGES; ++s) {
+        load(s);
+        advance();
     }
-    // (loads past the end are still writing zeros to the LDS, which nobody reads any more; they end before the block does)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-
-    // sums of two tiles side by side, lanes (q = lane / 16): 4q .. 4q + 3 of each; after the exchange eight columns of one tile
-    const auto eight = [&](const f32x4 &left, const f32x4 &right, float(&v)[8]) {
+    wait_and_meet<(S::STAGES - 1) * PER_STEP>();
+    read(0, 0);
+    uint32_t slot = 0;
+    for (uint32_t i = 0; i < steps; ++i) {
+        read(slot, 1);
+        multiply(0);
+        wait_and_meet<(S::STAGES - 2) * PER_STEP>();
+        load(slot);
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        read(slot, 0);
+        multiply(1);
+        advance();
+    }
+    // Sums to results by way of the LDS, some rows of tiles at a time, so that threads next to each other work on columns next to
+    // each other and memory sees whole rows of the tile (straight from the registers, in pieces of 64 bytes, 8192 x 8192 gates took
+    // 1020 us for 980).
+    constexpr int HIGH = S::TM < 2 ? 1 : 2, ROWS = S::WM * 16 * HIGH, PITCH = S::BN + 4; // four words: sixteen rows, all banks
+    constexpr int CHUNKS = COLUMNS / 8, ITEMS = ROWS * CHUNKS / S::THREADS;
+    static_assert(ROWS * PITCH * 4 <= S::LDS && ITEMS * S::THREADS == ROWS * CHUNKS, "the rows fit, and every thread has as many");
+    float *const rows = reinterpret_cast<float *>(lds);
+    const uint32_t mine = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS, c = c0 + 8 * chunk;
+    // (loads past the end have to be done writing zeros to the LDS)
+    wait_and_meet<0>();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(left[r]), __float_as_uint(right[r]), false, false);
-            v[r] = __uint_as_float(two[0]);
-            v[4 + r] = __uint_as_float(two[1]);
-        }
-    };
-    const uint32_t q = lane >> 4, within = 16 * (q & 1) + 8 * (q >> 1);
+    for (int step = 0; step < S::TM / HIGH; ++step) {
+        const auto row_of = [&](int item) {
+            const uint32_t r = mine + item * (S::THREADS / CHUNKS);
+            return m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
+        };
+        Pre pre[ITEMS];
+        if constexpr (KIND == SLOPE) // on their way while the sums are exchanged
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
-        const uint32_t m = m0 + (wm * S::TM + i) * 16 + (lane & 15);
-        if (KIND == GATE) {
+            for (int item = 0; item < ITEMS; ++item)
+                if (row_of(item) < p.M && c < p.N) load_pre(p.to, row_of(item), c, pre[item]);
+        if (step > 0) lds_barrier();
 #pragma unroll
-            for (int j = 0; j < S::TN / 2; j += 2) {
-                float g[8], u[8];
-                eight(sum[i][j], sum[i][j + 1], g);
-                eight(sum[i][S::TN / 2 + j], sum[i][S::TN / 2 + j + 1], u);
-                const uint32_t c = c0 + wn * HALF + j * 16 + within;
-                if (m < p.M && c < p.N) finish_gate<PARTS>(p.to, m, c, g, u);
+        for (int i = 0; i < HIGH; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+                *reinterpret_cast<f32x4 *>(rows + ((wm * HIGH + i) * 16 + (lane & 15)) * PITCH + (wn * S::TN + j) * 16 + 4 * (lane >> 4)) =
+                    sum[step * HIGH + i][j];
+        lds_barrier();
+#pragma unroll
+        for (int item = 0; item < ITEMS; ++item) {
+            const uint32_t m = row_of(item);
+            const float *row = rows + (mine + item * (S::THREADS / CHUNKS)) * PITCH;
+            if (m >= p.M || c >= p.N) continue;
+            // (of a wavefront's columns the first half are gates, the second the ups of the same units)
+            const uint32_t at = KIND == GATE ? 8 * chunk / HALF * (2 * HALF) + 8 * chunk % HALF : 8 * chunk;
+            float v[8], u[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                *reinterpret_cast<f32x4 *>(v + i) = *reinterpret_cast<const f32x4 *>(row + at + i);
+                if (KIND == GATE) *reinterpret_cast<f32x4 *>(u + i) = *reinterpret_cast<const f32x4 *>(row + at + HALF + i);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < S::TN; j += 2) {
-                float v[8];
-                eight(sum[i][j], sum[i][j + 1], v);
-                const uint32_t c = c0 + (wn * S::TN + j) * 16 + within;
-                if (m >= p.M || c >= p.N) continue;
-                if (KIND == STORE) finish_store<PARTS>(p.to, m, c, v);
-                if (KIND == SLOPE) finish_slope<PARTS>(p.to, m, c, v);
-                if (KIND == PARTIAL) store_eight((float *)p.to.out + ((uint64_t)share * p.M + m) * p.to.ld_out, c, (uint32_t)p.to.ld_out, v);
-            }
+            if constexpr (KIND == STORE) finish_store<PARTS>(p.to, m, c, v);
+            if constexpr (KIND == GATE) finish_gate<PARTS>(p.to, m, c, v, u);
+            if constexpr (KIND == SLOPE) finish_slope<PARTS>(p.to, m, c, v, pre[item]);
+            if constexpr (KIND == PARTIAL) store_eight((float *)p.to.out + ((uint64_t)share * p.M + m) * p.to.ld_out, c, (uint32_t)p.to.ld_out, v);
         }
     }
 }
@@ -410,7 +465,11 @@ __global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_
         float v[8];
         total(c, v);
         if (KIND == STORE) finish_store<PARTS>(to, m, c, v);
-        if (KIND == SLOPE) finish_slope<PARTS>(to, m, c, v);
+        if (KIND == SLOPE) {
+            Pre pre;
+            load_pre(to, m, c, pre);
+            finish_slope<PARTS>(to, m, c, v, pre);
+        }
         if (KIND == GATE) {
             float u[8];
             total(up + c, u);
