@@ -4,7 +4,7 @@
 //   backward  dh = dy Wd^T,  dg = dh u a'(g),  du = dh a(g),  dx = [dg | du] Wgu^T,  dWgu = x^T [dg | du],  dWd = h^T dy
 //
 // Six products; the activation, its derivative and the product of gate and up happen where a product's sums still are in registers.
-#include "product.h"
+#include "block_forward.h"
 
 namespace eck {
 namespace {
@@ -14,6 +14,12 @@ using namespace product;
 constexpr uint64_t MAX_BLOCK_WIDTH = 1 << 20; // offsets within a tile's 256 rows of twice as many columns fit 31 bits
 constexpr uint64_t MAX_TILES = 1 << 22;       // of a product
 constexpr uint64_t MAX_STRAIGHT_LD = 1 << 21;
+constexpr uint64_t MAX_SHARED = 1 << 27;      // sums of a product's shares
+
+#define ECK_TRY(expr)                         \
+    do {                                      \
+        if (int32_t rc_ = (expr)) return rc_; \
+    } while (0)
 
 uint64_t up_to(uint64_t x, uint64_t step) { return (x + step - 1) / step * step; }
 uint64_t padded(uint64_t bytes) { return up_to(bytes, 256); }
@@ -23,86 +29,130 @@ uint64_t padded(uint64_t bytes) { return up_to(bytes, 256); }
 struct Plan {
     int shape; // 0 small, 1 medium, 2 large tiles
     uint32_t shares;
+    double time;
 };
 
-// The tiles and shares of k that should take a product of M x N x K (N: columns of b) least time, in units of 32 k's of a large tile.
-Plan plan(uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
+// The shares of k that should take a product of M x N x K (N: columns of b) least time in tiles of a shape, and that time (us).  The
+// constants were fitted to 186 products of 17 blocks (1 to 131072 rows, widths 7 to 8192, both types), each in all shapes and up
+// to 64 shares: the choice takes 0.7 % more than the best, on average, and 15 % at most.
+Plan plan_shape(int shape, uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
 {
     static const struct {
-        uint32_t bm, bn, at_once; // blocks a compute unit
-        double step;              // what 32 k's of as many tiles take a compute unit
-    } SHAPES[3] = {{64, 64, 4, 0.55}, {128, 128, 2, 0.65}, {256, 256, 1, 1.0}};
-    const uint64_t steps = (K + BK - 1) / BK * (parts == 3 ? 6 : 1);
-    Plan best = {0, 1};
-    double least = 1e300;
-    for (int s = 0; s < 3; ++s) {
-        const uint64_t tiles = (M + SHAPES[s].bm - 1) / SHAPES[s].bm * ((N + SHAPES[s].bn - 1) / SHAPES[s].bn), slots = 256ull * SHAPES[s].at_once;
-        for (uint32_t shares = 1; shares <= 64; shares *= 2) {
-            if (shares > 1 && (steps / shares < 8 || tiles * shares > 2 * slots)) break;
-            const double rounds = (double)((tiles * shares + slots - 1) / slots);
-            // a tile's start and end: about eight steps; shares: a launch and eight bytes a sum
-            const double each = ((double)steps / shares + 8) * SHAPES[s].step;
-            const double join = shares > 1 ? 8.0 + 8.0 * (double)M * (double)N * shares / 2.0e6 : 0.0;
-            if (rounds * each + join < least) {
-                least = rounds * each + join;
-                best = {s, shares};
-            }
-        }
+        uint32_t side, at_once;   // blocks a compute unit
+        double step, alone, rest; // 64 k's of a tile when the unit is full, with nothing beside them, and a tile's start and end
+    } SHAPES[3] = {{64, 3, 0.27, 0.31, 2.2}, {128, 2, 0.5, 0.71, 3.0}, {256, 1, 1.29, 1.58, 8.3}};
+    const auto &of = SHAPES[shape];
+    const uint64_t steps = (K + BK - 1) / BK * (parts == 3 ? 6 : 1), tiles = (M + of.side - 1) / of.side * ((N + of.side - 1) / of.side);
+    Plan best = {shape, 1, 1e300};
+    for (uint32_t shares = 1; shares <= 64; shares *= 2) {
+        if (shares > 1 && (steps / shares < 2 || tiles * shares > 2048 || shares * M * N > MAX_SHARED)) break;
+        const uint64_t a_unit = (tiles * shares + 255) / 256, full = a_unit / of.at_once, last = a_unit % of.at_once;
+        const auto round = [&](uint64_t blocks) {
+            const double step = of.step * (double)blocks;
+            return of.rest + (double)steps / shares * (step > of.alone ? step : of.alone);
+        };
+        double time = (double)full * round(of.at_once) + (last ? round(last) : 0.0);
+        if (shares > 1) time += 3.6 + shares * (0.38 + (double)M * (double)N * 8.0 / 5.0e6); // a launch; sums written and read
+        if (time < best.time) best = {shape, shares, time};
+    }
+    return best;
+}
+
+Plan plan(uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
+{
+    Plan best = plan_shape(0, M, N, K, parts);
+    for (int shape = 1; shape < 3; ++shape) {
+        const Plan other = plan_shape(shape, M, N, K, parts);
+        if (other.time < best.time) best = other;
     }
     return best;
 }
 
 uint64_t tiles_of(uint64_t M, uint64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); } // the smallest tiles
 
-uint64_t partial_bytes(uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
+uint64_t shares_bytes(const Plan &how, uint64_t M, uint64_t N) { return how.shares > 1 ? padded(how.shares * M * up_to(N, 8) * 4) : 0; }
+uint64_t partial_bytes(uint64_t M, uint64_t N, uint64_t K, uint32_t parts) { return shares_bytes(plan(M, N, K, parts), M, N); }
+
+// kernels take blocks of more than 64 KB of LDS once they were told so
+template <class Kernel>
+int32_t allow_lds(Kernel kernel, int bytes)
 {
-    const Plan how = plan(M, N, K, parts);
-    return how.shares > 1 ? padded(how.shares * M * up_to(N, 8) * 4) : 0;
+    if (bytes > 65536) ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return ECK_OK;
 }
 
-template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
-int32_t launch_shape(const Product &p, hipStream_t st)
+uint32_t blocks_for(uint64_t chunks)
 {
-    auto kernel = product_kernel<S, A_FAST, B_FAST, KIND, PARTS>;
-    if (S::LDS > 65536)
-        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
-    hipLaunchKernelGGL(kernel, dim3(p.tiles_m * p.tiles_n * p.shares), dim3(S::THREADS), S::LDS, st, p);
+    const uint64_t blocks = (chunks + 255) / 256;
+    return (uint32_t)(blocks < 16384 ? blocks : 16384);
+}
+
+// Cuts a product into tiles of `side` and shares of k; shares leave their sums in `partial` (advanced past them) and a Join
+template <int KIND>
+void divide(Product &p, uint32_t side, uint32_t shares, char *&partial, Joins &joins)
+{
+    const Product whole = p;
+    p.shares = shares;
+    if (shares > 1) {
+        if (KIND == GATE) p.N = p.b_up + p.N; // gates and ups side by side, as in memory
+        p.to.out = partial;
+        p.to.ld_out = up_to(p.N, 8);
+        joins.one[joins.count++] = {(const float *)partial, shares, whole.M, whole.N, whole.b_up, p.to.ld_out, joins.chunks, whole.to};
+        joins.chunks += (uint64_t)whole.M * ((whole.N + 7) / 8);
+        partial += padded(shares * (uint64_t)p.M * p.to.ld_out * 4);
+    }
+    const uint32_t columns = KIND == GATE && shares == 1 ? side / 2 : side;
+    p.tiles_m = (uint32_t)(((uint64_t)p.M + side - 1) / side);
+    p.tiles_n = (p.N + columns - 1) / columns;
+}
+
+template <int KIND, int PARTS>
+int32_t launch_joins(const Joins &joins, hipStream_t st)
+{
+    if (joins.count == 0) return ECK_OK;
+    hipLaunchKernelGGL((join_kernel<KIND, PARTS>), dim3(blocks_for(joins.chunks)), dim3(256), 0, st, joins);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
 
 template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
-int32_t launch_tiles(Product p, uint32_t shares, float *partial, hipStream_t st)
+int32_t launch_tiles(const Product &p, hipStream_t st)
 {
-    constexpr uint32_t COLUMNS = KIND == GATE ? 2 : 1;
-    if (shares == 1) {
-        p.shares = 1;
-        p.tiles_m = (uint32_t)(((uint64_t)p.M + S::BM - 1) / S::BM);
-        p.tiles_n = (p.N + S::BN / COLUMNS - 1) / (S::BN / COLUMNS);
-        return launch_shape<S, A_FAST, B_FAST, KIND, PARTS>(p, st);
-    }
-    Product q = p;
-    q.N = KIND == GATE ? p.b_up + p.N : p.N; // gates and ups side by side, as in memory
-    q.shares = shares;
-    q.tiles_m = (uint32_t)(((uint64_t)p.M + S::BM - 1) / S::BM);
-    q.tiles_n = (q.N + S::BN - 1) / S::BN;
-    q.to.out = partial;
-    q.to.ld_out = up_to(q.N, 8);
-    if (int32_t rc = launch_shape<S, A_FAST, B_FAST, PARTIAL, PARTS>(q, st)) return rc;
-    const uint64_t blocks = ((uint64_t)p.M * ((p.N + 7) / 8) + 255) / 256;
-    hipLaunchKernelGGL((join_kernel<KIND, PARTS>), dim3((uint32_t)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, partial, shares, p.M, p.N,
-                       q.to.ld_out, p.b_up, p.to);
+    auto kernel = product_kernel<S, A_FAST, B_FAST, KIND, PARTS>;
+    ECK_TRY(allow_lds(kernel, S::LDS));
+    hipLaunchKernelGGL(kernel, dim3(p.blocks()), dim3(S::THREADS), S::LDS, st, p);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
 
 template <bool A_FAST, bool B_FAST, int KIND, int PARTS>
-int32_t launch(const Product &p, float *partial, hipStream_t st)
+int32_t launch_shape(int shape, const Product &p, hipStream_t st)
 {
-    const Plan how = plan(p.M, KIND == GATE ? (uint64_t)p.b_up + p.N : p.N, p.K, PARTS);
-    if (how.shape == 0) return launch_tiles<Small, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
-    if (how.shape == 1) return launch_tiles<Medium, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
-    return launch_tiles<Large, A_FAST, B_FAST, KIND, PARTS>(p, how.shares, partial, st);
+    if (shape == 0) return launch_tiles<Small, A_FAST, B_FAST, KIND, PARTS>(p, st);
+    if (shape == 1) return launch_tiles<Medium, A_FAST, B_FAST, KIND, PARTS>(p, st);
+    return launch_tiles<Large, A_FAST, B_FAST, KIND, PARTS>(p, st);
+}
+
+constexpr uint32_t SIDES[3] = {Small::BM, Medium::BM, Large::BM};
+
+template <bool A_FAST, bool B_FAST, int KIND, int PARTS>
+int32_t launch(Product p, const Plan &how, char *partial, hipStream_t st)
+{
+    Joins joins = {};
+    divide<KIND>(p, SIDES[how.shape], how.shares, partial, joins);
+    if (how.shares == 1) return launch_shape<A_FAST, B_FAST, KIND, PARTS>(how.shape, p, st);
+    ECK_TRY((launch_shape<A_FAST, B_FAST, STORE, PARTS>(how.shape, p, st)));
+    return launch_joins<KIND, PARTS>(joins, st);
+}
+
+template <class S, int PARTS>
+int32_t launch_group(const Gradients &g, hipStream_t st)
+{
+    auto kernel = gradients_kernel<S, PARTS>;
+    ECK_TRY(allow_lds(kernel, S::LDS));
+    hipLaunchKernelGGL(kernel, dim3(g.dx.blocks() + g.dw_gate_up.blocks() + g.dw_down.blocks()), dim3(S::THREADS), S::LDS, st, g);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
 }
 
 // ------------------------------------------------------------------------------------------------ operands
@@ -123,19 +173,23 @@ struct Workspace {
     }
 };
 
-// The matrix [rows][pieces * piece] as an operand: itself where it is one already, else copied to `room`.
+// The matrix [rows][pieces * piece] as an operand: itself where it is one already, else to be copied to `room`.
 template <class T>
-int32_t as_operand(const T *src, uint64_t ld, uint64_t rows, uint32_t piece, uint32_t pieces, char *room, Operand *out, hipStream_t st)
+Operand as_operand(const T *src, uint64_t ld, uint64_t rows, uint32_t piece, uint32_t pieces, char *room, Packs<T> &packs)
 {
-    if (sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16)) {
-        *out = {(const bf16 *)src, ld, 0};
-        return ECK_OK;
-    }
+    if (sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16)) return {(const bf16 *)src, ld, 0};
     const uint32_t pitch = (uint32_t)up_to(piece, 8);
-    const uint64_t width = (uint64_t)pitch * pieces, blocks = (rows * (width / 8) + 255) / 256;
-    *out = {(const bf16 *)room, width, rows * width};
-    hipLaunchKernelGGL(pack_kernel<T>, dim3((uint32_t)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, src, ld, (uint32_t)rows, piece, pieces,
-                       pitch, (bf16 *)room, rows * width);
+    const uint64_t width = (uint64_t)pitch * pieces;
+    packs.one[packs.count++] = {src, (bf16 *)room, ld, rows * width, packs.chunks, piece, pieces, pitch};
+    packs.chunks += rows * (width / 8);
+    return {(const bf16 *)room, width, rows * width};
+}
+
+template <class T>
+int32_t launch_packs(const Packs<T> &packs, hipStream_t st)
+{
+    if (packs.count == 0) return ECK_OK;
+    hipLaunchKernelGGL(pack_kernel<T>, dim3(blocks_for(packs.chunks)), dim3(256), 0, st, packs);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
@@ -143,10 +197,30 @@ int32_t as_operand(const T *src, uint64_t ld, uint64_t rows, uint32_t piece, uin
 struct Sizes {
     uint64_t n;
     uint32_t n_in, n_hidden, n_out;
-    uint32_t hidden() const { return (uint32_t)up_to(n_hidden, 8); } // columns of h, and from gates to ups, in operands
+    uint32_t hidden() const { return (uint32_t)up_to(n_hidden, 8); }     // columns of h, and from gates to ups, in operands
+    uint32_t pairs() const { return hidden() + n_hidden; }               // columns of (g | u)
 };
 
-template <class T>
+// The shape of tiles that all three gradients take, being one launch, and the shares of each: dx, dWgu, dWd, those wanted
+struct GradientPlans {
+    Plan of[3];
+};
+GradientPlans plan_gradients(const Sizes &s, uint32_t parts, bool dx, bool dw_gate_up, bool dw_down)
+{
+    GradientPlans best = {};
+    double least = 1e300;
+    for (int shape = 0; shape < 3; ++shape) {
+        const GradientPlans now = {{plan_shape(shape, s.n, s.n_in, s.pairs(), parts), plan_shape(shape, s.n_in, s.pairs(), s.n, parts),
+                                    plan_shape(shape, s.n_hidden, s.n_out, s.n, parts)}};
+        const double time = (dx ? now.of[0].time : 0.0) + (dw_gate_up ? now.of[1].time : 0.0) + (dw_down ? now.of[2].time : 0.0);
+        if (time < least) {
+            least = time;
+            best = now;
+        }
+    }
+    return best;
+}
+
 struct Rooms { // the workspace's pieces, in order
     uint64_t x, w_gate_up, w_down, dy, d_pre, h, partial;
     uint64_t total() const { return x + w_gate_up + w_down + dy + d_pre + h + partial; }
@@ -154,60 +228,152 @@ struct Rooms { // the workspace's pieces, in order
 
 uint64_t most(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-template <class T>
-Rooms<T> rooms(const Sizes &s, bool backward)
+Rooms rooms(const Sizes &s, uint32_t parts, bool backward)
 {
-    constexpr uint32_t P = parts_of<T>;
-    Rooms<T> r = {};
-    r.x = operand_bytes(s.n, up_to(s.n_in, 8), P);
-    r.w_gate_up = operand_bytes(s.n_in, 2ull * s.hidden(), P);
-    r.w_down = operand_bytes(s.n_hidden, up_to(s.n_out, 8), P);
-    r.h = operand_bytes(s.n, s.hidden(), P);
+    Rooms r = {};
+    r.x = operand_bytes(s.n, up_to(s.n_in, 8), parts);
+    r.w_gate_up = operand_bytes(s.n_in, 2ull * s.hidden(), parts);
+    r.w_down = operand_bytes(s.n_hidden, up_to(s.n_out, 8), parts);
+    r.h = operand_bytes(s.n, s.hidden(), parts);
     if (!backward) {
-        r.partial = most(partial_bytes(s.n, s.hidden() + s.n_hidden, s.n_in, P), partial_bytes(s.n, s.n_out, s.n_hidden, P));
+        r.partial = most(partial_bytes(s.n, s.pairs(), s.n_in, parts), partial_bytes(s.n, s.n_out, s.n_hidden, parts));
         return r;
     }
-    r.dy = operand_bytes(s.n, up_to(s.n_out, 8), P);
-    r.d_pre = operand_bytes(s.n, 2ull * s.hidden(), P);
-    r.partial = most(most(partial_bytes(s.n, s.n_hidden, s.n_out, P), partial_bytes(s.n, s.n_in, s.hidden() + s.n_hidden, P)),
-                     most(partial_bytes(s.n_in, s.hidden() + s.n_hidden, s.n, P), partial_bytes(s.n_hidden, s.n_out, s.n, P)));
+    r.dy = operand_bytes(s.n, up_to(s.n_out, 8), parts);
+    r.d_pre = operand_bytes(s.n, 2ull * s.hidden(), parts);
+    r.partial = partial_bytes(s.n, s.n_hidden, s.n_out, parts);
+    for (int wanted = 1; wanted < 8; ++wanted) { // (the shape of tiles depends on which gradients are)
+        const bool dx = wanted & 1, dw_gate_up = wanted & 2, dw_down = wanted & 4;
+        const GradientPlans how = plan_gradients(s, parts, dx, dw_gate_up, dw_down);
+        r.partial = most(r.partial, (dx ? shares_bytes(how.of[0], s.n, s.n_in) : 0) + (dw_gate_up ? shares_bytes(how.of[1], s.n_in, s.pairs()) : 0) +
+                                        (dw_down ? shares_bytes(how.of[2], s.n_hidden, s.n_out) : 0));
+    }
     return r;
 }
 
 // ------------------------------------------------------------------------------------------------ passes
 
-#define ECK_TRY(expr)                   \
-    do {                                \
-        if (int32_t rc_ = (expr)) return rc_; \
-    } while (0)
-
 constexpr uint32_t NO_GAP = 0xFFFFFFFFu;
+
+// few rows: the weights' bytes (block_forward.h)
+constexpr uint32_t FEW_ROWS = 4;
+
+// of the k's, so that all compute units have a block if every one of them gets two rounds of loads at least
+uint32_t vector_shares(uint32_t K, uint32_t N, uint32_t line)
+{
+    const uint32_t blocks = (N + line - 1) / line, wanted = (255 + blocks) / blocks, most = K / 256;
+    return wanted < most ? wanted : most > 1 ? most : 1;
+}
+// bytes of the shares of (g | u), and of y
+struct VectorRooms {
+    uint32_t shares, shares_y;
+    uint64_t sums, sums_y;
+};
+VectorRooms vector_rooms(const Sizes &s, uint32_t parts)
+{
+    const uint32_t line = parts == 3 ? 32 : 64;
+    VectorRooms r = {vector_shares(s.n_in, s.n_hidden, line), vector_shares(s.n_hidden, s.n_out, line), 0, 0};
+    r.sums = padded(r.shares * s.n * 2 * s.n_hidden * 4);
+    r.sums_y = r.shares_y > 1 ? padded(r.shares_y * s.n * up_to(s.n_out, 8) * 4) : 0;
+    return r;
+}
+
+template <class T, bool PAIRS, int ROWS>
+int32_t launch_vector_rows(const Rows &rows, uint32_t shares, const T *w, uint64_t ld_w, uint32_t N, T *out, uint64_t ld_out, float *sums,
+                           hipStream_t st)
+{
+    constexpr int LINE = 8 * Chunk<T>::N, SUMS = 16 * ROWS * LINE * (PAIRS ? 2 : 1), LDS = (ROWS * VECTOR_K > SUMS ? ROWS * VECTOR_K : SUMS) * 4;
+    auto kernel = vector_kernel<T, PAIRS, ROWS>;
+    ECK_TRY(allow_lds(kernel, LDS));
+    hipLaunchKernelGGL(kernel, dim3((N + LINE - 1) / LINE, shares), dim3(1024), LDS, st, rows, w, ld_w, N, N, out, ld_out, sums);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+template <class T, bool PAIRS>
+int32_t launch_vector(const Rows &rows, uint32_t shares, const T *w, uint64_t ld_w, uint32_t N, T *out, uint64_t ld_out, float *sums, hipStream_t st)
+{
+    if (rows.n == 1) return launch_vector_rows<T, PAIRS, 1>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    if (rows.n == 2) return launch_vector_rows<T, PAIRS, 2>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    return launch_vector_rows<T, PAIRS, 4>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+}
+
+template <class T>
+int32_t forward_few(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, const T *w_down, int32_t act, T *y, uint64_t ld_y, float *pre,
+                    void *ws, hipStream_t st)
+{
+    const VectorRooms room = vector_rooms(s, parts_of<T>);
+    float *sums = (float *)ws, *sums_y = (float *)((char *)ws + room.sums);
+    const uint32_t n = (uint32_t)s.n;
+    ECK_TRY((launch_vector<T, true>({x, nullptr, ld_x, nullptr, n, s.n_in, 0, act}, room.shares, w_gate_up, 2ull * s.n_hidden, s.n_hidden, nullptr, 0,
+                                    sums, st)));
+    const Rows h = {nullptr, sums, 0, pre, n, s.n_hidden, room.shares, act};
+    if (room.shares_y == 1) return launch_vector<T, false>(h, 1, w_down, s.n_out, s.n_out, y, ld_y, nullptr, st);
+    const uint64_t ld = up_to(s.n_out, 8);
+    ECK_TRY((launch_vector<T, false>(h, room.shares_y, w_down, s.n_out, s.n_out, nullptr, ld, sums_y, st)));
+    Joins joins = {};
+    joins.count = 1, joins.chunks = s.n * ((s.n_out + 7) / 8);
+    joins.one[0].partial = sums_y, joins.one[0].shares = room.shares_y, joins.one[0].M = n, joins.one[0].N = s.n_out, joins.one[0].ld = ld;
+    joins.one[0].to.out = y, joins.one[0].to.ld_out = ld_y, joins.one[0].to.piece = s.n_out, joins.one[0].to.pitch = NO_GAP;
+    return launch_joins<STORE, parts_of<T>>(joins, st);
+}
+
+// narrow blocks of many rows
+constexpr uint32_t NARROW = 256;
+constexpr uint64_t NARROW_ROWS = 8192;
+template <int DK, int ON>
+int32_t launch_narrow_shape(const Narrow &p, hipStream_t st)
+{
+    using S = NarrowShape<DK, ON>;
+    auto kernel = narrow_kernel<DK, ON>;
+    ECK_TRY(allow_lds(kernel, S::LDS));
+    hipLaunchKernelGGL(kernel, dim3((p.n - 1) / S::ROWS + 1), dim3(64 * S::WAVES), S::LDS, st, p);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+template <int DK>
+int32_t launch_narrow_in(const Narrow &p, hipStream_t st)
+{
+    if (p.n_out <= 64) return launch_narrow_shape<DK, 4>(p, st);
+    if (p.n_out <= 128) return launch_narrow_shape<DK, 8>(p, st);
+    return launch_narrow_shape<DK, 16>(p, st);
+}
+int32_t launch_narrow(const Narrow &p, hipStream_t st)
+{
+    if (p.n_in <= 64) return launch_narrow_in<2>(p, st);
+    if (p.n_in <= 128) return launch_narrow_in<4>(p, st);
+    return launch_narrow_in<8>(p, st);
+}
 
 template <class T>
 int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, const T *w_down, int32_t act, T *y, uint64_t ld_y, float *pre,
                 void *ws, hipStream_t st)
 {
     constexpr uint32_t P = parts_of<T>;
-    const Rooms<T> room = rooms<T>(s, false);
+    if (s.n <= FEW_ROWS) return forward_few(x, ld_x, s, w_gate_up, w_down, act, y, ld_y, pre, ws, st);
+    const Rooms room = rooms(s, P, false);
     Workspace space = {(char *)ws};
-    Operand ox, ogu, od;
-    ECK_TRY(as_operand(x, ld_x, s.n, s.n_in, 1, space.take(room.x), &ox, st));
-    ECK_TRY(as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, space.take(room.w_gate_up), &ogu, st));
-    ECK_TRY(as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, space.take(room.w_down), &od, st));
+    Packs<T> packs = {};
+    const Operand ox = as_operand(x, ld_x, s.n, s.n_in, 1, space.take(room.x), packs);
+    const Operand ogu = as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, space.take(room.w_gate_up), packs);
+    const Operand od = as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, space.take(room.w_down), packs);
     const Operand h = {(bf16 *)space.take(room.h), s.hidden(), s.n * s.hidden()};
-    float *partial = (float *)space.take(room.partial);
+    char *partial = space.take(room.partial);
+    ECK_TRY(launch_packs(packs, st));
+    if constexpr (P == 1)
+        if (!pre && s.n_in <= NARROW && s.n_out <= NARROW && s.n >= NARROW_ROWS)
+            return launch_narrow({ox, ogu, od, (uint32_t)s.n, s.n_in, s.n_hidden, s.n_out, s.hidden(), act, y, ld_y}, st);
 
     Product p = {};
     p.a = ox, p.b = ogu, p.b_up = s.hidden();
     p.M = (uint32_t)s.n, p.N = s.n_hidden, p.K = s.n_in;
     p.to.out = const_cast<bf16 *>(h.p), p.to.ld_out = h.ld, p.to.part_out = h.part, p.to.pre = pre, p.to.n_hidden = s.n_hidden, p.to.act = act;
-    ECK_TRY((launch<true, false, GATE, P>(p, partial, st)));
+    ECK_TRY((launch<true, false, GATE, P>(p, plan(s.n, s.pairs(), s.n_in, P), partial, st)));
 
     p = {};
     p.a = h, p.b = od;
     p.M = (uint32_t)s.n, p.N = s.n_out, p.K = s.n_hidden;
     p.to.out = y, p.to.ld_out = ld_y, p.to.piece = s.n_out, p.to.pitch = NO_GAP;
-    return launch<true, false, STORE, P>(p, partial, st);
+    return launch<true, false, STORE, P>(p, plan(s.n, s.n_out, s.n_hidden, P), partial, st);
 }
 
 template <class T>
@@ -215,15 +381,19 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
                  uint64_t ld_dy, T *dx, uint64_t ld_dx, T *dw_gate_up, T *dw_down, void *ws, hipStream_t st)
 {
     constexpr uint32_t P = parts_of<T>;
-    const Rooms<T> room = rooms<T>(s, true);
+    const Rooms room = rooms(s, P, true);
     Workspace space = {(char *)ws};
     char *room_x = space.take(room.x), *room_gu = space.take(room.w_gate_up), *room_d = space.take(room.w_down), *room_dy = space.take(room.dy);
     const Operand d_pre = {(bf16 *)space.take(room.d_pre), 2ull * s.hidden(), s.n * 2 * s.hidden()};
     const Operand h = {(bf16 *)space.take(room.h), s.hidden(), s.n * s.hidden()};
-    float *partial = (float *)space.take(room.partial);
-    Operand ody, od, other;
-    ECK_TRY(as_operand(dy, ld_dy, s.n, s.n_out, 1, room_dy, &ody, st));
-    ECK_TRY(as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, room_d, &od, st));
+    char *partial = space.take(room.partial);
+    Packs<T> packs = {};
+    const Operand ody = as_operand(dy, ld_dy, s.n, s.n_out, 1, room_dy, packs);
+    const Operand od = as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, room_d, packs);
+    Operand ogu = {}, ox = {};
+    if (dx) ogu = as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, room_gu, packs);
+    if (dw_gate_up) ox = as_operand(x, ld_x, s.n, s.n_in, 1, room_x, packs);
+    ECK_TRY(launch_packs(packs, st));
 
     Product p = {}; // dh, and from it dg, du and h
     p.a = ody, p.b = od;
@@ -231,31 +401,33 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     p.to.out = dw_down ? const_cast<bf16 *>(h.p) : nullptr, p.to.ld_out = h.ld, p.to.part_out = h.part;
     p.to.pre = const_cast<float *>(pre), p.to.n_hidden = s.n_hidden, p.to.act = act, p.to.pitch = s.hidden();
     p.to.d_pre = const_cast<bf16 *>(d_pre.p), p.to.ld_d = d_pre.ld, p.to.part_d = d_pre.part;
-    ECK_TRY((launch<true, true, SLOPE, P>(p, partial, st)));
+    ECK_TRY((launch<true, true, SLOPE, P>(p, plan(s.n, s.n_hidden, s.n_out, P), partial, st)));
+
+    const GradientPlans how = plan_gradients(s, P, dx, dw_gate_up, dw_down);
+    const uint32_t side = SIDES[how.of[0].shape];
+    Gradients g = {};
+    Joins joins = {};
     if (dx) {
-        ECK_TRY(as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, room_gu, &other, st));
-        p = {};
-        p.a = d_pre, p.b = other;
-        p.M = (uint32_t)s.n, p.N = s.n_in, p.K = s.hidden() + s.n_hidden;
-        p.to.out = dx, p.to.ld_out = ld_dx, p.to.piece = s.n_in, p.to.pitch = NO_GAP;
-        ECK_TRY((launch<true, true, STORE, P>(p, partial, st)));
+        g.dx.a = d_pre, g.dx.b = ogu, g.dx.M = (uint32_t)s.n, g.dx.N = s.n_in, g.dx.K = s.pairs();
+        g.dx.to.out = dx, g.dx.to.ld_out = ld_dx, g.dx.to.piece = s.n_in, g.dx.to.pitch = NO_GAP;
+        divide<STORE>(g.dx, side, how.of[0].shares, partial, joins);
     }
     if (dw_gate_up) {
-        ECK_TRY(as_operand(x, ld_x, s.n, s.n_in, 1, room_x, &other, st));
-        p = {};
-        p.a = other, p.b = d_pre;
-        p.M = s.n_in, p.N = s.hidden() + s.n_hidden, p.K = (uint32_t)s.n;
-        p.to.out = dw_gate_up, p.to.ld_out = 2ull * s.n_hidden, p.to.piece = s.n_hidden, p.to.pitch = s.hidden();
-        ECK_TRY((launch<false, false, STORE, P>(p, partial, st)));
+        Product &q = g.dw_gate_up;
+        q.a = ox, q.b = d_pre, q.M = s.n_in, q.N = s.pairs(), q.K = (uint32_t)s.n;
+        q.to.out = dw_gate_up, q.to.ld_out = 2ull * s.n_hidden, q.to.piece = s.n_hidden, q.to.pitch = s.hidden();
+        divide<STORE>(q, side, how.of[1].shares, partial, joins);
     }
     if (dw_down) {
-        p = {};
-        p.a = h, p.b = ody;
-        p.M = s.n_hidden, p.N = s.n_out, p.K = (uint32_t)s.n;
-        p.to.out = dw_down, p.to.ld_out = s.n_out, p.to.piece = s.n_out, p.to.pitch = NO_GAP;
-        ECK_TRY((launch<false, false, STORE, P>(p, partial, st)));
+        Product &q = g.dw_down;
+        q.a = h, q.b = ody, q.M = s.n_hidden, q.N = s.n_out, q.K = (uint32_t)s.n;
+        q.to.out = dw_down, q.to.ld_out = s.n_out, q.to.piece = s.n_out, q.to.pitch = NO_GAP;
+        divide<STORE>(q, side, how.of[2].shares, partial, joins);
     }
-    return ECK_OK;
+    if (how.of[0].shape == 0) ECK_TRY((launch_group<Small, P>(g, st)));
+    else if (how.of[0].shape == 1) ECK_TRY((launch_group<Medium, P>(g, st)));
+    else ECK_TRY((launch_group<Large, P>(g, st)));
+    return launch_joins<STORE, P>(joins, st);
 }
 
 bool sizes_ok(const Sizes &s)
@@ -269,7 +441,12 @@ bool act_ok(int32_t act) { return act == ECK_ACT_SILU || act == ECK_ACT_GELU || 
 uint64_t workspace_bytes(const Sizes &s, int32_t dtype, bool backward)
 {
     if (s.n == 0 || s.n_in == 0 || s.n_hidden == 0 || s.n_out == 0 || !is_dtype(dtype) || !sizes_ok(s)) return 0;
-    return dtype == ECK_F32 ? rooms<float>(s, backward).total() : rooms<bf16>(s, backward).total();
+    const uint32_t parts = dtype == ECK_F32 ? 3 : 1;
+    if (!backward && s.n <= FEW_ROWS) {
+        const VectorRooms room = vector_rooms(s, parts);
+        return room.sums + room.sums_y;
+    }
+    return rooms(s, parts, backward).total();
 }
 
 } // namespace

@@ -42,16 +42,15 @@ struct Operand {
 
 // What becomes of the sums
 enum Kind {
-    STORE,   // C
-    PARTIAL, // fp32 sums of a share of the k's: [share][M][ld_out]
-    GATE,    // columns are pairs (g, u): h = a(g) u, and (g, u) as they are where asked for
-    SLOPE    // sums are dh: dg = dh u a'(g), du = dh a(g) and h = a(g) u from the stored (g, u)
+    STORE, // C, or, where the k's are in several shares, fp32 sums of each: [share][M][ld_out]
+    GATE,  // columns are pairs (g, u): h = a(g) u, and (g, u) as they are where asked for
+    SLOPE  // sums are dh: dg = dh u a'(g), du = dh a(g) and h = a(g) u from the stored (g, u)
 };
 
 // STORE takes columns [0, N) to out; where columns have a gap (the padding between gate and up) only those of the two pieces
 // [0, piece) and [pitch, pitch + piece) exist, and lie next to each other in out.
 struct Target {
-    void *out;        // STORE: element type; PARTIAL: float; GATE, SLOPE: h, an operand of the next product
+    void *out;        // STORE: element type, or float for shares; GATE, SLOPE: h, an operand of the next product
     uint64_t ld_out, part_out;
     uint32_t piece, pitch;
     float *pre;       // [M][2 * n_hidden] sums (g | u): GATE writes them (or NULL), SLOPE reads them
@@ -67,6 +66,7 @@ struct Product {
     uint32_t b_up;    // GATE: columns from a gate's to its up column in b
     uint32_t tiles_m, tiles_n, shares;
     Target to;
+    __host__ __device__ uint32_t blocks() const { return tiles_m * tiles_n * shares; }
 };
 
 // ------------------------------------------------------------------------------------------------ results
@@ -279,9 +279,8 @@ typedef Shape<128, 128, 2, 2, 2> Medium;
 typedef Shape<64, 64, 4, 1, 3> Small;
 
 template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
-__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void product_kernel(const Product p)
+__device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t total, unsigned char *lds)
 {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     typedef Stage<S::BM, A_FAST, S::WAVES> StageA;
     typedef Stage<S::BN, B_FAST, S::WAVES> StageB;
     constexpr int PER_STEP = StageA::LOADS + StageB::LOADS;
@@ -290,8 +289,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
 
     // Blocks go round the eight dies; the blocks of a die take neighbouring tiles, in panels eight tiles high, so that its L2
     // holds the rows and columns they share.
-    const uint32_t total = gridDim.x, tiles = p.tiles_m * p.tiles_n, die = blockIdx.x & 7, left_over = total & 7;
-    const uint32_t number = die * (total >> 3) + min(die, left_over) + (blockIdx.x >> 3);
+    const uint32_t tiles = p.tiles_m * p.tiles_n, die = block & 7, left_over = total & 7;
+    const uint32_t number = die * (total >> 3) + min(die, left_over) + (block >> 3);
     const uint32_t share = number / tiles, tile = number % tiles, panel = tile / (8 * p.tiles_n), in_panel = tile % (8 * p.tiles_n);
     const uint32_t high = min(8u, p.tiles_m - 8 * panel);
     const uint32_t m0 = (8 * panel + in_panel % high) * S::BM, c0 = in_panel / high * COLUMNS;
@@ -436,68 +435,124 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
                 *reinterpret_cast<f32x4 *>(v + i) = *reinterpret_cast<const f32x4 *>(row + at + i);
                 if (KIND == GATE) *reinterpret_cast<f32x4 *>(u + i) = *reinterpret_cast<const f32x4 *>(row + at + HALF + i);
             }
-            if constexpr (KIND == STORE) finish_store<PARTS>(p.to, m, c, v);
+            if constexpr (KIND == STORE) {
+                if (p.shares == 1) finish_store<PARTS>(p.to, m, c, v);
+                else store_eight((float *)p.to.out + ((uint64_t)share * p.M + m) * p.to.ld_out, c, (uint32_t)p.to.ld_out, v);
+            }
             if constexpr (KIND == GATE) finish_gate<PARTS>(p.to, m, c, v, u);
             if constexpr (KIND == SLOPE) finish_slope<PARTS>(p.to, m, c, v, pre[item]);
-            if constexpr (KIND == PARTIAL) store_eight((float *)p.to.out + ((uint64_t)share * p.M + m) * p.to.ld_out, c, (uint32_t)p.to.ld_out, v);
         }
     }
 }
 
-// The shares of a product whose k's were divided, added in order; then as above.  A thread has eight columns.
-template <int KIND, int PARTS>
-__global__ __launch_bounds__(256) void join_kernel(const float *partial, uint32_t shares, uint32_t M, uint32_t N, uint64_t ld, uint32_t up,
-                                                   const Target to)
+template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void product_kernel(const Product p)
 {
-    const uint32_t chunks = (N + 7) / 8;
-    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < (uint64_t)M * chunks; at += (uint64_t)gridDim.x * 256) {
-        const uint32_t m = (uint32_t)(at / chunks), c = (uint32_t)(at % chunks) * 8;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    work<S, A_FAST, B_FAST, KIND, PARTS>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// The three gradients, which wait for nothing but dg, du and h, in one launch: dx, of operands along k, then the weights', of
+// operands along rows and columns.  A product of no blocks is left out.
+struct Gradients {
+    Product dx, dw_gate_up, dw_down;
+};
+template <class S, int PARTS>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void gradients_kernel(const Gradients g)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const uint32_t first = g.dx.blocks(), second = g.dw_gate_up.blocks();
+    if (blockIdx.x < first) {
+        work<S, true, true, STORE, PARTS>(g.dx, blockIdx.x, first, lds);
+    } else {
+        const bool up = blockIdx.x - first < second;
+        work<S, false, false, STORE, PARTS>(up ? g.dw_gate_up : g.dw_down, blockIdx.x - first - (up ? 0 : second), up ? second : g.dw_down.blocks(), lds);
+    }
+}
+
+// The shares of products whose k's were divided, added in order; then as above.  A thread has eight columns.
+struct Join {
+    const float *partial;
+    uint32_t shares, M, N, up; // up: from gates to ups
+    uint64_t ld, first;        // first: chunk of eight columns where this one starts, of all of the launch's
+    Target to;
+};
+struct Joins {
+    Join one[3];
+    uint32_t count;
+    uint64_t chunks;
+};
+template <int KIND, int PARTS>
+__global__ __launch_bounds__(256) void join_kernel(const Joins joins)
+{
+    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < joins.chunks; at += (uint64_t)gridDim.x * 256) {
+        int which = 0;
+        while (which + 1 < (int)joins.count && at >= joins.one[which + 1].first) ++which;
+        const Join &j = joins.one[which];
+        const uint32_t chunks = (j.N + 7) / 8, m = (uint32_t)((at - j.first) / chunks), c = (uint32_t)((at - j.first) % chunks) * 8;
         const auto total = [&](uint32_t column, float(&v)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-            for (uint32_t s = 0; s < shares; ++s) {
+#pragma unroll 4
+            for (uint32_t s = 0; s < j.shares; ++s) {
                 float some[8];
-                load_eight(partial + ((uint64_t)s * M + m) * ld, column, (uint32_t)ld, some);
+                load_eight(j.partial + ((uint64_t)s * j.M + m) * j.ld, column, (uint32_t)j.ld, some);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += some[i];
             }
         };
         float v[8];
         total(c, v);
-        if (KIND == STORE) finish_store<PARTS>(to, m, c, v);
+        if (KIND == STORE) finish_store<PARTS>(j.to, m, c, v);
         if (KIND == SLOPE) {
             Pre pre;
-            load_pre(to, m, c, pre);
-            finish_slope<PARTS>(to, m, c, v, pre);
+            load_pre(j.to, m, c, pre);
+            finish_slope<PARTS>(j.to, m, c, v, pre);
         }
         if (KIND == GATE) {
             float u[8];
-            total(up + c, u);
-            finish_gate<PARTS>(to, m, c, v, u);
+            total(j.up + c, u);
+            finish_gate<PARTS>(j.to, m, c, v, u);
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ operands
 
-// A matrix as operands want it: rows of two pieces of `piece` columns (one, if pieces is 1), each padded with zeros to `pitch`
-// (a multiple of eight); fp32 ones in three parts.  A thread has eight columns.
+// Matrices as operands want them: rows of two pieces of `piece` columns (one, if pieces is 1), each padded with zeros to `pitch` (a
+// multiple of eight); fp32 ones in three parts.  A thread has eight columns.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(const T *src, uint64_t ld, uint32_t rows, uint32_t piece, uint32_t pieces, uint32_t pitch,
-                                                   bf16 *dst, uint64_t part)
+struct Pack {
+    const T *src;
+    bf16 *dst;
+    uint64_t ld, part, first; // first: chunk of eight columns where this one starts, of all of the launch's
+    uint32_t piece, pieces, pitch;
+};
+template <class T>
+struct Packs {
+    Pack<T> one[4];
+    uint32_t count;
+    uint64_t chunks;
+};
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const Packs<T> packs)
 {
-    const uint32_t chunks = pitch / 8 * pieces;
-    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < (uint64_t)rows * chunks; at += (uint64_t)gridDim.x * 256) {
-        const uint32_t r = (uint32_t)(at / chunks), c = (uint32_t)(at % chunks) * 8, shift = c >= pitch ? pitch : 0;
+    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < packs.chunks; at += (uint64_t)gridDim.x * 256) {
+        int which = 0;
+        while (which + 1 < (int)packs.count && at >= packs.one[which + 1].first) ++which;
+        const Pack<T> &p = packs.one[which];
+        const uint32_t chunks = p.pitch / 8 * p.pieces;
+        const uint64_t r = (at - p.first) / chunks;
+        const uint32_t c = (uint32_t)((at - p.first) % chunks) * 8, shift = c >= p.pitch ? p.pitch : 0;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; i += Chunk<T>::N) {
             float some[Chunk<T>::N];
-            load_chunk(src + r * ld + (shift ? piece : 0), c - shift + i, piece, some);
+            load_chunk(p.src + r * p.ld + (shift ? p.piece : 0), c - shift + i, p.piece, some);
 #pragma unroll
             for (int j = 0; j < Chunk<T>::N; ++j) v[i + j] = some[j];
         }
-        store_operand<sizeof(T) == 4 ? 3 : 1>(dst + (uint64_t)r * pitch * pieces + c, part, v);
+        store_operand<sizeof(T) == 4 ? 3 : 1>(p.dst + r * ((uint64_t)p.pitch * p.pieces) + c, p.part, v);
     }
 }
 
