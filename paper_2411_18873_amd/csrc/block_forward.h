@@ -61,7 +61,7 @@ __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *
                         rows.pre[(uint64_t)r * 2 * K + k0 + k] = g;
                         rows.pre[(uint64_t)r * 2 * K + K + k0 + k] = u;
                     }
-                    x = (float)(T)(gate_of(rows.act, g).value * u);
+                    with_act(rows.act, [&](auto act) { x = (float)(T)(gate_as<decltype(act)::value>(g).value * u); });
                 }
                 shared[r * VECTOR_K + k] = x;
             }
@@ -127,7 +127,6 @@ __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *
 struct Narrow {
     Operand x, w_gate_up, w_down;
     uint32_t n, n_in, n_hidden, n_out, up;
-    int32_t act;
     bf16 *y;
     uint64_t ld_y;
 };
@@ -139,9 +138,12 @@ struct NarrowShape {
     static constexpr int PIECES_GU = 4 * DK, PIECES = PIECES_GU + ON, LOADS = PIECES / WAVES; // of 1 KB
     static constexpr int STAGE = PIECES * 1024, LDS = STAGE * SLOTS;
     static_assert(PIECES % WAVES == 0, "every wavefront issues the same number of loads");
+    // two sets of sums of gates and ups where the registers hold them (2^18 rows, us with and without: 128-512-128 114 and 128,
+    // 64-256-64 40.7 and 40.4, 16384 rows of it 8.5 and 9.0; 64-1024-256 228 and 215)
+    static constexpr bool AHEAD = ON <= 8;
 };
 
-template <int DK, int ON>
+template <int DK, int ON, int ACT>
 __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
 {
     using S = NarrowShape<DK, ON>;
@@ -198,43 +200,74 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
 #pragma unroll
         for (int j = 0; j < ON; ++j) y[i][j] = f32x4{0, 0, 0, 0};
 
-    load(0, 0);
-    load(32, 1);
-    uint32_t slot = 0;
-    for (uint32_t first = 0; first < p.n_hidden; first += 32) {
-        wait_and_meet<S::LOADS>(); // these units have come, and everybody is through with the ones before
+    const auto multiply_up = [&](uint32_t slot, f32x4(&to)[4][2]) {
         const uint32_t at = lds0 + slot * S::STAGE;
-        load(first + 64, slot >= 1 ? slot - 1 : 2);
-        f32x4 pre[4][2]; // gates 0 .. 15, 16 .. 31, ups
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) pre[t][i] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < 2; ++i) to[t][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < DK; ++k)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const bf16x8 w = StageGU::read(at, t, k);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) pre[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[i][k], pre[t][i], 0, 0, 0);
+                for (int i = 0; i < 2; ++i) to[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[i][k], to[t][i], 0, 0, 0);
             }
-        bf16x8 h[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = (bf16)(gate_of(p.act, pre[e / 4][i][e % 4]).value * pre[2 + e / 4][i][e % 4]);
+    };
+    const auto multiply_down = [&](uint32_t slot, const bf16x8(&h)[2]) {
+        typedef __attribute__((address_space(3))) s16x4 *Half;
+        const uint32_t at = lds0 + slot * S::STAGE + S::PIECES_GU * 1024, k = 4 * g + (r >> 2); // and 16 more
 #pragma unroll
         for (int j = 0; j < ON; ++j) {
-            typedef __attribute__((address_space(3))) s16x4 *Half;
-            const uint32_t k = 4 * g + (r >> 2); // and 16 more
-            const uint32_t from = at + S::PIECES_GU * 1024 + k * (ON * 32) + ((j ^ down_swizzle(k)) << 5) + ((r & 3) << 3);
+            const uint32_t from = at + k * (ON * 32) + ((j ^ down_swizzle(k)) << 5) + ((r & 3) << 3);
             const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half)(uintptr_t)from);
             const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half)(uintptr_t)(from + 16 * ON * 32));
             const bf16x8 w = __builtin_bit_cast(bf16x8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int i = 0; i < 2; ++i) y[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, h[i], y[i][j], 0, 0, 0);
         }
-        slot = slot == 2 ? 0 : slot + 1;
+    };
+
+    const auto activate = [&](const f32x4(&pre)[4][2], bf16x8(&h)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] = (bf16)(gate_as<ACT>(pre[e / 4][i][e % 4]).value * pre[2 + e / 4][i][e % 4]);
+    };
+
+    load(0, 0);
+    load(32, 1);
+    wait_and_meet<S::LOADS>();
+    uint32_t slot = 0;
+    f32x4 pre[2][4][2]; // gates 0 .. 15, 16 .. 31, ups
+    if constexpr (S::AHEAD) {
+        // The next units' gates and ups are multiplied while the activations of these are worked out, then these units' share of
+        // y.  At the meeting the next units have come, and everybody is through with the ones before these.
+        multiply_up(0, pre[0]);
+        for (uint32_t first = 0; first < p.n_hidden; first += 64) {
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) { // (units past the last: zeros)
+                const uint32_t next = slot == 2 ? 0 : slot + 1;
+                wait_and_meet<0>();
+                load(first + 32 * odd + 64, next == 2 ? 0 : next + 1);
+                multiply_up(next, pre[odd ^ 1]);
+                bf16x8 h[2];
+                activate(pre[odd], h);
+                multiply_down(slot, h);
+                slot = next;
+            }
+        }
+    } else {
+        for (uint32_t first = 0; first < p.n_hidden; first += 32) {
+            if (first) wait_and_meet<S::LOADS>(); // these units have come, and everybody is through with the ones before
+            load(first + 64, slot >= 1 ? slot - 1 : 2);
+            multiply_up(slot, pre[0]);
+            bf16x8 h[2];
+            activate(pre[0], h);
+            multiply_down(slot, h);
+            slot = slot == 2 ? 0 : slot + 1;
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // (zeros for units past the last end before the block does)
 

@@ -317,31 +317,37 @@ int32_t forward_few(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_u
     return launch_joins<STORE, parts_of<T>>(joins, st);
 }
 
-// narrow blocks of many rows
-constexpr uint32_t NARROW = 256;
-constexpr uint64_t NARROW_ROWS = 8192;
-template <int DK, int ON>
+// Narrow blocks of many rows.  One kernel against two products (us): 64-256-64 on 16384 and 65536 rows 8.5 and 12.1, 13.3 and 35;
+// 128-512-128 18.7 and 21.9, 33.7 and 64.7; 64-1024-256 36 and 38, 57 and 114; 128-512-256 24.8 and 25.1, 59 and 74; on 4096 rows
+// 9.9 and 8.8, 23 and 12 and 45 and 16; 256-1024-256 on 65536 203 and 177.
+constexpr uint32_t NARROW_IN = 128, NARROW_OUT = 256;
+bool narrow(const Sizes &s) { return s.n_in <= NARROW_IN && s.n_out <= NARROW_OUT && s.n >= 12288; }
+template <int ACT, int DK, int ON>
 int32_t launch_narrow_shape(const Narrow &p, hipStream_t st)
 {
     using S = NarrowShape<DK, ON>;
-    auto kernel = narrow_kernel<DK, ON>;
+    auto kernel = narrow_kernel<DK, ON, ACT>;
     ECK_TRY(allow_lds(kernel, S::LDS));
     hipLaunchKernelGGL(kernel, dim3((p.n - 1) / S::ROWS + 1), dim3(64 * S::WAVES), S::LDS, st, p);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
-template <int DK>
+template <int ACT, int DK>
 int32_t launch_narrow_in(const Narrow &p, hipStream_t st)
 {
-    if (p.n_out <= 64) return launch_narrow_shape<DK, 4>(p, st);
-    if (p.n_out <= 128) return launch_narrow_shape<DK, 8>(p, st);
-    return launch_narrow_shape<DK, 16>(p, st);
+    if (p.n_out <= 64) return launch_narrow_shape<ACT, DK, 4>(p, st);
+    if (p.n_out <= 128) return launch_narrow_shape<ACT, DK, 8>(p, st);
+    return launch_narrow_shape<ACT, DK, 16>(p, st);
 }
-int32_t launch_narrow(const Narrow &p, hipStream_t st)
+template <int ACT>
+int32_t launch_narrow_as(const Narrow &p, hipStream_t st)
 {
-    if (p.n_in <= 64) return launch_narrow_in<2>(p, st);
-    if (p.n_in <= 128) return launch_narrow_in<4>(p, st);
-    return launch_narrow_in<8>(p, st);
+    return p.n_in <= 64 ? launch_narrow_in<ACT, 2>(p, st) : launch_narrow_in<ACT, 4>(p, st);
+}
+int32_t launch_narrow(const Narrow &p, int32_t act, hipStream_t st)
+{
+    if (act == ECK_ACT_SILU) return launch_narrow_as<ECK_ACT_SILU>(p, st);
+    return act == ECK_ACT_GELU ? launch_narrow_as<ECK_ACT_GELU>(p, st) : launch_narrow_as<ECK_ACT_RELU>(p, st);
 }
 
 template <class T>
@@ -360,8 +366,8 @@ int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, c
     char *partial = space.take(room.partial);
     ECK_TRY(launch_packs(packs, st));
     if constexpr (P == 1)
-        if (!pre && s.n_in <= NARROW && s.n_out <= NARROW && s.n >= NARROW_ROWS)
-            return launch_narrow({ox, ogu, od, (uint32_t)s.n, s.n_in, s.n_hidden, s.n_out, s.hidden(), act, y, ld_y}, st);
+        if (!pre && narrow(s))
+            return launch_narrow({ox, ogu, od, (uint32_t)s.n, s.n_in, s.n_hidden, s.n_out, s.hidden(), y, ld_y}, act, st);
 
     Product p = {};
     p.a = ox, p.b = ogu, p.b_up = s.hidden();

@@ -9,6 +9,8 @@
 #pragma once
 #include "activations.h"
 
+#include <type_traits>
+
 namespace eck {
 namespace product {
 
@@ -21,17 +23,26 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 struct Gate {
     float value, slope;
 };
-__device__ __forceinline__ Gate gate_of(int32_t act, float g)
+template <int ACT>
+__device__ __forceinline__ Gate gate_as(float g)
 {
-    if (act == ECK_ACT_RELU) return {g > 0.0f ? g : g == g ? 0.0f : g, g > 0.0f ? 1.0f : 0.0f};
-    if (act == ECK_ACT_SILU) {
+    if (ACT == ECK_ACT_RELU) return {g > 0.0f ? g : g == g ? 0.0f : g, g > 0.0f ? 1.0f : 0.0f};
+    if (ACT == ECK_ACT_SILU) {
         // (exponential and reciprocal as the instructions give them, within 2^-23 of the value each: full ones are 25 more
-        // instructions an element, 70 us of the 1030 of 8192 x 8192 results)
+        // instructions an element)
         const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
         return {g * s, s * (1.0f + g * (1.0f - s))};
     }
     const float s = 0.5f * (1.0f + erff(g * 0.70710678f));
     return {g * s, s + g * 0.39894228f * expf(-0.5f * g * g)};
+}
+// calls f with the activation as a constant, once for all elements it works on
+template <class F>
+__device__ __forceinline__ void with_act(int32_t act, F &&f)
+{
+    if (act == ECK_ACT_SILU) f(std::integral_constant<int, ECK_ACT_SILU>{});
+    else if (act == ECK_ACT_GELU) f(std::integral_constant<int, ECK_ACT_GELU>{});
+    else f(std::integral_constant<int, ECK_ACT_RELU>{});
 }
 
 // An operand: 16-byte aligned, ld and the extent along its rows multiples of eight elements (zeros behind the matrix)
@@ -137,8 +148,10 @@ template <int PARTS>
 __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32_t c, const float (&g)[8], const float (&u)[8])
 {
     float h[8];
+    with_act(to.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = gate_of(to.act, g[i]).value * u[i];
+        for (int i = 0; i < 8; ++i) h[i] = gate_as<decltype(act)::value>(g[i]).value * u[i];
+    });
     store_operand<PARTS>((bf16 *)to.out + m * to.ld_out + c, to.part_out, h);
     if (to.pre) {
         float *row = to.pre + m * 2 * to.n_hidden;
@@ -162,13 +175,15 @@ template <int PARTS>
 __device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint32_t c, const float (&dh)[8], const Pre &pre)
 {
     float h[8], dg[8], du[8];
+    with_act(to.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const Gate gate = gate_of(to.act, pre.g[i]);
-        h[i] = gate.value * pre.u[i];
-        dg[i] = dh[i] * pre.u[i] * gate.slope;
-        du[i] = dh[i] * gate.value;
-    }
+        for (int i = 0; i < 8; ++i) {
+            const Gate gate = gate_as<decltype(act)::value>(pre.g[i]);
+            h[i] = gate.value * pre.u[i];
+            dg[i] = dh[i] * pre.u[i] * gate.slope;
+            du[i] = dh[i] * gate.value;
+        }
+    });
     if (to.out) store_operand<PARTS>((bf16 *)to.out + m * to.ld_out + c, to.part_out, h);
     bf16 *d = to.d_pre + m * to.ld_d + c;
     store_operand<PARTS>(d, to.part_d, dg);

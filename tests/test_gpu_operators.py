@@ -344,8 +344,8 @@ def test_gatedffn(shape, kind):
     ffn_case(*shape, kind, eck.ACT_GELU, seed=57, extra=3, offset=1)
 
 
-@pytest.mark.parametrize("shape", [(8192, 64, 256, 64), (8300, 40, 77, 1), (8193, 256, 96, 256), (9001, 130, 40, 200), (8211, 7, 33, 100),
-                                   (8192, 100, 64, 33)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shape", [(12288, 64, 256, 64), (12300, 40, 77, 1), (12289, 128, 96, 256), (13001, 100, 40, 200), (12311, 7, 33, 100),
+                                   (12288, 128, 31, 33), (8193, 256, 96, 256)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("act", [eck.ACT_SILU, eck.ACT_GELU])
 def test_gatedffn_of_many_rows(shape, act):
     ffn_case(*shape, "bf16", act, extra=8 * (act == eck.ACT_GELU))
@@ -359,7 +359,7 @@ def test_gatedffn_relu(kind):
 
 @pytest.mark.parametrize("kind", sorted(DTYPES))
 @pytest.mark.parametrize("n,n_in,n_hidden,n_out", [(5, 24, 40, 16), (200, 64, 96, 80), (515, 130, 258, 67), (1300, 320, 640, 264), (1, 700, 90, 33),
-                                                     (3, 64, 200, 130), (8200, 72, 104, 90)])
+                                                     (3, 64, 200, 130), (12400, 72, 104, 90)])
 def test_gatedffn_of_whole_numbers_is_exact(n, n_in, n_hidden, n_out, kind):
     """Few and small whole numbers: no sum and no rounding loses anything, so every element has one right value"""
     dtype, code, _ = DTYPES[kind]
