@@ -357,6 +357,22 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         }
     };
 
+    // the results: some rows of tiles at a time, threads with eight columns each
+    constexpr int HIGH = S::TM < 2 ? 1 : 2, ROWS = S::WM * 16 * HIGH, PITCH = S::BN + 4; // four words: sixteen rows, all banks
+    constexpr int CHUNKS = COLUMNS / 8, ITEMS = ROWS * CHUNKS / S::THREADS;
+    static_assert(ROWS * PITCH * 4 <= S::LDS && ITEMS * S::THREADS == ROWS * CHUNKS, "the rows fit, and every thread has as many");
+    const uint32_t mine = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS, c = c0 + 8 * chunk;
+    const auto row_of = [&](int step, int item) {
+        const uint32_t r = mine + item * (S::THREADS / CHUNKS);
+        return m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
+    };
+    constexpr bool EARLY = KIND == SLOPE && S::TM == 1; // the stored sums that a small tile needs are fetched before anything else
+    Pre early[EARLY ? ITEMS : 1];
+    if constexpr (EARLY)
+#pragma unroll
+        for (int item = 0; item < ITEMS; ++item)
+            if (row_of(0, item) < p.M && c < p.N) load_pre(p.to, row_of(0, item), c, early[item]);
+
     f32x4 sum[S::TM][S::TN];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
@@ -411,24 +427,16 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
     // Sums to results by way of the LDS, some rows of tiles at a time, so that threads next to each other work on columns next to
     // each other and memory sees whole rows of the tile (straight from the registers, in pieces of 64 bytes, 8192 x 8192 gates took
     // 1020 us for 980).
-    constexpr int HIGH = S::TM < 2 ? 1 : 2, ROWS = S::WM * 16 * HIGH, PITCH = S::BN + 4; // four words: sixteen rows, all banks
-    constexpr int CHUNKS = COLUMNS / 8, ITEMS = ROWS * CHUNKS / S::THREADS;
-    static_assert(ROWS * PITCH * 4 <= S::LDS && ITEMS * S::THREADS == ROWS * CHUNKS, "the rows fit, and every thread has as many");
     float *const rows = reinterpret_cast<float *>(lds);
-    const uint32_t mine = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS, c = c0 + 8 * chunk;
     // (loads past the end have to be done writing zeros to the LDS)
     wait_and_meet<0>();
 #pragma unroll
     for (int step = 0; step < S::TM / HIGH; ++step) {
-        const auto row_of = [&](int item) {
-            const uint32_t r = mine + item * (S::THREADS / CHUNKS);
-            return m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
-        };
         Pre pre[ITEMS];
-        if constexpr (KIND == SLOPE) // on their way while the sums are exchanged
+        if constexpr (KIND == SLOPE && !EARLY) // on their way while the sums are exchanged
 #pragma unroll
             for (int item = 0; item < ITEMS; ++item)
-                if (row_of(item) < p.M && c < p.N) load_pre(p.to, row_of(item), c, pre[item]);
+                if (row_of(step, item) < p.M && c < p.N) load_pre(p.to, row_of(step, item), c, pre[item]);
         if (step > 0) lds_barrier();
 #pragma unroll
         for (int i = 0; i < HIGH; ++i)
@@ -439,7 +447,7 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         lds_barrier();
 #pragma unroll
         for (int item = 0; item < ITEMS; ++item) {
-            const uint32_t m = row_of(item);
+            const uint32_t m = row_of(step, item);
             const float *row = rows + (mine + item * (S::THREADS / CHUNKS)) * PITCH;
             if (m >= p.M || c >= p.N) continue;
             // (of a wavefront's columns the first half are gates, the second the ups of the same units)
@@ -455,7 +463,7 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
                 else store_eight((float *)p.to.out + ((uint64_t)share * p.M + m) * p.to.ld_out, c, (uint32_t)p.to.ld_out, v);
             }
             if constexpr (KIND == GATE) finish_gate<PARTS>(p.to, m, c, v, u);
-            if constexpr (KIND == SLOPE) finish_slope<PARTS>(p.to, m, c, v, pre[item]);
+            if constexpr (KIND == SLOPE) finish_slope<PARTS>(p.to, m, c, v, EARLY ? early[item] : pre[item]);
         }
     }
 }
