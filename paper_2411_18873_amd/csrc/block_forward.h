@@ -147,7 +147,7 @@ template <int DK, int ON, int ACT>
 __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
 {
     using S = NarrowShape<DK, ON>;
-    typedef Stage<64, false, 4> StageGU; // 32 gates and 32 ups a row of k
+    typedef Stage<64, false, 4, 1> StageGU; // 32 gates and 32 ups a row of k
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;

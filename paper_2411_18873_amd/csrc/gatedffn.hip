@@ -26,6 +26,8 @@ uint64_t padded(uint64_t bytes) { return up_to(bytes, 256); }
 
 // ------------------------------------------------------------------------------------------------ which tiles
 
+int shapes_of(uint32_t parts) { return parts == 3 ? Shapes<3>::COUNT : Shapes<1>::COUNT; }
+
 struct Plan {
     int shape; // 0 small, 1 medium, 2 large tiles
     uint32_t shares;
@@ -39,10 +41,11 @@ Plan plan_shape(int shape, uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
 {
     static const struct {
         uint32_t side, at_once;   // blocks a compute unit
-        double step, alone, rest; // 64 k's of a tile when the unit is full, with nothing beside them, and a tile's start and end
-    } SHAPES[3] = {{64, 3, 0.27, 0.31, 2.2}, {128, 2, 0.5, 0.71, 3.0}, {256, 1, 1.29, 1.58, 8.3}};
-    const auto &of = SHAPES[shape];
-    const uint64_t steps = (K + BK - 1) / BK * (parts == 3 ? 6 : 1), tiles = (M + of.side - 1) / of.side * ((N + of.side - 1) / of.side);
+        double step, alone, rest; // a step of a tile when the unit is full, with nothing beside them, and a tile's start and end
+    } SHAPES[2][3] = {{{64, 3, 0.27, 0.31, 2.2}, {128, 2, 0.5, 0.71, 3.0}, {256, 1, 1.29, 1.58, 8.3}},
+                      {{64, 2, 0.3, 0.35, 2.2}, {128, 1, 0.8, 0.8, 5.0}, {}}}; // (parts)
+    const auto &of = SHAPES[parts == 3][shape];
+    const uint64_t steps = parts == 3 ? (K + STAGE_K<3> - 1) / STAGE_K<3> : (K + STAGE_K<1> - 1) / STAGE_K<1>, tiles = (M + of.side - 1) / of.side * ((N + of.side - 1) / of.side);
     Plan best = {shape, 1, 1e300};
     for (uint32_t shares = 1; shares <= 64; shares *= 2) {
         if (shares > 1 && (steps / shares < 2 || tiles * shares > 2048 || shares * M * N > MAX_SHARED)) break;
@@ -61,7 +64,7 @@ Plan plan_shape(int shape, uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
 Plan plan(uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
 {
     Plan best = plan_shape(0, M, N, K, parts);
-    for (int shape = 1; shape < 3; ++shape) {
+    for (int shape = 1; shape < shapes_of(parts); ++shape) {
         const Plan other = plan_shape(shape, M, N, K, parts);
         if (other.time < best.time) best = other;
     }
@@ -97,8 +100,9 @@ void divide(Product &p, uint32_t side, uint32_t shares, char *&partial, Joins &j
         if (KIND == GATE) p.N = p.b_up + p.N; // gates and ups side by side, as in memory
         p.to.out = partial;
         p.to.ld_out = up_to(p.N, 8);
-        joins.one[joins.count++] = {(const float *)partial, shares, whole.M, whole.N, whole.b_up, p.to.ld_out, joins.chunks, whole.to};
-        joins.chunks += (uint64_t)whole.M * ((whole.N + 7) / 8);
+        const uint32_t columns = KIND == SLOPE ? whole.to.pitch : whole.N;
+        joins.one[joins.count++] = {(const float *)partial, shares, whole.M, columns, whole.b_up, p.to.ld_out, joins.chunks, whole.to};
+        joins.chunks += (uint64_t)whole.M * ((columns + 7) / 8);
         partial += padded(shares * (uint64_t)p.M * p.to.ld_out * 4);
     }
     const uint32_t columns = KIND == GATE && shares == 1 ? side / 2 : side;
@@ -115,10 +119,10 @@ int32_t launch_joins(const Joins &joins, hipStream_t st)
     return ECK_OK;
 }
 
-template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
+template <class S, bool A_FAST, bool B_FAST, int KIND>
 int32_t launch_tiles(const Product &p, hipStream_t st)
 {
-    auto kernel = product_kernel<S, A_FAST, B_FAST, KIND, PARTS>;
+    auto kernel = product_kernel<S, A_FAST, B_FAST, KIND>;
     ECK_TRY(allow_lds(kernel, S::LDS));
     hipLaunchKernelGGL(kernel, dim3(p.blocks()), dim3(S::THREADS), S::LDS, st, p);
     ECK_HIP_TRY(hipGetLastError());
@@ -128,12 +132,14 @@ int32_t launch_tiles(const Product &p, hipStream_t st)
 template <bool A_FAST, bool B_FAST, int KIND, int PARTS>
 int32_t launch_shape(int shape, const Product &p, hipStream_t st)
 {
-    if (shape == 0) return launch_tiles<Small, A_FAST, B_FAST, KIND, PARTS>(p, st);
-    if (shape == 1) return launch_tiles<Medium, A_FAST, B_FAST, KIND, PARTS>(p, st);
-    return launch_tiles<Large, A_FAST, B_FAST, KIND, PARTS>(p, st);
+    using S = Shapes<PARTS>;
+    if (shape == 0) return launch_tiles<typename S::Small, A_FAST, B_FAST, KIND>(p, st);
+    if constexpr (S::COUNT == 3)
+        if (shape == 2) return launch_tiles<typename S::Large, A_FAST, B_FAST, KIND>(p, st);
+    return launch_tiles<typename S::Medium, A_FAST, B_FAST, KIND>(p, st);
 }
 
-constexpr uint32_t SIDES[3] = {Small::BM, Medium::BM, Large::BM};
+constexpr uint32_t SIDES[3] = {64, 128, 256};
 
 template <bool A_FAST, bool B_FAST, int KIND, int PARTS>
 int32_t launch(Product p, const Plan &how, char *partial, hipStream_t st)
@@ -145,14 +151,24 @@ int32_t launch(Product p, const Plan &how, char *partial, hipStream_t st)
     return launch_joins<KIND, PARTS>(joins, st);
 }
 
-template <class S, int PARTS>
+template <class S>
 int32_t launch_group(const Gradients &g, hipStream_t st)
 {
-    auto kernel = gradients_kernel<S, PARTS>;
+    auto kernel = gradients_kernel<S>;
     ECK_TRY(allow_lds(kernel, S::LDS));
     hipLaunchKernelGGL(kernel, dim3(g.dx.blocks() + g.dw_gate_up.blocks() + g.dw_down.blocks()), dim3(S::THREADS), S::LDS, st, g);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
+}
+
+template <int PARTS>
+int32_t launch_gradients(int shape, const Gradients &g, hipStream_t st)
+{
+    using S = Shapes<PARTS>;
+    if (shape == 0) return launch_group<typename S::Small>(g, st);
+    if constexpr (S::COUNT == 3)
+        if (shape == 2) return launch_group<typename S::Large>(g, st);
+    return launch_group<typename S::Medium>(g, st);
 }
 
 // ------------------------------------------------------------------------------------------------ operands
@@ -173,16 +189,19 @@ struct Workspace {
     }
 };
 
+// columns of a matrix of `width` as an operand
+uint64_t pitch_of(uint64_t width, uint32_t parts) { return up_to(width, parts == 3 ? 32 : 8); }
+
 // The matrix [rows][pieces * piece] as an operand: itself where it is one already, else to be copied to `room`.
 template <class T>
 Operand as_operand(const T *src, uint64_t ld, uint64_t rows, uint32_t piece, uint32_t pieces, char *room, Packs<T> &packs)
 {
-    if (sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16)) return {(const bf16 *)src, ld, 0};
-    const uint32_t pitch = (uint32_t)up_to(piece, 8);
+    if (sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16)) return {(const bf16 *)src, ld};
+    const uint32_t pitch = (uint32_t)pitch_of(piece, parts_of<T>);
     const uint64_t width = (uint64_t)pitch * pieces;
-    packs.one[packs.count++] = {src, (bf16 *)room, ld, rows * width, packs.chunks, piece, pieces, pitch};
+    packs.one[packs.count++] = {src, (bf16 *)room, ld, packs.chunks, piece, pieces, pitch};
     packs.chunks += rows * (width / 8);
-    return {(const bf16 *)room, width, rows * width};
+    return {(const bf16 *)room, width * parts_of<T>};
 }
 
 template <class T>
@@ -194,22 +213,26 @@ int32_t launch_packs(const Packs<T> &packs, hipStream_t st)
     return ECK_OK;
 }
 
+uint32_t parts_for(int32_t dtype) { return dtype == ECK_F32 ? 3 : 1; }
+
 struct Sizes {
     uint64_t n;
     uint32_t n_in, n_hidden, n_out;
-    uint32_t hidden() const { return (uint32_t)up_to(n_hidden, 8); }     // columns of h, and from gates to ups, in operands
-    uint32_t pairs() const { return hidden() + n_hidden; }               // columns of (g | u)
+    uint32_t parts;
+    uint32_t hidden() const { return (uint32_t)pitch_of(n_hidden, parts); } // columns of h, and from gates to ups, in operands
+    uint32_t pairs() const { return hidden() + n_hidden; }                  // columns of (g | u)
 };
 
 // The shape of tiles that all three gradients take, being one launch, and the shares of each: dx, dWgu, dWd, those wanted
 struct GradientPlans {
     Plan of[3];
 };
-GradientPlans plan_gradients(const Sizes &s, uint32_t parts, bool dx, bool dw_gate_up, bool dw_down)
+GradientPlans plan_gradients(const Sizes &s, bool dx, bool dw_gate_up, bool dw_down)
 {
+    const uint32_t parts = s.parts;
     GradientPlans best = {};
     double least = 1e300;
-    for (int shape = 0; shape < 3; ++shape) {
+    for (int shape = 0; shape < shapes_of(parts); ++shape) {
         const GradientPlans now = {{plan_shape(shape, s.n, s.n_in, s.pairs(), parts), plan_shape(shape, s.n_in, s.pairs(), s.n, parts),
                                     plan_shape(shape, s.n_hidden, s.n_out, s.n, parts)}};
         const double time = (dx ? now.of[0].time : 0.0) + (dw_gate_up ? now.of[1].time : 0.0) + (dw_down ? now.of[2].time : 0.0);
@@ -228,23 +251,24 @@ struct Rooms { // the workspace's pieces, in order
 
 uint64_t most(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-Rooms rooms(const Sizes &s, uint32_t parts, bool backward)
+Rooms rooms(const Sizes &s, bool backward)
 {
+    const uint32_t parts = s.parts;
     Rooms r = {};
-    r.x = operand_bytes(s.n, up_to(s.n_in, 8), parts);
+    r.x = operand_bytes(s.n, pitch_of(s.n_in, parts), parts);
     r.w_gate_up = operand_bytes(s.n_in, 2ull * s.hidden(), parts);
-    r.w_down = operand_bytes(s.n_hidden, up_to(s.n_out, 8), parts);
+    r.w_down = operand_bytes(s.n_hidden, pitch_of(s.n_out, parts), parts);
     r.h = operand_bytes(s.n, s.hidden(), parts);
     if (!backward) {
         r.partial = most(partial_bytes(s.n, s.pairs(), s.n_in, parts), partial_bytes(s.n, s.n_out, s.n_hidden, parts));
         return r;
     }
-    r.dy = operand_bytes(s.n, up_to(s.n_out, 8), parts);
+    r.dy = operand_bytes(s.n, pitch_of(s.n_out, parts), parts);
     r.d_pre = operand_bytes(s.n, 2ull * s.hidden(), parts);
     r.partial = partial_bytes(s.n, s.n_hidden, s.n_out, parts);
     for (int wanted = 1; wanted < 8; ++wanted) { // (the shape of tiles depends on which gradients are)
         const bool dx = wanted & 1, dw_gate_up = wanted & 2, dw_down = wanted & 4;
-        const GradientPlans how = plan_gradients(s, parts, dx, dw_gate_up, dw_down);
+        const GradientPlans how = plan_gradients(s, dx, dw_gate_up, dw_down);
         r.partial = most(r.partial, (dx ? shares_bytes(how.of[0], s.n, s.n_in) : 0) + (dw_gate_up ? shares_bytes(how.of[1], s.n_in, s.pairs()) : 0) +
                                         (dw_down ? shares_bytes(how.of[2], s.n_hidden, s.n_out) : 0));
     }
@@ -269,9 +293,9 @@ struct VectorRooms {
     uint32_t shares, shares_y;
     uint64_t sums, sums_y;
 };
-VectorRooms vector_rooms(const Sizes &s, uint32_t parts)
+VectorRooms vector_rooms(const Sizes &s)
 {
-    const uint32_t line = parts == 3 ? 32 : 64;
+    const uint32_t line = s.parts == 3 ? 32 : 64;
     VectorRooms r = {vector_shares(s.n_in, s.n_hidden, line), vector_shares(s.n_hidden, s.n_out, line), 0, 0};
     r.sums = padded(r.shares * s.n * 2 * s.n_hidden * 4);
     r.sums_y = r.shares_y > 1 ? padded(r.shares_y * s.n * up_to(s.n_out, 8) * 4) : 0;
@@ -301,7 +325,7 @@ template <class T>
 int32_t forward_few(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, const T *w_down, int32_t act, T *y, uint64_t ld_y, float *pre,
                     void *ws, hipStream_t st)
 {
-    const VectorRooms room = vector_rooms(s, parts_of<T>);
+    const VectorRooms room = vector_rooms(s);
     float *sums = (float *)ws, *sums_y = (float *)((char *)ws + room.sums);
     const uint32_t n = (uint32_t)s.n;
     ECK_TRY((launch_vector<T, true>({x, nullptr, ld_x, nullptr, n, s.n_in, 0, act}, room.shares, w_gate_up, 2ull * s.n_hidden, s.n_hidden, nullptr, 0,
@@ -356,13 +380,13 @@ int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, c
 {
     constexpr uint32_t P = parts_of<T>;
     if (s.n <= FEW_ROWS) return forward_few(x, ld_x, s, w_gate_up, w_down, act, y, ld_y, pre, ws, st);
-    const Rooms room = rooms(s, P, false);
+    const Rooms room = rooms(s, false);
     Workspace space = {(char *)ws};
     Packs<T> packs = {};
     const Operand ox = as_operand(x, ld_x, s.n, s.n_in, 1, space.take(room.x), packs);
     const Operand ogu = as_operand(w_gate_up, 2ull * s.n_hidden, s.n_in, s.n_hidden, 2, space.take(room.w_gate_up), packs);
     const Operand od = as_operand(w_down, s.n_out, s.n_hidden, s.n_out, 1, space.take(room.w_down), packs);
-    const Operand h = {(bf16 *)space.take(room.h), s.hidden(), s.n * s.hidden()};
+    const Operand h = {(bf16 *)space.take(room.h), (uint64_t)P * s.hidden()};
     char *partial = space.take(room.partial);
     ECK_TRY(launch_packs(packs, st));
     if constexpr (P == 1)
@@ -372,7 +396,7 @@ int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, c
     Product p = {};
     p.a = ox, p.b = ogu, p.b_up = s.hidden();
     p.M = (uint32_t)s.n, p.N = s.n_hidden, p.K = s.n_in;
-    p.to.out = const_cast<bf16 *>(h.p), p.to.ld_out = h.ld, p.to.part_out = h.part, p.to.pre = pre, p.to.n_hidden = s.n_hidden, p.to.act = act;
+    p.to.out = const_cast<bf16 *>(h.p), p.to.ld_out = h.ld, p.to.pre = pre, p.to.n_hidden = s.n_hidden, p.to.act = act;
     ECK_TRY((launch<true, false, GATE, P>(p, plan(s.n, s.pairs(), s.n_in, P), partial, st)));
 
     p = {};
@@ -387,11 +411,11 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
                  uint64_t ld_dy, T *dx, uint64_t ld_dx, T *dw_gate_up, T *dw_down, void *ws, hipStream_t st)
 {
     constexpr uint32_t P = parts_of<T>;
-    const Rooms room = rooms(s, P, true);
+    const Rooms room = rooms(s, true);
     Workspace space = {(char *)ws};
     char *room_x = space.take(room.x), *room_gu = space.take(room.w_gate_up), *room_d = space.take(room.w_down), *room_dy = space.take(room.dy);
-    const Operand d_pre = {(bf16 *)space.take(room.d_pre), 2ull * s.hidden(), s.n * 2 * s.hidden()};
-    const Operand h = {(bf16 *)space.take(room.h), s.hidden(), s.n * s.hidden()};
+    const Operand d_pre = {(bf16 *)space.take(room.d_pre), 2ull * P * s.hidden()};
+    const Operand h = {(bf16 *)space.take(room.h), (uint64_t)P * s.hidden()};
     char *partial = space.take(room.partial);
     Packs<T> packs = {};
     const Operand ody = as_operand(dy, ld_dy, s.n, s.n_out, 1, room_dy, packs);
@@ -404,12 +428,12 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     Product p = {}; // dh, and from it dg, du and h
     p.a = ody, p.b = od;
     p.M = (uint32_t)s.n, p.N = s.n_hidden, p.K = s.n_out;
-    p.to.out = dw_down ? const_cast<bf16 *>(h.p) : nullptr, p.to.ld_out = h.ld, p.to.part_out = h.part;
+    p.to.out = dw_down ? const_cast<bf16 *>(h.p) : nullptr, p.to.ld_out = h.ld;
     p.to.pre = const_cast<float *>(pre), p.to.n_hidden = s.n_hidden, p.to.act = act, p.to.pitch = s.hidden();
-    p.to.d_pre = const_cast<bf16 *>(d_pre.p), p.to.ld_d = d_pre.ld, p.to.part_d = d_pre.part;
+    p.to.d_pre = const_cast<bf16 *>(d_pre.p), p.to.ld_d = d_pre.ld;
     ECK_TRY((launch<true, true, SLOPE, P>(p, plan(s.n, s.n_hidden, s.n_out, P), partial, st)));
 
-    const GradientPlans how = plan_gradients(s, P, dx, dw_gate_up, dw_down);
+    const GradientPlans how = plan_gradients(s, dx, dw_gate_up, dw_down);
     const uint32_t side = SIDES[how.of[0].shape];
     Gradients g = {};
     Joins joins = {};
@@ -430,9 +454,7 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
         q.to.out = dw_down, q.to.ld_out = s.n_out, q.to.piece = s.n_out, q.to.pitch = NO_GAP;
         divide<STORE>(q, side, how.of[2].shares, partial, joins);
     }
-    if (how.of[0].shape == 0) ECK_TRY((launch_group<Small, P>(g, st)));
-    else if (how.of[0].shape == 1) ECK_TRY((launch_group<Medium, P>(g, st)));
-    else ECK_TRY((launch_group<Large, P>(g, st)));
+    ECK_TRY(launch_gradients<P>(how.of[0].shape, g, st));
     return launch_joins<STORE, P>(joins, st);
 }
 
@@ -447,12 +469,11 @@ bool act_ok(int32_t act) { return act == ECK_ACT_SILU || act == ECK_ACT_GELU || 
 uint64_t workspace_bytes(const Sizes &s, int32_t dtype, bool backward)
 {
     if (s.n == 0 || s.n_in == 0 || s.n_hidden == 0 || s.n_out == 0 || !is_dtype(dtype) || !sizes_ok(s)) return 0;
-    const uint32_t parts = dtype == ECK_F32 ? 3 : 1;
     if (!backward && s.n <= FEW_ROWS) {
-        const VectorRooms room = vector_rooms(s, parts);
+        const VectorRooms room = vector_rooms(s);
         return room.sums + room.sums_y;
     }
-    return rooms(s, parts, backward).total();
+    return rooms(s, backward).total();
 }
 
 } // namespace
@@ -462,14 +483,14 @@ using namespace eck;
 
 extern "C" uint64_t gatedffn_forward_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_hidden, uint32_t n_out, int32_t dtype)
 {
-    return workspace_bytes({n, n_in, n_hidden, n_out}, dtype, false);
+    return workspace_bytes({n, n_in, n_hidden, n_out, parts_for(dtype)}, dtype, false);
 }
 
 extern "C" int32_t gatedffn_forward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t n_in, uint32_t n_hidden,
                                     uint32_t n_out, const void *w_gate_up, const void *w_down, int32_t act, void *y, uint64_t ld_y,
                                     float *pre_out, void *ws, uint64_t ws_bytes, void *stream)
 {
-    const Sizes s = {n, n_in, n_hidden, n_out};
+    const Sizes s = {n, n_in, n_hidden, n_out, parts_for(dtype)};
     if (!x || !w_gate_up || !w_down || !y || n == 0 || n_in == 0 || n_hidden == 0 || n_out == 0 || !is_dtype(dtype) || !act_ok(act)) return ECK_EINVAL;
     if (ld_x < n_in || ld_y < n_out) return ECK_ESHAPE;
     if (!sizes_ok(s)) return ECK_EUNSUPPORTED;
@@ -484,7 +505,7 @@ extern "C" int32_t gatedffn_forward(const void *x, int32_t dtype, uint64_t ld_x,
 
 extern "C" uint64_t gatedffn_backward_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_hidden, uint32_t n_out, int32_t dtype)
 {
-    return workspace_bytes({n, n_in, n_hidden, n_out}, dtype, true);
+    return workspace_bytes({n, n_in, n_hidden, n_out, parts_for(dtype)}, dtype, true);
 }
 
 extern "C" int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t n_in, uint32_t n_hidden,
@@ -492,7 +513,7 @@ extern "C" int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x
                                      const void *dy, uint64_t ld_dy, void *dx_out, uint64_t ld_dx, void *dw_gate_up_out, void *dw_down_out,
                                      void *ws, uint64_t ws_bytes, void *stream)
 {
-    const Sizes s = {n, n_in, n_hidden, n_out};
+    const Sizes s = {n, n_in, n_hidden, n_out, parts_for(dtype)};
     if (!x || !w_gate_up || !w_down || !pre || !dy || n == 0 || n_in == 0 || n_hidden == 0 || n_out == 0 || !is_dtype(dtype)) return ECK_EINVAL;
     if ((!dx_out && !dw_gate_up_out && !dw_down_out) || !act_ok(act)) return ECK_EINVAL;
     if (ld_x < n_in || ld_dy < n_out || (dx_out && ld_dx < n_in)) return ECK_ESHAPE;

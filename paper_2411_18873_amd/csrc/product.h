@@ -4,8 +4,9 @@
 // staged as they lie, 64 values of k at a time, by loads that go straight into the LDS, and become matrix-core operands on the
 // way out of it (the second kind by the transposing LDS reads).  A block works on a tile of C, its wavefronts on parts of it.
 //
-// fp32 matrices come as three bfloat16 parts each (f32_split.h): of the nine products of parts the six largest are summed, one
-// after the other in the same accumulators, the smallest first.
+// fp32 matrices come as three bfloat16 parts each (f32_split.h): of the nine products of parts the six largest are summed, the
+// smallest first.  The parts of 32 neighbouring values of a row lie next to each other, so that one stage brings all of them and a
+// part that enters several products is loaded once.
 #pragma once
 #include "activations.h"
 
@@ -45,11 +46,16 @@ __device__ __forceinline__ void with_act(int32_t act, F &&f)
     else f(std::integral_constant<int, ECK_ACT_RELU>{});
 }
 
-// An operand: 16-byte aligned, ld and the extent along its rows multiples of eight elements (zeros behind the matrix)
+// An operand: 16-byte aligned, rows of a multiple of eight elements (zeros behind the matrix), or, in parts, of 32, the three parts of
+// each 32 one after the other
 struct Operand {
     const bf16 *p;
-    uint64_t ld, part; // elements between rows, and between the parts of an fp32 matrix
+    uint64_t ld; // elements between rows, those of all parts
 };
+// where in a row column c's first part is, c a multiple of eight, and from one part to the next
+template <int PARTS>
+__host__ __device__ __forceinline__ uint32_t in_row(uint32_t c) { return PARTS == 1 ? c : c / 32 * 96 + c % 32; }
+constexpr uint32_t PART = 32;
 
 // What becomes of the sums
 enum Kind {
@@ -62,11 +68,11 @@ enum Kind {
 // [0, piece) and [pitch, pitch + piece) exist, and lie next to each other in out.
 struct Target {
     void *out;        // STORE: element type, or float for shares; GATE, SLOPE: h, an operand of the next product
-    uint64_t ld_out, part_out;
+    uint64_t ld_out;
     uint32_t piece, pitch;
     float *pre;       // [M][2 * n_hidden] sums (g | u): GATE writes them (or NULL), SLOPE reads them
     bf16 *d_pre;      // SLOPE: (dg | du), an operand; du from column `pitch` on
-    uint64_t ld_d, part_d;
+    uint64_t ld_d;
     uint32_t n_hidden;
     int32_t act;
 };
@@ -85,8 +91,9 @@ struct Product {
 
 // value of eight columns as an operand of the next product: rounded to bfloat16, or in three parts
 template <int PARTS>
-__device__ __forceinline__ void store_operand(bf16 *p, uint64_t part, const float (&v)[8])
+__device__ __forceinline__ void store_operand(bf16 *row, uint32_t c, const float (&v)[8])
 {
+    bf16 *p = row + in_row<PARTS>(c);
     float rest[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) rest[i] = v[i];
@@ -98,7 +105,7 @@ __device__ __forceinline__ void store_operand(bf16 *p, uint64_t part, const floa
             out[i] = (bf16)rest[i];
             rest[i] -= (float)out[i];
         }
-        *reinterpret_cast<bf16x8 *>(p + s * part) = out;
+        *reinterpret_cast<bf16x8 *>(p + s * PART) = out;
     }
 }
 
@@ -152,7 +159,7 @@ __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] = gate_as<decltype(act)::value>(g[i]).value * u[i];
     });
-    store_operand<PARTS>((bf16 *)to.out + m * to.ld_out + c, to.part_out, h);
+    store_operand<PARTS>((bf16 *)to.out + m * to.ld_out, c, h);
     if (to.pre) {
         float *row = to.pre + m * 2 * to.n_hidden;
         store_eight(row, c, to.n_hidden, g);
@@ -184,15 +191,17 @@ __device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint3
             du[i] = dh[i] * gate.value;
         }
     });
-    if (to.out) store_operand<PARTS>((bf16 *)to.out + m * to.ld_out + c, to.part_out, h);
-    bf16 *d = to.d_pre + m * to.ld_d + c;
-    store_operand<PARTS>(d, to.part_d, dg);
-    store_operand<PARTS>(d + to.pitch, to.part_d, du);
+    if (to.out) store_operand<PARTS>((bf16 *)to.out + m * to.ld_out, c, h);
+    bf16 *d = to.d_pre + m * to.ld_d;
+    store_operand<PARTS>(d, c, dg);
+    store_operand<PARTS>(d, to.pitch + c, du);
 }
 
 // ------------------------------------------------------------------------------------------------ staging
 
-constexpr int BK = 64;
+// k's of a stage: 64, or 32 in three parts
+template <int PARTS>
+constexpr int STAGE_K = PARTS == 1 ? 64 : 32;
 constexpr uint32_t NOWHERE = 0x80000000u; // an offset outside every buffer: such loads bring zeros
 
 // 16 bytes per lane from base + offset into the LDS, lane after lane from lds_at (the same in all lanes)
@@ -208,20 +217,23 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// How 64 k's of ROWS rows (or columns) of an operand lie in the LDS.
+// How a stage of ROWS rows (or columns) of an operand lies in the LDS, each part by itself.
 //   K_FAST  rows of 128 bytes (so every load takes whole cache lines: of 32 k's at a time the L1 asked the L2 for each line twice,
 //           1.33e8 requests for 6.7e7 in a product of 8192^3), eight chunks of eight k's; chunk c of row r is stored in place
-//           c ^ (r / 2 % 8).  A read of sixteen rows takes four cycles if the lanes served in one (rows 0 .. 3 and 12 .. 15 of one
-//           chunk with 4 .. 11 of the next, or the other way round) take from all banks: so found from the bank conflicts counted.
-//   else    64 rows of k, ROWS values each, in units of sixteen.  The transposing read takes units of eight k's at a time (k % 4 and
+//           c ^ (r / 2 % 8).  In parts, rows of 64 bytes, four chunks, in place c ^ (0, 2, 3, 1)[r / 4 % 4].  A read of sixteen rows
+//           takes four cycles if the lanes served in one (rows 0 .. 3 and 12 .. 15 of one chunk with 4 .. 11 of the next, or the other
+//           way round) take from all banks: so found from the bank conflicts counted.
+//   else    rows of k, ROWS values each, in units of sixteen.  The transposing read takes units of eight k's at a time (k % 4 and
 //           k / 8 % 2 vary within half a wavefront): unit j of k is stored in place j ^ those three bits (two where a row has just
 //           four units and two rows share the banks).
-template <int ROWS, bool K_FAST, int WAVES>
+template <int ROWS, bool K_FAST, int WAVES, int PARTS>
 struct Stage {
-    static constexpr int BYTES = ROWS * BK * 2, LOADS = BYTES / 1024 / WAVES;
+    static constexpr int BK = STAGE_K<PARTS>, ONE = ROWS * BK * 2, BYTES = ONE * PARTS, LOADS = BYTES / 1024 / WAVES; // ONE: a part
     static_assert(BYTES % (1024 * WAVES) == 0, "every wavefront issues the same number of loads");
-    static constexpr int CHUNKS = ROWS / 8; // of a k's row
+    static constexpr int CHUNKS = ROWS / 8;   // of a k's row
+    static constexpr int SPAN = BK / 8;       // chunks of a row of k's
 
+    static __device__ __forceinline__ uint32_t row_swizzle(uint32_t r) { return PARTS == 1 ? r >> 1 & 7 : (r >> 2 & 1) << 1 ^ (r >> 3 & 1) * 3; }
     static __device__ __forceinline__ uint32_t unit_swizzle(uint32_t k)
     {
         return ROWS >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
@@ -239,17 +251,17 @@ struct Stage {
         lds_at = lds + wave * LOADS * 1024;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const uint32_t piece = wave * LOADS + j;
+            const uint32_t piece = (wave * LOADS + j) % (ONE / 1024), part = (wave * LOADS + j) / (ONE / 1024);
             if (K_FAST) {
-                const uint32_t r = piece * 8 + lane / 8, chunk = (lane & 7) ^ (r >> 1 & 7);
+                const uint32_t r = piece * (64 / SPAN) + lane / SPAN, chunk = (lane % SPAN) ^ row_swizzle(r);
                 const uint32_t at = place(r);
                 k_of[j] = chunk * 8;
-                offset[j] = at != NOWHERE ? (uint32_t)(at * ld * 2) + chunk * 16 : NOWHERE;
+                offset[j] = at != NOWHERE ? (uint32_t)(at * ld * 2) + (part * PART + chunk * 8) * 2 : NOWHERE;
             } else {
                 const uint32_t k = piece * (64 / CHUNKS) + lane / CHUNKS, chunk = (lane % CHUNKS) ^ unit_swizzle(k) << 1;
                 const uint32_t at = place(chunk * 8);
                 k_of[j] = k;
-                offset[j] = at != NOWHERE ? (uint32_t)(k * ld * 2) + at * 2 : NOWHERE;
+                offset[j] = at != NOWHERE ? (uint32_t)(k * ld * 2) + (in_row<PARTS>(at) + part * PART) * 2 : NOWHERE;
             }
         }
     }
@@ -262,14 +274,15 @@ struct Stage {
         for (int j = 0; j < LOADS; ++j) load_to_lds(lds_at + stage_at + j * 1024, k_of[j] < left ? offset[j] : NOWHERE, where);
     }
 
-    // operands of rows [16 t, 16 t + 16): lane (g = lane / 16, r) holds k's 32 half + 8g .. 8g + 7 of row r.  at: LDS address of the
-    // stage
-    static __device__ __forceinline__ bf16x8 read(uint32_t at, uint32_t t, uint32_t half)
+    // operands of rows [16 t, 16 t + 16): lane (g = lane / 16, r) holds 32 which + 8g .. 8g + 7 of row r's k's (in parts: 8g .. 8g + 7 of
+    // part `which`).  at: LDS address of the stage
+    static __device__ __forceinline__ bf16x8 read(uint32_t at, uint32_t t, uint32_t which)
     {
         typedef __attribute__((address_space(3))) const bf16x8 *Whole;
         typedef __attribute__((address_space(3))) s16x4 *Half;
-        const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-        if (K_FAST) return *(Whole)(uintptr_t)(at + t * 2048 + r * 128 + ((half * 4 + g ^ r >> 1) << 4));
+        const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, half = PARTS == 1 ? which : 0;
+        if (PARTS > 1) at += which * ONE;
+        if (K_FAST) return *(Whole)(uintptr_t)(at + (t * 16 + r) * (BK * 2) + ((half * 4 + g ^ row_swizzle(r)) << 4));
         // sixteen lanes: four k's, four values of sixteen columns each; lane r receives the four k's of column r
         const uint32_t k = 32 * half + 8 * g + (r >> 2);
         const uint32_t p = at + k * (ROWS * 2) + ((t ^ unit_swizzle(k)) << 5) + ((r & 3) << 3);
@@ -281,25 +294,37 @@ struct Stage {
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-// Tiles of BM x BN, wavefronts in WM rows and WN columns, STAGES of 64 k's in the LDS.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// Tiles of BM x BN, wavefronts in WM rows and WN columns, STAGES in the LDS.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int PARTS_>
 struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES, STAGES = STAGES_;
-    static constexpr int TM = BM / WM / 16, TN = BN / WN / 16; // 16 x 16 tiles of a wavefront
-    static constexpr int LDS = (BM + BN) * BK * 2 * STAGES;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES, STAGES = STAGES_, PARTS = PARTS_;
+    static constexpr int BK = STAGE_K<PARTS>, TM = BM / WM / 16, TN = BN / WN / 16; // 16 x 16 tiles of a wavefront
+    static constexpr int STAGE = (BM + BN) * BK * 2 * PARTS, LDS = STAGE * STAGES;
     static constexpr int AT_ONCE = 160 * 1024 / LDS * WAVES / 4; // wavefronts a SIMD: the registers may be used up to that
 };
-typedef Shape<256, 256, 2, 4, 2> Large;
-typedef Shape<128, 128, 2, 2, 2> Medium;
-typedef Shape<64, 64, 4, 1, 3> Small;
+// by type: small, medium and large ones (in parts, a large tile's stages do not fit the LDS)
+template <int PARTS>
+struct Shapes {
+    static constexpr int COUNT = 3;
+    typedef Shape<64, 64, 4, 1, 3, 1> Small;
+    typedef Shape<128, 128, 2, 2, 2, 1> Medium;
+    typedef Shape<256, 256, 2, 4, 2, 1> Large;
+};
+template <>
+struct Shapes<3> {
+    static constexpr int COUNT = 2;
+    typedef Shape<64, 64, 4, 1, 3, 3> Small;
+    typedef Shape<128, 128, 2, 4, 3, 3> Medium;
+};
 
-template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
+template <class S, bool A_FAST, bool B_FAST, int KIND>
 __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t total, unsigned char *lds)
 {
-    typedef Stage<S::BM, A_FAST, S::WAVES> StageA;
-    typedef Stage<S::BN, B_FAST, S::WAVES> StageB;
+    constexpr int PARTS = S::PARTS, BK = S::BK;
+    typedef Stage<S::BM, A_FAST, S::WAVES, PARTS> StageA;
+    typedef Stage<S::BN, B_FAST, S::WAVES, PARTS> StageB;
     constexpr int PER_STEP = StageA::LOADS + StageB::LOADS;
-    constexpr uint32_t STAGE = (S::BM + S::BN) * BK * 2;
+    constexpr uint32_t STAGE = S::STAGE;
     constexpr int COLUMNS = KIND == GATE ? S::BN / 2 : S::BN; // of the result
 
     // Blocks go round the eight dies; the blocks of a die take neighbouring tiles, in panels eight tiles high, so that its L2
@@ -318,30 +343,20 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
     // a tile of pairs: of each wavefront's columns the first half are gates, the second the ups of the same units
     constexpr uint32_t HALF = S::BN / S::WN / 2;
     sa.init(p.a.ld, lds0, [&](uint32_t r) { return m0 + r < p.M ? r : NOWHERE; });
-    sb.init(p.b.ld, lds0 + S::BM * BK * 2, [&](uint32_t c) {
+    sb.init(p.b.ld, lds0 + StageA::BYTES, [&](uint32_t c) {
         if (KIND != GATE) return c0 + c < p.N ? c : NOWHERE;
         const uint32_t unit = c / (2 * HALF) * HALF + c % HALF;
         return c0 + unit < p.N ? unit + (c % (2 * HALF) >= HALF ? p.b_up : 0) : NOWHERE;
     });
-    // (the tile's own place is added to the base: offsets within a tile and a step fit 32 bits)
-    const bf16 *a0 = p.a.p + (A_FAST ? m0 * p.a.ld : (uint64_t)m0), *b0 = p.b.p + (B_FAST ? c0 * p.b.ld : (uint64_t)c0);
-
-    // steps of 64 k's: all of the first pair of parts, then the next; this block's share of them
-    const uint32_t steps_k = (p.K + BK - 1) / BK;
-    const uint64_t all = (uint64_t)steps_k * (PARTS == 3 ? 6 : 1);
-    const uint32_t first = (uint32_t)(all * share / p.shares), steps = (uint32_t)(all * (share + 1) / p.shares) - first;
-    uint32_t to_come = steps, pair = first / steps_k, left; // steps not yet on their way, k's from the next one on
-    const bf16 *at_a, *at_b;
-    const auto begin_pair = [&](uint32_t k) {
-        // x0 w2, x2 w0, x1 w1, x0 w1, x1 w0, x0 w0
-        const uint32_t part_a = PARTS == 3 ? 0x010120u >> 4 * pair & 15 : 0, part_b = PARTS == 3 ? 0x001102u >> 4 * pair & 15 : 0;
-        at_a = a0 + part_a * p.a.part + (A_FAST ? (uint64_t)k : k * p.a.ld);
-        at_b = b0 + part_b * p.b.part + (B_FAST ? (uint64_t)k : k * p.b.ld);
-        left = p.K - k;
-    };
-    begin_pair(first % steps_k * BK);
-    const uint64_t step_a = A_FAST ? BK : BK * p.a.ld, step_b = B_FAST ? BK : BK * p.b.ld;
-    const auto load = [&](uint32_t slot) { // past the end: zeros
+    // steps of BK k's; this block's share of them.  (The tile's own place is added to the base: offsets within a tile and a step fit
+    // 32 bits.)
+    const uint32_t all = (p.K + BK - 1) / BK;
+    const uint32_t first = (uint32_t)((uint64_t)all * share / p.shares), steps = (uint32_t)((uint64_t)all * (share + 1) / p.shares) - first;
+    const uint64_t step_a = A_FAST ? in_row<PARTS>(BK) : BK * p.a.ld, step_b = B_FAST ? in_row<PARTS>(BK) : BK * p.b.ld;
+    const bf16 *at_a = p.a.p + (A_FAST ? m0 * p.a.ld : (uint64_t)in_row<PARTS>(m0)) + first * step_a;
+    const bf16 *at_b = p.b.p + (B_FAST ? c0 * p.b.ld : (uint64_t)in_row<PARTS>(c0)) + first * step_b;
+    uint32_t to_come = steps, left = p.K - first * BK; // steps not yet on their way, k's from the next one on
+    const auto load = [&](uint32_t slot) {             // past the end: zeros
         const uint32_t some = to_come ? left : 0;
         sa.load(at_a, some, slot * STAGE);
         sb.load(at_b, some, slot * STAGE);
@@ -350,11 +365,7 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         to_come = to_come ? to_come - 1 : 0;
         at_a += step_a;
         at_b += step_b;
-        left -= BK; // (past the end of the last pair nothing is to come)
-        if (PARTS == 3 && to_come && (int32_t)left <= 0) {
-            ++pair;
-            begin_pair(0);
-        }
+        left -= BK; // (past the last one nothing is to come)
     };
 
     // the results: some rows of tiles at a time, threads with eight columns each
@@ -366,35 +377,46 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         const uint32_t r = mine + item * (S::THREADS / CHUNKS);
         return m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
     };
+    const uint32_t last = KIND == SLOPE ? p.to.pitch : p.N; // (derivatives: zeros up to the operand's next piece, whose k's follow)
     constexpr bool EARLY = KIND == SLOPE && S::TM == 1; // the stored sums that a small tile needs are fetched before anything else
     Pre early[EARLY ? ITEMS : 1];
     if constexpr (EARLY)
 #pragma unroll
         for (int item = 0; item < ITEMS; ++item)
-            if (row_of(0, item) < p.M && c < p.N) load_pre(p.to, row_of(0, item), c, early[item]);
+            if (row_of(0, item) < p.M && c < last) load_pre(p.to, row_of(0, item), c, early[item]);
 
     f32x4 sum[S::TM][S::TN];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) sum[i][j] = f32x4{0, 0, 0, 0};
-    bf16x8 a[2][S::TM], b[2][S::TN];
-    const auto read = [&](uint32_t slot, int half) {
+    // operands: of the two halves of a step's k's, or of all parts of two steps
+    bf16x8 a[2][S::TM][PARTS], b[2][S::TN][PARTS];
+    const auto read = [&](uint32_t slot, int to) {
         const uint32_t at = lds0 + slot * STAGE;
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) b[half][j] = StageB::read(at + S::BM * BK * 2, wn * S::TN + j, half);
+        for (int part = 0; part < PARTS; ++part) {
+            const uint32_t which = PARTS == 1 ? to : part;
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i) a[half][i] = StageA::read(at, wm * S::TM + i, half);
+            for (int j = 0; j < S::TN; ++j) b[to][j][part] = StageB::read(at + StageA::BYTES, wn * S::TN + j, which);
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i) a[to][i][part] = StageA::read(at, wm * S::TM + i, which);
+        }
     };
-    const auto multiply = [&](int half) {
+    const auto multiply = [&](int from) {
         // columns as the first operand: a lane's four sums are neighbouring columns of one row
+        constexpr int PAIRS = PARTS == 1 ? 1 : 6;
+        constexpr int PART_A[6] = {0, 2 % PARTS, 1 % PARTS, 0, 1 % PARTS, 0}, PART_B[6] = {2 % PARTS, 0, 1 % PARTS, 1 % PARTS, 0, 0};
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i)
+        for (int pair = 0; pair < PAIRS; ++pair)
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[half][j], a[half][i], sum[i][j], 0, 0, 0);
-        // an LDS read (of the next half), a few products, and so on: left to itself the compiler reads every operand right before
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+                    sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[from][j][PART_B[pair]], a[from][i][PART_A[pair]], sum[i][j], 0, 0, 0);
+        // an LDS read (of what comes next), a few products, and so on: left to itself the compiler reads every operand right before
         // its use
-        constexpr int READS = S::TM * (A_FAST ? 1 : 2) + S::TN * (B_FAST ? 1 : 2), PRODUCTS = S::TM * S::TN;
+        constexpr int READS = PARTS * (S::TM * (A_FAST ? 1 : 2) + S::TN * (B_FAST ? 1 : 2)), PRODUCTS = PAIRS * S::TM * S::TN;
         constexpr int EACH = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
 #pragma unroll
         for (int r = 0; r < READS; ++r) {
@@ -403,9 +425,9 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         }
     };
 
-    // One half of a step's k's is multiplied from registers while the next half is read from the LDS and later steps are on their
-    // way.  At the meeting between the halves everybody has read the step's second half, so that its place is free, and the next
-    // step has come.  Steps past the end bring zeros.
+    // One half of a step's k's (or, in parts, one step) is multiplied from registers while the next is read from the LDS and later
+    // steps are on their way.  At a meeting everybody has read all of a step, so that its place is free, and the next step has come.
+    // Steps past the end bring zeros.
 #pragma unroll
     for (int s = 0; s < S::STAGES; ++s) {
         load(s);
@@ -414,15 +436,30 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
     wait_and_meet<(S::STAGES - 1) * PER_STEP>();
     read(0, 0);
     uint32_t slot = 0;
-    for (uint32_t i = 0; i < steps; ++i) {
-        read(slot, 1);
-        multiply(0);
+    const auto meet = [&]() {
         wait_and_meet<(S::STAGES - 2) * PER_STEP>();
         load(slot);
         slot = slot + 1 == S::STAGES ? 0 : slot + 1;
-        read(slot, 0);
-        multiply(1);
-        advance();
+    };
+    if constexpr (PARTS == 1) {
+        for (uint32_t i = 0; i < steps; ++i) {
+            read(slot, 1);
+            multiply(0);
+            meet();
+            read(slot, 0);
+            multiply(1);
+            advance();
+        }
+    } else {
+        for (uint32_t i = 0; i < steps; i += 2) {
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+                meet();
+                read(slot, odd ^ 1);
+                multiply(odd);
+                advance();
+            }
+        }
     }
     // Sums to results by way of the LDS, some rows of tiles at a time, so that threads next to each other work on columns next to
     // each other and memory sees whole rows of the tile (straight from the registers, in pieces of 64 bytes, 8192 x 8192 gates took
@@ -436,7 +473,7 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         if constexpr (KIND == SLOPE && !EARLY) // on their way while the sums are exchanged
 #pragma unroll
             for (int item = 0; item < ITEMS; ++item)
-                if (row_of(step, item) < p.M && c < p.N) load_pre(p.to, row_of(step, item), c, pre[item]);
+                if (row_of(step, item) < p.M && c < last) load_pre(p.to, row_of(step, item), c, pre[item]);
         if (step > 0) lds_barrier();
 #pragma unroll
         for (int i = 0; i < HIGH; ++i)
@@ -449,7 +486,7 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
         for (int item = 0; item < ITEMS; ++item) {
             const uint32_t m = row_of(step, item);
             const float *row = rows + (mine + item * (S::THREADS / CHUNKS)) * PITCH;
-            if (m >= p.M || c >= p.N) continue;
+            if (m >= p.M || c >= last) continue;
             // (of a wavefront's columns the first half are gates, the second the ups of the same units)
             const uint32_t at = KIND == GATE ? 8 * chunk / HALF * (2 * HALF) + 8 * chunk % HALF : 8 * chunk;
             float v[8], u[8];
@@ -468,11 +505,11 @@ __device__ __forceinline__ void work(const Product &p, uint32_t block, uint32_t 
     }
 }
 
-template <class S, bool A_FAST, bool B_FAST, int KIND, int PARTS>
+template <class S, bool A_FAST, bool B_FAST, int KIND>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void product_kernel(const Product p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    work<S, A_FAST, B_FAST, KIND, PARTS>(p, blockIdx.x, gridDim.x, lds);
+    work<S, A_FAST, B_FAST, KIND>(p, blockIdx.x, gridDim.x, lds);
 }
 
 // The three gradients, which wait for nothing but dg, du and h, in one launch: dx, of operands along k, then the weights', of
@@ -480,23 +517,23 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
 struct Gradients {
     Product dx, dw_gate_up, dw_down;
 };
-template <class S, int PARTS>
+template <class S>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void gradients_kernel(const Gradients g)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const uint32_t first = g.dx.blocks(), second = g.dw_gate_up.blocks();
     if (blockIdx.x < first) {
-        work<S, true, true, STORE, PARTS>(g.dx, blockIdx.x, first, lds);
+        work<S, true, true, STORE>(g.dx, blockIdx.x, first, lds);
     } else {
         const bool up = blockIdx.x - first < second;
-        work<S, false, false, STORE, PARTS>(up ? g.dw_gate_up : g.dw_down, blockIdx.x - first - (up ? 0 : second), up ? second : g.dw_down.blocks(), lds);
+        work<S, false, false, STORE>(up ? g.dw_gate_up : g.dw_down, blockIdx.x - first - (up ? 0 : second), up ? second : g.dw_down.blocks(), lds);
     }
 }
 
 // The shares of products whose k's were divided, added in order; then as above.  A thread has eight columns.
 struct Join {
     const float *partial;
-    uint32_t shares, M, N, up; // up: from gates to ups
+    uint32_t shares, M, N, up; // N: columns to be written; up: from gates to ups
     uint64_t ld, first;        // first: chunk of eight columns where this one starts, of all of the launch's
     Target to;
 };
@@ -543,12 +580,12 @@ __global__ __launch_bounds__(256) void join_kernel(const Joins joins)
 // ------------------------------------------------------------------------------------------------ operands
 
 // Matrices as operands want them: rows of two pieces of `piece` columns (one, if pieces is 1), each padded with zeros to `pitch` (a
-// multiple of eight); fp32 ones in three parts.  A thread has eight columns.
+// multiple of eight, or, for fp32 ones in three parts, of 32).  A thread has eight columns.
 template <class T>
 struct Pack {
     const T *src;
     bf16 *dst;
-    uint64_t ld, part, first; // first: chunk of eight columns where this one starts, of all of the launch's
+    uint64_t ld, first; // first: chunk of eight columns where this one starts, of all of the launch's
     uint32_t piece, pieces, pitch;
 };
 template <class T>
@@ -575,7 +612,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const Packs<T> packs)
 #pragma unroll
             for (int j = 0; j < Chunk<T>::N; ++j) v[i + j] = some[j];
         }
-        store_operand<sizeof(T) == 4 ? 3 : 1>(p.dst + r * ((uint64_t)p.pitch * p.pieces) + c, p.part, v);
+        constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+        store_operand<PARTS>(p.dst + r * ((uint64_t)p.pitch * p.pieces * PARTS), c, v);
     }
 }
 

@@ -263,6 +263,17 @@ def act_of(act, g):
     return g.clamp(min=0), (g > 0).double()
 
 
+class Workspace:
+    """as many bytes as the library asks for, and a mark behind them"""
+
+    def __init__(self, need):
+        self.flat = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        self.t = self.flat[:need]
+
+    def untouched(self):
+        return bool((self.flat[self.t.numel():] == 0x5A).all())
+
+
 def ffn_buffers(n, n_in, n_hidden, n_out, dtype, seed, extra, offset):
     x = Buffer(n, n_in, dtype, normal(seed, n, n_in).to(dtype), extra, offset)
     wgu = Buffer(n_in, 2 * n_hidden, dtype, normal(seed + 1, n_in, 2 * n_hidden, scale=n_in ** -0.5).to(dtype), 0, offset)
@@ -277,9 +288,10 @@ def ffn_case(n, n_in, n_hidden, n_out, kind, act, seed=41, extra=0, offset=0):
     y, served = (Buffer(n, n_out, dtype, None, extra, offset) for _ in range(2))
     pre = Buffer(n, 2 * n_hidden, torch.float32)
     sizes = (n, n_in, n_hidden, n_out, code)
-    ws = torch.empty(eck.gatedffn_forward_workspace_bytes(*sizes), dtype=torch.uint8, device="cuda")
-    eck.gatedffn_forward(x.t, wgu.t, wd.t, y.t, ws, pre_out=pre.t, act=act)
-    eck.gatedffn_forward(x.t, wgu.t, wd.t, served.t, ws, act=act)
+    ws = Workspace(eck.gatedffn_forward_workspace_bytes(*sizes))
+    eck.gatedffn_forward(x.t, wgu.t, wd.t, y.t, ws.t, pre_out=pre.t, act=act)
+    eck.gatedffn_forward(x.t, wgu.t, wd.t, served.t, ws.t, act=act)
+    assert ws.untouched()
     X, WGU, WD, DY = (b.t.double().cpu() for b in (x, wgu, wd, dy))
     want_pre = X @ WGU
     off_pre = (n_in + 2) * E * (X.abs() @ WGU.abs())
@@ -304,8 +316,8 @@ def ffn_case(n, n_in, n_hidden, n_out, kind, act, seed=41, extra=0, offset=0):
     a, slope = act_of(act, g)
     h = a * up
     dx, dwgu, dwd = Buffer(n, n_in, dtype, None, extra, offset), Buffer(n_in, 2 * n_hidden, dtype, None, 0, offset), Buffer(n_hidden, n_out, dtype, None, 0, offset)
-    ws = torch.empty(eck.gatedffn_backward_workspace_bytes(*sizes), dtype=torch.uint8, device="cuda")
-    eck.gatedffn_backward(x.t, wgu.t, wd.t, pre.t, dy.t, dx.t, dwgu.t, dwd.t, ws, act=act)
+    ws = Workspace(eck.gatedffn_backward_workspace_bytes(*sizes))
+    eck.gatedffn_backward(x.t, wgu.t, wd.t, pre.t, dy.t, dx.t, dwgu.t, dwd.t, ws.t, act=act)
     dh = DY @ WD.t()
     off_dh = (n_out + 2) * E * (DY.abs() @ WD.abs().t())
     off_a, off_s = 8 * E * g.abs(), 16 * E * (1 + g.abs())
@@ -315,6 +327,7 @@ def ffn_case(n, n_in, n_hidden, n_out, kind, act, seed=41, extra=0, offset=0):
     d, off = torch.cat((dg, du), 1), torch.cat((off_dg, off_du), 1)
     off += u * (d.abs() + off)
     off_h = off_a * up.abs() + u * h.abs() + 4 * E * h.abs()
+    bounds = []
     for got, A, off_A, B, off_B, K, what in ((dx.t, d, off, WGU.t(), 0 * WGU.t(), 2 * n_hidden, "dx"),
                                              (dwgu.t, X.t(), 0 * X.t(), d, off, n, "dw_gate_up"),
                                              (dwd.t, h.t(), off_h.t(), DY, 0 * DY, n, "dw_down")):
@@ -322,14 +335,16 @@ def ffn_case(n, n_in, n_hidden, n_out, kind, act, seed=41, extra=0, offset=0):
         # (1.01: what errors of errors add)
         bound = 1.01 * (off_A @ B.abs() + A.abs() @ off_B + (K + 2) * E * (A.abs() @ B.abs()) + u * want.abs())
         check(got, want, bound, what)
+        bounds.append(bound)
     for b in (x, wgu, wd, dy, pre, dx, dwgu, dwd):
         assert b.untouched()
     # each gradient by itself
     for k, whole in enumerate((dx, dwgu, dwd)):
         alone = [None] * 3
         alone[k] = torch.empty_like(whole.t)
-        eck.gatedffn_backward(x.t, wgu.t, wd.t, pre.t, dy.t, *alone, ws, act=act)
-        assert torch.equal(alone[k], whole.t), k
+        eck.gatedffn_backward(x.t, wgu.t, wd.t, pre.t, dy.t, *alone, ws.t, act=act)
+        check(alone[k], whole.t.double().cpu(), 2 * bounds[k], "alone")   # (other shares of k, another order of sums)
+    assert ws.untouched()
 
 
 SHAPES = [(1, 1, 1, 1), (1, 64, 256, 64), (3, 5, 7, 2), (2, 33, 130, 65), (17, 64, 128, 64), (33, 40, 72, 24), (64, 64, 64, 64), (130, 200, 77, 200),
