@@ -35,15 +35,15 @@ struct Plan {
 };
 
 // The shares of k that should take a product of M x N x K (N: columns of b) least time in tiles of a shape, and that time (us).  The
-// constants were fitted to 186 products of 17 blocks (1 to 131072 rows, widths 7 to 8192, both types), each in all shapes and up
-// to 64 shares: the choice takes 0.7 % more than the best, on average, and 15 % at most.
+// constants were fitted to 186 products of 17 blocks in bf16 and 90 of 15 blocks in parts (1 to 131072 rows, widths 7 to 8192), each in
+// all shapes and up to 64 shares: the choice takes 0.7 % more than the best, on average, and 15 (in parts 21) % at most.
 Plan plan_shape(int shape, uint64_t M, uint64_t N, uint64_t K, uint32_t parts)
 {
     static const struct {
         uint32_t side, at_once;   // blocks a compute unit
         double step, alone, rest; // a step of a tile when the unit is full, with nothing beside them, and a tile's start and end
     } SHAPES[2][3] = {{{64, 3, 0.27, 0.31, 2.2}, {128, 2, 0.5, 0.71, 3.0}, {256, 1, 1.29, 1.58, 8.3}},
-                      {{64, 2, 0.3, 0.35, 2.2}, {128, 1, 0.8, 0.8, 5.0}, {}}}; // (parts)
+                      {{64, 2, 0.53, 0.5, 2.1}, {128, 1, 0.8, 0.88, 5.1}, {}}}; // (parts)
     const auto &of = SHAPES[parts == 3][shape];
     const uint64_t steps = parts == 3 ? (K + STAGE_K<3> - 1) / STAGE_K<3> : (K + STAGE_K<1> - 1) / STAGE_K<1>, tiles = (M + of.side - 1) / of.side * ((N + of.side - 1) / of.side);
     Plan best = {shape, 1, 1e300};

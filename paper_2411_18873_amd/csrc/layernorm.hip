@@ -628,7 +628,8 @@ uint32_t at_most(uint64_t blocks, uint32_t most) { return (uint32_t)(blocks < mo
 // Blocks of the backward pass, each of which leaves a partial sum per column: what keeps 32 KB on their way to a compute unit, one
 // to four a unit, two at least of blocks that work on several rows at once.  (us by 1, 2, 3 and 4 a unit: 8192 rows of 4096 bf16
 // 52.9, 49.0, 54.7, 67.9; of fp32 81.6, 86.2, 93.9, 93.8; 32768 of 1024 bf16 39.8, 37.6, 38.7, 46.0; 50003 of 250 fp32 66.8, 44.3,
-// 37.0, 33.7; 16384 of 2000 bf16 57.4, 48.2.)
+// 37.0, 33.7; 16384 of 2000 bf16 57.4, 48.2.)  One where the partial sums, 16 bytes a column written and read, would be more than what the rows
+// move (1000 rows of 4096 bf16: 16.1 for 19.3; 1967 of 3840 stay at two, 23.1 for 25.7).
 uint32_t backward_blocks(uint64_t n, uint32_t width, int32_t dtype, int32_t order)
 {
     if (order == ECK_COLUMNS) return at_most((n + 31) / 32, 1024); // (32 candidates: the smallest tile)
@@ -639,6 +640,7 @@ uint32_t backward_blocks(uint64_t n, uint32_t width, int32_t dtype, int32_t orde
     uint64_t a_unit = 32768 / (2 * rows * width * size);
     a_unit = a_unit > 4 ? 4 : a_unit < 1 ? 1 : a_unit;
     if (rows > 1 && a_unit < 2) a_unit = 2;
+    if (16 * 256 * a_unit > n * 3 * size) a_unit = 1;
     return at_most((n + rows - 1) / rows, (uint32_t)(256 * a_unit));
 }
 constexpr uint32_t LONG_PARTS = 64;

@@ -550,12 +550,13 @@ def candidates_dedup(genes, n, flags, overwrite=False, ws=None):
 
 def _rows(t, name, dtype, shape=None):
     """a matrix of activations: CUDA, of dtype, values of a row side by side (rows may lie further apart); its row distance"""
-    if not (t.is_cuda and t.dtype is dtype and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+    is_shape, stride = t.shape, t.stride()
+    if not (t.is_cuda and t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or is_shape[1] == 1)):
         raise TypeError("%s must be a CUDA matrix of %s with adjacent columns" % (name, dtype))
-    if shape is not None and t.shape != shape:
+    if shape is not None and is_shape != shape:
         raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
     # (torch says any distance for a single row, and a matrix of one column may be a view of any)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return stride[0] if is_shape[0] > 1 else is_shape[1]
 
 
 def _vector(t, name, width):
@@ -574,10 +575,8 @@ def _ws(ws):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _normed(x, order, n, width, dtype, name):
-    """the row distance of a layer norm's input (or its gradient) of n candidates, in its order"""
-    if order != COLUMNS:
-        return _rows(x, name, dtype, (n, width))
+def _feature_rows(x, n, width, dtype, name):
+    """the row distance of a feature matrix (or its gradient) of n candidates"""
     ld = _rows(x, name, dtype)
     if x.shape[0] != width or x.shape[1] < n:
         raise ValueError("%s must be of shape (%d, %d or more)" % (name, width, n))
@@ -586,11 +585,12 @@ def _normed(x, order, n, width, dtype, name):
 
 def layernorm_forward(x, gamma, beta, y, mean_out=None, rstd_out=None, eps=1e-5, order=ROWS):
     """y [n][width] = layer norm of x: [n][width] (ROWS), or a feature matrix [width][n or more] (COLUMNS)"""
-    n, width = y.shape
-    ld_y = _rows(y, "y", y.dtype)
-    ld_x = _normed(x, order, n, width, y.dtype, "x")
+    shape, dtype = y.shape, y.dtype
+    n, width = shape
+    ld_y = _rows(y, "y", dtype)
+    ld_x = _rows(x, "x", dtype, shape) if order != COLUMNS else _feature_rows(x, n, width, dtype, "x")
     _check("layernorm_forward", lib().layernorm_forward(
-        x.data_ptr(), order, _FEAT_DTYPE[y.dtype], ld_x, n, width, _vector(gamma, "gamma", width), _vector(beta, "beta", width), eps,
+        x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, _vector(gamma, "gamma", width), _vector(beta, "beta", width), eps,
         y.data_ptr(), ld_y, _vector(mean_out, "mean_out", n), _vector(rstd_out, "rstd_out", n), _stream()))
 
 
@@ -600,13 +600,16 @@ def layernorm_backward_workspace_bytes(n, width, dtype):
 
 def layernorm_backward(x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, order=ROWS):
     """dx (as x, or None), dgamma and dbeta (float [width], or both None) from dy [n][width] and the forward call's statistics"""
-    n, width = dy.shape
-    ld_dy = _rows(dy, "dy", dy.dtype)
-    ld_x = _normed(x, order, n, width, dy.dtype, "x")
-    ld_dx = 0 if dx is None else _normed(dx, order, n, width, dy.dtype, "dx")
+    shape, dtype = dy.shape, dy.dtype
+    n, width = shape
+    ld_dy = _rows(dy, "dy", dtype)
+    if order != COLUMNS:
+        ld_x, ld_dx = _rows(x, "x", dtype, shape), 0 if dx is None else _rows(dx, "dx", dtype, shape)
+    else:
+        ld_x, ld_dx = _feature_rows(x, n, width, dtype, "x"), 0 if dx is None else _feature_rows(dx, n, width, dtype, "dx")
     ws_ptr, ws_bytes = _ws(ws)
     _check("layernorm_backward", lib().layernorm_backward(
-        x.data_ptr(), order, _FEAT_DTYPE[dy.dtype], ld_x, dy.data_ptr(), ld_dy, n, width, _vector(gamma, "gamma", width),
+        x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, dy.data_ptr(), ld_dy, n, width, _vector(gamma, "gamma", width),
         _vector(mean, "mean", n), _vector(rstd, "rstd", n), _ptr(dx), ld_dx, _vector(dgamma, "dgamma", width),
         _vector(dbeta, "dbeta", width), ws_ptr, ws_bytes, _stream()))
 
@@ -615,11 +618,12 @@ def dropout_apply(x, out, p_drop_q32, seed, round=0, first_row=0, residual=None)
     """out = residual + dropout(x) with probability p_drop_q32 / 2^32; on a gradient (no residual) the backward pass"""
     if not 0 <= p_drop_q32 < 1 << 32:
         raise ValueError("p_drop_q32 must be the probability times 2^32, below 2^32")
-    n, width = out.shape
-    ld_out = _rows(out, "out", out.dtype)
-    ld_x = _rows(x, "x", out.dtype, out.shape)
-    ld_res = 0 if residual is None else _rows(residual, "residual", out.dtype, out.shape)
-    _check("dropout_apply", lib().dropout_apply(x.data_ptr(), _FEAT_DTYPE[out.dtype], ld_x, n, width, p_drop_q32, seed, round, first_row,
+    shape, dtype = out.shape, out.dtype
+    n, width = shape
+    ld_out = _rows(out, "out", dtype)
+    ld_x = _rows(x, "x", dtype, shape)
+    ld_res = 0 if residual is None else _rows(residual, "residual", dtype, shape)
+    _check("dropout_apply", lib().dropout_apply(x.data_ptr(), _FEAT_DTYPE[dtype], ld_x, n, width, p_drop_q32, seed, round, first_row,
                                                 _ptr(residual), ld_res, out.data_ptr(), ld_out, _stream()))
 
 
