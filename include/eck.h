@@ -532,11 +532,19 @@ int32_t dropout_apply(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, u
  *   then up columns), w_down: device [n_hidden][n_out], contiguous ([fan_in]
  *   [fan_out] row-major, as in a model's state); y: device [n][ld_y]; all of
  *   dtype.  act: ECK_ACT_*.  pre_out: device float [n][2*n_hidden], receives
- *   [g | u] for gatedffn_backward, or NULL.
+ *   [g | u] for gatedffn_backward, or NULL (narrow blocks of many rows are
+ *   fastest then).
  * h is rounded to dtype before the second product; y must not overlap inputs.
+ * Up to four rows are multiplied in fp32 instructions; more on the matrix
+ * cores, fp32 ones as sums of six products of bfloat16 parts, as good as fp32
+ * products for magnitudes of 2^-100 to 2^127 (and zeros; an infinite input
+ * gives NaN or infinities in its row, smaller numbers lose low bits).
+ * ws: room for h, for shares of sums, and for copies of the operands of an
+ * fp32 block or of matrices that do not start on 16 bytes or whose rows are
+ * no multiple of eight elements.  The queries say 0 for sizes that are refused.
  * Errors: EINVAL (nulls, a zero size, bad dtype or act), ESHAPE (an ld too
- * small), EUNSUPPORTED (n > 2^31 or a width > 2^24, or more than 2^31 tiles),
- * EWORKSPACE, EALIGN. */
+ * small), EUNSUPPORTED (n > 2^31, a width > 2^20, or more than 2^22 tiles of
+ * 64 x 64 in a product's result), EWORKSPACE, EALIGN. */
 uint64_t gatedffn_forward_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_hidden, uint32_t n_out, int32_t dtype);
 int32_t gatedffn_forward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t n_in, uint32_t n_hidden,
                          uint32_t n_out, const void *w_gate_up, const void *w_down, int32_t act, void *y,

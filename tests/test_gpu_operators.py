@@ -478,9 +478,11 @@ def test_rows_more_than_2_31_elements_apart():
     assert torch.equal(x.contiguous(), want)
 
 
-def test_a_residual_block_on_a_stream_and_as_a_graph():
+@pytest.mark.parametrize("n,width,hidden,kind", [(300, 128, 256, "bf16"), (4096, 1024, 2048, "bf16"), (300, 128, 256, "f32"), (1500, 500, 1000, "f32"),
+                                                 (2, 100, 300, "bf16")])
+def test_a_residual_block_on_a_stream_and_as_a_graph(n, width, hidden, kind):
     """x + dropout(ffn(layernorm(x))), forward and backward, on a stream of its own and replayed, equals the eager calls bit for bit"""
-    n, width, hidden, p, dtype = 300, 128, 256, 1 << 30, torch.bfloat16
+    p, (dtype, code, _) = 1 << 30, DTYPES[kind]
     g = [t.cuda() for t in (normal(1, n, width).to(dtype), normal(2, width, 2 * hidden, scale=0.1).to(dtype),
                             normal(3, hidden, width, scale=0.1).to(dtype), normal(4, n, width).to(dtype))]
     x, wgu, wd, dy = g
@@ -489,9 +491,9 @@ def test_a_residual_block_on_a_stream_and_as_a_graph():
     xn, f, out, d_f, d_xn, dx = (make(n, width) for _ in range(6))
     pre, dwgu, dwd = make(n, 2 * hidden, d=torch.float32), torch.empty_like(wgu), torch.empty_like(wd)
     mean, rstd, dgamma, dbeta = (make(k, d=torch.float32) for k in (n, n, width, width))
-    sizes = (n, width, hidden, width, eck.BF16)
+    sizes = (n, width, hidden, width, code)
     ws = make(max(eck.gatedffn_forward_workspace_bytes(*sizes), eck.gatedffn_backward_workspace_bytes(*sizes),
-                  eck.layernorm_backward_workspace_bytes(n, width, eck.BF16)), d=torch.uint8)
+                  eck.layernorm_backward_workspace_bytes(n, width, code)), d=torch.uint8)
     outputs = (out, dx, dwgu, dwd, dgamma, dbeta)
 
     def block():
