@@ -12,10 +12,12 @@ namespace product {
 // Rows times a matrix [K][N]: every weight is read once, so the time is its bytes at the memory's rate.  A block takes a cache line of
 // columns, or one of gates and one of the ups of the same units, and a share of the k's: a compute unit alone draws no more than some
 // 50 GB/s, so all of them have to.  Sixteen wavefronts with eight loads of sixteen bytes each on their way (four, beside the sums of
-// four rows), the rows in the LDS.  The shares of (g | u) are joined by who reads them, as rows of the second product.  Sums in fp32
+// four rows and more), the rows in the LDS.  The shares of (g | u) are joined by who reads them, as rows of the second product.  Sums in fp32
 // instructions, whatever the type and the alignment, with no copies of the weights.
 
-constexpr int VECTOR_K = 4096; // values of a row in the LDS at a time
+// values of a row in the LDS at a time
+template <int ROWS>
+constexpr int VECTOR_K = ROWS <= 4 ? 4096 : 16384 / ROWS;
 
 struct Rows {
     const void *a;         // rows of T, or NULL: a(g) u from the shares of
@@ -31,8 +33,9 @@ template <class T, bool PAIRS, int ROWS>
 __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *w, uint64_t ld_w, uint32_t N, uint32_t up, T *out, uint64_t ld_out,
                                                       float *sums_out)
 {
-    constexpr int V = Chunk<T>::N, LINE = 8 * V, LANES = PAIRS ? 16 : 8, STEP = 64 / LANES, AHEAD = ROWS == 4 ? 4 : 8, WAVES = 16;
-    extern __shared__ __attribute__((aligned(16))) float shared[]; // ROWS x VECTOR_K, then the wavefronts' sums
+    constexpr int V = Chunk<T>::N, LINE = 8 * V, LANES = PAIRS ? 16 : 8, STEP = 64 / LANES, AHEAD = ROWS >= 4 ? 4 : 8, WAVES = 16;
+    constexpr int MOST = VECTOR_K<ROWS>;
+    extern __shared__ __attribute__((aligned(16))) float shared[]; // [k][ROWS], then the wavefronts' sums
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LANES, n = rows.n, K = rows.K;
     const uint32_t c0 = blockIdx.x * LINE, mine = c0 + j % 8 * V, here = mine < N ? (N - mine < V ? N - mine : V) : 0;
     const uint32_t begin = (uint32_t)((uint64_t)K * blockIdx.y / gridDim.y), end = (uint32_t)((uint64_t)K * (blockIdx.y + 1) / gridDim.y);
@@ -42,29 +45,30 @@ __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[r][i] = 0.0f;
-    for (uint32_t k0 = begin; k0 < end; k0 += VECTOR_K) {
-        const uint32_t some = end - k0 < VECTOR_K ? end - k0 : VECTOR_K;
+    for (uint32_t k0 = begin; k0 < end; k0 += MOST) {
+        const uint32_t some = end - k0 < MOST ? end - k0 : MOST;
         __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-            for (uint32_t k = threadIdx.x; k < some; k += 1024) {
-                float x = 0.0f;
-                if (r < (int)n && (PAIRS || rows.a)) x = (float)((const T *)rows.a)[r * rows.ld + k0 + k];
-                else if (r < (int)n) {
-                    float g = 0.0f, u = 0.0f;
-                    for (uint32_t s = 0; s < rows.shares; ++s) {
-                        const float *row = rows.sums + ((uint64_t)s * n + r) * 2 * K + k0 + k;
-                        g += row[0];
-                        u += row[K];
-                    }
-                    if (rows.pre && blockIdx.x == 0) {
-                        rows.pre[(uint64_t)r * 2 * K + k0 + k] = g;
-                        rows.pre[(uint64_t)r * 2 * K + K + k0 + k] = u;
-                    }
-                    with_act(rows.act, [&](auto act) { x = (float)(T)(gate_as<decltype(act)::value>(g).value * u); });
+#pragma unroll 4
+        for (uint32_t at = threadIdx.x; at < ROWS * some; at += 1024) { // (all rows at once: their loads wait together)
+            const uint32_t r = at / some, k = at % some;
+            float x = 0.0f;
+            if (r < n && (PAIRS || rows.a)) x = (float)((const T *)rows.a)[r * rows.ld + k0 + k];
+            else if (r < n) {
+                float g = 0.0f, u = 0.0f;
+#pragma unroll 4
+                for (uint32_t s = 0; s < rows.shares; ++s) {
+                    const float *row = rows.sums + ((uint64_t)s * n + r) * 2 * K + k0 + k;
+                    g += row[0];
+                    u += row[K];
                 }
-                shared[r * VECTOR_K + k] = x;
+                if (rows.pre && blockIdx.x == 0) {
+                    rows.pre[(uint64_t)r * 2 * K + k0 + k] = g;
+                    rows.pre[(uint64_t)r * 2 * K + K + k0 + k] = u;
+                }
+                with_act(rows.act, [&](auto act) { x = (float)(T)(gate_as<decltype(act)::value>(g).value * u); });
             }
+            shared[k * ROWS + r] = x;
+        }
         __syncthreads();
         for (uint32_t k = wave * STEP + lane / LANES; k < some; k += AHEAD * WAVES * STEP) {
             Chunk<T> some_w[AHEAD];
@@ -84,24 +88,38 @@ __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *
 #pragma unroll
             for (int t = 0; t < AHEAD; ++t) {
                 const uint32_t at = k + t * WAVES * STEP;
+                if (at >= some) break;
+                float x[ROWS];
+                __builtin_memcpy(x, __builtin_assume_aligned(shared + at * ROWS, ROWS >= 4 ? 16 : ROWS * 4), sizeof x);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
-                    const float x = at < some ? shared[r * VECTOR_K + at] : 0.0f;
+                for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sum[r][i] = fmaf(x, (float)some_w[t].v[i], sum[r][i]);
-                }
+                    for (int i = 0; i < V; ++i) sum[r][i] = fmaf(x[r], (float)some_w[t].v[i], sum[r][i]);
             }
         }
     }
-    // over the k's of a wavefront's lanes, then over the wavefronts
+    // Over the k's of a wavefront's lanes, then over the wavefronts.  Two halves of the lanes exchange two sums each, so that each half
+    // goes on with one of them: after two rounds a quarter of the lanes has a quarter of the sums (and not four exchanges for every sum,
+    // which took longer than the products of a small block).
+    constexpr int COUNT = ROWS * V;
+    float *const flat = &sum[0][0];
+#pragma unroll
+    for (int i = 0; i < COUNT / 2; ++i) {
+        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(flat[i]), __float_as_uint(flat[i + COUNT / 2]), false, false);
+        flat[i] = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT / 4; ++i) {
+        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(flat[i]), __float_as_uint(flat[i + COUNT / 4]), false, false);
+        flat[i] = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+        if (LANES == 8) flat[i] += __uint_as_float(lane_exchange(__float_as_uint(flat[i]), 8));
+    }
     __syncthreads();
+    if ((lane & 15) < LANES)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-#pragma unroll
-            for (uint32_t stride = LANES; stride < 64; stride <<= 1) sum[r][i] += __uint_as_float(lane_exchange(__float_as_uint(sum[r][i]), stride));
-            if (lane < LANES) shared[(wave * ROWS + r) * (LANES * V) + j * V + i] = sum[r][i];
+        for (int i = 0; i < COUNT / 4; ++i) {
+            const uint32_t which = i + (lane >> 5) * (COUNT / 2) + (lane >> 4 & 1) * (COUNT / 4); // row, column of this lane's V
+            shared[(wave * ROWS + which / V) * (LANES * V) + j * V + which % V] = flat[i];
         }
     __syncthreads();
     constexpr int COLUMNS = LANES * V; // gates, then ups

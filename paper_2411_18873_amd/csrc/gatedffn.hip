@@ -192,11 +192,17 @@ struct Workspace {
 // columns of a matrix of `width` as an operand
 uint64_t pitch_of(uint64_t width, uint32_t parts) { return up_to(width, parts == 3 ? 32 : 8); }
 
+template <class T>
+bool is_operand(const T *src, uint64_t ld, uint32_t piece)
+{
+    return sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16);
+}
+
 // The matrix [rows][pieces * piece] as an operand: itself where it is one already, else to be copied to `room`.
 template <class T>
 Operand as_operand(const T *src, uint64_t ld, uint64_t rows, uint32_t piece, uint32_t pieces, char *room, Packs<T> &packs)
 {
-    if (sizeof(T) == 2 && piece % 8 == 0 && ld % 8 == 0 && ld <= MAX_STRAIGHT_LD && aligned(src, 16)) return {(const bf16 *)src, ld};
+    if (is_operand(src, ld, piece)) return {(const bf16 *)src, ld};
     const uint32_t pitch = (uint32_t)pitch_of(piece, parts_of<T>);
     const uint64_t width = (uint64_t)pitch * pieces;
     packs.one[packs.count++] = {src, (bf16 *)room, ld, packs.chunks, piece, pieces, pitch};
@@ -279,8 +285,12 @@ Rooms rooms(const Sizes &s, bool backward)
 
 constexpr uint32_t NO_GAP = 0xFFFFFFFFu;
 
-// few rows: the weights' bytes (block_forward.h)
-constexpr uint32_t FEW_ROWS = 4;
+// Few rows: the weights' bytes (block_forward.h).  Up to how many rows that is faster than products of matrices.  us, products first:
+// 2048-5632-2048 of bf16 one row 23.7 and 23.5, two 23.7 and 28.6; 4096-8192-4096 one 54.4 and 51.9, two 53.3 and 53.7; where the
+// weights have to be copied, 1000-3001-1001, four rows 27.3 and 22.9, eight 27.5 and 27.2; of fp32, whose weights always have to be,
+// sixteen rows 43.3 and 39.8, 338.8 and 144.7 (4096-8192-4096).
+constexpr uint32_t FEW_ROWS = 1, FEW_COPIED = 8, FEW_F32 = 16;
+bool few(const Sizes &s, bool straight) { return s.n <= (s.parts == 3 ? FEW_F32 : straight ? FEW_ROWS : FEW_COPIED); }
 
 // of the k's, so that all compute units have a block if every one of them gets two rounds of loads at least
 uint32_t vector_shares(uint32_t K, uint32_t N, uint32_t line)
@@ -306,7 +316,8 @@ template <class T, bool PAIRS, int ROWS>
 int32_t launch_vector_rows(const Rows &rows, uint32_t shares, const T *w, uint64_t ld_w, uint32_t N, T *out, uint64_t ld_out, float *sums,
                            hipStream_t st)
 {
-    constexpr int LINE = 8 * Chunk<T>::N, SUMS = 16 * ROWS * LINE * (PAIRS ? 2 : 1), LDS = (ROWS * VECTOR_K > SUMS ? ROWS * VECTOR_K : SUMS) * 4;
+    constexpr int LINE = 8 * Chunk<T>::N, SUMS = 16 * ROWS * LINE * (PAIRS ? 2 : 1), VALUES = ROWS * VECTOR_K<ROWS>;
+    constexpr int LDS = (VALUES > SUMS ? VALUES : SUMS) * 4;
     auto kernel = vector_kernel<T, PAIRS, ROWS>;
     ECK_TRY(allow_lds(kernel, LDS));
     hipLaunchKernelGGL(kernel, dim3((N + LINE - 1) / LINE, shares), dim3(1024), LDS, st, rows, w, ld_w, N, N, out, ld_out, sums);
@@ -318,7 +329,10 @@ int32_t launch_vector(const Rows &rows, uint32_t shares, const T *w, uint64_t ld
 {
     if (rows.n == 1) return launch_vector_rows<T, PAIRS, 1>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
     if (rows.n == 2) return launch_vector_rows<T, PAIRS, 2>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
-    return launch_vector_rows<T, PAIRS, 4>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    if (rows.n <= 4) return launch_vector_rows<T, PAIRS, 4>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    if constexpr (sizeof(T) == 4)
+        if (rows.n > 8) return launch_vector_rows<T, PAIRS, 16>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    return launch_vector_rows<T, PAIRS, 8>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
 }
 
 template <class T>
@@ -379,7 +393,8 @@ int32_t forward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, c
                 void *ws, hipStream_t st)
 {
     constexpr uint32_t P = parts_of<T>;
-    if (s.n <= FEW_ROWS) return forward_few(x, ld_x, s, w_gate_up, w_down, act, y, ld_y, pre, ws, st);
+    if (few(s, is_operand(w_gate_up, 2ull * s.n_hidden, s.n_hidden) && is_operand(w_down, s.n_out, s.n_out)))
+        return forward_few(x, ld_x, s, w_gate_up, w_down, act, y, ld_y, pre, ws, st);
     const Rooms room = rooms(s, false);
     Workspace space = {(char *)ws};
     Packs<T> packs = {};
@@ -469,9 +484,9 @@ bool act_ok(int32_t act) { return act == ECK_ACT_SILU || act == ECK_ACT_GELU || 
 uint64_t workspace_bytes(const Sizes &s, int32_t dtype, bool backward)
 {
     if (s.n == 0 || s.n_in == 0 || s.n_hidden == 0 || s.n_out == 0 || !is_dtype(dtype) || !sizes_ok(s)) return 0;
-    if (!backward && s.n <= FEW_ROWS) {
+    if (!backward && few(s, false)) {
         const VectorRooms room = vector_rooms(s);
-        return room.sums + room.sums_y;
+        return few(s, true) ? room.sums + room.sums_y : most(room.sums + room.sums_y, rooms(s, false).total());
     }
     return rooms(s, backward).total();
 }

@@ -349,7 +349,8 @@ def ffn_case(n, n_in, n_hidden, n_out, kind, act, seed=41, extra=0, offset=0):
 
 SHAPES = [(1, 1, 1, 1), (1, 64, 256, 64), (3, 5, 7, 2), (2, 33, 130, 65), (17, 64, 128, 64), (33, 40, 72, 24), (64, 64, 64, 64), (130, 200, 77, 200),
           (257, 256, 512, 256), (512, 72, 1000, 1), (5, 300, 300, 300), (129, 136, 264, 520), (1025, 64, 96, 64), (300, 512, 256, 128),
-          (16, 1024, 2048, 1024), (1, 1000, 1001, 999), (8, 136, 520, 1), (700, 33, 65, 31)]
+          (16, 1024, 2048, 1024), (1, 1000, 1001, 999), (8, 136, 520, 1), (700, 33, 65, 31), (7, 5000, 90, 40),
+          (13, 700, 5001, 66), (4, 64, 8200, 300), (2, 9000, 40, 8), (17, 40, 64, 48)]
 
 
 @pytest.mark.parametrize("kind", sorted(DTYPES))
