@@ -535,10 +535,11 @@ int32_t dropout_apply(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, u
  *   [g | u] for gatedffn_backward, or NULL (narrow blocks of many rows are
  *   fastest then).
  * h is rounded to dtype before the second product; y must not overlap inputs.
- * Few rows (up to 16 of fp32, up to 8 of bf16) may be multiplied in fp32
- * instructions; more are on the matrix cores, fp32 ones as sums of six products of bfloat16 parts, as good as fp32
- * products for magnitudes of 2^-100 to 2^127 (and zeros; an infinite input
- * gives NaN or infinities in its row, smaller numbers lose low bits).
+ * Few rows (up to 16 of fp32, up to 4 of bf16) may be multiplied in fp32
+ * instructions; more are on the matrix cores, fp32 ones as sums of six
+ * products of bfloat16 parts, as good as fp32 products for magnitudes of
+ * 2^-100 to 2^127 (and zeros; an infinite input gives NaN or infinities in
+ * its row, smaller numbers lose low bits).
  * ws: room for h, for shares of sums, and for copies of the operands of an
  * fp32 block or of matrices that do not start on 16 bytes or whose rows are
  * no multiple of eight elements.  The queries say 0 for sizes that are refused.

@@ -286,10 +286,11 @@ Rooms rooms(const Sizes &s, bool backward)
 constexpr uint32_t NO_GAP = 0xFFFFFFFFu;
 
 // Few rows: the weights' bytes (block_forward.h).  Up to how many rows that is faster than products of matrices.  us, products first:
-// 2048-5632-2048 of bf16 one row 23.7 and 23.5, two 23.7 and 28.6; 4096-8192-4096 one 54.4 and 51.9, two 53.3 and 53.7; where the
-// weights have to be copied, 1000-3001-1001, four rows 27.3 and 22.9, eight 27.5 and 27.2; of fp32, whose weights always have to be,
-// sixteen rows 43.3 and 39.8, 338.8 and 144.7 (4096-8192-4096).
-constexpr uint32_t FEW_ROWS = 1, FEW_COPIED = 8, FEW_F32 = 16;
+// 2048-5632-2048 of bf16 one row 23.7 and 23.5, two 23.7 and 28.6; 4096-8192-4096 one 54.4 and 51.9, two 53.3 and 53.7.  Where the
+// weights have to be copied, four rows: 64-257-63 10.8 and 10.1, 1000-3001-1001 27.3 and 22.9, 4096-8191-4095 172 and 142, but
+// 500-1501-333 18.2 and 19.4, 2048-5631-2047 52.6 and 65.2; eight 18.8 and 24.1, 52.5 and 74.8, 27.5 and 27.2.  fp32, whose weights
+// always have to be, sixteen rows: 64-257-63 14.2 and 12.8, 500-1501-333 29.1 and 23.6, 4096-8192-4096 339 and 145.
+constexpr uint32_t FEW_ROWS = 1, FEW_COPIED = 4, FEW_F32 = 16;
 bool few(const Sizes &s, bool straight) { return s.n <= (s.parts == 3 ? FEW_F32 : straight ? FEW_ROWS : FEW_COPIED); }
 
 // of the k's, so that all compute units have a block if every one of them gets two rounds of loads at least
@@ -329,10 +330,11 @@ int32_t launch_vector(const Rows &rows, uint32_t shares, const T *w, uint64_t ld
 {
     if (rows.n == 1) return launch_vector_rows<T, PAIRS, 1>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
     if (rows.n == 2) return launch_vector_rows<T, PAIRS, 2>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
-    if (rows.n <= 4) return launch_vector_rows<T, PAIRS, 4>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
-    if constexpr (sizeof(T) == 4)
+    if constexpr (sizeof(T) == 4) {
         if (rows.n > 8) return launch_vector_rows<T, PAIRS, 16>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
-    return launch_vector_rows<T, PAIRS, 8>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+        if (rows.n > 4) return launch_vector_rows<T, PAIRS, 8>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
+    }
+    return launch_vector_rows<T, PAIRS, 4>(rows, shares, w, ld_w, N, out, ld_out, sums, st);
 }
 
 template <class T>
