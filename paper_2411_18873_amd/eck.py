@@ -576,11 +576,12 @@ def _ws(ws):
 
 
 def _feature_rows(x, n, width, dtype, name):
-    """the row distance of a feature matrix (or its gradient) of n candidates"""
+    """the row distance of a feature matrix (or its gradient) of n candidates, as it is: the library refuses one below n, that of a
+    broadcast or overlapping view"""
     ld = _rows(x, name, dtype)
     if x.shape[0] != width or x.shape[1] < n:
         raise ValueError("%s must be of shape (%d, %d or more)" % (name, width, n))
-    return max(ld, n)
+    return ld
 
 
 def layernorm_forward(x, gamma, beta, y, mean_out=None, rstd_out=None, eps=1e-5, order=ROWS):

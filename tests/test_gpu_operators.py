@@ -129,6 +129,28 @@ def test_layernorm_of_features(n, width, kind):
     layernorm_case(n, width, kind, eck.COLUMNS, 22 + n, 3, 1, 1e-3, n % 2 == 0)
 
 
+@pytest.mark.parametrize("kind", sorted(DTYPES))
+def test_layernorm_refuses_feature_matrices_whose_rows_overlap(kind):
+    """broadcast and overlapping views hold fewer values than their shape says: nothing may be read or written by it"""
+    dtype, code, _ = DTYPES[kind]
+    n, width = 1000, 64
+    flat = torch.full((width * 8 + n,), MARK, dtype=dtype, device="cuda")
+    views = flat[:n].expand(width, n), flat.as_strided((width, n), (8, 1))
+    whole, rows = torch.ones(width, n, dtype=dtype, device="cuda"), torch.full((n, width), MARK, dtype=dtype, device="cuda")
+    mean, rstd = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    ws = torch.empty(eck.layernorm_backward_workspace_bytes(n, width, code), dtype=torch.uint8, device="cuda")
+    sums = torch.full((2, width), MARK, device="cuda")
+    for view in views:
+        for call in (lambda: eck.layernorm_forward(view, None, None, rows, order=eck.COLUMNS),
+                     lambda: eck.layernorm_backward(view, rows, None, mean, rstd, None, sums[0], sums[1], ws, order=eck.COLUMNS),
+                     lambda: eck.layernorm_backward(whole, rows, None, mean, rstd, view, sums[0], sums[1], ws, order=eck.COLUMNS)):
+            with pytest.raises(eck.EckError) as refused:
+                call()
+            assert refused.value.code == eck.ESHAPE
+    for t in (flat, rows, sums):
+        assert (t == MARK).all()
+
+
 @pytest.mark.parametrize("width", [48, 300, 3000, 20000])
 def test_layernorm_in_place(width):
     n = 37

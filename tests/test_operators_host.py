@@ -104,3 +104,25 @@ def test_the_binding_refuses_tensors_that_are_not_what_they_should_be():
     for p in (-1, 1 << 32):
         with pytest.raises(ValueError):  # a probability that does not fit
             eck.dropout_apply(x, x, p, 1)
+
+
+class OnGpu:
+    """what the binding asks of a CUDA tensor, answered by a host one"""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.shape, self.dtype, self.stride = t.shape, t.dtype, t.stride
+
+
+@pytest.mark.parametrize("n", [1, 2, 1000])
+def test_the_binding_passes_the_row_distance_that_a_feature_matrix_has(n):
+    """a distance below n, which the library refuses, must not be replaced by one that the memory behind the view does not have"""
+    whole = torch.zeros(64, n + 3)
+    for view, ld in ((whole, n + 3), (whole[:, :n], n + 3), (whole[:, 3:], n + 3), (torch.zeros(1, n).expand(64, n), 0),
+                     (torch.zeros(64 * 8 + n).as_strided((64, n), (8, 1)), 8)):
+        assert eck._feature_rows(OnGpu(view), n, 64, torch.float32, "x") == ld
+    # a single feature's row has no next one, whatever torch says of its distance
+    assert eck._feature_rows(OnGpu(torch.zeros(n).as_strided((1, n), (0, 1))), n, 1, torch.float32, "x") == n
+    for shape in ((63, n), (64, n - 1)):
+        with pytest.raises(ValueError):
+            eck._feature_rows(OnGpu(torch.zeros(shape)), n, 64, torch.float32, "x")
