@@ -159,9 +159,11 @@ struct NarrowShape {
     // two sets of sums of gates and ups where the registers hold them (2^18 rows, us with and without: 128-512-128 114 and 128,
     // 64-256-64 40.7 and 40.4, 16384 rows of it 8.5 and 9.0; 64-1024-256 228 and 215)
     static constexpr bool AHEAD = ON <= 8;
+    static constexpr uint32_t UNITS = AHEAD ? 64 : 32; // hidden units of a turn
 };
 
-template <int DK, int ON, int ACT>
+// PADDED: n_hidden is no multiple of UNITS (a kernel of its own: the branch on it costs 64-256-64 of 16384 rows 8 %)
+template <int DK, int ON, int ACT, bool PADDED>
 __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
 {
     using S = NarrowShape<DK, ON>;
@@ -247,11 +249,18 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
         }
     };
 
-    const auto activate = [&](const f32x4(&pre)[4][2], bf16x8(&h)[2]) {
+    const auto activate = [&](uint32_t first, const f32x4(&pre)[4][2], bf16x8(&h)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[i][e] = (bf16)(gate_as<ACT>(pre[e / 4][i][e % 4]).value * pre[2 + e / 4][i][e % 4]);
+        if (!PADDED || first + 32 <= p.n_hidden) return;
+        // (units past the last, of zero weights, are NaN in rows with an infinity, and would be in y)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (first + 4 * g + e % 4 + (e < 4 ? 0 : 16) >= p.n_hidden) h[i][e] = (bf16)0.0f;
     };
 
     load(0, 0);
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
         // The next units' gates and ups are multiplied while the activations of these are worked out, then these units' share of
         // y.  At the meeting the next units have come, and everybody is through with the ones before these.
         multiply_up(0, pre[0]);
-        for (uint32_t first = 0; first < p.n_hidden; first += 64) {
+        for (uint32_t first = 0; first < p.n_hidden; first += S::UNITS) {
 #pragma unroll
             for (int odd = 0; odd < 2; ++odd) { // (units past the last: zeros)
                 const uint32_t next = slot == 2 ? 0 : slot + 1;
@@ -271,18 +280,18 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
                 load(first + 32 * odd + 64, next == 2 ? 0 : next + 1);
                 multiply_up(next, pre[odd ^ 1]);
                 bf16x8 h[2];
-                activate(pre[odd], h);
+                activate(first + 32 * odd, pre[odd], h);
                 multiply_down(slot, h);
                 slot = next;
             }
         }
     } else {
-        for (uint32_t first = 0; first < p.n_hidden; first += 32) {
+        for (uint32_t first = 0; first < p.n_hidden; first += S::UNITS) {
             if (first) wait_and_meet<S::LOADS>(); // these units have come, and everybody is through with the ones before
             load(first + 64, slot >= 1 ? slot - 1 : 2);
             multiply_up(slot, pre[0]);
             bf16x8 h[2];
-            activate(pre[0], h);
+            activate(first, pre[0], h);
             multiply_down(slot, h);
             slot = slot == 2 ? 0 : slot + 1;
         }

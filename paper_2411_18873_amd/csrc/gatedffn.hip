@@ -366,7 +366,7 @@ template <int ACT, int DK, int ON>
 int32_t launch_narrow_shape(const Narrow &p, hipStream_t st)
 {
     using S = NarrowShape<DK, ON>;
-    auto kernel = narrow_kernel<DK, ON, ACT>;
+    auto kernel = p.n_hidden % S::UNITS ? narrow_kernel<DK, ON, ACT, true> : narrow_kernel<DK, ON, ACT, false>;
     ECK_TRY(allow_lds(kernel, S::LDS));
     hipLaunchKernelGGL(kernel, dim3((p.n - 1) / S::ROWS + 1), dim3(64 * S::WAVES), S::LDS, st, p);
     ECK_HIP_TRY(hipGetLastError());

@@ -151,6 +151,16 @@ __device__ __forceinline__ void finish_store(const Target &to, uint64_t m, uint3
     else store_eight((float *)to.out + m * to.ld_out + base, c - shift, to.piece, v);
 }
 
+// Zeros for the columns that operands are padded with.  The products leave NaN there in rows with an infinity (times the other
+// operand's padding), and it would go from there into the row's results.
+__device__ __forceinline__ void clear_padding(uint32_t c, uint32_t width, float (&v)[8])
+{
+    if (c + 8 <= width) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i >= width) v[i] = 0.0f;
+}
+
 template <int PARTS>
 __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32_t c, const float (&g)[8], const float (&u)[8])
 {
@@ -159,6 +169,7 @@ __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] = gate_as<decltype(act)::value>(g[i]).value * u[i];
     });
+    clear_padding(c, to.n_hidden, h);
     store_operand<PARTS>((bf16 *)to.out + m * to.ld_out, c, h);
     if (to.pre) {
         float *row = to.pre + m * 2 * to.n_hidden;
@@ -167,7 +178,7 @@ __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32
     }
 }
 
-// what eight columns of dh are multiplied with (zeros past the end: the padding of h, dg and du is zero)
+// what eight columns of dh are multiplied with (zeros past the end)
 struct Pre {
     float g[8], u[8];
 };
@@ -191,6 +202,8 @@ __device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint3
             du[i] = dh[i] * gate.value;
         }
     });
+    clear_padding(c, to.n_hidden, dg);
+    clear_padding(c, to.n_hidden, du);
     if (to.out) store_operand<PARTS>((bf16 *)to.out + m * to.ld_out, c, h);
     bf16 *d = to.d_pre + m * to.ld_d;
     store_operand<PARTS>(d, c, dg);

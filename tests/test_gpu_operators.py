@@ -447,6 +447,34 @@ def test_gatedffn_rows_that_are_not_finite_stay_by_themselves():
             assert not torch.isfinite(dirty[[1, n - 1]].float()).all(1).any()
 
 
+def test_gatedffn_infinite_rows_stay_infinite_whatever_the_sizes_are_padded_to():
+    """Positive numbers and one infinity: by the formulas every result that it enters is infinite, and not NaN, as the products of an
+    infinity with the zeros that operands are padded with would be.  (fp32 blocks of more than 16 rows may say NaN instead.)"""
+    for n, n_in, n_hidden, n_out in ((40, 24, 1, 3), (40, 8, 63, 64), (300, 100, 129, 40), (208, 2961, 108, 1), (12300, 64, 33, 64), (12300, 40, 97, 200),
+                                     (3, 24, 9, 5)):
+        for act in (eck.ACT_SILU, eck.ACT_GELU, eck.ACT_RELU):
+            g = torch.Generator().manual_seed(n + n_hidden)
+            positive = lambda *s: (0.25 + torch.rand(*s, generator=g)).bfloat16().cuda()  # noqa: E731
+            x, wgu, wd, dy = positive(n, n_in), positive(n_in, 2 * n_hidden) / n_in, positive(n_hidden, n_out) / n_hidden, positive(n, n_out)
+            sizes = (n, n_in, n_hidden, n_out, eck.BF16)
+            ws = torch.empty(max(eck.gatedffn_forward_workspace_bytes(*sizes), eck.gatedffn_backward_workspace_bytes(*sizes)), dtype=torch.uint8,
+                             device="cuda")
+            pre = torch.empty(n, 2 * n_hidden, device="cuda")
+            served, y = torch.empty_like(dy), torch.empty_like(dy)
+            dx, dwgu, dwd = torch.empty_like(x), torch.empty_like(wgu), torch.empty_like(wd)
+            x[2, 5] = math.inf
+            eck.gatedffn_forward(x, wgu, wd, served, ws, act=act)
+            eck.gatedffn_forward(x, wgu, wd, y, ws, pre_out=pre, act=act)
+            for t in (served, y, pre):
+                assert torch.isposinf(t[2]).all() and torch.isfinite(t[:2]).all() and torch.isfinite(t[3:]).all()
+            x[2, 5] = 1.0
+            eck.gatedffn_forward(x, wgu, wd, y, ws, pre_out=pre, act=act)
+            dy[2] = math.inf
+            eck.gatedffn_backward(x, wgu, wd, pre, dy, dx, dwgu, dwd, ws, act=act)
+            assert torch.isposinf(dx[2]).all() and torch.isfinite(dx[:2]).all() and torch.isfinite(dx[3:]).all()
+            assert torch.isposinf(dwgu).all() and torch.isposinf(dwd).all()
+
+
 def test_gatedffn_gradients_against_differences():
     n, n_in, n_hidden, n_out, step = 4, 24, 40, 16, 2.0 ** -7
     for act in (eck.ACT_SILU, eck.ACT_GELU):
