@@ -466,7 +466,7 @@ int32_t treemodel_update(eck_trees *trees, const void *feat, int32_t feat_dtype,
  * blocks  x <- x + dropout(feedforward(layernorm(x)))  on rows of activations.
  * A matrix of activations is row-major: row i of an [n][ld] array, ld >= width
  * elements apart, is candidate i.  Elements are ECK_F32 or ECK_BF16; sums,
- * statistics and products accumulate in fp32, results are rounded once.
+ * statistics and products accumulate in fp32 or more, results are rounded once.
  * Pointers are aligned to their elements, nothing more is asked for (rows that
  * start on 16 bytes are fastest); workspaces start on 256 bytes.  Nothing
  * depends on the order of execution: equal calls give equal bits. */

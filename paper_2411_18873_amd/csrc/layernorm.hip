@@ -7,7 +7,8 @@
 // after the other: the squares of differences from the mean lose nothing to a large mean), shared by as many threads as sixteen
 // bytes each need: 8 to 64 lanes of a wavefront, or a block.  Threads keep their columns from row to row, so gamma and beta are
 // loaded once, and the parameters' gradients grow in registers: blocks leave one partial sum per column and a second launch adds
-// these in a fixed order.  Rows longer than a block's registers are read again for every pass.
+// these in a fixed order.  Rows longer than a block's registers are read again for every pass; their threads add up thousands of
+// values, and do it in 64 bits, sixteen bytes' sum at a time (in 32, 4096 equal values in a row are off by 650 roundings).
 #include "activations.h"
 #include "lanes.h"
 
@@ -131,19 +132,24 @@ __global__ __launch_bounds__(BLOCK) void forward_long_kernel(const T *x, uint64_
     const float share = 1.0f / (float)width;
     for (uint64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const T *row = x + r * ld_x;
-        float sum = 0.0f, squares = 0.0f, v[N];
+        double sum = 0.0, squares = 0.0;
+        float v[N];
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
+            float some = 0.0f;
             load_chunk(row, at, width, v);
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum += v[i];
+            for (int i = 0; i < N; ++i) some += v[i];
+            sum += (double)some;
         }
-        const float mean = block_sum(sum, scratch, 0) * share;
+        const float mean = block_sum((float)sum, scratch, 0) * share;
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
+            float some = 0.0f;
             load_chunk(row, at, width, v, mean);
 #pragma unroll
-            for (int i = 0; i < N; ++i) squares += (v[i] - mean) * (v[i] - mean);
+            for (int i = 0; i < N; ++i) some += (v[i] - mean) * (v[i] - mean);
+            squares += (double)some;
         }
-        const float rstd = 1.0f / sqrtf(block_sum(squares, scratch, 1) * share + eps);
+        const float rstd = 1.0f / sqrtf(block_sum((float)squares, scratch, 1) * share + eps);
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
             float ga[N], be[N];
             load_chunk(row, at, width, v);
@@ -264,19 +270,22 @@ __global__ __launch_bounds__(BLOCK) void backward_long_kernel(const T *x, uint64
     const float share = 1.0f / (float)width;
     for (uint64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const float m = mean[r], s = rstd[r];
-        float sum = 0.0f, dot = 0.0f, xh[N], d[N], ga[N];
+        double sums = 0.0, dots = 0.0;
+        float xh[N], d[N], ga[N];
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
+            float of_g = 0.0f, of_dot = 0.0f;
             load_chunk(x + r * ld_x, at, width, xh, m);
             load_chunk(dy + r * ld_dy, at, width, d);
             load_vector(gamma, at, width, 1.0f, ga);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                sum += d[i] * ga[i];
-                dot += d[i] * ga[i] * ((xh[i] - m) * s);
+                of_g += d[i] * ga[i];
+                of_dot += d[i] * ga[i] * ((xh[i] - m) * s);
             }
+            sums += (double)of_g;
+            dots += (double)of_dot;
         }
-        sum = block_sum(sum, scratch, 0) * share;
-        dot = block_sum(dot, scratch, 1) * share;
+        const float sum = block_sum((float)sums, scratch, 0) * share, dot = block_sum((float)dots, scratch, 1) * share;
         for (uint32_t at = threadIdx.x * N; at < width; at += BLOCK * N) {
             load_chunk(x + r * ld_x, at, width, xh);
             load_chunk(dy + r * ld_dy, at, width, d);
@@ -295,14 +304,14 @@ __global__ __launch_bounds__(BLOCK) void columns_long_kernel(const T *x, uint64_
 {
     const uint32_t c = blockIdx.x * BLOCK + threadIdx.x;
     if (c >= width) return;
-    float dgamma = 0.0f, dbeta = 0.0f;
+    double dgamma = 0.0, dbeta = 0.0;
     for (uint64_t r = blockIdx.y; r < n; r += gridDim.y) {
         const float d = (float)dy[r * ld_dy + c];
-        dgamma += d * (((float)x[r * ld_x + c] - mean[r]) * rstd[r]);
-        dbeta += d;
+        dgamma += (double)(d * (((float)x[r * ld_x + c] - mean[r]) * rstd[r]));
+        dbeta += (double)d;
     }
-    partial[(uint64_t)blockIdx.y * 2 * width + c] = dgamma;
-    partial[(uint64_t)blockIdx.y * 2 * width + width + c] = dbeta;
+    partial[(uint64_t)blockIdx.y * 2 * width + c] = (float)dgamma;
+    partial[(uint64_t)blockIdx.y * 2 * width + width + c] = (float)dbeta;
 }
 
 // dgamma and dbeta: the blocks' partial sums; sixteen columns a block, 64 threads each

@@ -130,6 +130,46 @@ def test_layernorm_of_features(n, width, kind):
 
 
 @pytest.mark.parametrize("kind", sorted(DTYPES))
+@pytest.mark.parametrize("n,width", [(3, 1 << 20), (2, (1 << 20) + 13), (40000, 8200)])
+def test_layernorm_sums_of_long_rows_and_many_rows_do_not_drift(n, width, kind):
+    """Values of one size and sign, whose roundings all go the same way where thousands are added one after the other: sums are within 64
+    additions' roundings all the same.  (A row of 0.1 that 256 threads add up is off by 650 of them at 2^20.)"""
+    dtype, code, u = DTYPES[kind]
+    x = torch.full((n, width), 0.1, dtype=dtype, device="cuda")
+    x[:, ::2] += 0.05
+    x[n - 1] = x[n - 1] + 100.0
+    dy = torch.full((n, width), 0.1, dtype=dtype, device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    dgamma, dbeta = torch.empty(width, device="cuda"), torch.empty(width, device="cuda")
+    ws = torch.empty(eck.layernorm_backward_workspace_bytes(n, width, code), dtype=torch.uint8, device="cuda")
+    eck.layernorm_forward(x, None, None, y, mean, rstd)
+    some = list(range(min(n, 3))) + [n - 1]
+    X = x[some].double()
+    m = X.mean(1)
+    var = ((X - m[:, None]) ** 2).mean(1) + 1e-5
+    assert ((mean[some].double() - m).abs() <= 64 * E * X.abs().mean(1)).all()
+    # (the variance: its sum, and the squares of differences from a mean that is off by the line above)
+    assert ((rstd[some].double() * var.sqrt() - 1).abs() <= 64 * E + 2 * (64 * E * X.abs().mean(1)) / var.sqrt()).all()
+    gamma = torch.where(torch.arange(width, device="cuda") % 2 == 0, 1.0, 0.5)
+    eck.layernorm_backward(x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    one = dy[0, 0].double()
+    assert ((dbeta.double() - n * one).abs() <= 64 * E * n * one).all()
+    total, size = torch.zeros(64, dtype=torch.float64, device="cuda"), torch.zeros(64, dtype=torch.float64, device="cuda")
+    for at in range(0, n, 1000):
+        xh = (x[at:at + 1000, :64].double() - mean[at:at + 1000, None].double()) * rstd[at:at + 1000, None].double()
+        total += (xh * one).sum(0)
+        size += (xh * one).abs().sum(0)
+    assert ((dgamma[:64].double() - total).abs() <= (64 + 4) * E * size).all()
+    g = gamma.double() * one
+    xh = (X - mean[some, None].double()) * rstd[some, None].double()
+    s1, s2 = g.mean(), (g * xh).mean(1, keepdim=True)
+    want = rstd[some, None].double() * (g - s1 - xh * s2)
+    room = 64 * E * (g.abs() + s1 + xh.abs() * (g * xh).abs().mean(1, keepdim=True)) * rstd[some, None].double() + u * want.abs()
+    assert ((dx[some].double() - want).abs() <= room).all()
+
+
+@pytest.mark.parametrize("kind", sorted(DTYPES))
 def test_layernorm_refuses_feature_matrices_whose_rows_overlap(kind):
     """broadcast and overlapping views hold fewer values than their shape says: nothing may be read or written by it"""
     dtype, code, _ = DTYPES[kind]
