@@ -65,7 +65,7 @@ __global__ __launch_bounds__(1024) void vector_kernel(const Rows rows, const T *
                     rows.pre[(uint64_t)r * 2 * K + k0 + k] = g;
                     rows.pre[(uint64_t)r * 2 * K + K + k0 + k] = u;
                 }
-                with_act(rows.act, [&](auto act) { x = (float)(T)(gate_as<decltype(act)::value>(g).value * u); });
+                with_act(rows.act, [&](auto act) { x = (float)(T)(gate_as<decltype(act)::value, sizeof(T) == 4>(g).value * u); });
             }
             shared[k * ROWS + r] = x;
         }
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = (bf16)(gate_as<ACT>(pre[e / 4][i][e % 4]).value * pre[2 + e / 4][i][e % 4]);
+            for (int e = 0; e < 8; ++e) h[i][e] = (bf16)(gate_as<ACT, false>(pre[e / 4][i][e % 4]).value * pre[2 + e / 4][i][e % 4]);
         if (!PADDED || first + 32 <= p.n_hidden) return;
         // (units past the last, of zero weights, are NaN in rows with an infinity, and would be in y)
 #pragma unroll

@@ -24,14 +24,16 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 struct Gate {
     float value, slope;
 };
-template <int ACT>
+// WHOLE: of fp32 blocks, to the last bits of fp32
+template <int ACT, bool WHOLE>
 __device__ __forceinline__ Gate gate_as(float g)
 {
     if (ACT == ECK_ACT_RELU) return {g > 0.0f ? g : g == g ? 0.0f : g, g > 0.0f ? 1.0f : 0.0f};
     if (ACT == ECK_ACT_SILU) {
-        // (exponential and reciprocal as the instructions give them, within 2^-23 of the value each: full ones are 25 more
-        // instructions an element)
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+        // (bf16: exponential and reciprocal as the instructions give them, within a unit of the last place each; rounding the
+        // exponential's argument adds about |g| 2^-24 of the value, ten units at g = -20, all far below a bf16's.  Full ones are 25 more
+        // instructions an element, which narrow blocks would wait for.)
+        const float s = WHOLE ? 1.0f / (1.0f + expf(-g)) : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
         return {g * s, s * (1.0f + g * (1.0f - s))};
     }
     const float s = 0.5f * (1.0f + erff(g * 0.70710678f));
@@ -167,7 +169,7 @@ __device__ __forceinline__ void finish_gate(const Target &to, uint64_t m, uint32
     float h[8];
     with_act(to.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = gate_as<decltype(act)::value>(g[i]).value * u[i];
+        for (int i = 0; i < 8; ++i) h[i] = gate_as<decltype(act)::value, PARTS == 3>(g[i]).value * u[i];
     });
     clear_padding(c, to.n_hidden, h);
     store_operand<PARTS>((bf16 *)to.out + m * to.ld_out, c, h);
@@ -196,7 +198,7 @@ __device__ __forceinline__ void finish_slope(const Target &to, uint64_t m, uint3
     with_act(to.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const Gate gate = gate_as<decltype(act)::value>(pre.g[i]);
+            const Gate gate = gate_as<decltype(act)::value, PARTS == 3>(pre.g[i]);
             h[i] = gate.value * pre.u[i];
             dg[i] = dh[i] * pre.u[i] * gate.slope;
             du[i] = dh[i] * gate.value;

@@ -472,6 +472,38 @@ def test_gatedffn_of_whole_numbers_is_exact(n, n_in, n_hidden, n_out, kind):
         assert torch.equal(got.cpu(), want.to(got.dtype)), what
 
 
+def single_gates(act, kind, rows, values):
+    """a(g), and from dy = 1 a'(g) and a(g) again, of one gate a row (u = 1, W_down = 1): each path's own activation, seen by itself"""
+    dtype, code, _ = DTYPES[kind]
+    g = values.to(dtype).repeat(rows // values.numel() + 1)[:rows]
+    n = g.numel()
+    x = torch.stack((g, torch.ones_like(g)), 1).cuda()
+    wgu, wd = torch.eye(2, dtype=dtype, device="cuda"), torch.ones(1, 1, dtype=dtype, device="cuda")
+    y, dy = torch.empty(n, 1, dtype=dtype, device="cuda"), torch.ones(n, 1, dtype=dtype, device="cuda")
+    pre, served, dx = torch.empty(n, 2, device="cuda"), torch.empty_like(y), torch.empty_like(x)
+    ws = torch.empty(max(eck.gatedffn_forward_workspace_bytes(n, 2, 1, 1, code), eck.gatedffn_backward_workspace_bytes(n, 2, 1, 1, code)),
+                     dtype=torch.uint8, device="cuda")
+    eck.gatedffn_forward(x, wgu, wd, served, ws, act=act)
+    eck.gatedffn_forward(x, wgu, wd, y, ws, pre_out=pre, act=act)
+    eck.gatedffn_backward(x, wgu, wd, pre, dy, dx, None, None, ws, act=act)
+    return g.double(), [t.double().cpu().view(-1) for t in (served, y, dx[:, 1], dx[:, 0])]
+
+
+@pytest.mark.parametrize("kind", sorted(DTYPES))
+@pytest.mark.parametrize("rows", [4, 16, 200, 12400])
+def test_gatedffn_silu_by_itself(rows, kind):
+    u = DTYPES[kind][2]
+    for shift in range(0, 400, rows) if rows < 400 else (0,):
+        g, (served, y, du, dg) = single_gates(eck.ACT_SILU, kind, rows, torch.linspace(-60.0, 40.0, 401, dtype=torch.float64).roll(-shift))
+        s = 1 / (1 + torch.exp(-g))
+        # Exponential, sum, quotient and product, each within a unit or two: 8 e of the value, and as much of its three parts in fp32
+        # products.  In bf16 the exponential's argument is rounded once more (|g| e), which a rounding to bf16 hides.
+        off = (16 if kind == "f32" else 16 + 4 * g.abs()) * E
+        for value in (served, y, du):
+            assert ((value - g * s).abs() <= (off + u) * (g * s).abs()).all()
+        assert ((dg - s * (1 + g * (1 - s))).abs() <= (off + u) * s * (1 + g.abs())).all()
+
+
 def test_gatedffn_rows_that_are_not_finite_stay_by_themselves():
     for n, n_in, n_hidden, n_out in ((40, 64, 128, 64), (300, 256, 384, 128), (3, 40, 56, 24)):
         for kind in sorted(DTYPES):
