@@ -504,6 +504,21 @@ def test_gatedffn_silu_by_itself(rows, kind):
         assert ((dg - s * (1 + g * (1 - s))).abs() <= (off + u) * s * (1 + g.abs())).all()
 
 
+@pytest.mark.parametrize("kind", sorted(DTYPES))
+@pytest.mark.parametrize("rows", [4, 16, 200, 12400])
+def test_gatedffn_gelu_by_itself(rows, kind):
+    u = DTYPES[kind][2]
+    for shift in range(0, 400, rows) if rows < 400 else (0,):
+        g, (served, y, du, dg) = single_gates(eck.ACT_GELU, kind, rows, torch.linspace(-10.0, 10.0, 401, dtype=torch.float64).roll(-shift))
+        s, bell = 0.5 * torch.erfc(-g / math.sqrt(2)), torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        # Far out on the left, where 1 + erf cancels, the share that is left is of the order of exp(-g^2 / 2): a unit and a half of its
+        # argument are 1.5 g^2 e of the value.  The functions, products and the three parts of fp32 products are some more units.
+        off = (24 + 4 * g * g) * E
+        for value in (served, y, du):
+            assert ((value - g * s).abs() <= (off + u) * (g * s).abs()).all()
+        assert ((dg - (s + g * bell)).abs() <= (off + u) * (s + g.abs() * bell)).all()
+
+
 def test_gatedffn_rows_that_are_not_finite_stay_by_themselves():
     for n, n_in, n_hidden, n_out in ((40, 64, 128, 64), (300, 256, 384, 128), (3, 40, 56, 24)):
         for kind in sorted(DTYPES):
