@@ -475,17 +475,17 @@ int32_t backward(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_up, 
     return launch_joins<STORE, P>(joins, st);
 }
 
-bool sizes_ok(const Sizes &s)
+bool sizes_ok(const Sizes &s, bool backward)
 {
-    const uint64_t hidden = s.hidden();
-    return s.n <= MAX_ROWS && s.n_in <= MAX_BLOCK_WIDTH && s.n_hidden <= MAX_BLOCK_WIDTH && s.n_out <= MAX_BLOCK_WIDTH &&
-           tiles_of(s.n, 2 * hidden) <= MAX_TILES && tiles_of(s.n, s.n_out) <= MAX_TILES && tiles_of(s.n, s.n_in) <= MAX_TILES &&
-           tiles_of(s.n_in, 2 * hidden) <= MAX_TILES && tiles_of(s.n_hidden, s.n_out) <= MAX_TILES;
+    const uint64_t pairs = 2ull * s.hidden();
+    if (s.n > MAX_ROWS || s.n_in > MAX_BLOCK_WIDTH || s.n_hidden > MAX_BLOCK_WIDTH || s.n_out > MAX_BLOCK_WIDTH) return false;
+    if (tiles_of(s.n, pairs) > MAX_TILES || tiles_of(s.n, s.n_out) > MAX_TILES) return false;
+    return !backward || (tiles_of(s.n, s.n_in) <= MAX_TILES && tiles_of(s.n_in, pairs) <= MAX_TILES && tiles_of(s.n_hidden, s.n_out) <= MAX_TILES);
 }
 bool act_ok(int32_t act) { return act == ECK_ACT_SILU || act == ECK_ACT_GELU || act == ECK_ACT_RELU; }
 uint64_t workspace_bytes(const Sizes &s, int32_t dtype, bool backward)
 {
-    if (s.n == 0 || s.n_in == 0 || s.n_hidden == 0 || s.n_out == 0 || !is_dtype(dtype) || !sizes_ok(s)) return 0;
+    if (s.n == 0 || s.n_in == 0 || s.n_hidden == 0 || s.n_out == 0 || !is_dtype(dtype) || !sizes_ok(s, backward)) return 0;
     if (!backward && few(s, false)) {
         const VectorRooms room = vector_rooms(s);
         return few(s, true) ? room.sums + room.sums_y : most(room.sums + room.sums_y, rooms(s, false).total());
@@ -510,7 +510,7 @@ extern "C" int32_t gatedffn_forward(const void *x, int32_t dtype, uint64_t ld_x,
     const Sizes s = {n, n_in, n_hidden, n_out, parts_for(dtype)};
     if (!x || !w_gate_up || !w_down || !y || n == 0 || n_in == 0 || n_hidden == 0 || n_out == 0 || !is_dtype(dtype) || !act_ok(act)) return ECK_EINVAL;
     if (ld_x < n_in || ld_y < n_out) return ECK_ESHAPE;
-    if (!sizes_ok(s)) return ECK_EUNSUPPORTED;
+    if (!sizes_ok(s, false)) return ECK_EUNSUPPORTED;
     if (!ws || ws_bytes < workspace_bytes(s, dtype, false)) return ECK_EWORKSPACE;
     const uint64_t size = element_bytes(dtype);
     if (!aligned(x, size) || !aligned(w_gate_up, size) || !aligned(w_down, size) || !aligned(y, size) || !aligned(pre_out, 4) || !aligned(ws, 256))
@@ -534,7 +534,7 @@ extern "C" int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x
     if (!x || !w_gate_up || !w_down || !pre || !dy || n == 0 || n_in == 0 || n_hidden == 0 || n_out == 0 || !is_dtype(dtype)) return ECK_EINVAL;
     if ((!dx_out && !dw_gate_up_out && !dw_down_out) || !act_ok(act)) return ECK_EINVAL;
     if (ld_x < n_in || ld_dy < n_out || (dx_out && ld_dx < n_in)) return ECK_ESHAPE;
-    if (!sizes_ok(s)) return ECK_EUNSUPPORTED;
+    if (!sizes_ok(s, true)) return ECK_EUNSUPPORTED;
     if (!ws || ws_bytes < workspace_bytes(s, dtype, true)) return ECK_EWORKSPACE;
     const uint64_t size = element_bytes(dtype);
     if (!aligned(x, size) || !aligned(w_gate_up, size) || !aligned(w_down, size) || !aligned(pre, 4) || !aligned(dy, size) ||

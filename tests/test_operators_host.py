@@ -126,3 +126,14 @@ def test_the_binding_passes_the_row_distance_that_a_feature_matrix_has(n):
     for shape in ((63, n), (64, n - 1)):
         with pytest.raises(ValueError):
             eck._feature_rows(OnGpu(torch.zeros(shape)), n, 64, torch.float32, "x")
+
+
+def test_gatedffn_passes_are_refused_for_their_own_products_only():
+    """2^22 tiles of 64 x 64 a product: dx and the weights' gradients are products of the backward pass, which a forward pass has not"""
+    L = eck.lib()
+    WF, WB = L.gatedffn_forward_workspace_bytes, L.gatedffn_backward_workspace_bytes
+    for sizes in ((1 << 24, 2048, 64, 64, 1), (1 << 20, 1 << 18, 64, 64, 1), (16, 1 << 18, 1 << 16, 64, 1), (16, 64, 1 << 18, 1 << 16, 0)):
+        assert WF(*sizes) > 0 and WB(*sizes) == 0, sizes
+    for sizes in ((1 << 24, 64, 1024, 64, 1), (1 << 24, 64, 64, 2048, 1)):      # [g | u], y
+        assert WF(*sizes) == WB(*sizes) == 0, sizes
+    assert WF(1 << 24, 64, 64, 64, 1) > 0 and WB(1 << 24, 64, 64, 64, 1) > 0
