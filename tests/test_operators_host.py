@@ -132,7 +132,7 @@ def test_gatedffn_passes_are_refused_for_their_own_products_only():
     """2^22 tiles of 64 x 64 a product: dx and the weights' gradients are products of the backward pass, which a forward pass has not"""
     L = eck.lib()
     WF, WB = L.gatedffn_forward_workspace_bytes, L.gatedffn_backward_workspace_bytes
-    for sizes in ((1 << 24, 2048, 64, 64, 1), (1 << 20, 1 << 18, 64, 64, 1), (16, 1 << 18, 1 << 16, 64, 1), (16, 64, 1 << 18, 1 << 16, 0)):
+    for sizes in ((1 << 24, 2048, 64, 64, 1), (1 << 20, 1 << 18, 64, 64, 1), (16, 1 << 18, 1 << 16, 64, 1), (16, 64, 1 << 18, 1 << 17, 0)):
         assert WF(*sizes) > 0 and WB(*sizes) == 0, sizes
     for sizes in ((1 << 24, 64, 1024, 64, 1), (1 << 24, 64, 64, 2048, 1)):      # [g | u], y
         assert WF(*sizes) == WB(*sizes) == 0, sizes
