@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2411_18873_amd import eck, gated
+from test_gpu_operators import draws
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +84,52 @@ def test_selection_by_a_gated_model():
     eck.topk_select(score, None, None, 1, k, idx, best, count, ws)
     order = np.argsort(score.cpu().numpy(), kind="stable")[:k]
     assert idx[0].cpu().numpy().tolist() == order.tolist()
+
+
+def normed(x, params, name):
+    m = x.mean(1, keepdim=True)
+    return (x - m) / torch.sqrt(((x - m) ** 2).mean(1, keepdim=True) + gated.EPS) * params[name + ".gamma"] + params[name + ".beta"]
+
+
+def fed(x, params, name):
+    g, u = (x @ params[name + ".gate_up"]).chunk(2, 1)
+    return (g * torch.sigmoid(g) * u) @ params[name + ".down"]
+
+
+def plain_with_dropout(model, feat, params, round):
+    """the network in 64 bits as a refit's step number `round` runs it: masks from the generator's definition"""
+    n, p = feat.shape[1], model.p_drop_q32
+
+    def branch(y, b):
+        kept = torch.from_numpy(draws(n, model.n_feat, model.seed + b, round, 0) >= p).cuda()
+        return torch.where(kept, y * (2.0 ** 32 / (2.0 ** 32 - p)), 0.0)
+
+    x = normed(feat.double().t(), params, "in")
+    for b in range(model.blocks):
+        x = x + branch(fed(normed(x, params, str(b)), params, str(b)), b)
+    return fed(normed(x, params, "head"), params, "head").view(-1)
+
+
+@pytest.mark.parametrize("step", [0, 3])
+def test_gradients_with_dropout(step):
+    """forward and backward pass drop the same elements, those of this step"""
+    n = 384
+    model = gated.GatedModel(hidden=128, blocks=2, head=64, p_drop=0.25, seed=14)
+    model.steps = step
+    feat = features(64, n, 15, torch.float32)
+    params = {k: p.double().requires_grad_(True) for k, p in model.params.items()}
+    d = torch.randn(n, generator=torch.Generator().manual_seed(16)).cuda() / n
+    want = plain_with_dropout(model, feat, params, step)
+    (want * d.double()).sum().backward()
+    score, kept = model._forward(feat, n, True)
+    grads = model._backward(feat, n, kept, d)
+    # as in test_scores and test_gradients_and_refit, the branches and their errors being up to 4 / 3 larger
+    assert (score.double() - want.detach()).square().mean().sqrt().item() <= 2 * 8e-3
+    for k, p in params.items():
+        assert ((grads[k].double() - p.grad).norm() / p.grad.norm()).item() <= 0.054, k
+    # masks of another step, or of the other block, would be seen
+    for round, swap in ((step + 1, False), (step, True)):
+        other = gated.GatedModel(hidden=128, blocks=2, head=64, p_drop=0.25, seed=14 + swap)
+        params = {k: p.detach().requires_grad_(True) for k, p in params.items()}
+        (plain_with_dropout(other, feat, params, round) * d.double()).sum().backward()
+        assert any(((grads[k].double() - p.grad).norm() / p.grad.norm()).item() > 0.2 for k, p in params.items())
