@@ -47,13 +47,15 @@ class GatedModel:
         return self._work["ws"]
 
     def _forward(self, feat, n, train):
-        """scores float [n]; train: with dropout, and what the backward pass needs of every layer"""
-        f, kept, p = self.n_feat, {}, self.params
+        """scores float [n]; train: with dropout, and what the backward pass needs of every layer, of which a scoring pass keeps none"""
+        f, p = self.n_feat, self.params
+        kept = {} if train else None
         rows = lambda width=f, dtype=torch.bfloat16: torch.empty(n, width, dtype=dtype, device="cuda")  # noqa: E731
         stats = lambda: [torch.empty(n, device="cuda") for _ in range(2)] if train else [None, None]  # noqa: E731
         x, s = rows(dtype=feat.dtype), stats()
         eck.layernorm_forward(feat, p["in.gamma"], p["in.beta"], x, *s, eps=EPS, order=eck.COLUMNS)
-        kept["in"] = s
+        if train:
+            kept["in"] = s
         x = x.bfloat16()
         ws = self._ws(max(eck.gatedffn_forward_workspace_bytes(n, f, self.hidden, f, eck.BF16),
                           eck.gatedffn_forward_workspace_bytes(n, f, self.head, 1, eck.F32)))
@@ -62,7 +64,8 @@ class GatedModel:
             pre = rows(2 * self.hidden, torch.float32) if train else None
             eck.layernorm_forward(x, p["%d.gamma" % b], p["%d.beta" % b], xn, *s, eps=EPS)
             eck.gatedffn_forward(xn, self.bf16["%d.gate_up" % b], self.bf16["%d.down" % b], out, ws, pre_out=pre)
-            kept[b] = x, xn, pre, s
+            if train:
+                kept[b] = x, xn, pre, s
             nxt = rows()
             eck.dropout_apply(out, nxt, self.p_drop_q32 if train else 0, self.seed + b, round=self.steps, residual=x)
             x = nxt
@@ -71,7 +74,8 @@ class GatedModel:
         score = rows(1, torch.float32)
         eck.layernorm_forward(x, p["head.gamma"], p["head.beta"], xn, *s, eps=EPS)
         eck.gatedffn_forward(xn, p["head.gate_up"], p["head.down"], score, ws, pre_out=pre)
-        kept["head"] = x, xn, pre, s
+        if train:
+            kept["head"] = x, xn, pre, s
         return score.view(n), kept
 
     def score(self, feat, n, score_out):

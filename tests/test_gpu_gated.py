@@ -133,3 +133,20 @@ def test_gradients_with_dropout(step):
         params = {k: p.detach().requires_grad_(True) for k, p in params.items()}
         (plain_with_dropout(other, feat, params, round) * d.double()).sum().backward()
         assert any(((grads[k].double() - p.grad).norm() / p.grad.norm()).item() > 0.2 for k, p in params.items())
+
+
+def test_scoring_keeps_no_layers():
+    """memory of a scoring pass does not grow with the number of blocks: nothing of a layer is kept that no backward pass will read"""
+    n, peaks = 1 << 16, []
+    feat = features(64, n, 17, torch.bfloat16)
+    score = torch.empty(n, device="cuda")
+    for blocks in (2, 8):
+        model = gated.GatedModel(hidden=64, blocks=blocks, head=64, seed=18)
+        model.score(feat, n, score)      # (the workspace)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        model.score(feat, n, score)
+        torch.cuda.synchronize()
+        peaks.append(torch.cuda.max_memory_allocated() - before)
+    assert peaks[1] <= peaks[0] + (1 << 20), peaks      # (a layer's rows alone are 8 MB)
