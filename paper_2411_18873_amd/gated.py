@@ -113,11 +113,19 @@ class GatedModel:
         return grads
 
     def refit(self, feat, energy_measured, n_steps, minibatch, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8):
-        """Adam on Eq. (1) over minibatches of measured kernels, as costmodel_update goes over them; the losses of all steps"""
+        """Adam on Eq. (1) over minibatches of measured kernels, as costmodel_update goes over them; the losses of all steps.  As there,
+        minibatches have to divide the pairs, and with an energy that is not positive and finite losses are NaN and the model is left
+        unchanged (which the host waits for, once a refit)."""
+        n, pairs, losses = int(minibatch), energy_measured.numel(), []
+        if n <= 0 or n_steps <= 0 or pairs == 0 or pairs % n:
+            raise ValueError("pairs must be a whole number of minibatches, steps one or more")
+        if feat.shape[1] < pairs:
+            raise ValueError("feat must have a candidate per energy")
+        if not bool(((energy_measured > 0) & torch.isfinite(energy_measured)).all()):
+            return torch.full((n_steps,), float("nan"), device="cuda")
         y_all = energy_measured / energy_measured.max()
-        n, losses = int(minibatch), []
         for step in range(n_steps):
-            first = step % (y_all.numel() // n) * n
+            first = step % (pairs // n) * n
             x, y = feat[:, first:first + n], y_all[first:first + n]
             pred, kept = self._forward(x, n, True)
             losses.append(((pred - y) ** 2 / y).mean())

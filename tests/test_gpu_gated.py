@@ -150,3 +150,28 @@ def test_scoring_keeps_no_layers():
         torch.cuda.synchronize()
         peaks.append(torch.cuda.max_memory_allocated() - before)
     assert peaks[1] <= peaks[0] + (1 << 20), peaks      # (a layer's rows alone are 8 MB)
+
+
+def test_refit_refuses_what_costmodel_update_refuses():
+    feat = features(64, 300, 19, torch.float32)
+    energy = 0.5 + torch.rand(300, generator=torch.Generator().manual_seed(20)).cuda()
+    model = gated.GatedModel(hidden=32, blocks=1, head=16, seed=21)
+    before = {k: p.clone() for k, p in model.params.items()}
+
+    def unchanged():
+        return (model.steps == 0 and all(torch.equal(model.params[k], p) for k, p in before.items())
+                and all((m == 0).all() and (v == 0).all() for m, v in model.moments.values()))
+
+    for pairs, minibatch, steps in ((300, 256, 4), (300, 301, 4), (300, 0, 4), (300, -100, 4), (300, 100, 0)):
+        with pytest.raises(ValueError):      # pairs that are no whole number of minibatches; nothing to do
+            model.refit(feat, energy[:pairs], steps, minibatch)
+    with pytest.raises(ValueError):          # fewer candidates than energies
+        model.refit(feat[:, :200], energy, 4, 100)
+    assert unchanged()
+    # a data error: losses of NaN, and the model is as it was
+    for bad in (0.0, -1.0, float("nan"), float("inf")):
+        wrong = energy.clone()
+        wrong[250] = bad
+        losses = model.refit(feat, wrong, 4, 100)
+        assert losses.shape == (4,) and torch.isnan(losses).all() and unchanged()
+    assert torch.isfinite(model.refit(feat, energy, 4, 100)).all() and not unchanged()
