@@ -6,8 +6,9 @@ Eq. (1) is the loss of a refit).
     x <- x + dropout(feedforward(layernorm(x)))              `blocks` times, in bf16
     score = feedforward(layernorm(x))                        one output, in fp32
 
-Everything per candidate runs in the library; torch holds the memory, Adam's arithmetic on the fp32 master parameters and
-the few operations on vectors of scores.  `python -m paper_2411_18873_amd.gated` fits one on simulated measurements and picks
+The operators run in the library.  torch holds the memory, and does what lies between them: changes of type before the first block
+and the head (and, in a refit, of their gradients), the sum of the residual's two gradients, the loss on vectors of scores, and
+Adam's arithmetic on the fp32 master parameters.  A model's calls share one workspace, so they belong on one stream.  `python -m paper_2411_18873_amd.gated` fits one on simulated measurements and picks
 candidates with it."""
 import numpy as np
 import torch
