@@ -1,5 +1,5 @@
-"""GPU: gated feed-forward blocks at sizes whose products take each of the library's tiles, undivided and in shares of k, against 64-bit
-evaluations on the device.  Every case names the kernels that it is there for and is checked to have launched them, so that another
+"""GPU: gated feed-forward blocks at sizes whose products take each of the library's tiles, undivided and in shares of k, or the kernels
+for narrow blocks, against 64-bit evaluations on the device.  Every case names the kernels that it is there for and is checked to have launched them, so that another
 choice of tiles cannot take a kernel out of the tests unnoticed."""
 import math
 import re
@@ -191,3 +191,38 @@ def test_whole_numbers_are_exact_in_every_tile(sizes, kind, kernels):
                             (b.grads[2], h.t() @ dy, "dw_down")):
         assert want.abs().max() < 1 << 24              # (and the sums in fp32; results are rounded once)
         assert torch.equal(got, want.to(got.dtype)), what
+
+
+ACTS = {"silu": eck.ACT_SILU, "gelu": eck.ACT_GELU, "relu": eck.ACT_RELU}
+# rows that a narrow block of so many hidden units is one kernel for, by widths: inputs to 64 or 128, outputs to 64, 128 or 256
+NARROW = [(n_in, n_out, n_hidden, n, act) for act in ACTS for n_in, n_out, rows in
+          ((64, 64, 20011), (40, 128, 32700), (64, 200, 32768), (128, 57, 32700), (96, 100, 32000), (128, 256, 32767))
+          for n_hidden, n in ((64, rows), (128, rows), (100, rows), (33, 70000 if n_in + n_out < 300 else 32767))]
+
+
+@pytest.mark.parametrize("n_in,n_out,n_hidden,n,act", NARROW)
+def test_narrow_blocks(n_in, n_out, n_hidden, n, act):
+    u = DTYPES["bf16"][2]
+    g = torch.Generator(device="cuda").manual_seed(n + n_hidden)
+    normal = lambda *s, scale=1.0: torch.randn(*s, generator=g, device="cuda", dtype=torch.float64) * scale  # noqa: E731
+    x, wgu, wd = (t.bfloat16() for t in (normal(n, n_in), normal(n_in, 2 * n_hidden, scale=n_in ** -0.5), normal(n_hidden, n_out, scale=n_hidden ** -0.5)))
+    y = torch.full((n, n_out), math.nan, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((eck.gatedffn_forward_workspace_bytes(n, n_in, n_hidden, n_out, eck.BF16),), 0xFF, dtype=torch.uint8, device="cuda")
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA], acc_events=True) as profile:
+        eck.gatedffn_forward(x, wgu, wd, y, ws, act=ACTS[act])
+        torch.cuda.synchronize()
+    turn = 64 if n_out <= 128 else 32
+    name = "narrow_kernel<%d, %d, %d, %s>" % (2 if n_in <= 64 else 4, 4 if n_out <= 64 else 8 if n_out <= 128 else 16, ACTS[act],
+                                              "true" if n_hidden % turn else "false")
+    assert any(name in e.name for e in profile.events()), [e.name for e in profile.events()]
+    x, wgu, wd = x.double(), wgu.double(), wd.double()
+    pre = x @ wgu
+    off_g, off_u = ((n_in + 2) * E * (x.abs() @ wgu.abs())).chunk(2, 1)
+    gate, up = pre.chunk(2, 1)
+    a = act_of(ACTS[act], gate)[0]
+    h = a * up
+    off_a = 1.13 * off_g + 8 * E * gate.abs()
+    off_h = off_a * up.abs() + (a.abs() + off_a) * off_u
+    off_h += u * (h.abs() + off_h)
+    want = h @ wd
+    hold(y, want, off_h @ wd.abs() + (n_hidden + 2) * E * (h.abs() @ wd.abs()) * 1.01 + u * want.abs() * 1.01, "y")
