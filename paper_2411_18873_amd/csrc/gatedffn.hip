@@ -285,11 +285,14 @@ Rooms rooms(const Sizes &s, bool backward)
 
 constexpr uint32_t NO_GAP = 0xFFFFFFFFu;
 
-// Few rows: the weights' bytes (block_forward.h).  Up to how many rows that is faster than products of matrices.  us, products first:
-// 2048-5632-2048 of bf16 one row 23.7 and 23.5, two 23.7 and 28.6; 4096-8192-4096 one 54.4 and 51.9, two 53.3 and 53.7.  Where the
-// weights have to be copied, four rows: 64-257-63 10.8 and 10.1, 1000-3001-1001 27.3 and 22.9, 4096-8191-4095 172 and 142, but
-// 500-1501-333 18.2 and 19.4, 2048-5631-2047 52.6 and 65.2; eight 18.8 and 24.1, 52.5 and 74.8, 27.5 and 27.2.  fp32, whose weights
-// always have to be, sixteen rows: 64-257-63 14.2 and 12.8, 500-1501-333 29.1 and 23.6, 4096-8192-4096 339 and 145.
+// Few rows: the weights' bytes (block_forward.h).  Up to how many rows that is faster than products of matrices, us, products first.
+// Aligned bf16 weights, one row: 512-2048-512 15.0 and 13.1, 2048-5632-2048 24.2 and 24.0, 4096-8192-4096 53.4 and 49.6; two 15.1 and
+// 14.1, 24.3 and 28.4, 53.4 and 53.2.  Where the weights have to be copied, four rows take 0.49 to 0.81 of the products' time if it is
+// for their address alone (4096-8192-4096 152 and 75, 512-2048-512 21.9 and 17.8) and 0.94 on average, 0.77 to 1.13, if it is for
+// widths (17 blocks: 64-257-63 13.6 and 12.9, 1000-3001-1001 28.4 and 23.0, 4096-8191-4095 171 and 143; but 500-1501-333 20.4 and
+// 22.6, 256-1023-255 17.3 and 19.4, 2048-5631-2047 58 and 65: few columns' blocks, or some more than units); eight rows 18.8 and
+// 24.1 at 500-1501-333, 52.5 and 74.8, 27.5 and 27.2 at 1000-3001-1001.  fp32, whose weights always have to be, sixteen rows:
+// 64-257-63 14.2 and 12.8, 500-1501-333 29.1 and 23.6, 4096-8192-4096 339 and 151.
 constexpr uint32_t FEW_ROWS = 1, FEW_COPIED = 4, FEW_F32 = 16;
 bool few(const Sizes &s, bool straight) { return s.n <= (s.parts == 3 ? FEW_F32 : straight ? FEW_ROWS : FEW_COPIED); }
 
