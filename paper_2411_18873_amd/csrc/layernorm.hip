@@ -625,10 +625,11 @@ template <class T, class F>
 void with_columns_shape(uint32_t width, F &&f)
 {
     static_assert(ECK_MAX_COLUMNS_WIDTH == 256, "no width is left out");
-    constexpr int MOST = 64 / sizeof(T);
-    if (width <= 1024 / MOST) f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 1>{});
-    else if (width <= 64) f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 2>{});
-    else if (width <= 128) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+    constexpr int MOST = 64 / sizeof(T), ONE = 1024 / MOST; // ONE: features that one four a thread holds then
+    if (width <= ONE) return f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 1>{});
+    if constexpr (ONE < 64)
+        if (width <= 64) return f(std::integral_constant<int, MOST>{}, std::integral_constant<int, 2>{});
+    if (width <= 128) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
     else f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
 }
 
