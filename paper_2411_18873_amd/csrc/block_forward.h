@@ -156,10 +156,7 @@ struct NarrowShape {
     static constexpr int PIECES_GU = 4 * DK, PIECES = PIECES_GU + ON, LOADS = PIECES / WAVES; // of 1 KB
     static constexpr int STAGE = PIECES * 1024, LDS = STAGE * SLOTS;
     static_assert(PIECES % WAVES == 0, "every wavefront issues the same number of loads");
-    // two sets of sums of gates and ups where the registers hold them (2^18 rows, us with and without: 128-512-128 114 and 128,
-    // 64-256-64 40.7 and 40.4, 16384 rows of it 8.5 and 9.0; 64-1024-256 228 and 215)
-    static constexpr bool AHEAD = ON <= 8;
-    static constexpr uint32_t UNITS = AHEAD ? 64 : 32; // hidden units of a turn
+    static constexpr uint32_t UNITS = 64; // hidden units of a turn
 };
 
 // PADDED: n_hidden is no multiple of UNITS (a kernel of its own: the branch on it costs 64-256-64 of 16384 rows 8 %)
@@ -267,33 +264,22 @@ __global__ __launch_bounds__(256) void narrow_kernel(const Narrow p)
     load(32, 1);
     wait_and_meet<S::LOADS>();
     uint32_t slot = 0;
+    // The next units' gates and ups are multiplied while the activations of these are worked out, then these units' share of y (2^18
+    // rows, us so and one after the other: 128-512-128 115 and 128, 64-256-64 35.5 and 37.0, 128-512-256 237 and 272; 16384 rows of
+    // 64-256-64 7.7 and 8.8).  At the meeting the next units have come, and everybody is through with the ones before these.
     f32x4 pre[2][4][2]; // gates 0 .. 15, 16 .. 31, ups
-    if constexpr (S::AHEAD) {
-        // The next units' gates and ups are multiplied while the activations of these are worked out, then these units' share of
-        // y.  At the meeting the next units have come, and everybody is through with the ones before these.
-        multiply_up(0, pre[0]);
-        for (uint32_t first = 0; first < p.n_hidden; first += S::UNITS) {
+    multiply_up(0, pre[0]);
+    for (uint32_t first = 0; first < p.n_hidden; first += S::UNITS) {
 #pragma unroll
-            for (int odd = 0; odd < 2; ++odd) { // (units past the last: zeros)
-                const uint32_t next = slot == 2 ? 0 : slot + 1;
-                wait_and_meet<0>();
-                load(first + 32 * odd + 64, next == 2 ? 0 : next + 1);
-                multiply_up(next, pre[odd ^ 1]);
-                bf16x8 h[2];
-                activate(first + 32 * odd, pre[odd], h);
-                multiply_down(slot, h);
-                slot = next;
-            }
-        }
-    } else {
-        for (uint32_t first = 0; first < p.n_hidden; first += S::UNITS) {
-            if (first) wait_and_meet<S::LOADS>(); // these units have come, and everybody is through with the ones before
-            load(first + 64, slot >= 1 ? slot - 1 : 2);
-            multiply_up(slot, pre[0]);
+        for (int odd = 0; odd < 2; ++odd) { // (units past the last: zeros)
+            const uint32_t next = slot == 2 ? 0 : slot + 1;
+            wait_and_meet<0>();
+            load(first + 32 * odd + 64, next == 2 ? 0 : next + 1);
+            multiply_up(next, pre[odd ^ 1]);
             bf16x8 h[2];
-            activate(first, pre[0], h);
+            activate(first + 32 * odd, pre[odd], h);
             multiply_down(slot, h);
-            slot = slot == 2 ? 0 : slot + 1;
+            slot = next;
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // (zeros for units past the last end before the block does)

@@ -363,10 +363,10 @@ int32_t forward_few(const T *x, uint64_t ld_x, const Sizes &s, const T *w_gate_u
 // Narrow blocks without (g | u): one kernel where it should take less time than the two products (us).  A block of it goes through all
 // hidden units for 128 rows, so up to 128 rows a compute unit its time does not depend on the rows, and with more it grows by whole
 // blocks a unit; a turn of 32 units is bound by the activations (GELU's are three times SiLU's), in wide blocks by the products.  The
-// constants were fitted to 493 pairs of measurements (14 to 23 shapes an activation, 200 to 131072 rows): the choice takes 0.3 % more
-// than the better one, on average, and 18 % at most.  One kernel and two products, us: 64-256-64 SiLU 4096 rows 7.6 and 8.5, 16384
-// 7.8 and 11.5, 131072 21 and 61; 128-2048-128 8192 rows 58 and 40, 32768 62 and 117; 64-8192-256 12288 rows 359 and 196, 65536
-// 433 and 897; GELU 64-1024-64 12288 rows 71 and 38, 65536 96 and 155; 128-4096-256 12288 rows 407 and 166, 131072 1679 and 1436.
+// constants were fitted to 583 pairs of measurements (28 shapes, 200 to 131072 rows, all activations): the choice takes 0.2 % more
+// than the better one, on average, and 14 % at most.  One kernel and two products, us: 64-256-64 SiLU 4096 rows 7.6 and 8.5, 16384
+// 7.7 and 11.5, 131072 21 and 61; 128-2048-128 8192 rows 58 and 40, 32768 62 and 117; 64-8192-256 12288 rows 320 and 197, 65536
+// 415 and 897; GELU 64-1024-64 12288 rows 71 and 38, 65536 96 and 155; 128-4096-256 12288 rows 360 and 162, 131072 1479 and 1428.
 // 256-1024-256 has no kernel: on 65536 rows it took 203 for 177.
 constexpr uint32_t NARROW_IN = 128, NARROW_OUT = 256;
 bool narrow(const Sizes &s, int32_t act)
@@ -374,14 +374,14 @@ bool narrow(const Sizes &s, int32_t act)
     if (s.n_in > NARROW_IN || s.n_out > NARROW_OUT) return false;
     static const struct {
         double one, more; // a turn with one block on a unit, and for each of several
-    } TURNS[2][2][3] = {{{{0.60, 0.51}, {0.75, 0.61}, {1.39, 0.87}}, {{1.01, 0.71}, {1.05, 0.91}, {1.81, 2.00}}},
-                        {{{2.17, 1.49}, {2.28, 1.55}, {2.88, 1.90}}, {{2.36, 1.60}, {2.31, 1.82}, {3.20, 3.37}}}}; // GELU
+    } TURNS[2][2][3] = {{{{0.60, 0.51}, {0.75, 0.61}, {1.24, 0.84}}, {{1.01, 0.71}, {1.05, 0.91}, {1.50, 1.58}}},
+                        {{{2.17, 1.49}, {2.28, 1.55}, {2.62, 1.74}}, {{2.36, 1.60}, {2.31, 1.82}, {2.80, 2.88}}}}; // GELU
     const bool gelu = act == ECK_ACT_GELU;
     const auto &turn = TURNS[gelu][s.n_in > 64][s.n_out <= 64 ? 0 : s.n_out <= 128 ? 1 : 2];
-    const uint64_t turns = up_to(s.n_hidden, s.n_out <= 128 ? 64 : 32) / 32, blocks = (s.n + 32767) / 32768; // (of 128 rows on 256 units)
+    const uint64_t turns = up_to(s.n_hidden, 64) / 32, blocks = (s.n + 32767) / 32768; // (of 128 rows on 256 units)
     const double values = (double)s.n * s.n_hidden * 1e-6, ends = (double)(s.n_in + s.n_out);
     const double products = 7.8 + values * (1.28 + 1.7e-3 * ends + (gelu ? 0.88 : 0.0)) + 0.155e-6 * (double)s.n * ends;
-    return 2.8 + (double)turns * (blocks == 1 ? turn.one : turn.more * (double)blocks) < products;
+    return (s.n_out <= 128 ? 2.8 : 5.0) + (double)turns * (blocks == 1 ? turn.one : turn.more * (double)blocks) < products;
 }
 template <int ACT, int DK, int ON>
 int32_t launch_narrow_shape(const Narrow &p, hipStream_t st)

@@ -211,9 +211,8 @@ def test_narrow_blocks(n_in, n_out, n_hidden, n, act):
     with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA], acc_events=True) as profile:
         eck.gatedffn_forward(x, wgu, wd, y, ws, act=ACTS[act])
         torch.cuda.synchronize()
-    turn = 64 if n_out <= 128 else 32
     name = "narrow_kernel<%d, %d, %d, %s>" % (2 if n_in <= 64 else 4, 4 if n_out <= 64 else 8 if n_out <= 128 else 16, ACTS[act],
-                                              "true" if n_hidden % turn else "false")
+                                              "true" if n_hidden % 64 else "false")
     assert any(name in e.name for e in profile.events()), [e.name for e in profile.events()]
     x, wgu, wd = x.double(), wgu.double(), wd.double()
     pre = x @ wgu
