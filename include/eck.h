@@ -468,8 +468,9 @@ int32_t treemodel_update(eck_trees *trees, const void *feat, int32_t feat_dtype,
  * elements apart, is candidate i.  Elements are ECK_F32 or ECK_BF16; sums,
  * statistics and products accumulate in fp32 or more, results are rounded once.
  * Pointers are aligned to their elements, nothing more is asked for (rows that
- * start on 16 bytes are fastest); workspaces start on 256 bytes.  Nothing
- * depends on the order of execution: equal calls give equal bits. */
+ * start on 16 bytes are fastest); workspaces start on 256 bytes.  Outputs and
+ * workspaces overlap neither each other nor inputs, but for what a call says.
+ * Nothing depends on the order of execution: equal calls give equal bits. */
 
 #define ECK_ROWS 0    /* x is an [n][ld] matrix of activations */
 #define ECK_COLUMNS 1 /* x is a [width][ld] matrix with a candidate per column, as features_compute writes it */
@@ -485,6 +486,8 @@ int32_t treemodel_update(eck_trees *trees, const void *feat, int32_t feat_dtype,
  *   reads as ones and zeros; y: device [n][ld_y] of dtype;
  *   mean_out, rstd_out: device float [n], both or neither NULL (what
  *   layernorm_backward wants to know).  In ROWS order y may be x.
+ *   Squares of differences from a row's mean have to be in fp32's range, and
+ *   with eps = 0 not all of them below it.
  * Errors: EINVAL (x or y NULL, one of mean_out / rstd_out alone, n or width 0,
  * bad x_order or dtype, eps negative or not finite), ESHAPE (ld_x, ld_y too
  * small), EUNSUPPORTED (COLUMNS with width > ECK_MAX_COLUMNS_WIDTH, n > 2^31,
@@ -534,7 +537,7 @@ int32_t dropout_apply(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, u
  *   dtype.  act: ECK_ACT_*.  pre_out: device float [n][2*n_hidden], receives
  *   [g | u] for gatedffn_backward, or NULL (narrow blocks of many rows are
  *   fastest then).
- * h is rounded to dtype before the second product; y must not overlap inputs.
+ * h is rounded to dtype before the second product.
  * Few rows (up to 16 of fp32, up to 4 of bf16) may be multiplied in fp32
  * instructions; more are on the matrix cores, fp32 ones as sums of six
  * products of bfloat16 parts, as good as fp32 products for magnitudes of

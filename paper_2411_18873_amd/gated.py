@@ -8,8 +8,8 @@ Eq. (1) is the loss of a refit).
 
 The operators run in the library.  torch holds the memory, and does what lies between them: changes of type before the first block
 and the head (and, in a refit, of their gradients), the sum of the residual's two gradients, the loss on vectors of scores, and
-Adam's arithmetic on the fp32 master parameters.  A model's calls share one workspace, so they belong on one stream.  `python -m paper_2411_18873_amd.gated` fits one on simulated measurements and picks
-candidates with it."""
+Adam's arithmetic on the fp32 master parameters.  A model's calls share one workspace, so they belong on one stream.
+`python -m paper_2411_18873_amd.gated` fits one on simulated measurements and picks candidates with it."""
 import numpy as np
 import torch
 
