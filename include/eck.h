@@ -542,7 +542,8 @@ int32_t dropout_apply(const void *x, int32_t dtype, uint64_t ld_x, uint64_t n, u
  * instructions; more are on the matrix cores, fp32 ones as sums of six
  * products of bfloat16 parts, as good as fp32 products for magnitudes of
  * 2^-100 to 2^127 (and zeros; an infinite input gives NaN or infinities in
- * its row, smaller numbers lose low bits).
+ * its row, smaller numbers lose low bits).  So a row's last bits, and in fp32
+ * its range, depend on how many rows go with it.
  * ws: room for h, for shares of sums, and for copies of the operands of an
  * fp32 block or of matrices that do not start on 16 bytes or whose rows are
  * no multiple of eight elements.  The queries say 0 for sizes that are refused.
