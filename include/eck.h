@@ -567,6 +567,63 @@ int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t 
                           const void *dy, uint64_t ld_dy, void *dx_out, uint64_t ld_dx, void *dw_gate_up_out,
                           void *dw_down_out, void *ws, uint64_t ws_bytes, void *stream);
 
+/* ------------------------------------------- refits of models of many tensors */
+
+/* A parameter tensor with its gradient and Adam's states.  Everything but the
+ * struct is device memory; elements are contiguous and aligned to their type.
+ * A tensor of no elements is passed over. */
+#define ECK_STATE_F32 0  /* m, v: float [n] */
+#define ECK_STATE_8BIT 1 /* m, v: uint8 [n], with a power of two for every ECK_STATE_BLOCK elements */
+#define ECK_STATE_BLOCK 128
+typedef struct {
+    float *param;         /* [n], updated */
+    const void *grad;     /* [n] of grad_dtype */
+    void *m, *v;          /* [n], updated: the gradient's mean and its square's */
+    uint8_t *m_scale;     /* 8BIT: [ceil(n / ECK_STATE_BLOCK)], updated; F32: not looked at */
+    uint8_t *v_scale;
+    void *bf16_out;       /* bf16 [n]: the new parameters, rounded; or NULL */
+    uint64_t n;
+    int32_t grad_dtype;   /* ECK_F32 or ECK_BF16 */
+    float weight_decay;
+} eck_parameter;
+
+/* One step of AdamW (decoupled weight decay; of Adam where that is 0) over all
+ * tensors, number t = step (the first is 1):
+ *   g = s grad,  m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
+ *   w <- w (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32.  step_more: device uint32 or NULL, added to step (a captured step
+ * that is replayed counts there).  grad_scale: device float s or NULL (1), as
+ * gradients_norm writes it; where it is not finite, the call changes nothing.
+ * 8BIT states: m in the float8 format e4m3, v in e5m2 (all bytes 0: a state of
+ * zeros), times 2^(scale - 127) of the block of ECK_STATE_BLOCK elements, which
+ * brings its largest finite one into [2^7, 2^8) or [2^14, 2^15) (scales of 27 to
+ * 227).  They are rounded up or down to the format's next number by 16-bit
+ * draws d: up iff d / 2^16 + (the way to the next lower one, in steps) >= 1; a v
+ * that is not 0 does not become 0, what is not finite becomes NaN.  Elements are
+ * numbered over the list, every tensor from a multiple of ECK_STATE_BLOCK on;
+ * those of 2j and 2j + 1 have the low and the high half of output number j + 1 of
+ * a SplitMix64 generator whose state starts at mix(seed + gamma*(t+1)), as in
+ * candidate_enumerate: the low half of that m's draw, the high half v's.
+ * parameters: host, read during the call.  No two tensors may overlap.  A
+ * launch takes some dozens of tensors.
+ * Errors: EINVAL (nulls, no element at all, a bad dtype or state, lr, eps or a
+ * decay negative or not finite, a beta outside [0, 1), step 0 without
+ * step_more), EUNSUPPORTED (n > 2^40), EALIGN. */
+int32_t adamw_step(const eck_parameter *parameters, uint32_t count, int32_t state, double lr, double beta1, double beta2,
+                   double eps, uint32_t step, const uint32_t *step_more, const float *grad_scale, uint64_t seed, void *stream);
+
+/* The norm of all gradients of a list (its grad, grad_dtype and n; nothing else
+ * of it is looked at), sqrt(sum g^2), summed in fp64 in a fixed order, and what
+ * they are to be multiplied with so that it is max_norm at most:
+ *   *norm_out = norm,  *scale_out = min(1, max_norm / norm), NaN where the norm
+ *   is not finite (device float; one may be NULL).
+ * The query says 0 for lists that are refused.
+ * Errors: EINVAL (nulls, no element at all, a bad dtype, max_norm not above 0),
+ * EUNSUPPORTED (n > 2^40), EWORKSPACE, EALIGN (ws: 256 bytes). */
+uint64_t gradients_norm_workspace_bytes(const eck_parameter *parameters, uint32_t count);
+int32_t gradients_norm(const eck_parameter *parameters, uint32_t count, float max_norm, float *norm_out, float *scale_out,
+                       void *ws, uint64_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,6 +24,8 @@ F32, BF16 = 0, 1
 SELECT_THRESHOLD, SELECT_RANK = 0, 1
 ROWS, COLUMNS = 0, 1
 ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
+STATE_F32, STATE_8BIT = 0, 1
+STATE_BLOCK = 128
 MAX_K = 4096
 MAX_BATCH = 128
 
@@ -37,7 +39,8 @@ EXPORTS = ["eck_version", "eck_space_create", "eck_space_upload", "eck_space_des
            "treemodel_score", "treemodel_update_workspace_bytes", "treemodel_update", "eck_k_step", "eck_k_count",
            "eck_candidates_dedup", "eck_candidates_dedup_workspace_bytes",
            "layernorm_forward", "layernorm_backward_workspace_bytes", "layernorm_backward", "dropout_apply",
-           "gatedffn_forward_workspace_bytes", "gatedffn_forward", "gatedffn_backward_workspace_bytes", "gatedffn_backward"]
+           "gatedffn_forward_workspace_bytes", "gatedffn_forward", "gatedffn_backward_workspace_bytes", "gatedffn_backward",
+           "adamw_step", "gradients_norm_workspace_bytes", "gradients_norm"]
 
 
 class EckError(RuntimeError):
@@ -57,6 +60,11 @@ class Problem(C.Structure):
         f = [int(v) for v in fields]
         assert len(f) == 15
         return cls(f[0], (C.c_int32 * 8)(*f[1:9]), *f[9:15])
+
+
+class Parameter(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("bf16_out", C.c_void_p), ("n", C.c_uint64), ("grad_dtype", C.c_int32), ("weight_decay", C.c_float)]
 
 
 _lib = None
@@ -126,13 +134,18 @@ def lib():
         L.gatedffn_backward_workspace_bytes.argtypes = [u64, u32, u32, u32, i32]
         L.gatedffn_backward_workspace_bytes.restype = u64
         L.gatedffn_backward.argtypes = [vp, i32, u64, u64, u32, u32, u32, vp, vp, i32, vp, vp, u64, vp, u64, vp, vp, vp, u64, vp]
+        L.adamw_step.argtypes = [vp, u32, i32, C.c_double, C.c_double, C.c_double, C.c_double, u32, vp, vp, u64, vp]
+        L.gradients_norm_workspace_bytes.argtypes = [vp, u32]
+        L.gradients_norm_workspace_bytes.restype = u64
+        L.gradients_norm.argtypes = [vp, u32, f32, vp, vp, vp, u64, vp]
         for name in EXPORTS:
             fn = getattr(L, name)
             if name not in ("eck_space_destroy", "eck_model_destroy", "topk_select_workspace_bytes",
                             "topk_select_rank_workspace_bytes", "eck_trees_destroy",
                             "eck_candidates_dedup_workspace_bytes", "treemodel_update_workspace_bytes",
                             "costmodel_update_workspace_bytes", "layernorm_backward_workspace_bytes",
-                            "gatedffn_forward_workspace_bytes", "gatedffn_backward_workspace_bytes"):
+                            "gatedffn_forward_workspace_bytes", "gatedffn_backward_workspace_bytes",
+                            "gradients_norm_workspace_bytes"):
                 fn.restype = i32
         _lib = L
     return _lib
@@ -670,3 +683,93 @@ def gatedffn_backward(x, w_gate_up, w_down, pre, dy, dx, dw_gate_up, dw_down, ws
         x.data_ptr(), _FEAT_DTYPE[dy.dtype], ld_x, n, n_in, n_hidden, n_out, w_gate_up.data_ptr(), w_down.data_ptr(), act,
         _vector(pre, "pre", 2 * n * n_hidden), dy.data_ptr(), ld_dy, _ptr(dx), ld_dx, _ptr(dw_gate_up), _ptr(dw_down), ws_ptr, ws_bytes,
         _stream()))
+
+
+# ------------------------------------------------------------------------------ refits of models of many tensors
+
+
+def _here(t, dtype, name):
+    """a contiguous CUDA tensor of dtype on the current device"""
+    _dev(t, dtype, name)
+    if t.get_device() != _device():
+        raise ValueError("%s must be on the current device" % name)
+    return t
+
+
+class Parameters:
+    """The tensors of a model as gradients_norm (grads alone) and adamw_step take them, checked once and kept: lists of contiguous CUDA tensors.
+    m, v: float32, or uint8 with m_scale, v_scale (uint8, one for each STATE_BLOCK elements); copies (bfloat16, or None in the list's or a
+    tensor's place) receive the new parameters.  weight_decay: one for all, or a list."""
+
+    def __init__(self, grads, params=None, m=None, v=None, m_scale=None, v_scale=None, copies=None, weight_decay=0.0):
+        count = len(grads)
+        self.count, self.state = count, STATE_F32
+        self._array = (Parameter * count)()
+        self._kept = {"params": params, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies}
+        for name, tensors in self._kept.items():
+            if tensors is not None and len(tensors) != count:
+                raise ValueError("%s must have a tensor for each of the %d gradients" % (name, count))
+        decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+        if len(decay) != count:
+            raise ValueError("weight_decay must be one number, or one for each gradient")
+        if params is not None:
+            if m is None or v is None:
+                raise ValueError("parameters need their states m and v")
+            if any(t.dtype is torch.uint8 for t in m):
+                self.state = STATE_8BIT
+                if m_scale is None or v_scale is None:
+                    raise ValueError("8-bit states need m_scale and v_scale")
+        for i, entry in enumerate(self._array):
+            entry.n, entry.weight_decay = grads[i].numel(), decay[i]
+            if params is None:
+                continue
+            of = torch.float32 if self.state == STATE_F32 else torch.uint8
+            blocks = -(-entry.n // STATE_BLOCK)
+            for field, tensors, dtype, n in (("param", params, torch.float32, entry.n), ("m", m, of, entry.n), ("v", v, of, entry.n),
+                                             ("m_scale", m_scale, torch.uint8, blocks), ("v_scale", v_scale, torch.uint8, blocks),
+                                             ("bf16_out", copies, torch.bfloat16, entry.n)):
+                if tensors is None or (field == "bf16_out" and tensors[i] is None) or (self.state == STATE_F32 and field.endswith("scale")):
+                    continue
+                if _here(tensors[i], dtype, field).numel() != n:
+                    raise ValueError("%s of tensor %d must have %d elements" % (field, i, n))
+                setattr(entry, field, tensors[i].data_ptr())
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        """other gradients of the same sizes, float32 or bfloat16"""
+        if len(grads) != self.count:
+            raise ValueError("there must be %d gradients" % self.count)
+        for entry, t in zip(self._array, grads):
+            if t.numel() != entry.n:
+                raise ValueError("a gradient must have as many elements as its parameter")
+            _here(t, t.dtype if t.dtype in _FEAT_DTYPE else torch.float32, "a gradient")
+            entry.grad, entry.grad_dtype = t.data_ptr(), _FEAT_DTYPE[t.dtype]
+        self._kept["grads"] = list(grads)
+
+
+def _one(t, dtype, name):
+    """the address of a single element on the device, or None"""
+    if t is None:
+        return None
+    if t.numel() != 1:
+        raise ValueError("%s must have one element" % name)
+    return _here(t, dtype, name).data_ptr()
+
+
+def adamw_step(parameters, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0, step_more=None):
+    """step number `step` (+ *step_more, an int32 tensor) over all of a Parameters; gradients times *grad_scale; seed: of 8-bit states' roundings"""
+    if not 0 <= step < 1 << 32:
+        raise ValueError("step must be a whole number of 32 bits")
+    _check("adamw_step", lib().adamw_step(parameters._array, parameters.count, parameters.state, lr, beta1, beta2, eps, step,
+                                          _one(step_more, torch.int32, "step_more"), _one(grad_scale, torch.float32, "grad_scale"), seed, _stream()))
+
+
+def gradients_norm_workspace_bytes(parameters):
+    return int(lib().gradients_norm_workspace_bytes(parameters._array, parameters.count))
+
+
+def gradients_norm(parameters, norm_out, scale_out, ws, max_norm=float("inf")):
+    """norm_out = the norm of all gradients, scale_out = what brings it to max_norm or less (one of them may be None)"""
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("gradients_norm", lib().gradients_norm(parameters._array, parameters.count, max_norm, _one(norm_out, torch.float32, "norm_out"),
+                                                  _one(scale_out, torch.float32, "scale_out"), ws_ptr, ws_bytes, _stream()))
