@@ -567,6 +567,47 @@ int32_t gatedffn_backward(const void *x, int32_t dtype, uint64_t ld_x, uint64_t 
                           const void *dy, uint64_t ld_dy, void *dx_out, uint64_t ld_dx, void *dw_gate_up_out,
                           void *dw_down_out, void *ws, uint64_t ws_bytes, void *stream);
 
+/* --------------------------------------------- scoring in 8-bit integers
+ *
+ * A matrix of 8-bit integers is row-major like one of activations, [rows][ld],
+ * and has a scale for each row (float): element k of row r stands for
+ * scale[r] q[r][k].  Rows start on 16 bytes (ld a multiple of 16), and what
+ * lies between a row's width and the next multiple of 16 belongs to it:
+ * quantise_rows writes zeros there, and product_int8 wants them in x or in w. */
+
+/* Rows in 8-bit integers, each by its largest magnitude m:
+ *   scale = m / 127,  q = x (127 / m) rounded to the nearest, halves to even,
+ * quotients and product in fp32.  A row whose m is below 2^-100 is all zeros, its
+ * scale too; one that holds a NaN or an infinity is zeros with the scale NaN.
+ *   x: device, of dtype, in x_order (ECK_COLUMNS: [width][ld_x], a row of the
+ *   result per column, as features_compute writes candidates; so the columns
+ *   of weights [fan_in][fan_out] become rows); q_out: device [n][ld_q];
+ *   scale_out: device float [n].
+ * Errors: EINVAL (nulls, a zero size, bad x_order or dtype), ESHAPE (an ld too
+ * small), EUNSUPPORTED (n > 2^31, width > 131071), EALIGN (also q_out not on 16
+ * bytes, ld_q no multiple of 16). */
+int32_t quantise_rows(const void *x, int32_t x_order, int32_t dtype, uint64_t ld_x, uint64_t n, uint32_t width,
+                      int8_t *q_out, uint64_t ld_q, float *scale_out, void *stream);
+
+#define ECK_ACT_NONE (-1) /* product_int8: no gate */
+
+/* Products of rows of 8-bit integers, and gates of them:
+ *   ECK_ACT_NONE: y[i][c] = ((sum_k x[i][k] w[c][k]) x_scale[i]) w_scale[c]
+ *   ECK_ACT_*:    y[i][c] = a(g) u, g so from w's row c, u from row n_out + c
+ * (the first product of a gated feed-forward block, gate rows then up rows).
+ * Sums are exact, what follows is fp32, y is rounded once.
+ *   x: device [n][ld_x], w: device [n_out or 2 n_out][ld_w], int8 matrices of
+ *   width n_in; x_scale, w_scale: device float, one for each of their rows;
+ *   y: device [n][ld_y] of dtype.  ws: where the query says 0, it may be NULL.
+ * Errors: EINVAL (nulls, a zero size, bad act or dtype), ESHAPE (an ld too
+ * small), EUNSUPPORTED (n > 2^31, n_in > 131071, n_out > 2^20, an ld of x or w
+ * above 2^22, more than 2^22 tiles of 64 x 64 in all products), EWORKSPACE,
+ * EALIGN (also x or w not on 16 bytes, their ld no multiple of 16). */
+uint64_t product_int8_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_out, int32_t act);
+int32_t product_int8(const int8_t *x, uint64_t ld_x, const float *x_scale, uint64_t n, uint32_t n_in, uint32_t n_out,
+                     const int8_t *w, uint64_t ld_w, const float *w_scale, int32_t act, int32_t dtype, void *y,
+                     uint64_t ld_y, void *ws, uint64_t ws_bytes, void *stream);
+
 /* ------------------------------------------- refits of models of many tensors */
 
 /* A parameter tensor with its gradient and Adam's states.  Everything but the

@@ -1,0 +1,417 @@
+// Products of matrices of 8-bit integers with a scale for each row of both, and gates of pairs of them, on the matrix cores (HIP, gfx950).
+//
+//   y[m][c] = (sum over k of x[m][k] w[c][k]) s_x[m] s_w[c],   or a(g) u of two such
+//
+// Sums are 32-bit integers, so they are exact whatever the order, in any number of shares of k.  Both operands lie along k; to the
+// staging of product.h two neighbouring integers are one of its elements (the sixteen bytes that a lane feeds to a matrix instruction lie
+// in memory and in the LDS as eight bfloat16 values do), so stages, their swizzles and their waits are those.
+#include "product.h"
+
+namespace eck {
+namespace {
+
+using namespace product;
+
+constexpr uint32_t MOST_IN = 131071;      // integers of magnitude 128: 131072 products of 2^14 are 2^31
+constexpr uint64_t MOST_OUT = 1u << 20;
+constexpr uint64_t MOST_TILES = 1u << 22; // of 64 x 64
+
+struct Result {
+    const float *x_scale, *w_scale;
+    void *y;
+    uint64_t ld_y;
+    uint32_t n_out; // columns of y, and rows of w from a gate to its up
+    int32_t act;    // ECK_ACT_*
+    int32_t f32;    // y's type
+};
+
+struct Int8Product {
+    const int8_t *x, *w;
+    uint64_t ld_x, ld_w;
+    uint32_t n, n_in;
+    uint32_t tiles_m, tiles_n, shares;
+    int32_t *partial; // shares > 1: sums of each, [share][n][columns]
+    uint32_t columns; // of w: n_out, or twice that
+    Result to;
+};
+
+template <class T, bool GATE_>
+__device__ __forceinline__ void finish_as(const Result &to, uint64_t m, uint32_t c, const int (&v)[8], const int (&u)[8])
+{
+    const float row = to.x_scale[m];
+    float y[8], up[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool there = c + i < to.n_out;
+        y[i] = there ? (float)v[i] * row * to.w_scale[c + i] : 0.0f;
+        if (GATE_) up[i] = there ? (float)u[i] * row * to.w_scale[to.n_out + c + i] : 0.0f;
+    }
+    if (GATE_)
+        with_act(to.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = gate_as<decltype(act)::value, sizeof(T) == 4>(y[i]).value * up[i];
+        });
+    store_eight((T *)to.y + m * to.ld_y, c, to.n_out, y);
+}
+template <bool GATE_>
+__device__ __forceinline__ void finish(const Result &to, uint64_t m, uint32_t c, const int (&v)[8], const int (&u)[8])
+{
+    if (to.f32) finish_as<float, GATE_>(to, m, c, v, u);
+    else finish_as<bf16, GATE_>(to, m, c, v, u);
+}
+
+// ------------------------------------------------------------------------------------------------ tiles
+
+template <class S, bool GATE_, bool SHARED>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::AT_ONCE, S::AT_ONCE))) void tiles_kernel(const Int8Product p)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    typedef Stage<S::BM, true, S::WAVES, 1> StageA;
+    typedef Stage<S::BN, true, S::WAVES, 1> StageB;
+    constexpr int PER_STEP = StageA::LOADS + StageB::LOADS, BK = S::BK; // BK: pairs of integers
+    constexpr uint32_t STAGE = S::STAGE;
+    constexpr bool PAIRED = GATE_ && !SHARED; // gates and their ups in one tile
+    constexpr int COLUMNS = PAIRED ? S::BN / 2 : S::BN;
+
+    // blocks go round the eight dies, whose blocks take neighbouring tiles, in panels eight tiles high
+    const uint32_t tiles = p.tiles_m * p.tiles_n, total = gridDim.x, die = blockIdx.x & 7, left_over = total & 7;
+    const uint32_t number = die * (total >> 3) + min(die, left_over) + (blockIdx.x >> 3);
+    const uint32_t share = number / tiles, tile = number % tiles, panel = tile / (8 * p.tiles_n), in_panel = tile % (8 * p.tiles_n);
+    const uint32_t high = min(8u, p.tiles_m - 8 * panel);
+    const uint32_t m0 = (8 * panel + in_panel % high) * S::BM, c0 = in_panel / high * COLUMNS;
+    const uint32_t N = PAIRED ? p.to.n_out : p.columns;
+
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t wm = wave / S::WN, wn = wave % S::WN;
+    StageA sa;
+    StageB sb;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    constexpr uint32_t HALF = S::BN / S::WN / 2; // of a wavefront's columns the first half are gates, the second the ups of the same units
+    sa.init(p.ld_x / 2, lds0, [&](uint32_t r) { return m0 + r < p.n ? r : NOWHERE; });
+    // (a gate's up may lie 2^32 bytes and more behind it: ups are loaded from a base of their own)
+    const int8_t *at_b = p.w + c0 * p.ld_w;
+    sb.init(p.ld_w / 2, lds0 + StageA::BYTES, [&](uint32_t c) {
+        if (!PAIRED) return c0 + c < N ? c : NOWHERE;
+        const uint32_t unit = c / (2 * HALF) * HALF + c % HALF;
+        return c0 + unit < N ? unit : NOWHERE;
+    });
+    // which of this wavefront's loads bring ups (the same for all lanes: a load brings eight rows)
+    static_assert(HALF % 8 == 0, "a load's rows are all gates or all ups");
+    const uint64_t up = PAIRED ? (uint64_t)p.to.n_out * p.ld_w : 0;
+
+    const uint32_t pairs = (p.n_in + 15) / 16 * 8, all = (pairs + BK - 1) / BK;
+    const uint32_t first = (uint32_t)((uint64_t)all * share / p.shares), steps = (uint32_t)((uint64_t)all * (share + 1) / p.shares) - first;
+    const int8_t *at_a = p.x + m0 * p.ld_x + (uint64_t)first * (2 * BK);
+    at_b += (uint64_t)first * (2 * BK);
+    uint32_t to_come = steps, left = pairs - first * BK;
+    const auto load_b = [&](uint32_t some, uint32_t stage_at) {
+#pragma unroll
+        for (int j = 0; j < StageB::LOADS; ++j) {
+            const uint32_t r = (wave * StageB::LOADS + j) * 8;
+            const bool second = PAIRED && r % (2 * HALF) >= HALF;
+            const uint64_t address = reinterpret_cast<uint64_t>(at_b + (second ? up : 0));
+            const i32x4 where = {(int)(uint32_t)address, (int)((uint32_t)(address >> 32) & 0xFFFF), 0x7FFFFFFF, 0x00020000};
+            load_to_lds(sb.lds_at + stage_at + j * 1024, sb.k_of[j] < some ? sb.offset[j] : NOWHERE, where);
+        }
+    };
+    const auto load = [&](uint32_t slot) { // past the end: zeros
+        const uint32_t some = to_come ? left : 0;
+        sa.load(reinterpret_cast<const bf16 *>(at_a), some, slot * STAGE);
+        load_b(some, slot * STAGE);
+    };
+    const auto advance = [&]() {
+        to_come = to_come ? to_come - 1 : 0;
+        at_a += 2 * BK;
+        at_b += 2 * BK;
+        left -= BK;
+    };
+
+    i32x4 sum[S::TM][S::TN];
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) sum[i][j] = i32x4{0, 0, 0, 0};
+    bf16x8 a[2][S::TM], b[2][S::TN];
+    const auto read = [&](uint32_t slot, int to) {
+        const uint32_t at = lds0 + slot * STAGE;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) b[to][j] = StageB::read(at + StageA::BYTES, wn * S::TN + j, to);
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) a[to][i] = StageA::read(at, wm * S::TM + i, to);
+    };
+    const auto multiply = [&](int from) {
+        // columns as the first operand: a lane's four sums are neighbouring columns of one row
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+                sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b[from][j]), __builtin_bit_cast(i32x4, a[from][i]), sum[i][j],
+                                                                  0, 0, 0);
+        constexpr int READS = S::TM + S::TN, PRODUCTS = S::TM * S::TN, EACH = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+#pragma unroll
+        for (int r = 0; r < READS; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
+        }
+    };
+
+    // One half of a step's k's is multiplied from registers while the next is read from the LDS and later steps are on their way.
+#pragma unroll
+    for (int s = 0; s < S::STAGES; ++s) {
+        load(s);
+        advance();
+    }
+    wait_and_meet<(S::STAGES - 1) * PER_STEP>();
+    read(0, 0);
+    uint32_t slot = 0;
+    for (uint32_t i = 0; i < steps; ++i) {
+        read(slot, 1);
+        multiply(0);
+        wait_and_meet<(S::STAGES - 2) * PER_STEP>();
+        load(slot);
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        read(slot, 0);
+        multiply(1);
+        advance();
+    }
+    wait_and_meet<0>(); // (loads past the end have to be done writing zeros to the LDS)
+
+    // Sums to results by way of the LDS, so that memory sees whole rows of the tile
+    constexpr int HIGH = S::TM < 2 ? 1 : 2, ROWS = S::WM * 16 * HIGH, PITCH = S::BN + 4;
+    constexpr int CHUNKS = COLUMNS / 8, ITEMS = ROWS * CHUNKS / S::THREADS;
+    static_assert(ROWS * PITCH * 4 <= S::LDS && ITEMS * S::THREADS == ROWS * CHUNKS, "the rows fit, and every thread has as many");
+    const uint32_t mine = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS, c = c0 + 8 * chunk;
+    int *const rows = reinterpret_cast<int *>(lds);
+#pragma unroll
+    for (int step = 0; step < S::TM / HIGH; ++step) {
+        if (step > 0) lds_barrier();
+#pragma unroll
+        for (int i = 0; i < HIGH; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j)
+                *reinterpret_cast<i32x4 *>(rows + ((wm * HIGH + i) * 16 + (lane & 15)) * PITCH + (wn * S::TN + j) * 16 + 4 * (lane >> 4)) =
+                    sum[step * HIGH + i][j];
+        lds_barrier();
+#pragma unroll
+        for (int item = 0; item < ITEMS; ++item) {
+            const uint32_t r = mine + item * (S::THREADS / CHUNKS);
+            const uint32_t m = m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
+            if (m >= p.n || c >= N) continue;
+            const int *row = rows + r * PITCH;
+            const uint32_t at = PAIRED ? 8 * chunk / HALF * (2 * HALF) + 8 * chunk % HALF : 8 * chunk;
+            int v[8], u[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                *reinterpret_cast<i32x4 *>(v + i) = *reinterpret_cast<const i32x4 *>(row + at + i);
+                if (PAIRED) *reinterpret_cast<i32x4 *>(u + i) = *reinterpret_cast<const i32x4 *>(row + at + HALF + i);
+            }
+            if constexpr (SHARED) {
+                int *to = p.partial + ((uint64_t)share * p.n + m) * p.columns;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < N) to[c + i] = v[i];
+            } else {
+                finish<GATE_>(p.to, m, c, v, u);
+            }
+        }
+    }
+}
+
+// shares of sums added up, eight columns a thread
+template <bool GATE_>
+__global__ __launch_bounds__(256) void join_kernel(const Int8Product p)
+{
+    const uint32_t chunks = (p.to.n_out + 7) / 8;
+    const uint64_t total = (uint64_t)p.n * chunks;
+    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (uint64_t)gridDim.x * 256) {
+        const uint64_t m = at / chunks;
+        const uint32_t c = (uint32_t)(at % chunks) * 8;
+        int v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (uint32_t s = 0; s < p.shares; ++s) {
+            const int *row = p.partial + ((uint64_t)s * p.n + m) * p.columns;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < p.to.n_out) {
+                    v[i] += row[c + i];
+                    if (GATE_) u[i] += row[p.to.n_out + c + i];
+                }
+        }
+        finish<GATE_>(p.to, m, c, v, u);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+
+// Up to 16 * TILES rows: the weights are read once, straight into the matrix instructions' registers.  A block has sixteen columns (GATE:
+// sixteen gates and their ups); its wavefronts take the k's in turn, 128 at a time, and add their sums up in the LDS.
+template <int WAVES, int TILES, bool GATE_>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product p)
+{
+    constexpr int SIDES = GATE_ ? 2 : 1, AHEAD = TILES == 1 ? 4 : 2; // steps on their way at a time
+    __shared__ __attribute__((aligned(16))) int sums[WAVES][SIDES * TILES][16 * 16];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const uint32_t c0 = blockIdx.x * 16, whole = (p.n_in + 15) / 16 * 16;
+    const bool column = c0 + r < p.to.n_out;
+    const int8_t *w = p.w + (uint64_t)(column ? c0 + r : 0) * p.ld_w, *w_up = w + (GATE_ ? (uint64_t)p.to.n_out * p.ld_w : 0);
+    const i32x4 none = {0, 0, 0, 0};
+    i32x4 sum[SIDES][TILES];
+#pragma unroll
+    for (int s = 0; s < SIDES; ++s)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) sum[s][t] = none;
+    for (uint32_t k0 = wave * 128; k0 < whole; k0 += WAVES * 128 * AHEAD) {
+        i32x4 a[AHEAD][2][SIDES], b[AHEAD][2][TILES];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t k = k0 + s * WAVES * 128 + h * 64 + g * 16;
+                const bool there = k < whole;
+                a[s][h][0] = there && column ? *reinterpret_cast<const i32x4 *>(w + k) : none;
+                if (GATE_) a[s][h][SIDES - 1] = there && column ? *reinterpret_cast<const i32x4 *>(w_up + k) : none;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+                    b[s][h][t] = there && t * 16 + r < p.n ? *reinterpret_cast<const i32x4 *>(p.x + (uint64_t)(t * 16 + r) * p.ld_x + k) : none;
+            }
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int side = 0; side < SIDES; ++side)
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) sum[side][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[s][h][side], b[s][h][t], sum[side][t], 0, 0, 0);
+    }
+    // a lane's four sums are columns 4 g .. 4 g + 3 of row r
+#pragma unroll
+    for (int side = 0; side < SIDES; ++side)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) *reinterpret_cast<i32x4 *>(&sums[wave][side * TILES + t][r * 16 + 4 * g]) = sum[side][t];
+    __syncthreads();
+    // two threads a row, eight columns each
+    for (uint32_t at = threadIdx.x; at < TILES * 32; at += 64 * WAVES) {
+        const uint32_t m = at / 2, c = at % 2 * 8, t = m / 16;
+        if (m >= p.n || c0 + c >= p.to.n_out) continue;
+        int v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int wv = 0; wv < WAVES; ++wv)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] += sums[wv][t][m % 16 * 16 + c + i];
+                if (GATE_) u[i] += sums[wv][TILES + t][m % 16 * 16 + c + i];
+            }
+        finish<GATE_>(p.to, m, c0 + c, v, u);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+struct Sizes {
+    uint64_t n;
+    uint32_t n_in, n_out;
+    int32_t act;
+    bool gate() const { return act != ECK_ACT_NONE; }
+    uint64_t columns() const { return (uint64_t)n_out * (gate() ? 2 : 1); }
+};
+
+int32_t check_sizes(const Sizes &s)
+{
+    if (s.n == 0 || s.n_in == 0 || s.n_out == 0 || s.act < ECK_ACT_NONE || s.act > ECK_ACT_RELU) return ECK_EINVAL;
+    if (s.n > MAX_ROWS || s.n_in > MOST_IN || s.n_out > MOST_OUT || (s.n + 63) / 64 * ((s.columns() + 63) / 64) > MOST_TILES) return ECK_EUNSUPPORTED;
+    return ECK_OK;
+}
+
+typedef Shapes<1>::Small Small;
+typedef Shapes<1>::Medium Medium;
+typedef Shapes<1>::Large Large;
+
+struct Int8Plan {
+    int shape; // 0, 1, 2: tiles of 64, 128, 256
+    uint32_t shares;
+};
+constexpr uint64_t FEW_ROWS = 64;
+
+Int8Plan plan(const Sizes &s)
+{
+    const auto tiles = [&](uint64_t side) { return (s.n + side - 1) / side * ((s.columns() + side - 1) / side); };
+    if (tiles(256) >= 256) return {2, 1};
+    if (tiles(128) >= 256) return {1, 1};
+    const uint64_t steps = (s.n_in + 127) / 128;
+    uint32_t shares = 1;
+    while (tiles(64) * shares < 256 && steps / (2 * shares) >= 4 && shares < 16) shares *= 2;
+    return {0, shares};
+}
+
+template <class S>
+int32_t launch_tiles(Int8Product p, bool gate, hipStream_t st)
+{
+    const bool shared = p.shares > 1;
+    const uint32_t across = gate && !shared ? S::BN / 2 : S::BN, N = gate && !shared ? p.to.n_out : p.columns;
+    p.tiles_m = (p.n + S::BM - 1) / S::BM;
+    p.tiles_n = (N + across - 1) / across;
+    const auto go = [&](auto kernel) -> int32_t {
+        if (S::LDS > 65536)
+            ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS));
+        hipLaunchKernelGGL(kernel, dim3(p.tiles_m * p.tiles_n * p.shares), dim3(S::THREADS), S::LDS, st, p);
+        ECK_HIP_TRY(hipGetLastError());
+        return ECK_OK;
+    };
+    if (!shared) return gate ? go(tiles_kernel<S, true, false>) : go(tiles_kernel<S, false, false>);
+    if (const int32_t rc = go(tiles_kernel<S, false, true>)) return rc;
+    const uint64_t chunks = (uint64_t)p.n * ((p.to.n_out + 7) / 8), blocks = (chunks + 255) / 256;
+    hipLaunchKernelGGL((gate ? join_kernel<true> : join_kernel<false>), dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+
+template <int WAVES, int TILES>
+int32_t launch_few(const Int8Product &p, bool gate, hipStream_t st)
+{
+    const dim3 grid((p.to.n_out + 15) / 16), block(64 * WAVES);
+    hipLaunchKernelGGL((gate ? few_rows_kernel<WAVES, TILES, true> : few_rows_kernel<WAVES, TILES, false>), grid, block, 0, st, p);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+
+} // namespace
+} // namespace eck
+
+using namespace eck;
+
+extern "C" uint64_t product_int8_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_out, int32_t act)
+{
+    const Sizes s = {n, n_in, n_out, act};
+    if (check_sizes(s) || n <= FEW_ROWS) return 0;
+    const Int8Plan how = plan(s);
+    return how.shares > 1 ? how.shares * n * s.columns() * 4 : 0;
+}
+
+extern "C" int32_t product_int8(const int8_t *x, uint64_t ld_x, const float *x_scale, uint64_t n, uint32_t n_in, uint32_t n_out, const int8_t *w,
+                                uint64_t ld_w, const float *w_scale, int32_t act, int32_t dtype, void *y, uint64_t ld_y, void *ws,
+                                uint64_t ws_bytes, void *stream)
+{
+    const Sizes s = {n, n_in, n_out, act};
+    if (!x || !x_scale || !w || !w_scale || !y || !is_dtype(dtype)) return ECK_EINVAL;
+    const int32_t sizes = check_sizes(s);
+    if (sizes == ECK_EINVAL) return sizes;
+    if (ld_x < n_in || ld_w < n_in || ld_y < n_out) return ECK_ESHAPE;
+    if (sizes) return sizes;
+    if (ld_x > (1u << 22) || ld_w > (1u << 22)) return ECK_EUNSUPPORTED; // offsets within a tile are of 32 bits
+    const uint64_t need = product_int8_workspace_bytes(n, n_in, n_out, act);
+    if (need && (!ws || ws_bytes < need)) return ECK_EWORKSPACE;
+    if (!aligned(x, 16) || !aligned(w, 16) || ld_x % 16 || ld_w % 16 || !aligned(x_scale, 4) || !aligned(w_scale, 4) ||
+        !aligned(y, element_bytes(dtype)) || (need && !aligned(ws, 256)))
+        return ECK_EALIGN;
+    Int8Product p = {x, w, ld_x, ld_w, (uint32_t)n, n_in, 0, 0, 1, (int32_t *)ws, (uint32_t)s.columns(),
+                     {x_scale, w_scale, y, ld_y, n_out, act, dtype == ECK_F32}};
+    const hipStream_t st = as_stream(stream);
+    if (n <= FEW_ROWS) {
+        if (n <= 16) return (n_out + 15) / 16 < 512 ? launch_few<16, 1>(p, s.gate(), st) : launch_few<4, 1>(p, s.gate(), st);
+        if (n <= 32) return launch_few<4, 2>(p, s.gate(), st);
+        return launch_few<4, 4>(p, s.gate(), st);
+    }
+    const Int8Plan how = plan(s);
+    p.shares = how.shares;
+    if (how.shape == 2) return launch_tiles<Large>(p, s.gate(), st);
+    if (how.shape == 1) return launch_tiles<Medium>(p, s.gate(), st);
+    return launch_tiles<Small>(p, s.gate(), st);
+}

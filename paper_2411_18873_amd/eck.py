@@ -23,7 +23,7 @@ MODE_EXHAUSTIVE, MODE_SAMPLE, MODE_MUTATE, MODE_CROSSOVER = 0, 1, 2, 3
 F32, BF16 = 0, 1
 SELECT_THRESHOLD, SELECT_RANK = 0, 1
 ROWS, COLUMNS = 0, 1
-ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_RELU = -1, 0, 1, 2
 STATE_F32, STATE_8BIT = 0, 1
 STATE_BLOCK = 128
 MAX_K = 4096
@@ -40,6 +40,7 @@ EXPORTS = ["eck_version", "eck_space_create", "eck_space_upload", "eck_space_des
            "eck_candidates_dedup", "eck_candidates_dedup_workspace_bytes",
            "layernorm_forward", "layernorm_backward_workspace_bytes", "layernorm_backward", "dropout_apply",
            "gatedffn_forward_workspace_bytes", "gatedffn_forward", "gatedffn_backward_workspace_bytes", "gatedffn_backward",
+           "quantise_rows", "product_int8_workspace_bytes", "product_int8",
            "adamw_step", "gradients_norm_workspace_bytes", "gradients_norm"]
 
 
@@ -134,6 +135,10 @@ def lib():
         L.gatedffn_backward_workspace_bytes.argtypes = [u64, u32, u32, u32, i32]
         L.gatedffn_backward_workspace_bytes.restype = u64
         L.gatedffn_backward.argtypes = [vp, i32, u64, u64, u32, u32, u32, vp, vp, i32, vp, vp, u64, vp, u64, vp, vp, vp, u64, vp]
+        L.quantise_rows.argtypes = [vp, i32, i32, u64, u64, u32, vp, u64, vp, vp]
+        L.product_int8_workspace_bytes.argtypes = [u64, u32, u32, i32]
+        L.product_int8_workspace_bytes.restype = u64
+        L.product_int8.argtypes = [vp, u64, vp, u64, u32, u32, vp, u64, vp, i32, i32, vp, u64, vp, u64, vp]
         L.adamw_step.argtypes = [vp, u32, i32, C.c_double, C.c_double, C.c_double, C.c_double, u32, vp, vp, u64, vp]
         L.gradients_norm_workspace_bytes.argtypes = [vp, u32]
         L.gradients_norm_workspace_bytes.restype = u64
@@ -145,7 +150,7 @@ def lib():
                             "eck_candidates_dedup_workspace_bytes", "treemodel_update_workspace_bytes",
                             "costmodel_update_workspace_bytes", "layernorm_backward_workspace_bytes",
                             "gatedffn_forward_workspace_bytes", "gatedffn_backward_workspace_bytes",
-                            "gradients_norm_workspace_bytes"):
+                            "gradients_norm_workspace_bytes", "product_int8_workspace_bytes"):
                 fn.restype = i32
         _lib = L
     return _lib
@@ -685,7 +690,7 @@ def gatedffn_backward(x, w_gate_up, w_down, pre, dy, dx, dw_gate_up, dw_down, ws
         _stream()))
 
 
-# ------------------------------------------------------------------------------ refits of models of many tensors
+# ------------------------------------------------------------------------------ scoring in 8-bit integers
 
 
 def _here(t, dtype, name):
@@ -694,6 +699,71 @@ def _here(t, dtype, name):
     if t.get_device() != _device():
         raise ValueError("%s must be on the current device" % name)
     return t
+
+
+def _here_rows(t, name, dtype, shape=None):
+    """_rows of a matrix on the current device"""
+    ld = _rows(t, name, dtype, shape)
+    if t.get_device() != _device():
+        raise ValueError("%s must be on the current device" % name)
+    return ld
+
+
+def int8_rows(n, width):
+    """an int8 matrix [n][width] whose rows lie the next multiple of sixteen apart, as quantise_rows writes and product_int8 reads them"""
+    return torch.zeros(n, -(-width // 16) * 16, dtype=torch.int8, device="cuda")[:, :width]
+
+
+def _int8(t, name, width):
+    """the row distance of an int8 matrix of that width: of a single row the next multiple of sixteen.  Its last row has to have all of its
+    sixteens in memory"""
+    ld, whole = _here_rows(t, name, torch.int8), -(-width // 16) * 16
+    n = t.shape[0]
+    if n <= 1:
+        ld = whole
+    if t.shape[1] != width:
+        raise ValueError("%s must have rows of %d" % (name, width))
+    if t.storage_offset() + (n - 1) * ld + whole > t.untyped_storage().nbytes():
+        raise ValueError("%s must have its rows whole sixteens long in memory" % name)
+    return ld
+
+
+def _scales(t, name, n):
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return _here(t, torch.float32, name).data_ptr()
+
+
+def quantise_rows(x, q, scale, order=ROWS):
+    """q [n][width] (int8) and scale [n]: rows of x [n][width] (ROWS), or its first n columns [width][n or more] (COLUMNS), by their largest"""
+    n, width = q.shape
+    dtype = x.dtype if x.dtype in _FEAT_DTYPE else torch.float32
+    if order != COLUMNS:
+        ld_x = _here_rows(x, "x", dtype, q.shape)
+    else:
+        ld_x = _feature_rows(x, n, width, dtype, "x")
+    _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", width),
+                                                _scales(scale, "scale", n), _stream()))
+
+
+def product_int8_workspace_bytes(n, n_in, n_out, act=ACT_NONE):
+    return int(lib().product_int8_workspace_bytes(n, n_in, n_out, act))
+
+
+def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
+    """y [n][n_out] = x w^T times both scales, of int8 matrices [n][n_in] and [n_out][n_in]; with an activation, a(g) u of w [2 n_out][n_in]"""
+    (n, n_in), n_out = x.shape, y.shape[1]
+    if w.shape[0] != (n_out if act == ACT_NONE else 2 * n_out):
+        raise ValueError("w must have %d rows" % (n_out if act == ACT_NONE else 2 * n_out))
+    dtype = y.dtype if y.dtype in _FEAT_DTYPE else torch.float32
+    ld_y = _here_rows(y, "y", dtype, (n, n_out))
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("product_int8", lib().product_int8(
+        x.data_ptr(), _int8(x, "x", n_in), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", n_in),
+        _scales(w_scale, "w_scale", w.shape[0]), act, _FEAT_DTYPE[dtype], y.data_ptr(), ld_y, ws_ptr, ws_bytes, _stream()))
+
+
+# ------------------------------------------------------------------------------ refits of models of many tensors
 
 
 class Parameters:

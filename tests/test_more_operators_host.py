@@ -71,3 +71,39 @@ def test_parameters_are_checked_by_the_binding():
         eck.Parameters([cpu], weight_decay=[0.1, 0.2])
     with pytest.raises(ValueError):
         eck.Parameters([cpu], [cpu], [torch.zeros(4, dtype=torch.uint8)], [torch.zeros(4, dtype=torch.uint8)])
+
+
+def test_quantise_rows_validates_before_launch():
+    vp = C.c_void_p
+
+    def call(x=FAKE, order=0, dtype=1, ld_x=64, n=16, width=64, q=FAKE, ld_q=64, scale=FAKE):
+        of = lambda a: None if a is None else vp(a)  # noqa: E731
+        return eck.lib().quantise_rows(of(x), order, dtype, ld_x, n, width, of(q), ld_q, of(scale), None)
+
+    assert call(x=None) == call(q=None) == call(scale=None) == call(n=0) == call(width=0) == call(order=2) == call(dtype=2) == eck.EINVAL
+    assert call(ld_x=63) == call(ld_q=48) == call(order=1, n=65) == eck.ESHAPE
+    assert call(n=(1 << 31) + 1) == call(width=131072, ld_x=1 << 18, ld_q=1 << 18) == eck.EUNSUPPORTED
+    assert call(x=FAKE + 1) == call(x=FAKE + 2, dtype=0) == call(q=FAKE + 8) == call(ld_q=72) == call(scale=FAKE + 2) == eck.EALIGN
+
+
+def test_product_int8_validates_before_launch():
+    vp = C.c_void_p
+    W = eck.lib().product_int8_workspace_bytes
+
+    def call(x=FAKE, ld_x=64, xs=FAKE, n=16, n_in=64, n_out=32, w=FAKE, ld_w=64, scale=FAKE, act=-1, dtype=1, y=FAKE, ld_y=32, ws=None, ws_bytes=0):
+        of = lambda a: None if a is None else vp(a)  # noqa: E731
+        return eck.lib().product_int8(of(x), ld_x, of(xs), n, n_in, n_out, of(w), ld_w, of(scale), act, dtype, of(y), ld_y, of(ws), ws_bytes, None)
+
+    assert call(x=None) == call(xs=None) == call(w=None) == call(scale=None) == call(y=None) == eck.EINVAL
+    assert call(n=0) == call(n_in=0) == call(n_out=0) == call(act=-2) == call(act=3) == call(dtype=2) == eck.EINVAL
+    assert call(ld_x=48) == call(ld_w=48) == call(ld_y=31) == eck.ESHAPE
+    assert call(n=(1 << 31) + 1) == call(n_in=131072, ld_x=1 << 18, ld_w=1 << 18) == call(n_out=(1 << 20) + 1, ld_y=1 << 21) == eck.EUNSUPPORTED
+    assert call(n=1 << 24, n_out=2048, ld_y=2048) == call(ld_x=1 << 23) == call(ld_w=1 << 23) == eck.EUNSUPPORTED
+    assert call(x=FAKE + 8) == call(w=FAKE + 4) == call(ld_x=72) == call(ld_w=72) == eck.EALIGN
+    assert call(xs=FAKE + 1) == call(scale=FAKE + 2) == call(y=FAKE + 1) == call(y=FAKE + 2, dtype=0) == eck.EALIGN
+    assert W(0, 64, 64, -1) == W(16, 0, 64, -1) == W(16, 64, 0, -1) == W(16, 64, 64, 3) == W(1, 4096, 4096, 0) == 0
+    need = W(100, 8192, 130, -1)
+    assert need >= 100 * 130 * 4 * 2
+    big = dict(n=100, n_in=8192, n_out=130, ld_x=8192, ld_w=8192, ld_y=130)
+    assert call(**big) == call(ws=FAKE, ws_bytes=need - 1, **big) == eck.EWORKSPACE
+    assert call(ws=FAKE + 16, ws_bytes=need, **big) == eck.EALIGN
