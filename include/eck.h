@@ -359,6 +359,35 @@ int32_t topk_select_static(const float *energy, const float *latency, const uint
                            uint32_t n_segments, uint32_t k, int32_t mode, float alpha, uint32_t m_latency,
                            uint32_t *idx_out, float *energy_out, uint32_t *count_out, void *stream);
 
+/* Selection by drawing: parents of the next generation in proportion to what
+ * the model thinks of them, so that a generation keeps its variety (Alg. 1's
+ * reproduction step does not say how parents are drawn).  In each of n_segments
+ * equal consecutive segments candidate i has the weight
+ *   w_i = exp(-(energy_i - least) / temperature),  least: the segment's least
+ * energy.  Only legal candidates of finite energy are drawn.  In order of
+ * energy, equal ones (-0 = +0) by index, the kept ones are a prefix:
+ *   the k least (k = 0: all);  of these the fewest that have the share top_p of
+ *   their weight (1: all);  of these the ones with w >= min_p (0: all).
+ * temperature 0 keeps the least alone.  Draw d of a segment, with the number
+ * u = uniform[segment][d] from [0, 1), takes the first kept candidate, by index,
+ * at which the running sum of weights passes u times the sum of all kept ones;
+ * past the end (u >= 1) the last one of a weight above 0.  Draws are with
+ * replacement; the numbers are the caller's.  Weights and sums are fp64.
+ *   uniform: device float [n_segments][draws]; idx_out: device uint32
+ *   [n_segments][draws], index within the segment, 0xFFFFFFFF where a segment has
+ *   nothing to draw from; logprob_out: device float [n_segments][draws] or NULL,
+ *   log(w / sum of the kept weights), -inf there; count_out: device uint32
+ *   [n_segments] or NULL, how many are kept.  legal: device uint8 [n] or NULL.
+ *   ws: 256-byte aligned, what the query says (0: may be NULL).
+ * The result does not depend on the order of execution.
+ * Errors: EINVAL (nulls, a zero size, temperature negative or not finite, top_p
+ * outside (0, 1], min_p outside [0, 1]), ESHAPE (n % n_segments), EUNSUPPORTED
+ * (a segment longer than 2^31), EWORKSPACE, EALIGN. */
+uint64_t sample_select_workspace_bytes(uint64_t n, uint32_t n_segments, uint32_t draws);
+int32_t sample_select(const float *energy, const uint8_t *legal, uint64_t n, uint32_t n_segments, const float *uniform,
+                      uint32_t draws, float temperature, uint32_t k, float top_p, float min_p, uint32_t *idx_out,
+                      float *logprob_out, uint32_t *count_out, void *ws, uint64_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------ update */
 
 uint64_t costmodel_update_workspace_bytes(const eck_model *model, uint64_t n_pairs, int32_t minibatch);

@@ -40,6 +40,7 @@ EXPORTS = ["eck_version", "eck_space_create", "eck_space_upload", "eck_space_des
            "eck_candidates_dedup", "eck_candidates_dedup_workspace_bytes",
            "layernorm_forward", "layernorm_backward_workspace_bytes", "layernorm_backward", "dropout_apply",
            "gatedffn_forward_workspace_bytes", "gatedffn_forward", "gatedffn_backward_workspace_bytes", "gatedffn_backward",
+           "sample_select_workspace_bytes", "sample_select",
            "quantise_rows", "product_int8_workspace_bytes", "product_int8",
            "adamw_step", "gradients_norm_workspace_bytes", "gradients_norm"]
 
@@ -135,6 +136,9 @@ def lib():
         L.gatedffn_backward_workspace_bytes.argtypes = [u64, u32, u32, u32, i32]
         L.gatedffn_backward_workspace_bytes.restype = u64
         L.gatedffn_backward.argtypes = [vp, i32, u64, u64, u32, u32, u32, vp, vp, i32, vp, vp, u64, vp, u64, vp, vp, vp, u64, vp]
+        L.sample_select_workspace_bytes.argtypes = [u64, u32, u32]
+        L.sample_select_workspace_bytes.restype = u64
+        L.sample_select.argtypes = [vp, vp, u64, u32, vp, u32, f32, u32, f32, f32, vp, vp, vp, vp, u64, vp]
         L.quantise_rows.argtypes = [vp, i32, i32, u64, u64, u32, vp, u64, vp, vp]
         L.product_int8_workspace_bytes.argtypes = [u64, u32, u32, i32]
         L.product_int8_workspace_bytes.restype = u64
@@ -150,7 +154,8 @@ def lib():
                             "eck_candidates_dedup_workspace_bytes", "treemodel_update_workspace_bytes",
                             "costmodel_update_workspace_bytes", "layernorm_backward_workspace_bytes",
                             "gatedffn_forward_workspace_bytes", "gatedffn_backward_workspace_bytes",
-                            "gradients_norm_workspace_bytes", "product_int8_workspace_bytes"):
+                            "gradients_norm_workspace_bytes", "product_int8_workspace_bytes",
+                            "sample_select_workspace_bytes"):
                 fn.restype = i32
         _lib = L
     return _lib
@@ -843,3 +848,31 @@ def gradients_norm(parameters, norm_out, scale_out, ws, max_norm=float("inf")):
     ws_ptr, ws_bytes = _ws(ws)
     _check("gradients_norm", lib().gradients_norm(parameters._array, parameters.count, max_norm, _one(norm_out, torch.float32, "norm_out"),
                                                   _one(scale_out, torch.float32, "scale_out"), ws_ptr, ws_bytes, _stream()))
+
+
+# ------------------------------------------------------------------------------ selection by drawing
+
+
+def sample_select_workspace_bytes(n, n_segments, draws):
+    return int(lib().sample_select_workspace_bytes(n, n_segments, draws))
+
+
+def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, count_out, ws, temperature=1.0, k=0, top_p=1.0, min_p=0.0):
+    """idx_out [n_segments][draws] = candidates drawn by exp(-energy / temperature) with the numbers uniform [n_segments][draws], of the k least
+    (0: all) that have the share top_p of the weight and min_p of the best one's or more; logprob_out (as idx_out) and count_out may be None"""
+    if uniform.dim() != 2 or uniform.shape[0] != n_segments:
+        raise ValueError("uniform must be of shape (%d, draws)" % n_segments)
+    _here(energy, torch.float32, "energy")
+    _here(uniform, torch.float32, "uniform")
+    draws = uniform.shape[1]
+    for t, name, n, size in ((legal, "legal", energy.numel(), 1), (idx_out, "idx_out", n_segments * draws, 4),
+                             (logprob_out, "logprob_out", n_segments * draws, 4), (count_out, "count_out", n_segments, 4)):
+        if t is None and name != "idx_out":
+            continue
+        if t.numel() != n or t.element_size() != size:
+            raise ValueError("%s must have %d elements of %d bytes" % (name, n, size))
+        _here(t, torch.float32 if name == "logprob_out" else t.dtype, name)
+    ws_ptr, ws_bytes = _ws(ws)
+    _check("sample_select", lib().sample_select(
+        energy.data_ptr(), _ptr(legal), energy.numel(), n_segments, uniform.data_ptr(), draws, temperature, k, top_p, min_p, idx_out.data_ptr(),
+        _ptr(logprob_out), _ptr(count_out), ws_ptr, ws_bytes, _stream()))

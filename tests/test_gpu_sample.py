@@ -1,0 +1,206 @@
+"""GPU: selection by drawing against its definition in 64 bits.  Which candidates are kept and drawn has to be as defined; where a border lies
+within 1e-12 of the sum of weights (sums of up to 2^22 numbers in another order) either side of it is right."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_18873_amd import eck
+
+pytestmark = pytest.mark.gpu
+
+NEAR = 1e-12
+NOBODY = 0xFFFFFFFF
+
+
+def sample(energy, legal, uniform, **how):
+    """all of it through the library, numpy to numpy, with marks around the results"""
+    seg, draws = uniform.shape
+    n = energy.size
+    put = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    idx = torch.full((seg + 2, draws), -77, dtype=torch.int32, device="cuda")
+    logprob, count = torch.full((seg + 2, draws), -77.0, device="cuda"), torch.full((seg + 2,), -77, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(1, eck.sample_select_workspace_bytes(n, seg, draws)),), 0x5A, dtype=torch.uint8, device="cuda")
+    eck.sample_select(put(energy.reshape(-1)), None if legal is None else put(legal.reshape(-1)), seg, put(uniform), idx[1:-1], logprob[1:-1],
+                      count[1:-1], ws, **how)
+    torch.cuda.synchronize()
+    for t in (idx, logprob, count):
+        assert (t[[0, -1]] == -77).all()
+    return idx[1:-1].cpu().numpy().view(np.uint32), logprob[1:-1].cpu().numpy(), count[1:-1].cpu().numpy()
+
+
+def check_segment(e, legal, u, got, temperature=1.0, k=0, top_p=1.0, min_p=0.0):
+    idx, logprob, count = got
+    f32 = lambda x: float(np.float32(x))  # noqa: E731
+    fit = np.isfinite(e) & (np.ones(e.size, bool) if legal is None else legal != 0)
+    at = np.flatnonzero(fit)
+    if at.size == 0:
+        assert (idx == NOBODY).all() and (logprob == -np.inf).all() and count == 0
+        return
+    at = at[np.argsort(e[at] + np.float32(0), kind="stable")]
+    sure = True
+    if temperature == 0:
+        at, w = at[:1], np.ones(1)
+    else:
+        x = e[at].astype(np.float64)
+        w = np.exp(-(x - x[0]) / f32(temperature))
+        if k:
+            at, w = at[:k], w[:k]
+        if top_p < 1:
+            to = np.cumsum(w)
+            target = f32(top_p) * math.fsum(w)
+            keep = int((to < target).sum()) + 1
+            sure = np.abs(to - target).min() > NEAR * to[-1]
+            if not sure and count != keep:  # either side of a border
+                assert abs(int(count) - keep) <= 2
+                keep = int(count)
+            at, w = at[:keep], w[:keep]
+        if min_p > 0:
+            stay = w >= f32(min_p)
+            if np.abs(w - f32(min_p)).min() <= NEAR * f32(min_p):
+                stay[:] = np.arange(w.size) < count
+            at, w = at[stay], w[stay]
+    assert count == at.size
+    order = np.argsort(at)
+    at, w = at[order], w[order]
+    to = np.cumsum(w)
+    total = to[-1]
+    assert (np.isin(idx, at)).all()
+    place = np.searchsorted(at, idx)
+    assert (w[place] > 0).all()
+    target = np.maximum(u.astype(np.float64), 0) * total
+    inside = target < total * (1 - NEAR)
+    assert (to[place] >= target - NEAR * total)[inside].all() and ((to - w)[place] <= target + NEAR * total).all()
+    assert (place[~inside & (u >= 1)] == np.flatnonzero(w > 0)[-1]).all()
+    want = np.log(w[place] / total)
+    assert np.abs(logprob - want).max() <= 2.0 ** -24 * max(1e-9, np.abs(want).max()) + 1e-11
+
+
+def check(energy, legal, uniform, **how):
+    got = sample(energy, legal, uniform, **how)
+    for s in range(uniform.shape[0]):
+        check_segment(energy[s], None if legal is None else legal[s], uniform[s], [g[s] for g in got], **how)
+    again = sample(energy, legal, uniform, **how)
+    assert all(np.array_equal(a, b) for a, b in zip(got, again))
+
+
+def inputs(seg, n, draws, seed, steps=0, legal=0.7):
+    g = np.random.default_rng(seed)
+    e = (0.2 + 0.6 * g.random((seg, 1)) + 0.15 * g.standard_normal((seg, n))).astype(np.float32)
+    if steps:
+        e = (np.round(e * steps) / steps).astype(np.float32)
+    flags = None if legal is None else (g.random((seg, n)) < legal).astype(np.uint8) * g.integers(1, 255, (seg, n)).astype(np.uint8)
+    return e, flags, g.random((seg, draws)).astype(np.float32)
+
+
+HOW = [dict(temperature=0.05), dict(temperature=0.05, k=7), dict(temperature=0.3, top_p=0.9), dict(temperature=0.1, min_p=0.05),
+       dict(temperature=0.05, k=300, top_p=0.8, min_p=0.02), dict(temperature=0.0), dict(temperature=1e-3, top_p=0.5), dict(temperature=100.0, top_p=0.99)]
+
+
+@pytest.mark.parametrize("how", HOW, ids=str)
+@pytest.mark.parametrize("seg,n,draws", [(1, 1, 3), (3, 2, 5), (7, 5, 1), (64, 63, 4), (5, 64, 70), (5, 65, 9), (3, 1000, 33), (2, 4096, 100), (2, 4097, 64),
+                                         (2, 16384, 30), (3, 16385, 30), (2, 70001, 40), (1, 300000, 50)])
+def test_draws(seg, n, draws, how):
+    check(*inputs(seg, n, draws, seg * n + draws), **how)
+
+
+@pytest.mark.parametrize("steps", [4, 64, 4096])
+@pytest.mark.parametrize("seg,n", [(4, 500), (3, 6000), (2, 40000), (1, 400000)])
+@pytest.mark.parametrize("how", [dict(k=33), dict(k=1), dict(k=450, top_p=0.5), dict(top_p=0.37), dict(top_p=0.9, min_p=0.2)], ids=str)
+def test_equal_energies(seg, n, steps, how):
+    check(*inputs(seg, n, 40, steps + n, steps=steps), temperature=0.07, **how)
+
+
+@pytest.mark.parametrize("n", [9, 5000, 20000, 500000])
+def test_all_energies_equal(n):
+    """weights of one: every border is a whole number, and sums are exact"""
+    e, u = np.full((2, n), 0.25, np.float32), np.random.default_rng(n).random((2, 60)).astype(np.float32)
+    e[1] = -0.0
+    e[1, ::3] = 0.0
+    for how, kept in ((dict(), n), (dict(k=5), min(5, n)), (dict(top_p=0.5), -(-n // 2)), (dict(k=n - 1, top_p=0.25), -(-(n - 1) // 4)), (dict(min_p=1.0), n)):
+        idx, logprob, count = sample(e, None, u, temperature=0.5, **how)
+        assert (count == kept).all()
+        assert np.array_equal(idx, np.floor(u.astype(np.float64) * kept).astype(np.uint32))
+        assert np.abs(logprob + math.log(kept)).max() <= 2.0 ** -23 * max(1.0, math.log(kept))
+
+
+def test_uniform_numbers_at_and_past_the_ends():
+    u = np.array([[0.0, 1.0, 1.5, -1.0, 0.99999994, np.inf]], np.float32)
+    for n in (10, 5000, 50000):
+        e, flags, _ = inputs(1, n, 1, n)
+        e[0, :3], e[0, -4:] = 80.0, 80.0  # of weight 0 at this temperature, though kept
+        flags[:] = 1
+        flags[0, 3], flags[0, -5] = 1, 1
+        e[0, 3] = e[0, -5] = e.min()
+        idx, logprob, count = sample(e, flags, u, temperature=0.05)
+        assert idx[0, 0] == idx[0, 3] == 3 and (idx[0, [1, 2, 5]] == n - 5).all() and count[0] == n
+        assert np.isfinite(logprob).all()
+
+
+@pytest.mark.parametrize("n", [12, 3000, 9000, 60000])
+def test_what_is_not_finite_or_legal_is_never_drawn(n):
+    e, flags, u = inputs(6, n, 50, n)
+    e[0] = np.nan
+    flags[1] = 0
+    e[2, ::2] = -np.inf
+    e[3, ::2], e[3, 1::2] = np.inf, -np.inf
+    e[4, 1:], flags[4, 0] = np.nan, 1
+    e[5, 5], e[5, 6], e[5, 7] = -3e38, 3e38, 1e-42
+    flags[5, 5:8] = 1
+    for how in (dict(temperature=0.1), dict(temperature=0.1, k=3), dict(temperature=0.1, top_p=0.9, min_p=0.01), dict(temperature=1e38, top_p=0.7)):
+        check(e, flags, u, **how)
+    idx, _, count = sample(e, flags, u, temperature=0.1, k=4, top_p=0.5)
+    assert (idx[[0, 1, 3]] == NOBODY).all() and (count[[0, 1, 3]] == 0).all() and (idx[4] == 0).all() and (idx[5] == 5).all()
+
+
+def test_results_that_are_not_wanted_may_be_left_out():
+    e, flags, u = inputs(3, 700, 20, 1)
+    put = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    want, _, _ = sample(e, flags, u, temperature=0.1, top_p=0.9)
+    idx = torch.zeros(3, 20, dtype=torch.int32, device="cuda")
+    eck.sample_select(put(e), put(flags), 3, put(u), idx, None, None, None, temperature=0.1, top_p=0.9)
+    assert np.array_equal(idx.cpu().numpy().view(np.uint32), want)
+
+
+@pytest.mark.parametrize("seg,n", [(1, 2 ** 22 + 5), (4, 2 ** 20), (600, 3001), (64, 2 ** 14 + 1)])
+def test_long_and_many_segments(seg, n):
+    e, flags, u = inputs(seg, n, 64, n, legal=0.9)
+    check(e, flags, u, temperature=0.05, k=4096, top_p=0.95, min_p=0.01)
+    check(e, flags, u, temperature=0.2, top_p=0.9)
+
+
+def test_draws_come_as_often_as_their_weights():
+    """40 000 draws over 16 candidates: counts within six standard deviations"""
+    e = np.linspace(0.0, 1.5, 16, dtype=np.float32)[None]
+    u = np.random.default_rng(3).random((1, 40000)).astype(np.float32)
+    idx, logprob, _ = sample(e, None, u, temperature=0.5)
+    p = np.exp(-e[0].astype(np.float64) / 0.5)
+    p /= p.sum()
+    assert (np.abs(np.bincount(idx[0], minlength=16) - 40000 * p) <= 6 * np.sqrt(40000 * p * (1 - p))).all()
+    assert np.abs(np.exp(logprob[0].astype(np.float64)) - p[idx[0]]).max() <= 1e-6
+
+
+@pytest.mark.parametrize("seg,n,how", [(8, 3000, dict(k=100, top_p=0.9)), (2, 300000, dict(k=100, top_p=0.9)), (2, 300000, dict(top_p=0.9, min_p=0.001))])
+def test_as_a_graph(seg, n, how):
+    """two graphs that share a workspace, replayed in turn with the program's own work between"""
+    sides = []
+    ws = torch.empty(max(1, eck.sample_select_workspace_bytes(seg * n, seg, 30)), dtype=torch.uint8, device="cuda")
+    for s in range(2):
+        e, flags, u = (torch.from_numpy(a).cuda() for a in inputs(seg, n, 30, s))
+        out = [(torch.zeros(seg, 30, dtype=torch.int32, device="cuda"), torch.zeros(seg, 30, device="cuda"),
+                torch.zeros(seg, dtype=torch.int32, device="cuda")) for _ in range(2)]
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            eck.sample_select(e, flags, seg, u, *out[0], ws, temperature=0.1, **how)
+        sides.append((e, flags, u, out, graph))
+    for step in range(4):
+        for e, flags, u, out, graph in sides:
+            e.mul_(0.9).add_(0.01 * step)
+            u.copy_(torch.rand(u.shape, generator=torch.Generator().manual_seed(step)))
+            graph.replay()
+            torch.cuda.synchronize()
+            eck.sample_select(e, flags, seg, u, *out[1], ws, temperature=0.1, **how)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(*out))

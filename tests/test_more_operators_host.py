@@ -107,3 +107,23 @@ def test_product_int8_validates_before_launch():
     big = dict(n=100, n_in=8192, n_out=130, ld_x=8192, ld_w=8192, ld_y=130)
     assert call(**big) == call(ws=FAKE, ws_bytes=need - 1, **big) == eck.EWORKSPACE
     assert call(ws=FAKE + 16, ws_bytes=need, **big) == eck.EALIGN
+
+
+def test_sample_select_validates_before_launch():
+    vp = C.c_void_p
+    W = eck.lib().sample_select_workspace_bytes
+
+    def call(energy=FAKE, legal=None, n=1 << 12, seg=4, uniform=FAKE, draws=8, t=0.5, k=0, top_p=0.9, min_p=0.1, idx=FAKE, logprob=FAKE, count=FAKE,
+             ws=FAKE, ws_bytes=1 << 40):
+        of = lambda a: None if a is None else vp(a)  # noqa: E731
+        return eck.lib().sample_select(of(energy), of(legal), n, seg, of(uniform), draws, t, k, top_p, min_p, of(idx), of(logprob), of(count), of(ws),
+                                       ws_bytes, None)
+
+    nan, inf = float("nan"), float("inf")
+    assert call(energy=None) == call(uniform=None) == call(idx=None) == call(n=0) == call(seg=0) == call(draws=0) == eck.EINVAL
+    assert call(t=-0.1) == call(t=nan) == call(t=inf) == call(top_p=0.0) == call(top_p=1.01) == call(top_p=nan) == eck.EINVAL
+    assert call(min_p=-0.1) == call(min_p=1.01) == call(min_p=nan) == eck.EINVAL
+    assert call(seg=3) == eck.ESHAPE
+    assert call(n=(1 << 31) + 1, seg=1) == eck.EUNSUPPORTED
+    assert call(energy=FAKE + 2) == call(uniform=FAKE + 1) == call(idx=FAKE + 2) == call(logprob=FAKE + 2) == call(count=FAKE + 1) == eck.EALIGN
+    assert W(0, 1, 1) == W(10, 3, 1) == W(10, 0, 1) == W(10, 1, 0) == 0
