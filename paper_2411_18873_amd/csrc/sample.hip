@@ -4,18 +4,22 @@
 // least, of these the fewest that have the share top_p of their weight, of these the ones of weight min_p and more.  A draw u takes the
 // first kept candidate, by index, at which the sum of weights passes u times all of it.
 //
-// Nothing is sorted.  The end of a prefix is found in a histogram of the energies' order keys over the range in question, count and weight
-// of every bin, then again within the bin where the end lies, down to a single key: eleven bits at a time, three times at most.  Weights
-// are 64-bit floating point, and in histograms whole multiples of 2^-60, held as two numbers of thirty bits, whose sums do not depend on
-// the order in which the atomics come.  Of equal energies that the prefix ends among, the index of the last is found by counting.
+// Nothing is sorted but a few.  The end of a prefix is looked for in a histogram of the energies' order keys over the range in question,
+// count and weight of every bin, then in the bin where it lies, until that holds so few candidates that they can be put in order, or equal
+// ones alone, which are counted by index.  (Keys are close to logarithms of energies, so a range over both signs, or one outlier, leaves
+// most candidates in a few bins: a second histogram is what that costs.)  Weights are 64-bit floating point, and in histograms whole
+// multiples of 2^-60, held as two numbers of thirty bits, whose sums do not depend on the order in which the atomics come.
+//
+// Segments of up to 16 384 candidates: a block each, keys in registers, one launch.  Longer ones: blocks by the piece, a launch for each
+// time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws).
 #include "activations.h"
 
 namespace eck {
 namespace {
 
-constexpr uint32_t BINS = 2048, BIN_BITS = 11, STRIPS = 1024, NO_KEY = 0xFFFFFFFFu;
+constexpr uint32_t BINS = 2048, BIN_BITS = 11, NO_KEY = 0xFFFFFFFFu, NOBODY = 0xFFFFFFFFu;
 constexpr uint64_t MOST_CANDIDATES = 1ull << 31;
-constexpr uint32_t NOBODY = 0xFFFFFFFFu;
+constexpr uint32_t MOST_SEGMENTS = 1u << 20;
 
 struct Draws {
     const float *energy;
@@ -80,6 +84,7 @@ __device__ __forceinline__ V block_prefix(V v, V *of_waves)
         const V other = __shfl_up(v, stride);
         if ((int)lane >= stride) v += other;
     }
+    if (THREADS == 64) return v;
     __syncthreads(); // (of_waves may still be read from the last time)
     if (lane == 63) of_waves[wave] = v;
     __syncthreads();
@@ -88,100 +93,162 @@ __device__ __forceinline__ V block_prefix(V v, V *of_waves)
     return before + v;
 }
 
+typedef unsigned long long u64;
+
 struct Histogram {
+    u64 high[BINS], low[BINS];
     uint32_t count[BINS];
-    unsigned long long high[BINS], low[BINS];
 };
 
-// where a prefix ends: with `kept` of the candidates of this key, of which there are `all`
-struct End {
-    uint32_t key, kept, all;
-};
-
-struct Search {
-    uint32_t lo, hi;     // keys in question
-    uint32_t shift;
-    uint32_t before;     // candidates below lo, and their weight
+// Keys lo .. hi, `number` candidates of them; how many are below, and their weight
+struct Range {
+    uint32_t lo, hi, number, before;
     Mass mass;
 };
-__device__ __forceinline__ uint32_t shift_for(uint32_t lo, uint32_t hi)
+__device__ __forceinline__ uint32_t shift_of(const Range &r)
 {
-    const int bits = 32 - __builtin_clz((hi - lo) | 1);
+    const int bits = 32 - __builtin_clz((r.hi - r.lo) | 1);
     return bits > (int)BIN_BITS ? bits - BIN_BITS : 0;
 }
 
-template <int THREADS>
-struct Shared {
-    Histogram bins;
+// what a prefix ends with: a key, and of the candidates of that key the index of the last
+struct Cut {
+    uint32_t key, index;
+};
+__device__ __forceinline__ bool within(uint32_t key, uint32_t index, const Cut &cut) { return key < cut.key || (key == cut.key && index <= cut.index); }
+
+template <int THREADS, int LIST_>
+struct Scratch { // of a block that looks for ends
+    static constexpr int LIST = LIST_;
+    u64 list[LIST], sorted[LIST];
+    u64 wide[2][THREADS / 64];
     uint32_t small[THREADS / 64];
-    unsigned long long wide[2][THREADS / 64];
-    double real[THREADS / 64];
-    Search found;
-    uint32_t number, least, most;
-    double sums[STRIPS], sums_to[STRIPS]; // of strips, and up to and including each
-    uint32_t counts[STRIPS];
+    Range found[2];
+    Cut cut;
+    Mass total;
+    uint32_t listed;
+};
+
+// which prefix: the `need` least candidates, or the fewest of a weight of `target` (from and up to, while that is not known)
+struct Goal {
+    bool by_weight;
+    uint32_t need;
+    double target[2];
+    __device__ __forceinline__ bool reached(int which, uint32_t count, const Mass &mass) const
+    {
+        return by_weight ? mass.value() >= target[which] : count >= need;
+    }
 };
 
 template <int THREADS>
-__device__ __forceinline__ void clear_bins(Shared<THREADS> &s, bool weights)
+__device__ __forceinline__ void clear_bins(Histogram &bins)
 {
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < BINS; b += THREADS) {
-        s.bins.count[b] = 0;
-        if (weights) s.bins.high[b] = s.bins.low[b] = 0;
+        bins.count[b] = 0;
+        bins.high[b] = bins.low[b] = 0;
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ void add_to_bins(Histogram &bins, uint32_t bin, const double *weight)
+__device__ __forceinline__ void add_to_bins(Histogram &bins, uint32_t bin, bool weights, double w)
 {
     atomicAdd(&bins.count[bin], 1u);
-    if (weight) {
-        const Mass m = mass_of(*weight);
-        atomicAdd(&bins.high[bin], (unsigned long long)m.high);
-        atomicAdd(&bins.low[bin], (unsigned long long)m.low);
+    if (weights) {
+        const Mass m = mass_of(w);
+        atomicAdd(&bins.high[bin], (u64)m.high);
+        atomicAdd(&bins.low[bin], (u64)m.low);
     }
 }
 
-// The bin where the prefix of `need` candidates (or, by weight, of `target`) ends, and the search within it.  `weights`: whether the bins
-// hold weights
-template <int THREADS>
-__device__ __forceinline__ void narrow(Shared<THREADS> &s, Search &at, bool by_weight, uint32_t need, double target, bool weights)
+// The bins of `at` in which the prefix ends, or may end: s.found[0] from the first of them to the last.  All threads get the result.
+template <int THREADS, class S>
+__device__ __forceinline__ Range narrow(S &s, const Histogram &bins, const Range &at, const Goal &goal)
 {
     constexpr uint32_t EACH = BINS / THREADS;
+    const uint32_t first = threadIdx.x * EACH, shift = shift_of(at);
     uint32_t count = 0;
     Mass mass = {0, 0};
+#pragma unroll
     for (uint32_t i = 0; i < EACH; ++i) {
-        const uint32_t b = threadIdx.x * EACH + i;
-        count += s.bins.count[b];
-        if (weights) mass = mass + Mass{s.bins.high[b], s.bins.low[b]};
+        count += bins.count[first + i];
+        mass = mass + Mass{bins.high[first + i], bins.low[first + i]};
     }
-    const uint32_t count_to = block_prefix<THREADS>(count, s.small);
-    Mass mass_to = {0, 0};
-    if (weights) mass_to = {block_prefix<THREADS>((unsigned long long)mass.high, s.wide[0]), block_prefix<THREADS>((unsigned long long)mass.low, s.wide[1])};
-    // up to the last bin, whatever roundings say
-    uint32_t before = at.before + count_to - count;
-    Mass mass_before = {at.mass.high + mass_to.high - mass.high, at.mass.low + mass_to.low - mass.low};
-    const auto reached = [&](uint32_t c, const Mass &m) { return by_weight ? m.value() >= target : c >= need; };
-    const bool mine = !reached(before, mass_before) && reached(before + count, mass_before + mass);
-    __syncthreads();
-    if (mine || (threadIdx.x == 0 && reached(before, mass_before))) {
-        uint32_t b = threadIdx.x * EACH;
-        for (; b < threadIdx.x * EACH + EACH - 1; ++b) {
-            const uint32_t c = s.bins.count[b];
-            const Mass m = weights ? Mass{s.bins.high[b], s.bins.low[b]} : Mass{0, 0};
-            if (reached(before + c, mass_before + m)) break;
-            before += c;
-            mass_before = mass_before + m;
+    const uint32_t to = at.before + block_prefix<THREADS>(count, s.small);
+    const Mass mass_to = at.mass + Mass{block_prefix<THREADS>((u64)mass.high, s.wide[0]), block_prefix<THREADS>((u64)mass.low, s.wide[1])};
+    const uint32_t from = to - count;
+    const Mass mass_from = {mass_to.high - mass.high, mass_to.low - mass.low};
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        // (the last thread's, should none reach it)
+        const bool mine = (threadIdx.x == 0 || !goal.reached(which, from, mass_from)) && (threadIdx.x == THREADS - 1 || goal.reached(which, to, mass_to));
+        if (mine) {
+            uint32_t c = from, b = first;
+            Mass m = mass_from;
+            for (; b < first + EACH - 1; ++b) {
+                const Mass next = m + Mass{bins.high[b], bins.low[b]};
+                if (goal.reached(which, c + bins.count[b], next)) break;
+                c += bins.count[b];
+                m = next;
+            }
+            const uint32_t lo = at.lo + (b << shift);
+            s.found[which] = {lo, min(at.hi, lo + ((1u << shift) - 1)), bins.count[b], c, m};
         }
-        Search next;
-        next.lo = at.lo + (b << at.shift);
-        next.hi = min(at.hi, next.lo + ((1u << at.shift) - 1));
-        next.before = before;
-        next.mass = mass_before;
-        next.shift = shift_for(next.lo, next.hi);
-        s.found = next;
-        s.number = s.bins.count[b];
+    }
+    __syncthreads();
+    Range r = s.found[0];
+    const Range last = s.found[1];
+    if (last.lo > r.lo) { // (by weight, of which the end is not known yet)
+        r.hi = last.hi;
+        r.number = last.before + last.number - r.before;
+    }
+    __syncthreads();
+    return r;
+}
+
+// s.sorted = the `c` first of s.list, least first (no two are equal)
+template <int THREADS, class S>
+__device__ __forceinline__ void sort_list(S &s, uint32_t c)
+{
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < c; i += THREADS) {
+        const u64 mine = s.list[i];
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (uint32_t j = 0; j < c; ++j) rank += s.list[j] < mine;
+        s.sorted[rank] = mine;
+    }
+    __syncthreads();
+}
+
+// Where the prefix ends among the range's candidates, all of them in s.sorted: s.cut; and the weight up to there: s.total
+template <int THREADS, class S, class W>
+__device__ __forceinline__ void cut_sorted(S &s, const Range &at, const Goal &goal, bool weights, W &&weight)
+{
+    constexpr uint32_t EACH = (S::LIST + THREADS - 1) / THREADS;
+    const uint32_t c = at.number, first = threadIdx.x * EACH;
+    Mass mass[EACH], sum = {0, 0};
+#pragma unroll
+    for (uint32_t i = 0; i < EACH; ++i) {
+        mass[i] = weights && first + i < c ? mass_of(weight((uint32_t)(s.sorted[first + i] >> 32))) : Mass{0, 0};
+        sum = sum + mass[i];
+    }
+    Mass to = at.mass;
+    if (weights) {
+        to = to + Mass{block_prefix<THREADS>((u64)sum.high, s.wide[0]), block_prefix<THREADS>((u64)sum.low, s.wide[1])};
+        to = {to.high - sum.high, to.low - sum.low};
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < EACH; ++i) {
+        if (first + i >= c) break;
+        const Mass next = to + mass[i];
+        const uint32_t count = at.before + first + i;
+        // (the last one, should none reach it)
+        if ((first + i == 0 || !goal.reached(0, count, to)) && (first + i == c - 1 || goal.reached(0, count + 1, next))) {
+            s.cut = {(uint32_t)(s.sorted[first + i] >> 32), (uint32_t)s.sorted[first + i]};
+            s.total = next;
+        }
+        to = next;
     }
     __syncthreads();
 }
@@ -192,285 +259,899 @@ __device__ __forceinline__ uint32_t enough(double before, double w, uint32_t all
     if (!(w > 0.0)) return all;
     double j = ceil((target - before) / w);
     j = fmin(fmax(j, 1.0), (double)all);
-    while (j > 1.0 && before + (j - 1.0) * w >= target) j -= 1.0;
-    while (j < (double)all && before + j * w < target) j += 1.0;
+    if (j > 1.0 && before + (j - 1.0) * w >= target) j -= 1.0;
+    if (j < (double)all && before + j * w < target) j += 1.0;
     return (uint32_t)j;
 }
 
-// A block a segment.  HELD: its keys stay in registers, sixteen a thread
-template <int THREADS, bool HELD>
-__global__ __launch_bounds__(THREADS) void segment_kernel(const Draws a)
+// Of candidates of one key, the number of the last in the prefix (from 1), and the weight up to there: s.total
+template <class S>
+__device__ __forceinline__ uint32_t last_of_equal(S &s, const Range &at, const Goal &goal, double w)
 {
-    __shared__ Shared<THREADS> s;
-    const uint64_t n = a.n;
-    const float *energy = a.energy + blockIdx.x * n;
-    const uint8_t *legal = a.legal ? a.legal + blockIdx.x * n : nullptr;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, waves = THREADS / 64;
-
-    constexpr int HOLD = HELD ? 4 : 1;
-    uint32_t held[HOLD][4];
-    if (HELD)
-#pragma unroll
-        for (int h = 0; h < HOLD; ++h) load_keys(energy, legal, ((uint64_t)h * THREADS + threadIdx.x) * 4, n, held[h]);
-    const auto each = [&](auto &&f) { // of the candidates that may be drawn
-        if (HELD) {
-#pragma unroll
-            for (int h = 0; h < HOLD; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (held[h][i] != NO_KEY) f(held[h][i]);
-        } else {
-            for (uint64_t at = threadIdx.x * 4; at < n; at += THREADS * 4) {
-                uint32_t key[4];
-                load_keys(energy, legal, at, n, key);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (key[i] != NO_KEY) f(key[i]);
-            }
-        }
-    };
-
-    // the range of keys
-    if (threadIdx.x == 0) {
-        s.least = NO_KEY;
-        s.most = 0;
-        s.number = 0;
-    }
+    const uint32_t j = goal.by_weight ? enough(at.mass.value(), w, at.number, goal.target[0]) : min(max(goal.need - at.before, 1u), at.number);
+    const Mass one = mass_of(w);
     __syncthreads();
-    {
-        uint32_t least = NO_KEY, most = 0, number = 0;
-        each([&](uint32_t key) {
-            least = min(least, key);
-            most = max(most, key);
-            ++number;
+    if (threadIdx.x == 0) s.total = at.mass + Mass{j * one.high, j * one.low};
+    __syncthreads();
+    return j;
+}
+
+// The end of a prefix within the range `at`, from the candidates themselves: source.each(f) calls f(key, index) for those that may be drawn,
+// source.nth(key, j) is the index of the j-th one of a key.  Sets s.cut and s.total.
+template <int THREADS, class S, class Source, class W>
+__device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool weights, const Source &source, W &&weight)
+{
+    for (int round = 0; round < 4; ++round) { // (three rounds leave one key)
+        if (at.number <= (uint32_t)S::LIST) {
+            __syncthreads();
+            if (threadIdx.x == 0) s.listed = 0;
+            __syncthreads();
+            source.each([&](uint32_t key, uint32_t index) {
+                if (key < at.lo || key > at.hi) return;
+                const uint32_t place = atomicAdd(&s.listed, 1u);
+                if (place < (uint32_t)S::LIST) s.list[place] = (u64)key << 32 | index;
+            });
+            sort_list<THREADS>(s, at.number);
+            cut_sorted<THREADS>(s, at, goal, weights, weight);
+            return;
+        }
+        if (at.lo == at.hi) {
+            const uint32_t j = last_of_equal(s, at, goal, weight(at.lo)), index = source.nth(at.lo, j);
+            if (threadIdx.x == 0) s.cut = {at.lo, index};
+            __syncthreads();
+            return;
+        }
+        clear_bins<THREADS>(bins);
+        const uint32_t shift = shift_of(at);
+        source.each([&](uint32_t key, uint32_t) {
+            if (key >= at.lo && key <= at.hi) add_to_bins(bins, (key - at.lo) >> shift, weights, weights ? weight(key) : 0.0);
         });
+        __syncthreads();
+        at = narrow<THREADS>(s, bins, at, goal);
+    }
+}
+
+__device__ __forceinline__ void nothing_to_draw(const Draws &a, uint64_t segment, uint32_t first, uint32_t step)
+{
+    for (uint32_t d = first; d < a.draws; d += step) {
+        a.idx[segment * a.draws + d] = NOBODY;
+        if (a.logprob) a.logprob[segment * a.draws + d] = -__builtin_inff();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ short segments
+
+// Keys of a block's candidates, EACH neighbouring ones a thread
+template <int THREADS, int EACH, class S>
+struct Held {
+    uint32_t (&key)[EACH];
+    S &s;
+    template <class F>
+    __device__ __forceinline__ void each(F &&f) const
+    {
 #pragma unroll
-        for (int stride = 1; stride < 64; stride <<= 1) {
-            least = min(least, (uint32_t)__shfl_xor((int)least, stride));
-            most = max(most, (uint32_t)__shfl_xor((int)most, stride));
-            number += (uint32_t)__shfl_xor((int)number, stride);
-        }
-        if (lane == 0) {
-            atomicMin(&s.least, least);
-            atomicMax(&s.most, most);
-            atomicAdd(&s.number, number);
+        for (int i = 0; i < EACH; ++i)
+            if (key[i] != NO_KEY) f(key[i], threadIdx.x * EACH + i);
+    }
+    __device__ uint32_t nth(uint32_t of, uint32_t j) const
+    {
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) mine += key[i] == of;
+        uint32_t before = block_prefix<THREADS>(mine, s.small) - mine;
+        __syncthreads();
+        if (before < j && before + mine >= j)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (key[i] == of && ++before == j) s.listed = threadIdx.x * EACH + i;
+        __syncthreads();
+        return s.listed;
+    }
+};
+
+template <int THREADS, int EACH>
+struct Short {
+    // few candidates are put in order at once, more are binned first
+    static constexpr bool BINNED = THREADS * EACH > 256;
+    typedef Scratch<THREADS, 256> S;
+    struct Ends {
+        S s;
+        Histogram bins[BINNED ? 1 : 0];
+    };
+    union {
+        Ends ends;
+        double to[THREADS * EACH]; // sums of weights up to and including each candidate
+    };
+    double of_waves[THREADS / 64];
+    uint32_t least[THREADS / 64], most[THREADS / 64], number[THREADS / 64];
+};
+
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    typedef Short<THREADS, EACH> Lds;
+    Lds &s = *reinterpret_cast<Lds *>(lds);
+    const uint32_t n = (uint32_t)a.n, lane = threadIdx.x & 63, wave = threadIdx.x / 64, first = threadIdx.x * EACH;
+    const uint64_t segment = blockIdx.x;
+    const float *energy = a.energy + segment * n;
+    const uint8_t *legal = a.legal ? a.legal + segment * n : nullptr;
+    uint32_t key[EACH], least = NO_KEY, most = 0, number = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; i += 4) {
+        uint32_t four[4] = {NO_KEY, NO_KEY, NO_KEY, NO_KEY};
+        if (first + i < n) load_keys(energy, legal, first + i, n, four);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[i + j] = four[j];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        least = min(least, key[i]);
+        most = key[i] != NO_KEY ? max(most, key[i]) : most;
+        number += key[i] != NO_KEY;
+    }
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) {
+        least = min(least, (uint32_t)__shfl_xor((int)least, stride));
+        most = max(most, (uint32_t)__shfl_xor((int)most, stride));
+        number += (uint32_t)__shfl_xor((int)number, stride);
+    }
+    if (THREADS > 64) {
+        if (lane == 0) s.least[wave] = least, s.most[wave] = most, s.number[wave] = number;
+        __syncthreads();
+        number = 0;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            least = min(least, s.least[w]);
+            most = max(most, s.most[w]);
+            number += s.number[w];
         }
     }
-    __syncthreads();
-    const uint32_t number = s.number;
-    const Search whole = {s.least, s.most, shift_for(s.least, s.most), 0, {0, 0}};
-    uint32_t *const idx = a.idx + (uint64_t)blockIdx.x * a.draws;
-    float *const logprob = a.logprob ? a.logprob + (uint64_t)blockIdx.x * a.draws : nullptr;
     if (number == 0) {
-        for (uint32_t d = threadIdx.x; d < a.draws; d += THREADS) {
-            idx[d] = NOBODY;
-            if (logprob) logprob[d] = -__builtin_inff();
-        }
-        if (threadIdx.x == 0 && a.count) a.count[blockIdx.x] = 0;
+        nothing_to_draw(a, segment, threadIdx.x, THREADS);
+        if (threadIdx.x == 0 && a.count) a.count[segment] = 0;
         return;
     }
-    const double least = (double)energy_of(whole.lo);
-
+    const double best = (double)energy_of(least);
+    const auto weight = [&](uint32_t k) { return weight_of(k, best, a.per_temperature); };
     const bool weights = a.top_p < 1.0;
-    End end = {whole.hi, 1, 1};
-    double total = 0.0; // of the k least
-    const auto find = [&](bool by_weight, uint32_t need, double target) { // narrowed down to one key
-        Search at = whole;
-        at.hi = by_weight ? end.key : at.hi;
-        at.shift = shift_for(at.lo, at.hi);
-        for (int round = 0; round < 3; ++round) { // (32 bits, 21, 10)
-            clear_bins(s, weights);
-            each([&](uint32_t key) {
-                if (key < at.lo || key > at.hi) return;
-                const double w = weights ? weight_of(key, least, a.per_temperature) : 0.0;
-                add_to_bins(s.bins, (key - at.lo) >> at.shift, weights ? &w : nullptr);
+
+    Cut cut = {most, n};
+    {
+        typename Lds::S &sc = s.ends.s;
+        Histogram &bins = s.ends.bins[0];
+        const Held<THREADS, EACH, typename Lds::S> held = {key, sc};
+        Range whole = {least, most, number, 0, {0, 0}};
+        Goal goal = {false, a.k, {0.0, 0.0}};
+        bool binned = false; // bins hold the whole range
+        const auto find = [&]() {
+            if (!Lds::BINNED || number <= (uint32_t)Lds::S::LIST) {
+                find_cut<THREADS>(sc, bins, whole, goal, weights, held, weight);
+                return;
+            }
+            if constexpr (Lds::BINNED) {
+                const uint32_t shift = shift_of(whole);
+                if (!binned) {
+                    clear_bins<THREADS>(bins);
+                    held.each([&](uint32_t k, uint32_t) { add_to_bins(bins, (k - whole.lo) >> shift, weights, weights ? weight(k) : 0.0); });
+                    __syncthreads();
+                }
+                const Range at = narrow<THREADS>(sc, bins, whole, goal);
+                binned = at.number <= (uint32_t)Lds::S::LIST || at.lo == at.hi; // else they are overwritten
+                find_cut<THREADS>(sc, bins, at, goal, weights, held, weight);
+            }
+        };
+        double total = 0.0; // of the k least
+        if (a.k && a.k < number) {
+            if (a.k == 1 && !weights) { // the first of the least
+                const uint32_t index = held.nth(least, 1);
+                cut = {least, index};
+            } else {
+                find();
+                cut = sc.cut;
+                total = sc.total.value();
+            }
+        } else if (weights) {
+            u64 high = 0, low = 0;
+            held.each([&](uint32_t k, uint32_t) {
+                const Mass m = mass_of(weight(k));
+                high += m.high;
+                low += m.low;
             });
+            high = block_prefix<THREADS>(high, sc.wide[0]);
+            low = block_prefix<THREADS>(low, sc.wide[1]);
             __syncthreads();
-            narrow(s, at, by_weight, need, target, weights);
-            const uint32_t shift = at.shift;
-            at = s.found;
-            if (shift == 0) break;
+            if (threadIdx.x == THREADS - 1) sc.total = {high, low};
+            __syncthreads();
+            total = sc.total.value();
         }
-        const uint32_t all = s.number;
-        __syncthreads();
-        end.key = at.lo;
-        end.all = all;
-        return at;
-    };
-    bool cut = false;
-    if (a.k && a.k < number) {
-        const Search at = find(false, a.k, 0.0);
-        end.kept = a.k - at.before;
-        cut = true;
         if (weights) {
-            const Mass each_one = mass_of(weight_of(end.key, least, a.per_temperature));
-            total = Mass{at.mass.high + end.kept * each_one.high, at.mass.low + end.kept * each_one.low}.value();
+            goal = {true, 0, {a.top_p * total, a.top_p * total}};
+            find();
+            // (not past the k least, whatever roundings say)
+            const Cut by_weight = sc.cut;
+            if (within(by_weight.key, by_weight.index, cut)) cut = by_weight;
         }
-    } else if (weights) {
-        clear_bins(s, true);
-        unsigned long long high = 0, low = 0;
-        each([&](uint32_t key) {
-            const Mass m = mass_of(weight_of(key, least, a.per_temperature));
-            high += m.high;
-            low += m.low;
-        });
+    }
+    __syncthreads(); // (what is written now lies where that was)
+
+    double w[EACH], sum = 0.0;
+    uint32_t kept = 0;
 #pragma unroll
-        for (int stride = 1; stride < 64; stride <<= 1) {
-            high += __shfl_xor(high, stride);
-            low += __shfl_xor(low, stride);
+    for (int i = 0; i < EACH; ++i) {
+        w[i] = key[i] != NO_KEY && within(key[i], first + i, cut) ? weight(key[i]) : -1.0;
+        const bool stays = w[i] >= a.min_p && w[i] >= 0.0;
+        kept += stays;
+        w[i] = stays ? w[i] : 0.0;
+        sum += w[i];
+    }
+    double to = block_prefix<THREADS>(sum, s.of_waves) - sum;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        to += w[i];
+        if (first + i < n) s.to[first + i] = to;
+    }
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) kept += (uint32_t)__shfl_xor((int)kept, stride);
+    if (lane == 0) s.number[wave] = kept;
+    __syncthreads();
+    if (threadIdx.x == 0 && a.count) {
+        for (int o = 1; o < THREADS / 64; ++o) kept += s.number[o];
+        a.count[segment] = kept;
+    }
+    const double all = s.to[n - 1];
+    const auto kept_weight = [&](uint32_t i) {
+        const uint32_t k = key_of(energy[i], !legal || legal[i]);
+        const double x = k != NO_KEY && within(k, i, cut) ? weight(k) : 0.0;
+        return x >= a.min_p ? x : 0.0;
+    };
+    for (uint32_t d = threadIdx.x; d < a.draws; d += THREADS) {
+        const double target = fmax((double)a.uniform[segment * a.draws + d] * all, 0.0);
+        uint32_t lo = 0, hi = n - 1; // the first sum that passes the target, or the last
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (s.to[mid] > target) hi = mid;
+            else lo = mid + 1;
         }
-        if (lane == 0) {
-            atomicAdd(&s.bins.high[0], high);
-            atomicAdd(&s.bins.low[0], low);
+        // (between two threads' candidates sums may differ in their last bit where nothing is added; and past the end the last one is wanted)
+        double x = kept_weight(lo);
+        while (!(x > 0.0) && lo + 1 < n && s.to[n - 1] > target) x = kept_weight(++lo);
+        while (!(x > 0.0) && lo > 0) x = kept_weight(--lo);
+        a.idx[segment * a.draws + d] = lo;
+        if (a.logprob) a.logprob[segment * a.draws + d] = (float)log(x / all);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ long segments
+
+constexpr int LONG_THREADS = 1024;
+constexpr uint32_t LIST = 4096;       // candidates at the ends that are listed, of a segment
+constexpr uint32_t MOST_PIECES = 512; // blocks of a segment
+typedef Scratch<LONG_THREADS, 1024> LongScratch;
+
+struct Bounds { // of a block's piece
+    uint32_t least, most, number, unused;
+};
+struct Equal { // candidates of a range in a block's piece: their least and largest key, and how many
+    uint32_t least, most, number, unused;
+};
+struct Segment {
+    uint32_t least, most, number, listed;
+    Range by_count, by_weight;
+    double total; // weight of all, where no k least are taken
+    Cut cut;
+};
+struct Long {
+    Draws a;
+    uint64_t segments;
+    uint32_t pieces;     // blocks a segment
+    uint64_t piece;      // candidates of a block: a multiple of 4096
+    uint64_t strip;      // candidates of a strip: a multiple of 64; 64 strips are a chunk
+    uint32_t chunks;     // of a segment
+    Bounds *bounds;      // [segments][pieces]
+    Histogram *parts;    // [2][segments][pieces]
+    Histogram *whole;    // [2][segments], of several pieces; else parts
+    Segment *segment;    // [segments]
+    u64 *list;           // [segments][LIST]
+    Equal *equal;        // [2][segments][pieces]: by count, by weight
+    double *strip_sums;  // [segments][chunks][64]
+    double *chunk_sums;  // [segments][chunks]
+    uint32_t *chunk_counts;
+    __device__ __forceinline__ Histogram *histogram(int which, uint64_t s) const
+    {
+        return pieces > 1 ? whole + which * segments + s : parts + which * segments + s;
+    }
+};
+
+__device__ __forceinline__ bool by_count(const Long &p, uint32_t number) { return p.a.k && p.a.k < number; }
+
+template <class F>
+__device__ __forceinline__ void each_of_piece(const Draws &a, uint64_t segment, uint64_t from, uint64_t to, F &&f)
+{
+    const float *energy = a.energy + segment * a.n;
+    const uint8_t *legal = a.legal ? a.legal + segment * a.n : nullptr;
+    constexpr int AHEAD = 4;
+    for (uint64_t at = from + threadIdx.x * 4; at < to; at += LONG_THREADS * 4 * AHEAD) {
+        uint32_t key[AHEAD][4];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const uint64_t here = at + (uint64_t)k * LONG_THREADS * 4;
+            if (here < to) load_keys(energy, legal, here, to, key[k]);
+            else key[k][0] = key[k][1] = key[k][2] = key[k][3] = NO_KEY;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (key[k][i] != NO_KEY) f(key[k][i], (uint32_t)(at + (uint64_t)k * LONG_THREADS * 4 + i));
+    }
+}
+
+// least and largest key and how many, over a block
+__device__ __forceinline__ Bounds block_bounds(Bounds b, Bounds *of_waves)
+{
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) {
+        b.least = min(b.least, (uint32_t)__shfl_xor((int)b.least, stride));
+        b.most = max(b.most, (uint32_t)__shfl_xor((int)b.most, stride));
+        b.number += (uint32_t)__shfl_xor((int)b.number, stride);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) of_waves[threadIdx.x / 64] = b;
+    __syncthreads();
+    b = of_waves[0];
+    for (int w = 1; w < LONG_THREADS / 64; ++w) {
+        b.least = min(b.least, of_waves[w].least);
+        b.most = max(b.most, of_waves[w].most);
+        b.number += of_waves[w].number;
+    }
+    return b;
+}
+
+__global__ __launch_bounds__(LONG_THREADS) void bounds_kernel(const Long p)
+{
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    Bounds b = {NO_KEY, 0, 0, 0};
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
+        b.least = min(b.least, key);
+        b.most = max(b.most, key);
+        ++b.number;
+    });
+    b = block_bounds(b, of_waves);
+    if (threadIdx.x == 0) p.bounds[blockIdx.x] = b;
+}
+
+// of all pieces of a segment
+__device__ __forceinline__ Bounds segment_bounds(const Long &p, uint64_t segment, Bounds *of_waves)
+{
+    Bounds b = {NO_KEY, 0, 0, 0};
+    if (threadIdx.x < p.pieces) b = p.bounds[segment * p.pieces + threadIdx.x];
+    return block_bounds(b, of_waves);
+}
+
+__device__ __forceinline__ void write_bins(Histogram &to, const Histogram &from)
+{
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) {
+        to.count[b] = from.count[b];
+        to.high[b] = from.high[b];
+        to.low[b] = from.low[b];
+    }
+}
+
+__global__ __launch_bounds__(LONG_THREADS) void first_bins_kernel(const Long p)
+{
+    __shared__ Histogram bins;
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    const Bounds b = segment_bounds(p, segment, of_waves);
+    if (b.number == 0) return;
+    const bool weights = p.a.top_p < 1.0;
+    const double best = (double)energy_of(b.least);
+    const Range whole = {b.least, b.most, b.number, 0, {0, 0}};
+    const uint32_t shift = shift_of(whole);
+    clear_bins<LONG_THREADS>(bins);
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
+        add_to_bins(bins, (key - whole.lo) >> shift, weights, weights ? weight_of(key, best, p.a.per_temperature) : 0.0);
+    });
+    write_bins(p.parts[blockIdx.x], bins);
+}
+
+// histograms of a segment's pieces added up: blocks of 256 bins
+__global__ __launch_bounds__(256) void join_bins_kernel(const Long p, int which)
+{
+    const uint64_t segment = blockIdx.x / (BINS / 256);
+    const uint32_t b = blockIdx.x % (BINS / 256) * 256 + threadIdx.x;
+    const Histogram *from = p.parts + (which * p.segments + segment) * p.pieces;
+    uint32_t count = 0;
+    Mass mass = {0, 0};
+#pragma unroll 8
+    for (uint32_t i = 0; i < p.pieces; ++i) {
+        count += from[i].count[b];
+        mass = mass + Mass{from[i].high[b], from[i].low[b]};
+    }
+    Histogram &to = p.whole[which * p.segments + segment];
+    to.count[b] = count;
+    to.high[b] = mass.high;
+    to.low[b] = mass.low;
+}
+
+__device__ __forceinline__ void read_bins(Histogram &to, const Histogram &from)
+{
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) {
+        to.count[b] = from.count[b];
+        to.high[b] = from.high[b];
+        to.low[b] = from.low[b];
+    }
+    __syncthreads();
+}
+
+// Where the weight's share ends: between those of the least and the largest sum that the k least may have
+__device__ __forceinline__ Goal weight_goal(const Draws &a, bool limited, const Range &by_count, const Mass &of_range, double total)
+{
+    const double from = limited ? by_count.mass.value() : total, to = limited ? (by_count.mass + of_range).value() : total;
+    return {true, 0, {a.top_p * from, a.top_p * to}};
+}
+
+// weight of the bin that narrow() found within `at`
+__device__ __forceinline__ Mass mass_in(const Histogram &bins, const Range &at, const Range &found)
+{
+    const uint32_t b = (found.lo - at.lo) >> shift_of(at);
+    return {bins.high[b], bins.low[b]};
+}
+
+// The ranges that the ends lie in, from the histogram over all keys, and a histogram of each
+__global__ __launch_bounds__(LONG_THREADS) void second_bins_kernel(const Long p)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    Histogram *const bins = reinterpret_cast<Histogram *>(lds);
+    __shared__ LongScratch s;
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    const Bounds b = segment_bounds(p, segment, of_waves);
+    Segment &of = p.segment[segment];
+    const bool weights = p.a.top_p < 1.0, limited = by_count(p, b.number), first = blockIdx.x % p.pieces == 0 && threadIdx.x == 0;
+    if (first) of.least = b.least, of.most = b.most, of.number = b.number, of.listed = 0;
+    if (b.number == 0) return;
+    const double best = (double)energy_of(b.least);
+    const Range whole = {b.least, b.most, b.number, 0, {0, 0}};
+    read_bins(bins[0], *p.histogram(0, segment));
+    Range at[2] = {whole, whole};
+    double total = 0.0;
+    if (limited) at[0] = narrow<LONG_THREADS>(s, bins[0], whole, {false, p.a.k, {0.0, 0.0}});
+    if (weights) {
+        Mass of_range = {0, 0};
+        if (limited) {
+            of_range = mass_in(bins[0], whole, at[0]);
+        } else {
+            u64 high = 0, low = 0;
+            for (uint32_t i = threadIdx.x; i < BINS; i += LONG_THREADS) high += bins[0].high[i], low += bins[0].low[i];
+            high = block_prefix<LONG_THREADS>(high, s.wide[0]);
+            low = block_prefix<LONG_THREADS>(low, s.wide[1]);
+            __syncthreads();
+            if (threadIdx.x == LONG_THREADS - 1) s.total = {high, low};
+            __syncthreads();
+            total = s.total.value();
+        }
+        at[1] = narrow<LONG_THREADS>(s, bins[0], whole, weight_goal(p.a, limited, at[0], of_range, total));
+    }
+    if (first) of.by_count = at[0], of.by_weight = at[1], of.total = total;
+    clear_bins<LONG_THREADS>(bins[0]);
+    clear_bins<LONG_THREADS>(bins[1]);
+    const uint32_t shift[2] = {shift_of(at[0]), shift_of(at[1])};
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
+        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
+        if (!in[0] && !in[1]) return;
+        const double w = weights ? weight_of(key, best, p.a.per_temperature) : 0.0;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (in[r]) add_to_bins(bins[r], (key - at[r].lo) >> shift[r], weights, w);
+    });
+    __syncthreads();
+    if (limited) write_bins(p.parts[blockIdx.x], bins[0]); // (the first ones are not needed again)
+    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], bins[1]);
+}
+
+// The ranges again, by the second histograms, and the candidates in them
+__global__ __launch_bounds__(LONG_THREADS) void list_kernel(const Long p)
+{
+    __shared__ Histogram bins;
+    __shared__ LongScratch s;
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    Segment &of = p.segment[segment];
+    const uint32_t number = of.number;
+    if (number == 0) return;
+    const bool weights = p.a.top_p < 1.0, limited = by_count(p, number);
+    Range at[2] = {of.by_count, of.by_weight};
+    Mass of_range = {0, 0};
+    if (limited) {
+        read_bins(bins, *p.histogram(0, segment));
+        const Range within_it = at[0];
+        at[0] = narrow<LONG_THREADS>(s, bins, within_it, {false, p.a.k, {0.0, 0.0}});
+        of_range = mass_in(bins, within_it, at[0]);
+    }
+    if (weights) {
+        read_bins(bins, *p.histogram(1, segment));
+        at[1] = narrow<LONG_THREADS>(s, bins, at[1], weight_goal(p.a, limited, at[0], of_range, of.total));
+    }
+    Bounds found[2] = {{NO_KEY, 0, 0, 0}, {NO_KEY, 0, 0, 0}};
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t index) {
+        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
+        if (!in[0] && !in[1]) return;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (in[r]) {
+                found[r].least = min(found[r].least, key);
+                found[r].most = max(found[r].most, key);
+                ++found[r].number;
+            }
+        // (a place in the list for all of a wavefront's lanes that are here at once)
+        const u64 here = __ballot(true);
+        const int leader = __builtin_ctzll(here);
+        uint32_t place = 0;
+        if ((int)(threadIdx.x & 63) == leader) place = atomicAdd(&of.listed, (uint32_t)__builtin_popcountll(here));
+        place = __shfl(place, leader) + __builtin_popcountll(here & ((1ull << (threadIdx.x & 63)) - 1));
+        if (place < LIST) p.list[segment * LIST + place] = (u64)key << 32 | index;
+    });
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const Bounds all = block_bounds(found[r], of_waves);
+        if (threadIdx.x == 0) p.equal[r * p.segments * p.pieces + blockIdx.x] = {all.least, all.most, all.number, 0};
+    }
+    // the next kernel works on from here; blocks of this one read it no more once the last has counted its candidates, which is why the
+    // ranges go to a place of their own
+    if (blockIdx.x % p.pieces == 0 && threadIdx.x == 0) {
+        Segment &next = p.segment[p.segments + segment];
+        next.by_count = at[0];
+        next.by_weight = at[1];
+    }
+}
+
+// All of a segment, for a block by itself
+struct Stream {
+    const Draws &a;
+    uint64_t segment;
+    Bounds *of_waves;
+    template <class F>
+    __device__ __forceinline__ void each(F &&f) const { each_of_piece(a, segment, 0, a.n, f); }
+    // by index, a block's threads at a time
+    __device__ uint32_t nth_from(uint64_t from, uint64_t to, uint32_t of, uint32_t j) const
+    {
+        const float *energy = a.energy + segment * a.n;
+        const uint8_t *legal = a.legal ? a.legal + segment * a.n : nullptr;
+        __shared__ uint32_t small[LONG_THREADS / 64], found;
+        uint32_t passed = 0;
+        if (threadIdx.x == 0) found = (uint32_t)(to - 1);
+        for (uint64_t at = from; at < to; at += LONG_THREADS * 4) {
+            uint32_t key[4] = {NO_KEY, NO_KEY, NO_KEY, NO_KEY}, mine = 0;
+            const uint64_t here = at + threadIdx.x * 4;
+            if (here < to) load_keys(energy, legal, here, to, key);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine += key[i] == of;
+            uint32_t up_to = passed + block_prefix<LONG_THREADS>(mine, small);
+            uint32_t before = up_to - mine;
+            if (before < j && up_to >= j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key[i] == of && ++before == j) found = (uint32_t)(here + i);
+            __syncthreads();
+            for (int w = 0; w < LONG_THREADS / 64; ++w) passed += small[w];
+            if (passed >= j) break;
         }
         __syncthreads();
-        total = Mass{s.bins.high[0], s.bins.low[0]}.value();
+        return found;
+    }
+    __device__ uint32_t nth(uint32_t of, uint32_t j) const { return nth_from(0, a.n, of, j); }
+};
+
+// The ends of both prefixes, a block a segment
+__global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
+{
+    __shared__ Histogram bins;
+    __shared__ LongScratch s;
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    __shared__ uint32_t which_piece, left_there;
+    const uint64_t segment = blockIdx.x;
+    Segment &of = p.segment[segment];
+    const bool weights = p.a.top_p < 1.0, any = p.a.k || weights;
+    if (!any) { // (nothing went before but the bounds)
+        const Bounds b = segment_bounds(p, segment, of_waves);
+        if (threadIdx.x == 0) {
+            of.least = b.least, of.most = b.most, of.number = b.number;
+            of.cut = {b.most, 0xFFFFFFFFu};
+        }
+        return;
+    }
+    const uint32_t number = of.number, listed = of.listed;
+    if (number == 0) return;
+    const bool limited = by_count(p, number);
+    const double best = (double)energy_of(of.least);
+    const auto weight = [&](uint32_t key) { return weight_of(key, best, p.a.per_temperature); };
+    const Stream stream = {p.a, segment, of_waves};
+    const Segment &ranges = p.segment[p.segments + segment];
+
+    const auto find = [&](const Range &at, const Goal &goal, int r) {
+        if (listed <= LIST && at.number <= (uint32_t)LongScratch::LIST) {
+            __syncthreads();
+            if (threadIdx.x == 0) s.listed = 0;
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < listed; i += LONG_THREADS) {
+                const u64 one = p.list[segment * LIST + i];
+                const uint32_t key = (uint32_t)(one >> 32);
+                if (key < at.lo || key > at.hi) continue;
+                const uint32_t place = atomicAdd(&s.listed, 1u);
+                if (place < (uint32_t)LongScratch::LIST) s.list[place] = one;
+            }
+            sort_list<LONG_THREADS>(s, at.number);
+            cut_sorted<LONG_THREADS>(s, at, goal, weights, weight);
+            return;
+        }
+        const Equal *equal = p.equal + (r * p.segments + segment) * p.pieces;
+        Bounds b = {NO_KEY, 0, 0, 0};
+        if (threadIdx.x < p.pieces) b = {equal[threadIdx.x].least, equal[threadIdx.x].most, equal[threadIdx.x].number, 0};
+        const uint32_t mine = b.number;
+        b = block_bounds(b, of_waves);
+        if (b.least != b.most) { // many, and not equal
+            find_cut<LONG_THREADS>(s, bins, at, goal, weights, stream, weight);
+            return;
+        }
+        Range one = at;
+        one.lo = one.hi = b.least;
+        const uint32_t j = last_of_equal(s, one, goal, weight(b.least));
+        if (threadIdx.x == 0) which_piece = 0, left_there = 1;
+        const uint32_t to = block_prefix<LONG_THREADS>(mine, s.small); // (and a barrier)
+        if (to >= j && to - mine < j) {
+            which_piece = threadIdx.x;
+            left_there = j - (to - mine);
+        }
+        __syncthreads();
+        const uint64_t from = which_piece * p.piece;
+        const uint32_t index = stream.nth_from(from, min(p.a.n, from + p.piece), b.least, left_there);
+        if (threadIdx.x == 0) s.cut = {b.least, index};
+        __syncthreads();
+    };
+
+    Cut cut = {of.most, 0xFFFFFFFFu};
+    double total = of.total;
+    if (limited) {
+        find(ranges.by_count, {false, p.a.k, {0.0, 0.0}}, 0);
+        cut = s.cut;
+        total = s.total.value();
         __syncthreads();
     }
     if (weights) {
-        const double target = a.top_p * total;
-        const uint32_t at_most = cut ? end.kept : 0, key_most = end.key;
-        const Search at = find(true, 0, target);
-        uint32_t most = end.all;
-        if (cut && end.key == key_most) most = at_most; // (of the k least's last ones)
-        end.kept = enough(at.mass.value(), weight_of(end.key, least, a.per_temperature), most, target);
-        cut = true;
+        find(ranges.by_weight, {true, 0, {p.a.top_p * total, p.a.top_p * total}}, 1);
+        if (within(s.cut.key, s.cut.index, cut)) cut = s.cut;
     }
+    if (threadIdx.x == 0) of.cut = cut;
+}
 
-    // strips of candidates, a wavefront each at a time
-    const uint64_t strip = (n + STRIPS - 1) / STRIPS <= 64 ? 64 : ((n + STRIPS - 1) / STRIPS + 63) / 64 * 64;
-    const uint32_t strips = (uint32_t)((n + strip - 1) / strip);
-    const auto key_at = [&](uint64_t i) { return i < n ? key_of(energy[i], !legal || legal[i]) : NO_KEY; };
-    uint64_t last = n; // of the candidates of the last key, those before it stay
-    if (cut && end.kept < end.all) {
-        for (uint32_t t = wave; t < strips; t += waves) {
-            uint32_t some = 0;
-            for (uint64_t i = t * strip; i < min(n, (t + 1) * strip); i += 64) some += __builtin_popcountll(__ballot(key_at(i + lane) == end.key));
-            if (lane == 0) s.counts[t] = some;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            uint32_t left = end.kept;
-            for (uint32_t t = 0; t < strips; t += 64) {
-                const uint32_t mine = t + lane < strips ? s.counts[t + lane] : 0;
-                uint32_t to = mine;
-#pragma unroll
-                for (int stride = 1; stride < 64; stride <<= 1) {
-                    const uint32_t other = __shfl_up(to, stride);
-                    if ((int)lane >= stride) to += other;
-                }
-                const uint64_t there = __ballot(to >= left);
-                if (there == 0) {
-                    left -= __shfl(to, 63);
-                    continue;
-                }
-                const int l = __builtin_ctzll(there);
-                left -= __shfl(to - mine, l);
-                uint64_t i = (t + l) * strip;
-                for (const uint64_t to_here = i + strip; i < to_here; i += 64) {
-                    uint64_t equal = __ballot(key_at(i + lane) == end.key);
-                    const uint32_t some = __builtin_popcountll(equal);
-                    if (some < left) {
-                        left -= some;
-                        continue;
-                    }
-                    while (--left) equal &= equal - 1;
-                    i += __builtin_ctzll(equal) + 1;
-                    break;
-                }
-                if (lane == 0) {
-                    s.found.lo = (uint32_t)i;
-                    s.found.hi = (uint32_t)(i >> 32);
-                }
-                break;
-            }
-        }
-        __syncthreads();
-        last = (uint64_t)s.found.hi << 32 | s.found.lo;
-    }
-    const auto kept_weight = [&](uint64_t i, bool &kept) {
-        const uint32_t key = key_at(i);
-        kept = key < end.key || (key == end.key && i < last);
-        if (!kept) return 0.0;
-        const double w = weight_of(key, least, a.per_temperature);
-        kept = w >= a.min_p;
-        return kept ? w : 0.0;
-    };
-
-    for (uint32_t t = wave; t < STRIPS; t += waves) {
+// Sums of the kept candidates' weights over strips, and over chunks of 64 strips: a wavefront a chunk
+__global__ __launch_bounds__(256) void sums_kernel(const Long p)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t chunk = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (chunk >= p.segments * p.chunks) return;
+    const uint64_t segment = chunk / p.chunks, from = chunk % p.chunks * (64 * p.strip);
+    const Segment &of = p.segment[segment];
+    if (of.number == 0) return;
+    const Cut cut = of.cut;
+    const double best = (double)energy_of(of.least);
+    const float *energy = p.a.energy + segment * p.a.n;
+    const uint8_t *legal = p.a.legal ? p.a.legal + segment * p.a.n : nullptr;
+    // sixteen lanes a strip, four strips at a time
+    double all = 0.0;
+    uint32_t kept = 0;
+    for (uint32_t t = 0; t < 64; t += 4) {
+        const uint64_t begin = from + (t + lane / 16) * p.strip, end = min(p.a.n, begin + p.strip);
         double sum = 0.0;
-        uint32_t some = 0;
-        if (t < strips)
-            for (uint64_t i = t * strip; i < min(n, (t + 1) * strip); i += 64) {
-                bool kept;
-                sum += kept_weight(i + lane, kept);
-                some += __builtin_popcountll(__ballot(kept));
-            }
+        for (uint64_t i = begin + lane % 16 * 4; i < end; i += 64) {
+            uint32_t key[4];
+            load_keys(energy, legal, i, end, key);
 #pragma unroll
-        for (int stride = 1; stride < 64; stride <<= 1) sum += __shfl_xor(sum, stride);
-        if (lane == 0) {
-            s.sums[t] = sum;
-            s.counts[t] = some;
+            for (int k = 0; k < 4; ++k) {
+                if (key[k] == NO_KEY || !within(key[k], (uint32_t)(i + k), cut)) continue;
+                const double w = weight_of(key[k], best, p.a.per_temperature);
+                if (w >= p.a.min_p) {
+                    sum += w;
+                    ++kept;
+                }
+            }
         }
+#pragma unroll
+        for (int stride = 1; stride < 16; stride <<= 1) sum += __shfl_xor(sum, stride);
+        if (lane % 16 == 0) p.strip_sums[chunk * 64 + t + lane / 16] = sum;
+        all += lane % 16 == 0 ? sum : 0.0;
     }
-    __syncthreads();
-    // sums up to and including each strip
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) {
+        all += __shfl_xor(all, stride);
+        kept += (uint32_t)__shfl_xor((int)kept, stride);
+    }
+    if (lane == 0) {
+        p.chunk_sums[chunk] = all;
+        p.chunk_counts[chunk] = kept;
+    }
+}
+
+constexpr int DRAW_THREADS = 512, MOST_CHUNKS = 4096;
+
+// sums of a wavefront's lanes up to and including each
+__device__ __forceinline__ double wave_sums(double x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) {
+        const double other = __shfl_up(x, stride);
+        if (lane >= stride) x += other;
+    }
+    return x;
+}
+// Of a wavefront's lanes with a weight, the first whose sum passes the target, or the last
+__device__ __forceinline__ int lane_of(double w, double to, double target)
+{
+    const u64 some = __ballot(w > 0.0), passes = __ballot(w > 0.0 && to > target);
+    return passes ? __builtin_ctzll(passes) : some ? 63 - __builtin_clzll(some) : -1;
+}
+
+// A wavefront a draw: its chunk, its strip, its candidate
+__global__ __launch_bounds__(DRAW_THREADS) void draws_kernel(const Long p, uint32_t blocks)
+{
+    __shared__ double to[MOST_CHUNKS];
+    __shared__ double of_waves[DRAW_THREADS / 64];
+    __shared__ uint32_t small[DRAW_THREADS / 64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, waves = DRAW_THREADS / 64;
+    const uint64_t segment = blockIdx.x / blocks;
+    const uint32_t first = blockIdx.x % blocks;
+    const Segment &of = p.segment[segment];
+    if (of.number == 0) {
+        nothing_to_draw(p.a, segment, first * DRAW_THREADS + threadIdx.x, blocks * DRAW_THREADS);
+        if (first == 0 && threadIdx.x == 0 && p.a.count) p.a.count[segment] = 0;
+        return;
+    }
+    const double *sums = p.chunk_sums + segment * p.chunks;
+    constexpr uint32_t EACH = MOST_CHUNKS / DRAW_THREADS;
     {
-        constexpr uint32_t EACH = STRIPS / THREADS;
-        double to[EACH], sum = 0.0;
-        uint32_t some = 0;
+        double mine[EACH], sum = 0.0;
+        uint32_t kept = 0;
+#pragma unroll
         for (uint32_t i = 0; i < EACH; ++i) {
-            sum += s.sums[threadIdx.x * EACH + i];
-            some += s.counts[threadIdx.x * EACH + i];
-            to[i] = sum;
+            const uint32_t c = threadIdx.x * EACH + i;
+            mine[i] = c < p.chunks ? sums[c] : 0.0;
+            kept += c < p.chunks ? p.chunk_counts[segment * p.chunks + c] : 0;
+            sum += mine[i];
         }
-        const double up_to = block_prefix<THREADS>(sum, s.real) - sum;
-        const uint32_t all = block_prefix<THREADS>(some, s.small);
-        for (uint32_t i = 0; i < EACH; ++i) s.sums_to[threadIdx.x * EACH + i] = up_to + to[i];
-        if (threadIdx.x == THREADS - 1 && a.count) a.count[blockIdx.x] = all;
+        double up_to = block_prefix<DRAW_THREADS>(sum, of_waves) - sum;
+#pragma unroll
+        for (uint32_t i = 0; i < EACH; ++i) {
+            up_to += mine[i];
+            to[threadIdx.x * EACH + i] = up_to;
+        }
+        kept = block_prefix<DRAW_THREADS>(kept, small);
+        if (first == 0 && threadIdx.x == DRAW_THREADS - 1 && p.a.count) p.a.count[segment] = kept;
     }
     __syncthreads();
-    const double of_all = s.sums_to[STRIPS - 1];
-    for (uint32_t d = wave; d < a.draws; d += waves) {
-        const double target = fmax((double)a.uniform[(uint64_t)blockIdx.x * a.draws + d] * of_all, 0.0);
-        // the first strip that adds something and passes it, or the last that adds anything
-        uint32_t t = STRIPS, last_one = 0;
-        for (uint32_t t0 = 0; t0 < STRIPS; t0 += 64) {
-            const bool some = s.sums[t0 + lane] > 0.0;
-            const uint64_t passes = __ballot(some && s.sums_to[t0 + lane] > target), adds = __ballot(some);
-            if (adds) last_one = t0 + 63 - __builtin_clzll(adds);
-            if (passes) {
-                t = t0 + __builtin_ctzll(passes);
-                break;
-            }
+    const Cut cut = of.cut;
+    const double best = (double)energy_of(of.least), all = to[MOST_CHUNKS - 1];
+    const float *energy = p.a.energy + segment * p.a.n;
+    const uint8_t *legal = p.a.legal ? p.a.legal + segment * p.a.n : nullptr;
+    for (uint32_t d = first * waves + wave; d < p.a.draws; d += blocks * waves) {
+        const double target = fmax((double)p.a.uniform[segment * p.a.draws + d] * all, 0.0);
+        uint32_t lo = 0, hi = p.chunks - 1;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (to[mid] > target) hi = mid;
+            else lo = mid + 1;
         }
-        const bool past = t == STRIPS;
-        if (past) t = last_one;
-        double left = past ? __builtin_inf() : target - (t ? s.sums_to[t - 1] : 0.0), w_found = 0.0;
-        uint64_t found = 0;
-        for (uint64_t i = t * strip; i < min(n, (t + 1) * strip); i += 64) {
-            bool kept;
-            const double w = kept_weight(i + lane, kept);
-            double to = w;
-#pragma unroll
-            for (int stride = 1; stride < 64; stride <<= 1) {
-                const double other = __shfl_up(to, stride);
-                if ((int)lane >= stride) to += other;
-            }
-            const uint64_t some = __ballot(w > 0.0), passes = __ballot(w > 0.0 && to > left);
-            if (some) { // where roundings leave none that passes, the last
-                const int l = passes ? __builtin_ctzll(passes) : 63 - __builtin_clzll(some);
+        // (between two threads' chunks sums may differ in their last bit where nothing is added; and past the end the last one is wanted)
+        while (!(sums[lo] > 0.0) && lo + 1 < p.chunks && all > target) ++lo;
+        while (!(sums[lo] > 0.0) && lo > 0) --lo;
+        double left = all > target ? target - (lo ? to[lo - 1] : 0.0) : __builtin_inf();
+        const uint64_t chunk = segment * p.chunks + lo;
+        const double of_strip = p.strip_sums[chunk * 64 + lane], strips_to = wave_sums(of_strip);
+        const int t = max(lane_of(of_strip, strips_to, left), 0);
+        left -= t ? __shfl(strips_to, t - 1) : 0.0;
+        const uint64_t begin = ((uint64_t)lo * 64 + t) * p.strip, end = min(p.a.n, begin + p.strip);
+        uint64_t found = begin;
+        double of_found = 0.0;
+        for (uint64_t i = begin; i < end; i += 64) {
+            const uint32_t key = i + lane < end ? key_of(energy[i + lane], !legal || legal[i + lane]) : NO_KEY;
+            double w = key != NO_KEY && within(key, (uint32_t)(i + lane), cut) ? weight_of(key, best, p.a.per_temperature) : 0.0;
+            w = w >= p.a.min_p ? w : 0.0;
+            const double up_to = wave_sums(w);
+            const int l = lane_of(w, up_to, left);
+            if (l >= 0) {
                 found = i + l;
-                w_found = __shfl(w, l);
+                of_found = __shfl(w, l);
             }
-            if (passes) break;
-            left -= __shfl(to, 63);
+            if (__ballot(w > 0.0 && up_to > left)) break;
+            left -= __shfl(up_to, 63);
         }
         if (lane == 0) {
-            idx[d] = (uint32_t)found;
-            if (logprob) logprob[d] = (float)log(w_found / of_all);
+            p.a.idx[segment * p.a.draws + d] = (uint32_t)found;
+            if (p.a.logprob) p.a.logprob[segment * p.a.draws + d] = (float)log(of_found / all);
         }
     }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+constexpr uint64_t SHORT = 16384;
+
+uint64_t padded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// sizes of a call on long segments, and the places in its workspace
+uint64_t lay_out(Long &p, void *ws)
+{
+    const uint64_t n = p.a.n, s = p.segments;
+    uint64_t pieces = (MOST_PIECES + s - 1) / s;
+    if (pieces > (n + 16383) / 16384) pieces = (n + 16383) / 16384;
+    p.piece = ((n + pieces - 1) / pieces + 4095) / 4096 * 4096;
+    p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
+    p.strip = 64;
+    while ((n + 64 * p.strip - 1) / (64 * p.strip) > MOST_CHUNKS) p.strip *= 2;
+    p.chunks = (uint32_t)((n + 64 * p.strip - 1) / (64 * p.strip));
+    char *at = (char *)ws;
+    const auto take = [&](uint64_t bytes) {
+        char *here = at;
+        at += padded(bytes);
+        return (void *)here;
+    };
+    p.segment = (Segment *)take(2 * s * sizeof(Segment));
+    p.bounds = (Bounds *)take(s * p.pieces * sizeof(Bounds));
+    p.parts = (Histogram *)take(2 * s * p.pieces * sizeof(Histogram));
+    p.whole = (Histogram *)take(p.pieces > 1 ? 2 * s * sizeof(Histogram) : 0);
+    p.list = (u64 *)take(s * LIST * sizeof(u64));
+    p.equal = (Equal *)take(2 * s * p.pieces * sizeof(Equal));
+    p.strip_sums = (double *)take(s * p.chunks * 64 * sizeof(double));
+    p.chunk_sums = (double *)take(s * p.chunks * sizeof(double));
+    p.chunk_counts = (uint32_t *)take(s * p.chunks * sizeof(uint32_t));
+    return (uint64_t)(at - (char *)ws);
+}
+
+template <int THREADS, int EACH>
+int32_t launch_short(const Draws &a, uint32_t segments, hipStream_t st)
+{
+    constexpr int bytes = sizeof(Short<THREADS, EACH>);
+    if (bytes > 65536)
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(short_kernel<THREADS, EACH>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    hipLaunchKernelGGL((short_kernel<THREADS, EACH>), dim3(segments), dim3(THREADS), bytes, st, a);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+
+int32_t launch_long(const Draws &a, uint32_t segments, void *ws, hipStream_t st)
+{
+    Long p;
+    p.a = a;
+    p.segments = segments;
+    lay_out(p, ws);
+    const dim3 pieces(segments * p.pieces), threads(LONG_THREADS);
+    const bool weights = a.top_p < 1.0;
+    hipLaunchKernelGGL(bounds_kernel, pieces, threads, 0, st, p);
+    if (a.k || weights) {
+        const auto join = [&](int which) {
+            if (p.pieces > 1) hipLaunchKernelGGL(join_bins_kernel, dim3(segments * (BINS / 256)), dim3(256), 0, st, p, which);
+        };
+        constexpr int two = 2 * sizeof(Histogram);
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(second_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, two));
+        hipLaunchKernelGGL(first_bins_kernel, pieces, threads, 0, st, p);
+        join(0);
+        hipLaunchKernelGGL(second_bins_kernel, pieces, threads, two, st, p);
+        if (a.k) join(0);
+        if (weights) join(1);
+        hipLaunchKernelGGL(list_kernel, pieces, threads, 0, st, p);
+    }
+    hipLaunchKernelGGL(ends_kernel, dim3(segments), threads, 0, st, p);
+    hipLaunchKernelGGL(sums_kernel, dim3((uint32_t)((p.segments * p.chunks + 3) / 4)), dim3(256), 0, st, p);
+    // some draws a wavefront, so that a block's sums over chunks serve several
+    const uint32_t most = (a.draws + DRAW_THREADS / 64 - 1) / (DRAW_THREADS / 64), wanted = (1024 + segments - 1) / segments;
+    const uint32_t blocks = most < wanted ? most : wanted;
+    hipLaunchKernelGGL(draws_kernel, dim3(segments * blocks), dim3(DRAW_THREADS), 0, st, p, blocks);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
 }
 
 } // namespace
@@ -480,7 +1161,12 @@ using namespace eck;
 
 extern "C" uint64_t sample_select_workspace_bytes(uint64_t n, uint32_t n_segments, uint32_t draws)
 {
-    return 0;
+    if (n == 0 || n_segments == 0 || draws == 0 || n % n_segments || n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS) return 0;
+    if (n / n_segments <= SHORT) return 0;
+    Long p;
+    p.a.n = n / n_segments;
+    p.segments = n_segments;
+    return lay_out(p, nullptr);
 }
 
 extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint64_t n, uint32_t n_segments, const float *uniform, uint32_t draws,
@@ -490,7 +1176,7 @@ extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint
     if (!energy || !uniform || !idx_out || n == 0 || n_segments == 0 || draws == 0) return ECK_EINVAL;
     if (!(temperature >= 0.0f && temperature < __builtin_inff()) || !(top_p > 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f)) return ECK_EINVAL;
     if (n % n_segments) return ECK_ESHAPE;
-    if (n / n_segments > MOST_CANDIDATES) return ECK_EUNSUPPORTED;
+    if (n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS) return ECK_EUNSUPPORTED;
     if (!aligned(energy, 4) || !aligned(uniform, 4) || !aligned(idx_out, 4) || !aligned(logprob_out, 4) || !aligned(count_out, 4)) return ECK_EALIGN;
     const uint64_t need = sample_select_workspace_bytes(n, n_segments, draws);
     if (need && (!ws || ws_bytes < need)) return ECK_EWORKSPACE;
@@ -504,11 +1190,10 @@ extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint
         a.top_p = 1.0;
         a.min_p = 0.0;
     }
-    const dim3 grid(n_segments);
     const hipStream_t st = as_stream(stream);
-    if (a.n <= 256 * 16) hipLaunchKernelGGL((segment_kernel<256, true>), grid, dim3(256), 0, st, a);
-    else if (a.n <= 1024 * 16) hipLaunchKernelGGL((segment_kernel<1024, true>), grid, dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL((segment_kernel<1024, false>), grid, dim3(1024), 0, st, a);
-    ECK_HIP_TRY(hipGetLastError());
-    return ECK_OK;
+    if (a.n <= 256) return launch_short<64, 4>(a, n_segments, st);
+    if (a.n <= 1024) return launch_short<256, 4>(a, n_segments, st);
+    if (a.n <= 4096) return launch_short<512, 8>(a, n_segments, st);
+    if (a.n <= SHORT) return launch_short<1024, 16>(a, n_segments, st);
+    return launch_long(a, n_segments, ws, st);
 }

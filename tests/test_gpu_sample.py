@@ -154,6 +154,16 @@ def test_what_is_not_finite_or_legal_is_never_drawn(n):
     assert (idx[[0, 1, 3]] == NOBODY).all() and (count[[0, 1, 3]] == 0).all() and (idx[4] == 0).all() and (idx[5] == 5).all()
 
 
+@pytest.mark.parametrize("n", [3000, 16000, 200000, 1 << 20])
+def test_energies_next_to_each_other_with_outliers(n):
+    """most of a segment within a hundred units of the last place, some candidates far out on both sides"""
+    g = np.random.default_rng(n)
+    e = (1.0 + g.integers(0, 100, (2, n)) * 2.0 ** -23).astype(np.float32)
+    e[:, 7], e[:, 11], e[0, 13] = 1e30, -0.001, -3e37
+    for how in (dict(k=n // 2), dict(k=n // 2, top_p=0.6), dict(top_p=0.9), dict(k=2), dict(top_p=0.5, min_p=0.5)):
+        check(e, None, g.random((2, 20)).astype(np.float32), temperature=3.0, **how)
+
+
 def test_results_that_are_not_wanted_may_be_left_out():
     e, flags, u = inputs(3, 700, 20, 1)
     put = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
