@@ -11,8 +11,10 @@
 // multiples of 2^-60, held as two numbers of thirty bits, whose sums do not depend on the order in which the atomics come.
 //
 // Segments of up to 16 384 candidates: a block each, keys in registers, one launch.  Longer ones: blocks by the piece, a launch for each
-// time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws).
+// time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws; where few are kept,
+// range, histogram, list, draws).
 #include "activations.h"
+#include "lanes.h"
 
 namespace eck {
 namespace {
@@ -74,23 +76,38 @@ __device__ __forceinline__ void load_keys(const float *energy, const uint8_t *le
 
 // ------------------------------------------------------------------------------------------------ blocks
 
-// sums over a block's threads up to and including each
+// sums over a wavefront's lanes up to and including each
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v) { return wave_prefix_sum(v); }
+__device__ __forceinline__ unsigned long long wave_sums(unsigned long long v) { return (unsigned long long)wave_prefix_sum((int64_t)v); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved_real(double v) { return __builtin_bit_cast(double, moved<CTRL, ROWS>(__builtin_bit_cast(int64_t, v))); }
+__device__ __forceinline__ double wave_sums(double v) // (the steps of wave_prefix_sum)
+{
+    v += moved_real<0x111, 0xF>(v);
+    v += moved_real<0x112, 0xF>(v);
+    v += moved_real<0x114, 0xF>(v);
+    v += moved_real<0x118, 0xF>(v);
+    v += moved_real<0x142, 0xA>(v);
+    v += moved_real<0x143, 0xC>(v);
+    return v;
+}
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ unsigned long long of_lane(unsigned long long v, int lane) { return (unsigned long long)lane_value((int64_t)v, lane); }
+__device__ __forceinline__ double of_lane(double v, int lane) { return __builtin_bit_cast(double, lane_value(__builtin_bit_cast(int64_t, v), lane)); }
+
+// sums over a block's threads up to and including each (of at most sixteen wavefronts)
 template <int THREADS, class V>
 __device__ __forceinline__ V block_prefix(V v, V *of_waves)
 {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-#pragma unroll
-    for (int stride = 1; stride < 64; stride <<= 1) {
-        const V other = __shfl_up(v, stride);
-        if ((int)lane >= stride) v += other;
-    }
+    v = wave_sums(v);
     if (THREADS == 64) return v;
+    constexpr int WAVES = THREADS / 64;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     __syncthreads(); // (of_waves may still be read from the last time)
     if (lane == 63) of_waves[wave] = v;
     __syncthreads();
-    V before = 0;
-    for (uint32_t w = 0; w < wave; ++w) before += of_waves[w];
-    return before + v;
+    const V to = wave_sums(lane < WAVES ? of_waves[lane] : (V)0);
+    return wave ? of_lane(to, wave - 1) + v : v;
 }
 
 typedef unsigned long long u64;
@@ -141,12 +158,12 @@ struct Goal {
 };
 
 template <int THREADS>
-__device__ __forceinline__ void clear_bins(Histogram &bins)
+__device__ __forceinline__ void clear_bins(Histogram &bins, bool weights)
 {
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < BINS; b += THREADS) {
         bins.count[b] = 0;
-        bins.high[b] = bins.low[b] = 0;
+        if (weights) bins.high[b] = bins.low[b] = 0;
     }
     __syncthreads();
 }
@@ -162,8 +179,9 @@ __device__ __forceinline__ void add_to_bins(Histogram &bins, uint32_t bin, bool 
 }
 
 // The bins of `at` in which the prefix ends, or may end: s.found[0] from the first of them to the last.  All threads get the result.
+// weights: whether the bins hold any.
 template <int THREADS, class S>
-__device__ __forceinline__ Range narrow(S &s, const Histogram &bins, const Range &at, const Goal &goal)
+__device__ __forceinline__ Range narrow(S &s, const Histogram &bins, const Range &at, const Goal &goal, bool weights)
 {
     constexpr uint32_t EACH = BINS / THREADS;
     const uint32_t first = threadIdx.x * EACH, shift = shift_of(at);
@@ -172,10 +190,11 @@ __device__ __forceinline__ Range narrow(S &s, const Histogram &bins, const Range
 #pragma unroll
     for (uint32_t i = 0; i < EACH; ++i) {
         count += bins.count[first + i];
-        mass = mass + Mass{bins.high[first + i], bins.low[first + i]};
+        if (weights) mass = mass + Mass{bins.high[first + i], bins.low[first + i]};
     }
     const uint32_t to = at.before + block_prefix<THREADS>(count, s.small);
-    const Mass mass_to = at.mass + Mass{block_prefix<THREADS>((u64)mass.high, s.wide[0]), block_prefix<THREADS>((u64)mass.low, s.wide[1])};
+    Mass mass_to = at.mass;
+    if (weights) mass_to = mass_to + Mass{block_prefix<THREADS>((u64)mass.high, s.wide[0]), block_prefix<THREADS>((u64)mass.low, s.wide[1])};
     const uint32_t from = to - count;
     const Mass mass_from = {mass_to.high - mass.high, mass_to.low - mass.low};
 #pragma unroll
@@ -186,7 +205,7 @@ __device__ __forceinline__ Range narrow(S &s, const Histogram &bins, const Range
             uint32_t c = from, b = first;
             Mass m = mass_from;
             for (; b < first + EACH - 1; ++b) {
-                const Mass next = m + Mass{bins.high[b], bins.low[b]};
+                const Mass next = weights ? m + Mass{bins.high[b], bins.low[b]} : m;
                 if (goal.reached(which, c + bins.count[b], next)) break;
                 c += bins.count[b];
                 m = next;
@@ -301,13 +320,13 @@ __device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool
             __syncthreads();
             return;
         }
-        clear_bins<THREADS>(bins);
+        clear_bins<THREADS>(bins, weights);
         const uint32_t shift = shift_of(at);
         source.each([&](uint32_t key, uint32_t) {
             if (key >= at.lo && key <= at.hi) add_to_bins(bins, (key - at.lo) >> shift, weights, weights ? weight(key) : 0.0);
         });
         __syncthreads();
-        at = narrow<THREADS>(s, bins, at, goal);
+        at = narrow<THREADS>(s, bins, at, goal, weights);
     }
 }
 
@@ -321,17 +340,18 @@ __device__ __forceinline__ void nothing_to_draw(const Draws &a, uint64_t segment
 
 // ------------------------------------------------------------------------------------------------ short segments
 
-// Keys of a block's candidates, EACH neighbouring ones a thread
+// Keys of a block's candidates, EACH neighbouring ones a thread; those up to a cut
 template <int THREADS, int EACH, class S>
 struct Held {
     uint32_t (&key)[EACH];
     S &s;
+    const Cut &cut;
     template <class F>
     __device__ __forceinline__ void each(F &&f) const
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (key[i] != NO_KEY) f(key[i], threadIdx.x * EACH + i);
+            if (within(key[i], threadIdx.x * EACH + i, cut)) f(key[i], threadIdx.x * EACH + i); // (NO_KEY is above any)
     }
     __device__ uint32_t nth(uint32_t of, uint32_t j) const
     {
@@ -392,9 +412,9 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
     }
 #pragma unroll
     for (int stride = 1; stride < 64; stride <<= 1) {
-        least = min(least, (uint32_t)__shfl_xor((int)least, stride));
-        most = max(most, (uint32_t)__shfl_xor((int)most, stride));
-        number += (uint32_t)__shfl_xor((int)number, stride);
+        least = min(least, lane_exchange(least, stride));
+        most = max(most, lane_exchange(most, stride));
+        number += lane_exchange(number, stride);
     }
     if (THREADS > 64) {
         if (lane == 0) s.least[wave] = least, s.most[wave] = most, s.number[wave] = number;
@@ -413,44 +433,26 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
     }
     const double best = (double)energy_of(least);
     const auto weight = [&](uint32_t k) { return weight_of(k, best, a.per_temperature); };
-    const bool weights = a.top_p < 1.0;
 
     Cut cut = {most, n};
     {
         typename Lds::S &sc = s.ends.s;
         Histogram &bins = s.ends.bins[0];
-        const Held<THREADS, EACH, typename Lds::S> held = {key, sc};
-        Range whole = {least, most, number, 0, {0, 0}};
-        Goal goal = {false, a.k, {0.0, 0.0}};
-        bool binned = false; // bins hold the whole range
-        const auto find = [&]() {
-            if (!Lds::BINNED || number <= (uint32_t)Lds::S::LIST) {
-                find_cut<THREADS>(sc, bins, whole, goal, weights, held, weight);
-                return;
-            }
-            if constexpr (Lds::BINNED) {
-                const uint32_t shift = shift_of(whole);
-                if (!binned) {
-                    clear_bins<THREADS>(bins);
-                    held.each([&](uint32_t k, uint32_t) { add_to_bins(bins, (k - whole.lo) >> shift, weights, weights ? weight(k) : 0.0); });
-                    __syncthreads();
-                }
-                const Range at = narrow<THREADS>(sc, bins, whole, goal);
-                binned = at.number <= (uint32_t)Lds::S::LIST || at.lo == at.hi; // else they are overwritten
-                find_cut<THREADS>(sc, bins, at, goal, weights, held, weight);
-            }
-        };
-        double total = 0.0; // of the k least
+        const Held<THREADS, EACH, typename Lds::S> held = {key, sc, cut};
+        uint32_t kept = number;
         if (a.k && a.k < number) {
-            if (a.k == 1 && !weights) { // the first of the least
-                const uint32_t index = held.nth(least, 1);
-                cut = {least, index};
+            Cut found;
+            if (a.k == 1) { // the first of the least
+                found = {least, held.nth(least, 1)};
             } else {
-                find();
-                cut = sc.cut;
-                total = sc.total.value();
+                find_cut<THREADS>(sc, bins, {least, most, number, 0, {0, 0}}, {false, a.k, {0.0, 0.0}}, false, held, weight);
+                found = sc.cut;
+                __syncthreads();
             }
-        } else if (weights) {
+            cut = found; // (`held` goes by it from here on)
+            kept = a.k;
+        }
+        if (a.top_p < 1.0 && kept > 1) {
             u64 high = 0, low = 0;
             held.each([&](uint32_t k, uint32_t) {
                 const Mass m = mass_of(weight(k));
@@ -462,14 +464,9 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
             __syncthreads();
             if (threadIdx.x == THREADS - 1) sc.total = {high, low};
             __syncthreads();
-            total = sc.total.value();
-        }
-        if (weights) {
-            goal = {true, 0, {a.top_p * total, a.top_p * total}};
-            find();
-            // (not past the k least, whatever roundings say)
-            const Cut by_weight = sc.cut;
-            if (within(by_weight.key, by_weight.index, cut)) cut = by_weight;
+            const double target = a.top_p * sc.total.value();
+            find_cut<THREADS>(sc, bins, {least, cut.key, kept, 0, {0, 0}}, {true, 0, {target, target}}, true, held, weight);
+            cut = sc.cut;
         }
     }
     __syncthreads(); // (what is written now lies where that was)
@@ -491,7 +488,7 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
         if (first + i < n) s.to[first + i] = to;
     }
 #pragma unroll
-    for (int stride = 1; stride < 64; stride <<= 1) kept += (uint32_t)__shfl_xor((int)kept, stride);
+    for (int stride = 1; stride < 64; stride <<= 1) kept += lane_exchange(kept, stride);
     if (lane == 0) s.number[wave] = kept;
     __syncthreads();
     if (threadIdx.x == 0 && a.count) {
@@ -528,14 +525,15 @@ constexpr uint32_t LIST = 4096;       // candidates at the ends that are listed,
 constexpr uint32_t MOST_PIECES = 512; // blocks of a segment
 typedef Scratch<LONG_THREADS, 1024> LongScratch;
 
-struct Bounds { // of a block's piece
-    uint32_t least, most, number, unused;
+struct Bounds { // of a block's piece; gate: the largest of its threads' least keys, threads: of those that have any
+    uint32_t least, most, number, gate, threads;
 };
 struct Equal { // candidates of a range in a block's piece: their least and largest key, and how many
     uint32_t least, most, number, unused;
 };
 struct Segment {
-    uint32_t least, most, number, listed;
+    uint32_t least, most, number, listed, listed_below;
+    uint32_t need, before, at_end; // how many are kept, below the end's bin and in it
     Range by_count, by_weight;
     double total; // weight of all, where no k least are taken
     Cut cut;
@@ -591,18 +589,23 @@ __device__ __forceinline__ Bounds block_bounds(Bounds b, Bounds *of_waves)
 {
 #pragma unroll
     for (int stride = 1; stride < 64; stride <<= 1) {
-        b.least = min(b.least, (uint32_t)__shfl_xor((int)b.least, stride));
-        b.most = max(b.most, (uint32_t)__shfl_xor((int)b.most, stride));
-        b.number += (uint32_t)__shfl_xor((int)b.number, stride);
+        b.least = min(b.least, lane_exchange(b.least, stride));
+        b.most = max(b.most, lane_exchange(b.most, stride));
+        b.number += lane_exchange(b.number, stride);
+        b.gate = max(b.gate, lane_exchange(b.gate, stride));
+        b.threads += lane_exchange(b.threads, stride);
     }
     __syncthreads();
     if ((threadIdx.x & 63) == 0) of_waves[threadIdx.x / 64] = b;
     __syncthreads();
-    b = of_waves[0];
-    for (int w = 1; w < LONG_THREADS / 64; ++w) {
-        b.least = min(b.least, of_waves[w].least);
-        b.most = max(b.most, of_waves[w].most);
-        b.number += of_waves[w].number;
+    b = of_waves[threadIdx.x % (LONG_THREADS / 64)];
+#pragma unroll
+    for (int stride = 1; stride < LONG_THREADS / 64; stride <<= 1) {
+        b.least = min(b.least, lane_exchange(b.least, stride));
+        b.most = max(b.most, lane_exchange(b.most, stride));
+        b.number += lane_exchange(b.number, stride);
+        b.gate = max(b.gate, lane_exchange(b.gate, stride));
+        b.threads += lane_exchange(b.threads, stride);
     }
     return b;
 }
@@ -611,7 +614,7 @@ __global__ __launch_bounds__(LONG_THREADS) void bounds_kernel(const Long p)
 {
     __shared__ Bounds of_waves[LONG_THREADS / 64];
     const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
-    Bounds b = {NO_KEY, 0, 0, 0};
+    Bounds b = {NO_KEY, 0, 0, 0, 0};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
         b.least = min(b.least, key);
         b.most = max(b.most, key);
@@ -624,7 +627,7 @@ __global__ __launch_bounds__(LONG_THREADS) void bounds_kernel(const Long p)
 // of all pieces of a segment
 __device__ __forceinline__ Bounds segment_bounds(const Long &p, uint64_t segment, Bounds *of_waves)
 {
-    Bounds b = {NO_KEY, 0, 0, 0};
+    Bounds b = {NO_KEY, 0, 0, 0, 0};
     if (threadIdx.x < p.pieces) b = p.bounds[segment * p.pieces + threadIdx.x];
     return block_bounds(b, of_waves);
 }
@@ -650,7 +653,7 @@ __global__ __launch_bounds__(LONG_THREADS) void first_bins_kernel(const Long p)
     const double best = (double)energy_of(b.least);
     const Range whole = {b.least, b.most, b.number, 0, {0, 0}};
     const uint32_t shift = shift_of(whole);
-    clear_bins<LONG_THREADS>(bins);
+    clear_bins<LONG_THREADS>(bins, weights);
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
         add_to_bins(bins, (key - whole.lo) >> shift, weights, weights ? weight_of(key, best, p.a.per_temperature) : 0.0);
     });
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(LONG_THREADS) void second_bins_kernel(const Long p)
     read_bins(bins[0], *p.histogram(0, segment));
     Range at[2] = {whole, whole};
     double total = 0.0;
-    if (limited) at[0] = narrow<LONG_THREADS>(s, bins[0], whole, {false, p.a.k, {0.0, 0.0}});
+    if (limited) at[0] = narrow<LONG_THREADS>(s, bins[0], whole, {false, p.a.k, {0.0, 0.0}}, weights);
     if (weights) {
         Mass of_range = {0, 0};
         if (limited) {
@@ -734,11 +737,11 @@ __global__ __launch_bounds__(LONG_THREADS) void second_bins_kernel(const Long p)
             __syncthreads();
             total = s.total.value();
         }
-        at[1] = narrow<LONG_THREADS>(s, bins[0], whole, weight_goal(p.a, limited, at[0], of_range, total));
+        at[1] = narrow<LONG_THREADS>(s, bins[0], whole, weight_goal(p.a, limited, at[0], of_range, total), true);
     }
     if (first) of.by_count = at[0], of.by_weight = at[1], of.total = total;
-    clear_bins<LONG_THREADS>(bins[0]);
-    clear_bins<LONG_THREADS>(bins[1]);
+    clear_bins<LONG_THREADS>(bins[0], weights);
+    clear_bins<LONG_THREADS>(bins[1], weights);
     const uint32_t shift[2] = {shift_of(at[0]), shift_of(at[1])};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
         const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
@@ -769,14 +772,14 @@ __global__ __launch_bounds__(LONG_THREADS) void list_kernel(const Long p)
     if (limited) {
         read_bins(bins, *p.histogram(0, segment));
         const Range within_it = at[0];
-        at[0] = narrow<LONG_THREADS>(s, bins, within_it, {false, p.a.k, {0.0, 0.0}});
+        at[0] = narrow<LONG_THREADS>(s, bins, within_it, {false, p.a.k, {0.0, 0.0}}, weights);
         of_range = mass_in(bins, within_it, at[0]);
     }
     if (weights) {
         read_bins(bins, *p.histogram(1, segment));
-        at[1] = narrow<LONG_THREADS>(s, bins, at[1], weight_goal(p.a, limited, at[0], of_range, of.total));
+        at[1] = narrow<LONG_THREADS>(s, bins, at[1], weight_goal(p.a, limited, at[0], of_range, of.total), true);
     }
-    Bounds found[2] = {{NO_KEY, 0, 0, 0}, {NO_KEY, 0, 0, 0}};
+    Bounds found[2] = {{NO_KEY, 0, 0, 0, 0}, {NO_KEY, 0, 0, 0, 0}};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t index) {
         const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
         if (!in[0] && !in[1]) return;
@@ -889,8 +892,8 @@ __global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
             return;
         }
         const Equal *equal = p.equal + (r * p.segments + segment) * p.pieces;
-        Bounds b = {NO_KEY, 0, 0, 0};
-        if (threadIdx.x < p.pieces) b = {equal[threadIdx.x].least, equal[threadIdx.x].most, equal[threadIdx.x].number, 0};
+        Bounds b = {NO_KEY, 0, 0, 0, 0};
+        if (threadIdx.x < p.pieces) b = {equal[threadIdx.x].least, equal[threadIdx.x].most, equal[threadIdx.x].number, 0, 0};
         const uint32_t mine = b.number;
         b = block_bounds(b, of_waves);
         if (b.least != b.most) { // many, and not equal
@@ -961,14 +964,14 @@ __global__ __launch_bounds__(256) void sums_kernel(const Long p)
             }
         }
 #pragma unroll
-        for (int stride = 1; stride < 16; stride <<= 1) sum += __shfl_xor(sum, stride);
+        for (int stride = 1; stride < 16; stride <<= 1) sum += lane_exchange(sum, stride);
         if (lane % 16 == 0) p.strip_sums[chunk * 64 + t + lane / 16] = sum;
         all += lane % 16 == 0 ? sum : 0.0;
     }
 #pragma unroll
     for (int stride = 1; stride < 64; stride <<= 1) {
-        all += __shfl_xor(all, stride);
-        kept += (uint32_t)__shfl_xor((int)kept, stride);
+        all += lane_exchange(all, stride);
+        kept += lane_exchange(kept, stride);
     }
     if (lane == 0) {
         p.chunk_sums[chunk] = all;
@@ -978,17 +981,6 @@ __global__ __launch_bounds__(256) void sums_kernel(const Long p)
 
 constexpr int DRAW_THREADS = 512, MOST_CHUNKS = 4096;
 
-// sums of a wavefront's lanes up to and including each
-__device__ __forceinline__ double wave_sums(double x)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int stride = 1; stride < 64; stride <<= 1) {
-        const double other = __shfl_up(x, stride);
-        if (lane >= stride) x += other;
-    }
-    return x;
-}
 // Of a wavefront's lanes with a weight, the first whose sum passes the target, or the last
 __device__ __forceinline__ int lane_of(double w, double to, double target)
 {
@@ -1067,12 +1059,446 @@ __global__ __launch_bounds__(DRAW_THREADS) void draws_kernel(const Long p, uint3
                 of_found = __shfl(w, l);
             }
             if (__ballot(w > 0.0 && up_to > left)) break;
-            left -= __shfl(up_to, 63);
+            left -= of_lane(up_to, 63);
         }
         if (lane == 0) {
             p.a.idx[segment * p.a.draws + d] = (uint32_t)found;
             if (p.a.logprob) p.a.logprob[segment * p.a.draws + d] = (float)log(of_found / all);
         }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ long segments, few kept
+//
+// Where k is at most FEW, the k least of a segment fit a block's LDS.  The largest of all threads' least candidates is an upper bound for the
+// k-th least once k threads have any (at 2^18 candidates a third of them lie below it), so one histogram of counts, linear in energy from the
+// least up to that, has bins of some dozens where the k-th lies; what lies below goes to a list, which one block finishes, draws included.
+
+constexpr uint32_t FEW = 4096;
+
+struct Few {
+    Draws a;
+    uint64_t segments;
+    uint32_t pieces;
+    uint64_t piece;
+    Bounds *bounds;   // [segments][pieces]
+    uint32_t *bins;   // [segments][pieces][BINS]
+    uint32_t *joined; // [segments][BINS], of many pieces
+    Segment *segment; // [segments]
+    u64 *below, *at;  // [segments][FEW] each: candidates of the bins below the end's, and of that
+    Equal *equal;     // [segments][pieces]: of the end's bin
+};
+
+// energies from the least up to a bound, in bins of one width
+struct Linear {
+    float least, scale;
+    uint32_t last; // key of the bound
+    __device__ __forceinline__ Linear(uint32_t from, uint32_t to) : least(energy_of(from)), last(to)
+    {
+        const float width = energy_of(to) - least;
+        scale = width > 0.0f ? (float)BINS / width : 0.0f;
+        if (!(scale < __builtin_inff())) scale = 0.0f;
+    }
+    // (every step keeps the order of energies: subtraction, product, rounding down)
+    __device__ __forceinline__ uint32_t bin(uint32_t key) const { return (uint32_t)fminf((energy_of(key) - least) * scale, (float)(BINS - 1)); }
+};
+
+// how many are kept, and the bound of the range that holds them
+__device__ __forceinline__ uint32_t needed(const Few &p, const Bounds &b) { return min(p.a.k, b.number); }
+__device__ __forceinline__ Linear range_of(const Few &p, const Bounds &b) { return Linear(b.least, b.threads >= needed(p, b) ? b.gate : b.most); }
+
+// keys of a thread's share of a piece, so many at a time
+constexpr int FEW_AHEAD = 8;
+template <class F>
+__device__ __forceinline__ void some_of_piece(const Draws &a, uint64_t segment, uint64_t from, uint64_t to, F &&f)
+{
+    const float *energy = a.energy + segment * a.n;
+    const uint8_t *legal = a.legal ? a.legal + segment * a.n : nullptr;
+    for (uint64_t at = from; at < to; at += LONG_THREADS * 4 * FEW_AHEAD) { // (all threads go round as often)
+        uint32_t key[FEW_AHEAD][4];
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k) {
+            const uint64_t here = at + ((uint64_t)k * LONG_THREADS + threadIdx.x) * 4;
+            if (here < to) load_keys(energy, legal, here, to, key[k]);
+            else key[k][0] = key[k][1] = key[k][2] = key[k][3] = NO_KEY;
+        }
+        f(key, (uint32_t)at + threadIdx.x * 4);
+    }
+}
+
+__global__ __launch_bounds__(LONG_THREADS) void few_bounds_kernel(const Few p)
+{
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    Bounds b = {NO_KEY, 0, 0, 0, 0};
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
+        b.least = min(b.least, key);
+        b.most = max(b.most, key);
+        ++b.number;
+    });
+    if (b.number) b.gate = b.least, b.threads = 1;
+    b = block_bounds(b, of_waves);
+    if (threadIdx.x == 0) p.bounds[blockIdx.x] = b;
+}
+
+__device__ __forceinline__ Bounds few_bounds(const Few &p, uint64_t segment, Bounds *of_waves)
+{
+    Bounds b = {NO_KEY, 0, 0, 0, 0};
+    if (threadIdx.x < p.pieces) b = p.bounds[segment * p.pieces + threadIdx.x];
+    return block_bounds(b, of_waves);
+}
+
+__global__ __launch_bounds__(LONG_THREADS) void few_bins_kernel(const Few p)
+{
+    __shared__ uint32_t bins[BINS];
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) bins[b] = 0;
+    const Bounds b = few_bounds(p, segment, of_waves); // (and barriers)
+    if (blockIdx.x % p.pieces == 0 && threadIdx.x == 0) {
+        Segment &of = p.segment[segment];
+        of.least = b.least, of.most = b.most, of.number = b.number, of.listed = 0, of.listed_below = 0;
+    }
+    if (b.number == 0) return;
+    const Linear range = range_of(p, b);
+    some_of_piece(p.a, segment, from, to, [&](const uint32_t(&key)[FEW_AHEAD][4], uint32_t) {
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (key[k][i] <= range.last) atomicAdd(&bins[range.bin(key[k][i])], 1u);
+    });
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < BINS; i += LONG_THREADS) p.bins[(uint64_t)blockIdx.x * BINS + i] = bins[i];
+}
+
+constexpr uint32_t JOINED_ABOVE = 16; // pieces whose bins are not added up by every block that reads them
+
+__global__ __launch_bounds__(256) void few_join_kernel(const Few p)
+{
+    const uint64_t segment = blockIdx.x / (BINS / 256);
+    const uint32_t b = blockIdx.x % (BINS / 256) * 256 + threadIdx.x;
+    uint32_t count = 0;
+#pragma unroll 8
+    for (uint32_t i = 0; i < p.pieces; ++i) count += p.bins[(segment * p.pieces + i) * BINS + b];
+    p.joined[segment * BINS + b] = count;
+}
+
+__global__ __launch_bounds__(LONG_THREADS) void few_list_kernel(const Few p)
+{
+    __shared__ Bounds of_waves[LONG_THREADS / 64];
+    __shared__ uint32_t small[LONG_THREADS / 64], found[3];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    const uint32_t lane = threadIdx.x & 63;
+    // the bin of the last that is kept
+    static_assert(BINS == 2 * LONG_THREADS, "two bins a thread");
+    uint32_t two[2] = {0, 0};
+    if (p.pieces > JOINED_ABOVE) {
+        two[0] = p.joined[segment * BINS + 2 * threadIdx.x], two[1] = p.joined[segment * BINS + 2 * threadIdx.x + 1];
+    } else {
+        for (uint32_t i = 0; i < p.pieces; ++i) {
+            const uint2 some = *reinterpret_cast<const uint2 *>(p.bins + (segment * p.pieces + i) * BINS + 2 * threadIdx.x);
+            two[0] += some.x, two[1] += some.y;
+        }
+    }
+    const Bounds b = few_bounds(p, segment, of_waves);
+    if (b.number == 0) return;
+    const uint32_t need = needed(p, b);
+    const uint32_t up_to = block_prefix<LONG_THREADS>(two[0] + two[1], small), before = up_to - two[0] - two[1];
+    if (before < need && up_to >= need) {
+        const bool second = before + two[0] < need;
+        found[0] = 2 * threadIdx.x + second;
+        found[1] = before + (second ? two[0] : 0);
+        found[2] = two[second];
+    }
+    __syncthreads();
+    const uint32_t end = found[0];
+    Segment &of = p.segment[segment];
+    if (blockIdx.x % p.pieces == 0 && threadIdx.x == 0) of.before = found[1], of.at_end = found[2], of.need = need;
+
+    const Linear range = range_of(p, b);
+    Bounds equal = {NO_KEY, 0, 0, 0, 0};
+    some_of_piece(p.a, segment, from, to, [&](const uint32_t(&key)[FEW_AHEAD][4], uint32_t first) {
+        // which are below the end's bin and which in it: a place in a list for each of a wavefront's at once
+        uint32_t below = 0, at = 0, state[FEW_AHEAD / 4] = {};
+        static_assert(FEW_AHEAD % 4 == 0, "two bits a candidate");
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = key[k][i], bin = x <= range.last ? range.bin(x) : BINS;
+                const uint32_t is_below = bin < end, is_at = bin == end;
+                below += is_below;
+                at += is_at;
+                state[k / 4] |= (is_below | is_at << 1) << (k % 4 * 8 + i * 2);
+            }
+        if (__ballot(below | at) == 0) return;
+        const uint32_t below_to = wave_sums(below), at_to = wave_sums(at);
+        uint32_t place_below = 0, place_at = 0;
+        if (lane == 63) {
+            if (below_to) place_below = atomicAdd(&of.listed_below, below_to);
+            if (at_to) place_at = atomicAdd(&of.listed, at_to);
+        }
+        place_below = of_lane(place_below, 63) + below_to - below;
+        place_at = of_lane(place_at, 63) + at_to - at;
+        if (below | at)
+#pragma unroll
+            for (int k = 0; k < FEW_AHEAD; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t is = state[k / 4] >> (k % 4 * 8 + i * 2) & 3;
+                    if (is == 0) continue;
+                    const u64 one = (u64)key[k][i] << 32 | (first + (uint32_t)k * LONG_THREADS * 4 + i);
+                    if (is == 1) {
+                        if (place_below < FEW) p.below[segment * FEW + place_below] = one;
+                        ++place_below;
+                    } else {
+                        if (place_at < FEW) p.at[segment * FEW + place_at] = one;
+                        ++place_at;
+                        equal.least = min(equal.least, key[k][i]);
+                        equal.most = max(equal.most, key[k][i]);
+                        ++equal.number;
+                    }
+                }
+    });
+    equal = block_bounds(equal, of_waves);
+    if (threadIdx.x == 0) p.equal[blockIdx.x] = {equal.least, equal.most, equal.number, 0};
+}
+
+struct FewLds {
+    LongScratch s;
+    Bounds of_waves[LONG_THREADS / 64];
+    double real[LONG_THREADS / 64];
+    uint32_t entries, which_piece, left_there;
+    u64 kept[FEW];
+    double to[FEW];
+    union {
+        Histogram bins;
+        struct {
+            u64 scattered[FEW];
+            uint32_t start[BINS + 1];
+        };
+    };
+};
+
+// Candidates in the LDS, in any order, up to a cut
+struct Listed {
+    const u64 *kept;
+    uint32_t number;
+    uint32_t &found;
+    template <class F>
+    __device__ __forceinline__ void each(F &&f) const
+    {
+        for (uint32_t i = threadIdx.x; i < number; i += LONG_THREADS) f((uint32_t)(kept[i] >> 32), (uint32_t)kept[i]);
+    }
+    __device__ uint32_t nth(uint32_t of, uint32_t j) const
+    {
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < number; i += LONG_THREADS) {
+            if ((uint32_t)(kept[i] >> 32) != of) continue;
+            uint32_t rank = 1;
+            for (uint32_t o = 0; o < number; ++o) rank += (uint32_t)(kept[o] >> 32) == of && (uint32_t)kept[o] < (uint32_t)kept[i];
+            if (rank == j) found = (uint32_t)kept[i];
+        }
+        __syncthreads();
+        return found;
+    }
+};
+
+__global__ __launch_bounds__(LONG_THREADS) void few_draws_kernel(const Few p)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    FewLds &l = *reinterpret_cast<FewLds *>(lds);
+    LongScratch &s = l.s;
+    const Draws &a = p.a;
+    const uint64_t segment = blockIdx.x;
+    const Segment &of = p.segment[segment];
+    if (of.number == 0) {
+        nothing_to_draw(a, segment, threadIdx.x, LONG_THREADS);
+        if (threadIdx.x == 0 && a.count) a.count[segment] = 0;
+        return;
+    }
+    const uint32_t need = of.need, at_end = of.at_end, below = of.before;
+    const double best = (double)energy_of(of.least);
+    const auto weight = [&](uint32_t key) { return weight_of(key, best, a.per_temperature); };
+    const Stream stream = {a, segment, l.of_waves};
+
+    // the k least
+    const u64 *list = p.at + segment * FEW;
+    if (at_end <= (uint32_t)LongScratch::LIST) {
+        for (uint32_t i = threadIdx.x; i < at_end; i += LONG_THREADS) s.list[i] = list[i];
+        sort_list<LONG_THREADS>(s, at_end);
+        if (threadIdx.x == 0) {
+            const u64 one = s.sorted[min(max(need - below, 1u), at_end) - 1];
+            s.cut = {(uint32_t)(one >> 32), (uint32_t)one};
+        }
+    } else {
+        const Equal *equal = p.equal + segment * p.pieces;
+        Bounds b = {NO_KEY, 0, 0, 0, 0};
+        if (threadIdx.x < p.pieces) b = {equal[threadIdx.x].least, equal[threadIdx.x].most, equal[threadIdx.x].number, 0, 0};
+        const uint32_t mine = b.number, j = need - below;
+        b = block_bounds(b, l.of_waves);
+        if (b.least == b.most) { // all equal: by index, from the piece that holds the last one
+            if (threadIdx.x == 0) l.which_piece = 0, l.left_there = 1;
+            const uint32_t to = block_prefix<LONG_THREADS>(mine, s.small); // (and a barrier)
+            if (to >= j && to - mine < j) {
+                l.which_piece = threadIdx.x;
+                l.left_there = j - (to - mine);
+            }
+            __syncthreads();
+            const uint64_t from = l.which_piece * p.piece;
+            const uint32_t index = stream.nth_from(from, min(a.n, from + p.piece), b.least, l.left_there);
+            if (threadIdx.x == 0) s.cut = {b.least, index};
+        } else { // so many next to each other, or one candidate far below all others
+            find_cut<LONG_THREADS>(s, l.bins, {of.least, of.most, of.number, 0, {0, 0}}, {false, need, {0.0, 0.0}}, false, stream, weight);
+        }
+    }
+    if (threadIdx.x == 0) l.entries = 0;
+    __syncthreads();
+    Cut cut = s.cut;
+    const auto keep = [&](u64 one) {
+        const uint32_t place = atomicAdd(&l.entries, 1u);
+        if (place < FEW) l.kept[place] = one;
+    };
+    if (at_end <= FEW) {
+        for (uint32_t i = threadIdx.x; i < below; i += LONG_THREADS) keep(p.below[segment * FEW + i]);
+        for (uint32_t i = threadIdx.x; i < at_end; i += LONG_THREADS)
+            if (within((uint32_t)(list[i] >> 32), (uint32_t)list[i], cut)) keep(list[i]);
+    } else { // (more than the list takes: from the candidates themselves)
+        stream.each([&](uint32_t key, uint32_t index) {
+            if (within(key, index, cut)) keep((u64)key << 32 | index);
+        });
+    }
+    __syncthreads();
+    const uint32_t entries = min(l.entries, FEW);
+
+    // a share of their weight
+    if (a.top_p < 1.0 && entries > 1) {
+        Mass mine = {0, 0};
+        for (uint32_t i = threadIdx.x; i < entries; i += LONG_THREADS) mine = mine + mass_of(weight((uint32_t)(l.kept[i] >> 32)));
+        const u64 high = block_prefix<LONG_THREADS>((u64)mine.high, s.wide[0]), low = block_prefix<LONG_THREADS>((u64)mine.low, s.wide[1]);
+        __syncthreads();
+        if (threadIdx.x == LONG_THREADS - 1) s.total = {high, low};
+        __syncthreads();
+        const double target = a.top_p * s.total.value();
+        const Listed listed = {l.kept, entries, s.listed};
+        find_cut<LONG_THREADS>(s, l.bins, {of.least, cut.key, entries, 0, {0, 0}}, {true, 0, {target, target}}, true, listed, weight);
+        cut = s.cut;
+        __syncthreads();
+    }
+
+    // by index: into buckets of neighbouring ones, and in order within each
+    const uint32_t shift = 64 - __builtin_clzll((a.n - 1) | 1) > (int)BIN_BITS ? 64 - __builtin_clzll((a.n - 1) | 1) - BIN_BITS : 0;
+    for (uint32_t i = threadIdx.x; i <= BINS; i += LONG_THREADS) l.start[i] = 0;
+    __syncthreads();
+    const auto stays = [&](u64 one) {
+        const uint32_t key = (uint32_t)(one >> 32);
+        return within(key, (uint32_t)one, cut) && (a.min_p <= 0.0 || weight(key) >= a.min_p);
+    };
+    constexpr int EACH = FEW / LONG_THREADS;
+    u64 mine[EACH];
+    uint32_t bucket[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint32_t e = threadIdx.x + i * LONG_THREADS;
+        bucket[i] = BINS;
+        if (e < entries) {
+            mine[i] = l.kept[e];
+            if (stays(mine[i])) {
+                bucket[i] = (uint32_t)mine[i] >> shift;
+                atomicAdd(&l.start[bucket[i]], 1u);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t count[2] = {l.start[2 * threadIdx.x], l.start[2 * threadIdx.x + 1]};
+    const uint32_t up_to = block_prefix<LONG_THREADS>(count[0] + count[1], s.small); // (and barriers)
+    l.start[2 * threadIdx.x] = up_to - count[1] - count[0];
+    l.start[2 * threadIdx.x + 1] = up_to - count[1];
+    if (threadIdx.x == LONG_THREADS - 1) l.entries = up_to;
+    __syncthreads();
+    const uint32_t kept = l.entries;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (bucket[i] < BINS) l.scattered[atomicAdd(&l.start[bucket[i]], 1u)] = (u64)(uint32_t)mine[i] << 32 | (uint32_t)(mine[i] >> 32);
+    __syncthreads();
+    // (a bucket's start is now its end)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (bucket[i] == BINS) continue;
+        const uint32_t from = bucket[i] ? l.start[bucket[i] - 1] : 0, to = l.start[bucket[i]];
+        uint32_t place = from;
+        for (uint32_t o = from; o < to; ++o) place += (uint32_t)(l.scattered[o] >> 32) < (uint32_t)mine[i];
+        l.kept[place] = mine[i];
+    }
+    __syncthreads();
+
+    double w[EACH], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint32_t e = threadIdx.x * EACH + i;
+        w[i] = e < kept ? weight((uint32_t)(l.kept[e] >> 32)) : 0.0;
+        sum += w[i];
+    }
+    double to = block_prefix<LONG_THREADS>(sum, l.real) - sum;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        to += w[i];
+        l.to[threadIdx.x * EACH + i] = to;
+    }
+    if (threadIdx.x == 0 && a.count) a.count[segment] = kept;
+    __syncthreads();
+    const double all = l.to[kept - 1];
+    for (uint32_t d = threadIdx.x; d < a.draws; d += LONG_THREADS) {
+        const double target = fmax((double)a.uniform[segment * a.draws + d] * all, 0.0);
+        uint32_t lo = 0, hi = kept - 1;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (l.to[mid] > target) hi = mid;
+            else lo = mid + 1;
+        }
+        double x = weight((uint32_t)(l.kept[lo] >> 32));
+        while (!(x > 0.0) && lo + 1 < kept && all > target) x = weight((uint32_t)(l.kept[++lo] >> 32));
+        while (!(x > 0.0) && lo > 0) x = weight((uint32_t)(l.kept[--lo] >> 32));
+        a.idx[segment * a.draws + d] = (uint32_t)l.kept[lo];
+        if (a.logprob) a.logprob[segment * a.draws + d] = (float)log(x / all);
+    }
+}
+
+// k = 1: the first of the least, in every draw
+__global__ __launch_bounds__(LONG_THREADS) void least_kernel(const Few p)
+{
+    __shared__ u64 of_waves[LONG_THREADS / 64];
+    const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    u64 least = ~0ull;
+    each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t index) { least = min(least, (u64)key << 32 | index); });
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) least = min(least, (u64)lane_exchange((uint64_t)least, stride));
+    if ((threadIdx.x & 63) == 0) of_waves[threadIdx.x / 64] = least;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < LONG_THREADS / 64; ++w) least = min(least, of_waves[w]);
+    p.below[blockIdx.x] = least;
+}
+__global__ __launch_bounds__(256) void least_draws_kernel(const Few p)
+{
+    const uint64_t segment = blockIdx.x;
+    __shared__ u64 of_waves[4];
+    u64 least = ~0ull;
+    for (uint32_t i = threadIdx.x; i < p.pieces; i += 256) least = min(least, p.below[segment * p.pieces + i]);
+#pragma unroll
+    for (int stride = 1; stride < 64; stride <<= 1) least = min(least, (u64)lane_exchange((uint64_t)least, stride));
+    if ((threadIdx.x & 63) == 0) of_waves[threadIdx.x / 64] = least;
+    __syncthreads();
+    least = min(min(of_waves[0], of_waves[1]), min(of_waves[2], of_waves[3]));
+    if (threadIdx.x == 0 && p.a.count) p.a.count[segment] = least != ~0ull;
+    if (least == ~0ull) {
+        nothing_to_draw(p.a, segment, threadIdx.x, 256);
+        return;
+    }
+    for (uint32_t d = threadIdx.x; d < p.a.draws; d += 256) {
+        p.a.idx[segment * p.a.draws + d] = (uint32_t)least;
+        if (p.a.logprob) p.a.logprob[segment * p.a.draws + d] = 0.0f;
     }
 }
 
@@ -1111,6 +1537,29 @@ uint64_t lay_out(Long &p, void *ws)
     return (uint64_t)(at - (char *)ws);
 }
 
+uint64_t lay_out_few(Few &p, void *ws)
+{
+    const uint64_t n = p.a.n, s = p.segments;
+    uint64_t pieces = (MOST_PIECES + s - 1) / s;
+    if (pieces > (n + 32767) / 32768) pieces = (n + 32767) / 32768;
+    p.piece = ((n + pieces - 1) / pieces + 4095) / 4096 * 4096;
+    p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
+    char *at = (char *)ws;
+    const auto take = [&](uint64_t bytes) {
+        char *here = at;
+        at += padded(bytes);
+        return (void *)here;
+    };
+    p.segment = (Segment *)take(s * sizeof(Segment));
+    p.bounds = (Bounds *)take(s * p.pieces * sizeof(Bounds));
+    p.bins = (uint32_t *)take(s * p.pieces * BINS * 4);
+    p.joined = (uint32_t *)take(p.pieces > JOINED_ABOVE ? s * BINS * 4 : 0);
+    p.below = (u64 *)take(s * FEW * sizeof(u64));
+    p.at = (u64 *)take(s * FEW * sizeof(u64));
+    p.equal = (Equal *)take(s * p.pieces * sizeof(Equal));
+    return (uint64_t)(at - (char *)ws);
+}
+
 template <int THREADS, int EACH>
 int32_t launch_short(const Draws &a, uint32_t segments, hipStream_t st)
 {
@@ -1118,6 +1567,28 @@ int32_t launch_short(const Draws &a, uint32_t segments, hipStream_t st)
     if (bytes > 65536)
         ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(short_kernel<THREADS, EACH>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     hipLaunchKernelGGL((short_kernel<THREADS, EACH>), dim3(segments), dim3(THREADS), bytes, st, a);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+
+int32_t launch_few(const Draws &a, uint32_t segments, void *ws, hipStream_t st)
+{
+    Few p;
+    p.a = a;
+    p.segments = segments;
+    lay_out_few(p, ws);
+    const dim3 pieces(segments * p.pieces), threads(LONG_THREADS);
+    if (a.k == 1) {
+        hipLaunchKernelGGL(least_kernel, pieces, threads, 0, st, p);
+        hipLaunchKernelGGL(least_draws_kernel, dim3(segments), dim3(256), 0, st, p);
+    } else {
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(few_draws_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewLds)));
+        hipLaunchKernelGGL(few_bounds_kernel, pieces, threads, 0, st, p);
+        hipLaunchKernelGGL(few_bins_kernel, pieces, threads, 0, st, p);
+        if (p.pieces > JOINED_ABOVE) hipLaunchKernelGGL(few_join_kernel, dim3(segments * (BINS / 256)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL(few_list_kernel, pieces, threads, 0, st, p);
+        hipLaunchKernelGGL(few_draws_kernel, dim3(segments), threads, sizeof(FewLds), st, p);
+    }
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
 }
@@ -1163,10 +1634,14 @@ extern "C" uint64_t sample_select_workspace_bytes(uint64_t n, uint32_t n_segment
 {
     if (n == 0 || n_segments == 0 || draws == 0 || n % n_segments || n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS) return 0;
     if (n / n_segments <= SHORT) return 0;
-    Long p;
+    Long p; // (the query does not know k: room for either way)
     p.a.n = n / n_segments;
     p.segments = n_segments;
-    return lay_out(p, nullptr);
+    Few f;
+    f.a.n = p.a.n;
+    f.segments = n_segments;
+    const uint64_t all = lay_out(p, nullptr), few = lay_out_few(f, nullptr);
+    return all > few ? all : few;
 }
 
 extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint64_t n, uint32_t n_segments, const float *uniform, uint32_t draws,
@@ -1194,6 +1669,8 @@ extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint
     if (a.n <= 256) return launch_short<64, 4>(a, n_segments, st);
     if (a.n <= 1024) return launch_short<256, 4>(a, n_segments, st);
     if (a.n <= 4096) return launch_short<512, 8>(a, n_segments, st);
+    if (a.n <= 8192) return launch_short<1024, 8>(a, n_segments, st);
     if (a.n <= SHORT) return launch_short<1024, 16>(a, n_segments, st);
+    if (a.k && a.k <= FEW) return launch_few(a, n_segments, ws, st);
     return launch_long(a, n_segments, ws, st);
 }

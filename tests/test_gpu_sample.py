@@ -180,6 +180,25 @@ def test_long_and_many_segments(seg, n):
     check(e, flags, u, temperature=0.2, top_p=0.9)
 
 
+@pytest.mark.parametrize("k", [2, 1023, 1025, 4095, 4096, 4097, 30000])
+@pytest.mark.parametrize("legal", [0.9, 0.01, 0.00005])
+def test_few_and_many_of_long_segments(k, legal):
+    e, flags, u = inputs(3, 60000, 300, k, legal=legal)
+    for how in (dict(), dict(top_p=0.8), dict(min_p=0.3), dict(top_p=0.95, min_p=0.001)):
+        check(e, flags, u, temperature=0.1, k=k, **how)
+
+
+@pytest.mark.parametrize("n", [17000, 100000])
+def test_the_kept_all_next_to_each_other(n):
+    """the best candidates neighbours by index, equal ones among them"""
+    e, _, u = inputs(2, n, 64, n)
+    e[0, 5000:9000] = np.sort(np.random.default_rng(1).random(4000).astype(np.float32)) - 3
+    e[1, 5000:9000] = -3
+    e[1, 6000:9000:2] = -3.25
+    for how in (dict(k=4000), dict(k=3000, top_p=0.5), dict(k=2500), dict(k=1700, top_p=0.9), dict(k=4096, min_p=0.2)):
+        check(e, None, u, temperature=0.4, **how)
+
+
 def test_draws_come_as_often_as_their_weights():
     """40 000 draws over 16 candidates: counts within six standard deviations"""
     e = np.linspace(0.0, 1.5, 16, dtype=np.float32)[None]
