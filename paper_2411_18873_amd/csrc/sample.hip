@@ -295,6 +295,21 @@ __device__ __forceinline__ uint32_t last_of_equal(S &s, const Range &at, const G
     return j;
 }
 
+// energies from the least up to a bound, in bins of one width
+struct Linear {
+    float least, last, scale;
+    __device__ __forceinline__ Linear(uint32_t from, uint32_t to) : least(energy_of(from)), last(energy_of(to))
+    {
+        const float width = last - least;
+        scale = width > 0.0f ? (float)BINS / width : 0.0f;
+        if (!(scale < __builtin_inff())) scale = 0.0f;
+    }
+    __device__ __forceinline__ bool holds(float e) const { return e >= least && e <= last; } // (no NaN)
+    // the bin is this rounded down: every step keeps the order of energies (a width past fp32's range times 0 is taken for the last bin's)
+    __device__ __forceinline__ float place(float e) const { return fminf((e - least) * scale, (float)(BINS - 1)); }
+    __device__ __forceinline__ uint32_t bin(float e) const { return (uint32_t)place(e); }
+};
+
 // The end of a prefix within the range `at`, from the candidates themselves: source.each(f) calls f(key, index) for those that may be drawn,
 // source.nth(key, j) is the index of the j-th one of a key.  Sets s.cut and s.total.
 template <int THREADS, class S, class Source, class W>
@@ -328,6 +343,34 @@ __device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool
         __syncthreads();
         at = narrow<THREADS>(s, bins, at, goal, weights);
     }
+}
+
+// The same over all keys from..to of the source, `number` candidates, most of them far from each other: a first histogram linear in energy has
+// few of them in a bin, and none that all threads add to at once
+template <int THREADS, class S, class Source, class W>
+__device__ void find_cut_of(S &s, Histogram &bins, uint32_t from, uint32_t to, uint32_t number, const Goal &goal, bool weights, const Source &source,
+                            W &&weight)
+{
+    if (number > (uint32_t)S::LIST) {
+        const Linear linear(from, to);
+        clear_bins<THREADS>(bins, weights);
+        source.each([&](uint32_t key, uint32_t) { add_to_bins(bins, linear.bin(energy_of(key)), weights, weights ? weight(key) : 0.0); });
+        __syncthreads();
+        const Range bin = narrow<THREADS>(s, bins, {0, BINS - 1, number, 0, {0, 0}}, goal, weights);
+        if (bin.number <= (uint32_t)S::LIST && bin.lo == bin.hi) {
+            if (threadIdx.x == 0) s.listed = 0;
+            __syncthreads();
+            source.each([&](uint32_t key, uint32_t index) {
+                if (linear.bin(energy_of(key)) != bin.lo) return;
+                const uint32_t place = atomicAdd(&s.listed, 1u);
+                if (place < (uint32_t)S::LIST) s.list[place] = (u64)key << 32 | index;
+            });
+            sort_list<THREADS>(s, bin.number);
+            cut_sorted<THREADS>(s, bin, goal, weights, weight);
+            return;
+        }
+    }
+    find_cut<THREADS>(s, bins, {from, to, number, 0, {0, 0}}, goal, weights, source, weight);
 }
 
 __device__ __forceinline__ void nothing_to_draw(const Draws &a, uint64_t segment, uint32_t first, uint32_t step)
@@ -445,7 +488,7 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
             if (a.k == 1) { // the first of the least
                 found = {least, held.nth(least, 1)};
             } else {
-                find_cut<THREADS>(sc, bins, {least, most, number, 0, {0, 0}}, {false, a.k, {0.0, 0.0}}, false, held, weight);
+                find_cut_of<THREADS>(sc, bins, least, most, number, {false, a.k, {0.0, 0.0}}, false, held, weight);
                 found = sc.cut;
                 __syncthreads();
             }
@@ -465,7 +508,7 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
             if (threadIdx.x == THREADS - 1) sc.total = {high, low};
             __syncthreads();
             const double target = a.top_p * sc.total.value();
-            find_cut<THREADS>(sc, bins, {least, cut.key, kept, 0, {0, 0}}, {true, 0, {target, target}}, true, held, weight);
+            find_cut_of<THREADS>(sc, bins, least, cut.key, kept, {true, 0, {target, target}}, true, held, weight);
             cut = sc.cut;
         }
     }
@@ -1089,42 +1132,38 @@ struct Few {
     Equal *equal;     // [segments][pieces]: of the end's bin
 };
 
-// energies from the least up to a bound, in bins of one width
-struct Linear {
-    float least, scale;
-    uint32_t last; // key of the bound
-    __device__ __forceinline__ Linear(uint32_t from, uint32_t to) : least(energy_of(from)), last(to)
-    {
-        const float width = energy_of(to) - least;
-        scale = width > 0.0f ? (float)BINS / width : 0.0f;
-        if (!(scale < __builtin_inff())) scale = 0.0f;
-    }
-    // (every step keeps the order of energies: subtraction, product, rounding down)
-    __device__ __forceinline__ uint32_t bin(uint32_t key) const { return (uint32_t)fminf((energy_of(key) - least) * scale, (float)(BINS - 1)); }
-};
-
 // how many are kept, and the bound of the range that holds them
 __device__ __forceinline__ uint32_t needed(const Few &p, const Bounds &b) { return min(p.a.k, b.number); }
 __device__ __forceinline__ Linear range_of(const Few &p, const Bounds &b) { return Linear(b.least, b.threads >= needed(p, b) ? b.gate : b.most); }
 
-// keys of a thread's share of a piece, so many at a time
+// energies of a thread's share of a piece, so many at a time, and NaN where there is no legal candidate
 constexpr int FEW_AHEAD = 8;
-template <class F>
-__device__ __forceinline__ void some_of_piece(const Draws &a, uint64_t segment, uint64_t from, uint64_t to, F &&f)
-{
-    const float *energy = a.energy + segment * a.n;
-    const uint8_t *legal = a.legal ? a.legal + segment * a.n : nullptr;
-    for (uint64_t at = from; at < to; at += LONG_THREADS * 4 * FEW_AHEAD) { // (all threads go round as often)
-        uint32_t key[FEW_AHEAD][4];
+constexpr uint64_t FEW_ROUND = (uint64_t)LONG_THREADS * 4 * FEW_AHEAD; // of a block
+struct Some {
+    Chunk<float, 4> four[FEW_AHEAD];
+    Chunk<uint8_t, 4> flags[FEW_AHEAD];
+    // from candidate `at` of a segment on, up to `to`
+    __device__ __forceinline__ void load(const float *energy, const uint8_t *legal, uint64_t at, uint64_t to)
+    {
 #pragma unroll
         for (int k = 0; k < FEW_AHEAD; ++k) {
             const uint64_t here = at + ((uint64_t)k * LONG_THREADS + threadIdx.x) * 4;
-            if (here < to) load_keys(energy, legal, here, to, key[k]);
-            else key[k][0] = key[k][1] = key[k][2] = key[k][3] = NO_KEY;
+            if (here + 4 <= to) {
+                four[k] = *reinterpret_cast<const Chunk<float, 4> *>(energy + here);
+                if (legal) flags[k] = *reinterpret_cast<const Chunk<uint8_t, 4> *>(legal + here);
+                else flags[k].v = 1;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool there = here + i < to;
+                    four[k].v[i] = there ? energy[here + i] : 0.0f;
+                    flags[k].v[i] = there && (!legal || legal[here + i]);
+                }
+            }
         }
-        f(key, (uint32_t)at + threadIdx.x * 4);
     }
-}
+    __device__ __forceinline__ float energy(int k, int i) const { return flags[k].v[i] ? four[k].v[i] : __builtin_nanf(""); }
+};
 
 __global__ __launch_bounds__(LONG_THREADS) void few_bounds_kernel(const Few p)
 {
@@ -1153,6 +1192,10 @@ __global__ __launch_bounds__(LONG_THREADS) void few_bins_kernel(const Few p)
     __shared__ uint32_t bins[BINS];
     __shared__ Bounds of_waves[LONG_THREADS / 64];
     const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
+    const float *energy = p.a.energy + segment * p.a.n;
+    const uint8_t *legal = p.a.legal ? p.a.legal + segment * p.a.n : nullptr;
+    Some now; // (on its way while the range is worked out)
+    now.load(energy, legal, from, to);
     for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) bins[b] = 0;
     const Bounds b = few_bounds(p, segment, of_waves); // (and barriers)
     if (blockIdx.x % p.pieces == 0 && threadIdx.x == 0) {
@@ -1161,13 +1204,18 @@ __global__ __launch_bounds__(LONG_THREADS) void few_bins_kernel(const Few p)
     }
     if (b.number == 0) return;
     const Linear range = range_of(p, b);
-    some_of_piece(p.a, segment, from, to, [&](const uint32_t(&key)[FEW_AHEAD][4], uint32_t) {
+    for (uint64_t at = from;;) {
 #pragma unroll
         for (int k = 0; k < FEW_AHEAD; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (key[k][i] <= range.last) atomicAdd(&bins[range.bin(key[k][i])], 1u);
-    });
+            for (int i = 0; i < 4; ++i) {
+                const float e = now.energy(k, i);
+                if (range.holds(e)) atomicAdd(&bins[range.bin(e)], 1u);
+            }
+        at += FEW_ROUND;
+        if (at >= to) break;
+        now.load(energy, legal, at, to);
+    }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < BINS; i += LONG_THREADS) p.bins[(uint64_t)blockIdx.x * BINS + i] = bins[i];
 }
@@ -1189,17 +1237,22 @@ __global__ __launch_bounds__(LONG_THREADS) void few_list_kernel(const Few p)
     __shared__ Bounds of_waves[LONG_THREADS / 64];
     __shared__ uint32_t small[LONG_THREADS / 64], found[3];
     const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
-    const uint32_t lane = threadIdx.x & 63;
+    const float *energy = p.a.energy + segment * p.a.n;
+    const uint8_t *legal = p.a.legal ? p.a.legal + segment * p.a.n : nullptr;
+    Some now; // (on its way while the end's bin is looked for)
+    now.load(energy, legal, from, to);
     // the bin of the last that is kept
     static_assert(BINS == 2 * LONG_THREADS, "two bins a thread");
     uint32_t two[2] = {0, 0};
     if (p.pieces > JOINED_ABOVE) {
         two[0] = p.joined[segment * BINS + 2 * threadIdx.x], two[1] = p.joined[segment * BINS + 2 * threadIdx.x + 1];
     } else {
-        for (uint32_t i = 0; i < p.pieces; ++i) {
-            const uint2 some = *reinterpret_cast<const uint2 *>(p.bins + (segment * p.pieces + i) * BINS + 2 * threadIdx.x);
-            two[0] += some.x, two[1] += some.y;
-        }
+        uint2 some[JOINED_ABOVE];
+#pragma unroll
+        for (uint32_t i = 0; i < JOINED_ABOVE; ++i)
+            some[i] = i < p.pieces ? *reinterpret_cast<const uint2 *>(p.bins + (segment * p.pieces + i) * BINS + 2 * threadIdx.x) : make_uint2(0, 0);
+#pragma unroll
+        for (uint32_t i = 0; i < JOINED_ABOVE; ++i) two[0] += some[i].x, two[1] += some[i].y;
     }
     const Bounds b = few_bounds(p, segment, of_waves);
     if (b.number == 0) return;
@@ -1215,52 +1268,65 @@ __global__ __launch_bounds__(LONG_THREADS) void few_list_kernel(const Few p)
     const uint32_t end = found[0];
     Segment &of = p.segment[segment];
     if (blockIdx.x % p.pieces == 0 && threadIdx.x == 0) of.before = found[1], of.at_end = found[2], of.need = need;
+    // (found is written again after the next barrier)
 
     const Linear range = range_of(p, b);
     Bounds equal = {NO_KEY, 0, 0, 0, 0};
-    some_of_piece(p.a, segment, from, to, [&](const uint32_t(&key)[FEW_AHEAD][4], uint32_t first) {
-        // which are below the end's bin and which in it: a place in a list for each of a wavefront's at once
-        uint32_t below = 0, at = 0, state[FEW_AHEAD / 4] = {};
-        static_assert(FEW_AHEAD % 4 == 0, "two bits a candidate");
+    const float from_here = (float)end, to_here = end == BINS - 1 ? __builtin_inff() : (float)(end + 1);
+    for (uint64_t here = from;;) {
+        const uint32_t first = (uint32_t)here + threadIdx.x * 4;
+        // which are below the end's bin and which in it: a place in a list for each of a block's at once
+        uint32_t below = 0, at = 0;
+        static_assert(FEW_AHEAD * 4 <= 32, "a bit a candidate");
 #pragma unroll
         for (int k = 0; k < FEW_AHEAD; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t x = key[k][i], bin = x <= range.last ? range.bin(x) : BINS;
-                const uint32_t is_below = bin < end, is_at = bin == end;
-                below += is_below;
-                at += is_at;
-                state[k / 4] |= (is_below | is_at << 1) << (k % 4 * 8 + i * 2);
+                const float e = now.energy(k, i), place = range.place(e);
+                const bool held = range.holds(e);
+                below |= (uint32_t)(held && place < from_here) << (4 * k + i);
+                at |= (uint32_t)(held && !(place < from_here) && place < to_here) << (4 * k + i);
             }
-        if (__ballot(below | at) == 0) return;
-        const uint32_t below_to = wave_sums(below), at_to = wave_sums(at);
-        uint32_t place_below = 0, place_at = 0;
-        if (lane == 63) {
-            if (below_to) place_below = atomicAdd(&of.listed_below, below_to);
-            if (at_to) place_at = atomicAdd(&of.listed, at_to);
+        static_assert(FEW_ROUND < 65536, "both counts in a word");
+        const uint32_t counts = __builtin_popcount(below) << 16 | __builtin_popcount(at), counted = block_prefix<LONG_THREADS>(counts, small);
+        __syncthreads();
+        if (threadIdx.x == LONG_THREADS - 1) {
+            found[1] = counted >> 16 ? atomicAdd(&of.listed_below, counted >> 16) : 0;
+            found[2] = counted & 0xFFFF ? atomicAdd(&of.listed, counted & 0xFFFF) : 0;
         }
-        place_below = of_lane(place_below, 63) + below_to - below;
-        place_at = of_lane(place_at, 63) + at_to - at;
-        if (below | at)
+        __syncthreads();
+        uint32_t place_below = found[1] + (counted >> 16) - (counts >> 16), place_at = found[2] + (counted & 0xFFFF) - (counts & 0xFFFF);
+        // few of a thread's are listed; they are read again, some at once
+        for (uint32_t both = below | at; both;) {
+            uint32_t bit[4];
+            float e[4];
 #pragma unroll
-            for (int k = 0; k < FEW_AHEAD; ++k)
+            for (int i = 0; i < 4; ++i) {
+                bit[i] = both ? __builtin_ctz(both) : 32;
+                both &= both - (both != 0);
+                e[i] = bit[i] < 32 ? energy[first + bit[i] / 4 * (LONG_THREADS * 4) + bit[i] % 4] : 0.0f;
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t is = state[k / 4] >> (k % 4 * 8 + i * 2) & 3;
-                    if (is == 0) continue;
-                    const u64 one = (u64)key[k][i] << 32 | (first + (uint32_t)k * LONG_THREADS * 4 + i);
-                    if (is == 1) {
-                        if (place_below < FEW) p.below[segment * FEW + place_below] = one;
-                        ++place_below;
-                    } else {
-                        if (place_at < FEW) p.at[segment * FEW + place_at] = one;
-                        ++place_at;
-                        equal.least = min(equal.least, key[k][i]);
-                        equal.most = max(equal.most, key[k][i]);
-                        ++equal.number;
-                    }
+            for (int i = 0; i < 4; ++i) {
+                if (bit[i] == 32) break;
+                const uint32_t key = key_of(e[i], true);
+                const u64 one = (u64)key << 32 | (first + bit[i] / 4 * (LONG_THREADS * 4) + bit[i] % 4);
+                if (below >> bit[i] & 1) {
+                    if (place_below < FEW) p.below[segment * FEW + place_below] = one;
+                    ++place_below;
+                } else {
+                    if (place_at < FEW) p.at[segment * FEW + place_at] = one;
+                    ++place_at;
+                    equal.least = min(equal.least, key);
+                    equal.most = max(equal.most, key);
+                    ++equal.number;
                 }
-    });
+            }
+        }
+        here += FEW_ROUND;
+        if (here >= to) break;
+        now.load(energy, legal, here, to);
+    }
     equal = block_bounds(equal, of_waves);
     if (threadIdx.x == 0) p.equal[blockIdx.x] = {equal.least, equal.most, equal.number, 0};
 }
@@ -1382,7 +1448,7 @@ __global__ __launch_bounds__(LONG_THREADS) void few_draws_kernel(const Few p)
         __syncthreads();
         const double target = a.top_p * s.total.value();
         const Listed listed = {l.kept, entries, s.listed};
-        find_cut<LONG_THREADS>(s, l.bins, {of.least, cut.key, entries, 0, {0, 0}}, {true, 0, {target, target}}, true, listed, weight);
+        find_cut_of<LONG_THREADS>(s, l.bins, of.least, cut.key, entries, {true, 0, {target, target}}, true, listed, weight);
         cut = s.cut;
         __syncthreads();
     }
