@@ -311,12 +311,12 @@ struct Linear {
 };
 
 // The end of a prefix within the range `at`, from the candidates themselves: source.each(f) calls f(key, index) for those that may be drawn,
-// source.nth(key, j) is the index of the j-th one of a key.  Sets s.cut and s.total.
+// source.nth(key, j) is the index of the j-th one of a key; Source::FITS: a list takes all there can be.  Sets s.cut and s.total.
 template <int THREADS, class S, class Source, class W>
 __device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool weights, const Source &source, W &&weight)
 {
     for (int round = 0; round < 4; ++round) { // (three rounds leave one key)
-        if (at.number <= (uint32_t)S::LIST) {
+        if (Source::FITS || at.number <= (uint32_t)S::LIST) {
             __syncthreads();
             if (threadIdx.x == 0) s.listed = 0;
             __syncthreads();
@@ -329,19 +329,21 @@ __device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool
             cut_sorted<THREADS>(s, at, goal, weights, weight);
             return;
         }
-        if (at.lo == at.hi) {
-            const uint32_t j = last_of_equal(s, at, goal, weight(at.lo)), index = source.nth(at.lo, j);
-            if (threadIdx.x == 0) s.cut = {at.lo, index};
+        if constexpr (!Source::FITS) {
+            if (at.lo == at.hi) {
+                const uint32_t j = last_of_equal(s, at, goal, weight(at.lo)), index = source.nth(at.lo, j);
+                if (threadIdx.x == 0) s.cut = {at.lo, index};
+                __syncthreads();
+                return;
+            }
+            clear_bins<THREADS>(bins, weights);
+            const uint32_t shift = shift_of(at);
+            source.each([&](uint32_t key, uint32_t) {
+                if (key >= at.lo && key <= at.hi) add_to_bins(bins, (key - at.lo) >> shift, weights, weights ? weight(key) : 0.0);
+            });
             __syncthreads();
-            return;
+            at = narrow<THREADS>(s, bins, at, goal, weights);
         }
-        clear_bins<THREADS>(bins, weights);
-        const uint32_t shift = shift_of(at);
-        source.each([&](uint32_t key, uint32_t) {
-            if (key >= at.lo && key <= at.hi) add_to_bins(bins, (key - at.lo) >> shift, weights, weights ? weight(key) : 0.0);
-        });
-        __syncthreads();
-        at = narrow<THREADS>(s, bins, at, goal, weights);
     }
 }
 
@@ -351,7 +353,7 @@ template <int THREADS, class S, class Source, class W>
 __device__ void find_cut_of(S &s, Histogram &bins, uint32_t from, uint32_t to, uint32_t number, const Goal &goal, bool weights, const Source &source,
                             W &&weight)
 {
-    if (number > (uint32_t)S::LIST) {
+    if (!Source::FITS && number > (uint32_t)S::LIST) {
         const Linear linear(from, to);
         clear_bins<THREADS>(bins, weights);
         source.each([&](uint32_t key, uint32_t) { add_to_bins(bins, linear.bin(energy_of(key)), weights, weights ? weight(key) : 0.0); });
@@ -386,6 +388,7 @@ __device__ __forceinline__ void nothing_to_draw(const Draws &a, uint64_t segment
 // Keys of a block's candidates, EACH neighbouring ones a thread; those up to a cut
 template <int THREADS, int EACH, class S>
 struct Held {
+    static constexpr bool FITS = THREADS * EACH <= S::LIST; // all of them in a list
     uint32_t (&key)[EACH];
     S &s;
     const Cut &cut;
@@ -514,22 +517,23 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
     }
     __syncthreads(); // (what is written now lies where that was)
 
-    double w[EACH], sum = 0.0;
+    double sum = 0.0;
     uint32_t kept = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        w[i] = key[i] != NO_KEY && within(key[i], first + i, cut) ? weight(key[i]) : -1.0;
-        const bool stays = w[i] >= a.min_p && w[i] >= 0.0;
-        kept += stays;
-        w[i] = stays ? w[i] : 0.0;
-        sum += w[i];
+        if (within(key[i], first + i, cut)) { // (NO_KEY is above any)
+            const double w = weight(key[i]);
+            if (w >= a.min_p) {
+                sum += w;
+                ++kept;
+            }
+        }
+        if (first + i < n) s.to[first + i] = sum;
     }
-    double to = block_prefix<THREADS>(sum, s.of_waves) - sum;
+    const double before = block_prefix<THREADS>(sum, s.of_waves) - sum;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        to += w[i];
-        if (first + i < n) s.to[first + i] = to;
-    }
+    for (int i = 0; i < EACH; ++i)
+        if (first + i < n) s.to[first + i] += before;
 #pragma unroll
     for (int stride = 1; stride < 64; stride <<= 1) kept += lane_exchange(kept, stride);
     if (lane == 0) s.number[wave] = kept;
@@ -748,7 +752,7 @@ __device__ __forceinline__ Mass mass_in(const Histogram &bins, const Range &at, 
 }
 
 // The ranges that the ends lie in, from the histogram over all keys, and a histogram of each
-__global__ __launch_bounds__(LONG_THREADS) void second_bins_kernel(const Long p)
+__global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8))) void second_bins_kernel(const Long p)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     Histogram *const bins = reinterpret_cast<Histogram *>(lds);
@@ -800,7 +804,7 @@ __global__ __launch_bounds__(LONG_THREADS) void second_bins_kernel(const Long p)
 }
 
 // The ranges again, by the second histograms, and the candidates in them
-__global__ __launch_bounds__(LONG_THREADS) void list_kernel(const Long p)
+__global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8))) void list_kernel(const Long p)
 {
     __shared__ Histogram bins;
     __shared__ LongScratch s;
@@ -857,6 +861,7 @@ __global__ __launch_bounds__(LONG_THREADS) void list_kernel(const Long p)
 
 // All of a segment, for a block by itself
 struct Stream {
+    static constexpr bool FITS = false;
     const Draws &a;
     uint64_t segment;
     Bounds *of_waves;
@@ -1137,7 +1142,7 @@ __device__ __forceinline__ uint32_t needed(const Few &p, const Bounds &b) { retu
 __device__ __forceinline__ Linear range_of(const Few &p, const Bounds &b) { return Linear(b.least, b.threads >= needed(p, b) ? b.gate : b.most); }
 
 // energies of a thread's share of a piece, so many at a time, and NaN where there is no legal candidate
-constexpr int FEW_AHEAD = 8;
+constexpr int FEW_AHEAD = 4;
 constexpr uint64_t FEW_ROUND = (uint64_t)LONG_THREADS * 4 * FEW_AHEAD; // of a block
 struct Some {
     Chunk<float, 4> four[FEW_AHEAD];
@@ -1232,7 +1237,7 @@ __global__ __launch_bounds__(256) void few_join_kernel(const Few p)
     p.joined[segment * BINS + b] = count;
 }
 
-__global__ __launch_bounds__(LONG_THREADS) void few_list_kernel(const Few p)
+__global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8))) void few_list_kernel(const Few p)
 {
     __shared__ Bounds of_waves[LONG_THREADS / 64];
     __shared__ uint32_t small[LONG_THREADS / 64], found[3];
@@ -1247,12 +1252,15 @@ __global__ __launch_bounds__(LONG_THREADS) void few_list_kernel(const Few p)
     if (p.pieces > JOINED_ABOVE) {
         two[0] = p.joined[segment * BINS + 2 * threadIdx.x], two[1] = p.joined[segment * BINS + 2 * threadIdx.x + 1];
     } else {
-        uint2 some[JOINED_ABOVE];
+        for (uint32_t first = 0; first < p.pieces; first += 4) {
+            uint2 some[4];
 #pragma unroll
-        for (uint32_t i = 0; i < JOINED_ABOVE; ++i)
-            some[i] = i < p.pieces ? *reinterpret_cast<const uint2 *>(p.bins + (segment * p.pieces + i) * BINS + 2 * threadIdx.x) : make_uint2(0, 0);
+            for (uint32_t i = 0; i < 4; ++i)
+                some[i] = first + i < p.pieces ? *reinterpret_cast<const uint2 *>(p.bins + (segment * p.pieces + first + i) * BINS + 2 * threadIdx.x)
+                                               : make_uint2(0, 0);
 #pragma unroll
-        for (uint32_t i = 0; i < JOINED_ABOVE; ++i) two[0] += some[i].x, two[1] += some[i].y;
+            for (uint32_t i = 0; i < 4; ++i) two[0] += some[i].x, two[1] += some[i].y;
+        }
     }
     const Bounds b = few_bounds(p, segment, of_waves);
     if (b.number == 0) return;
@@ -1349,6 +1357,7 @@ struct FewLds {
 
 // Candidates in the LDS, in any order, up to a cut
 struct Listed {
+    static constexpr bool FITS = false;
     const u64 *kept;
     uint32_t number;
     uint32_t &found;
