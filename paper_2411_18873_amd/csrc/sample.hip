@@ -52,11 +52,11 @@ struct Mass {
     __device__ __forceinline__ double value() const { return (double)high * 0x1p-30 + (double)low * 0x1p-60; }
     __device__ __forceinline__ Mass operator+(const Mass &o) const { return {high + o.high, low + o.low}; }
 };
-__device__ __forceinline__ Mass mass_of(double w)
+__device__ __forceinline__ Mass mass_of(double w) // (of at most 1: both parts fit 32 bits, to which one instruction converts)
 {
     const double t = w * 0x1p30;
-    const uint64_t high = (uint64_t)t;
-    return {high, (uint64_t)((t - (double)high) * 0x1p30)};
+    const uint32_t high = (uint32_t)t;
+    return {high, (uint32_t)((t - (double)high) * 0x1p30)};
 }
 
 // four candidates from `at` on, as keys
@@ -679,19 +679,42 @@ __device__ __forceinline__ Bounds segment_bounds(const Long &p, uint64_t segment
     return block_bounds(b, of_waves);
 }
 
-__device__ __forceinline__ void write_bins(Histogram &to, const Histogram &from)
+// Places of energies on a scale of 32 bits, linear from the least up to where weights are below e^-64 or energies end: what the share of the
+// weight is looked for with.  (Of order keys a range over both signs has eight bins a binade, which all threads add to at once: first
+// histograms of 2^24 candidates took 51 us.)
+struct Scale {
+    float least, factor;
+    static constexpr uint32_t LAST = 0xFFFFFF00u; // the largest that a float holds
+    __device__ __forceinline__ Scale(const Draws &a, uint32_t least_key, uint32_t most_key) : least(energy_of(least_key))
+    {
+        const float far = (float)((double)least + 64.0 / a.per_temperature), most = energy_of(most_key), last = far < most ? far : most;
+        factor = last > least ? (float)LAST / (last - least) : 0.0f;
+        if (!(last > least) && most > least) factor = __builtin_inff(); // nothing but the least has a weight
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t key) const
+    {
+        const float e = energy_of(key);
+        return e == least ? 0 : (uint32_t)fminf((e - least) * factor, (float)LAST);
+    }
+};
+constexpr Range SCALE = {0, 0xFFFFFFFFu, 0, 0, {0, 0}};
+
+__device__ __forceinline__ void write_bins(Histogram &to, const Histogram &from, bool weights)
 {
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) {
         to.count[b] = from.count[b];
+        if (!weights) continue;
         to.high[b] = from.high[b];
         to.low[b] = from.low[b];
     }
 }
 
-__global__ __launch_bounds__(LONG_THREADS) void first_bins_kernel(const Long p)
+// By key for the k least, by weight for a share: one of the two or both
+__global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8))) void first_bins_kernel(const Long p)
 {
-    __shared__ Histogram bins;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    Histogram *const bins = reinterpret_cast<Histogram *>(lds);
     __shared__ Bounds of_waves[LONG_THREADS / 64];
     const uint64_t segment = blockIdx.x / p.pieces, from = blockIdx.x % p.pieces * p.piece, to = min(p.a.n, from + p.piece);
     const Bounds b = segment_bounds(p, segment, of_waves);
@@ -699,26 +722,45 @@ __global__ __launch_bounds__(LONG_THREADS) void first_bins_kernel(const Long p)
     const bool weights = p.a.top_p < 1.0;
     const double best = (double)energy_of(b.least);
     const Range whole = {b.least, b.most, b.number, 0, {0, 0}};
-    const uint32_t shift = shift_of(whole);
-    clear_bins<LONG_THREADS>(bins, weights);
+    const Scale scale(p.a, b.least, b.most);
+    const uint32_t shift = shift_of(whole), shift_weight = shift_of(SCALE);
+    const bool limited = by_count(p, b.number);
+    clear_bins<LONG_THREADS>(bins[0], weights);
+    if (limited && weights) clear_bins<LONG_THREADS>(bins[1], weights);
+    Histogram &by_weight = bins[limited ? 1 : 0];
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
-        add_to_bins(bins, (key - whole.lo) >> shift, weights, weights ? weight_of(key, best, p.a.per_temperature) : 0.0);
+        const double w = weights ? weight_of(key, best, p.a.per_temperature) : 0.0;
+        if (limited) add_to_bins(bins[0], (key - whole.lo) >> shift, weights, w);
+        if (weights) add_to_bins(by_weight, scale(key) >> shift_weight, true, w);
     });
-    write_bins(p.parts[blockIdx.x], bins);
+    if (limited) write_bins(p.parts[blockIdx.x], bins[0], weights);
+    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], by_weight, true);
 }
 
-// histograms of a segment's pieces added up: blocks of 256 bins
-__global__ __launch_bounds__(256) void join_bins_kernel(const Long p, int which)
+// histograms of a segment's pieces added up: a block has 64 bins, each wavefront some of the pieces
+constexpr uint32_t JOIN_BLOCKS = BINS / 64;
+__global__ __launch_bounds__(LONG_THREADS) void join_bins_kernel(const Long p, int which)
 {
-    const uint64_t segment = blockIdx.x / (BINS / 256);
-    const uint32_t b = blockIdx.x % (BINS / 256) * 256 + threadIdx.x;
+    __shared__ Mass masses[LONG_THREADS / 64][64];
+    __shared__ uint32_t counts[LONG_THREADS / 64][64];
+    const uint64_t segment = blockIdx.x / JOIN_BLOCKS;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, b = blockIdx.x % JOIN_BLOCKS * 64 + lane;
     const Histogram *from = p.parts + (which * p.segments + segment) * p.pieces;
+    const bool weights = p.a.top_p < 1.0;
     uint32_t count = 0;
     Mass mass = {0, 0};
-#pragma unroll 8
-    for (uint32_t i = 0; i < p.pieces; ++i) {
+#pragma unroll 4
+    for (uint32_t i = wave; i < p.pieces; i += LONG_THREADS / 64) {
         count += from[i].count[b];
-        mass = mass + Mass{from[i].high[b], from[i].low[b]};
+        if (weights) mass = mass + Mass{from[i].high[b], from[i].low[b]};
+    }
+    counts[wave][lane] = count;
+    masses[wave][lane] = mass;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < LONG_THREADS / 64; ++w) {
+        count += counts[w][lane];
+        mass = mass + masses[w][lane];
     }
     Histogram &to = p.whole[which * p.segments + segment];
     to.count[b] = count;
@@ -726,11 +768,12 @@ __global__ __launch_bounds__(256) void join_bins_kernel(const Long p, int which)
     to.low[b] = mass.low;
 }
 
-__device__ __forceinline__ void read_bins(Histogram &to, const Histogram &from)
+__device__ __forceinline__ void read_bins(Histogram &to, const Histogram &from, bool weights)
 {
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < BINS; b += LONG_THREADS) {
         to.count[b] = from.count[b];
+        if (!weights) continue;
         to.high[b] = from.high[b];
         to.low[b] = from.low[b];
     }
@@ -766,15 +809,19 @@ __global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8)
     if (b.number == 0) return;
     const double best = (double)energy_of(b.least);
     const Range whole = {b.least, b.most, b.number, 0, {0, 0}};
-    read_bins(bins[0], *p.histogram(0, segment));
-    Range at[2] = {whole, whole};
+    const Scale scale(p.a, b.least, b.most);
+    Range at[2] = {whole, SCALE};
+    at[1].number = b.number;
     double total = 0.0;
-    if (limited) at[0] = narrow<LONG_THREADS>(s, bins[0], whole, {false, p.a.k, {0.0, 0.0}}, weights);
+    Mass of_range = {0, 0};
+    if (limited) {
+        read_bins(bins[0], *p.histogram(0, segment), weights);
+        at[0] = narrow<LONG_THREADS>(s, bins[0], whole, {false, p.a.k, {0.0, 0.0}}, weights);
+        if (weights) of_range = mass_in(bins[0], whole, at[0]);
+    }
     if (weights) {
-        Mass of_range = {0, 0};
-        if (limited) {
-            of_range = mass_in(bins[0], whole, at[0]);
-        } else {
+        read_bins(bins[0], *p.histogram(1, segment), true);
+        if (!limited) {
             u64 high = 0, low = 0;
             for (uint32_t i = threadIdx.x; i < BINS; i += LONG_THREADS) high += bins[0].high[i], low += bins[0].low[i];
             high = block_prefix<LONG_THREADS>(high, s.wide[0]);
@@ -784,23 +831,24 @@ __global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8)
             __syncthreads();
             total = s.total.value();
         }
-        at[1] = narrow<LONG_THREADS>(s, bins[0], whole, weight_goal(p.a, limited, at[0], of_range, total), true);
+        at[1] = narrow<LONG_THREADS>(s, bins[0], at[1], weight_goal(p.a, limited, at[0], of_range, total), true);
     }
     if (first) of.by_count = at[0], of.by_weight = at[1], of.total = total;
     clear_bins<LONG_THREADS>(bins[0], weights);
     clear_bins<LONG_THREADS>(bins[1], weights);
     const uint32_t shift[2] = {shift_of(at[0]), shift_of(at[1])};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
-        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
+        const uint32_t place[2] = {key, scale(key)};
+        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && place[1] >= at[1].lo && place[1] <= at[1].hi};
         if (!in[0] && !in[1]) return;
         const double w = weights ? weight_of(key, best, p.a.per_temperature) : 0.0;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-            if (in[r]) add_to_bins(bins[r], (key - at[r].lo) >> shift[r], weights, w);
+            if (in[r]) add_to_bins(bins[r], (place[r] - at[r].lo) >> shift[r], weights, w);
     });
     __syncthreads();
-    if (limited) write_bins(p.parts[blockIdx.x], bins[0]); // (the first ones are not needed again)
-    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], bins[1]);
+    if (limited) write_bins(p.parts[blockIdx.x], bins[0], weights); // (the first ones are not needed again)
+    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], bins[1], true);
 }
 
 // The ranges again, by the second histograms, and the candidates in them
@@ -816,19 +864,21 @@ __global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8)
     const bool weights = p.a.top_p < 1.0, limited = by_count(p, number);
     Range at[2] = {of.by_count, of.by_weight};
     Mass of_range = {0, 0};
+    const Scale scale(p.a, of.least, of.most);
     if (limited) {
-        read_bins(bins, *p.histogram(0, segment));
+        read_bins(bins, *p.histogram(0, segment), weights);
         const Range within_it = at[0];
         at[0] = narrow<LONG_THREADS>(s, bins, within_it, {false, p.a.k, {0.0, 0.0}}, weights);
-        of_range = mass_in(bins, within_it, at[0]);
+        if (weights) of_range = mass_in(bins, within_it, at[0]);
     }
     if (weights) {
-        read_bins(bins, *p.histogram(1, segment));
+        read_bins(bins, *p.histogram(1, segment), true);
         at[1] = narrow<LONG_THREADS>(s, bins, at[1], weight_goal(p.a, limited, at[0], of_range, of.total), true);
     }
     Bounds found[2] = {{NO_KEY, 0, 0, 0, 0}, {NO_KEY, 0, 0, 0, 0}};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t index) {
-        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && key >= at[1].lo && key <= at[1].hi};
+        const uint32_t place_of = scale(key);
+        const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && place_of >= at[1].lo && place_of <= at[1].hi};
         if (!in[0] && !in[1]) return;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -922,6 +972,7 @@ __global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
     const auto weight = [&](uint32_t key) { return weight_of(key, best, p.a.per_temperature); };
     const Stream stream = {p.a, segment, of_waves};
     const Segment &ranges = p.segment[p.segments + segment];
+    const Scale scale(p.a, of.least, of.most);
 
     const auto find = [&](const Range &at, const Goal &goal, int r) {
         if (listed <= LIST && at.number <= (uint32_t)LongScratch::LIST) {
@@ -930,8 +981,8 @@ __global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < listed; i += LONG_THREADS) {
                 const u64 one = p.list[segment * LIST + i];
-                const uint32_t key = (uint32_t)(one >> 32);
-                if (key < at.lo || key > at.hi) continue;
+                const uint32_t key = (uint32_t)(one >> 32), place_of = r ? scale(key) : key;
+                if (place_of < at.lo || place_of > at.hi) continue;
                 const uint32_t place = atomicAdd(&s.listed, 1u);
                 if (place < (uint32_t)LongScratch::LIST) s.list[place] = one;
             }
@@ -945,7 +996,7 @@ __global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
         const uint32_t mine = b.number;
         b = block_bounds(b, of_waves);
         if (b.least != b.most) { // many, and not equal
-            find_cut<LONG_THREADS>(s, bins, at, goal, weights, stream, weight);
+            find_cut<LONG_THREADS>(s, bins, {of.least, of.most, number, 0, {0, 0}}, goal, weights, stream, weight);
             return;
         }
         Range one = at;
@@ -1227,13 +1278,18 @@ __global__ __launch_bounds__(LONG_THREADS) void few_bins_kernel(const Few p)
 
 constexpr uint32_t JOINED_ABOVE = 16; // pieces whose bins are not added up by every block that reads them
 
-__global__ __launch_bounds__(256) void few_join_kernel(const Few p)
+__global__ __launch_bounds__(LONG_THREADS) void few_join_kernel(const Few p)
 {
-    const uint64_t segment = blockIdx.x / (BINS / 256);
-    const uint32_t b = blockIdx.x % (BINS / 256) * 256 + threadIdx.x;
+    __shared__ uint32_t counts[LONG_THREADS / 64][64];
+    const uint64_t segment = blockIdx.x / JOIN_BLOCKS;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, b = blockIdx.x % JOIN_BLOCKS * 64 + lane;
     uint32_t count = 0;
 #pragma unroll 8
-    for (uint32_t i = 0; i < p.pieces; ++i) count += p.bins[(segment * p.pieces + i) * BINS + b];
+    for (uint32_t i = wave; i < p.pieces; i += LONG_THREADS / 64) count += p.bins[(segment * p.pieces + i) * BINS + b];
+    counts[wave][lane] = count;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < LONG_THREADS / 64; ++w) count += counts[w][lane];
     p.joined[segment * BINS + b] = count;
 }
 
@@ -1660,7 +1716,7 @@ int32_t launch_few(const Draws &a, uint32_t segments, void *ws, hipStream_t st)
         ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(few_draws_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewLds)));
         hipLaunchKernelGGL(few_bounds_kernel, pieces, threads, 0, st, p);
         hipLaunchKernelGGL(few_bins_kernel, pieces, threads, 0, st, p);
-        if (p.pieces > JOINED_ABOVE) hipLaunchKernelGGL(few_join_kernel, dim3(segments * (BINS / 256)), dim3(256), 0, st, p);
+        if (p.pieces > JOINED_ABOVE) hipLaunchKernelGGL(few_join_kernel, dim3(segments * JOIN_BLOCKS), threads, 0, st, p);
         hipLaunchKernelGGL(few_list_kernel, pieces, threads, 0, st, p);
         hipLaunchKernelGGL(few_draws_kernel, dim3(segments), threads, sizeof(FewLds), st, p);
     }
@@ -1679,12 +1735,15 @@ int32_t launch_long(const Draws &a, uint32_t segments, void *ws, hipStream_t st)
     hipLaunchKernelGGL(bounds_kernel, pieces, threads, 0, st, p);
     if (a.k || weights) {
         const auto join = [&](int which) {
-            if (p.pieces > 1) hipLaunchKernelGGL(join_bins_kernel, dim3(segments * (BINS / 256)), dim3(256), 0, st, p, which);
+            if (p.pieces > 1) hipLaunchKernelGGL(join_bins_kernel, dim3(segments * JOIN_BLOCKS), threads, 0, st, p, which);
         };
         constexpr int two = 2 * sizeof(Histogram);
         ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(second_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, two));
-        hipLaunchKernelGGL(first_bins_kernel, pieces, threads, 0, st, p);
-        join(0);
+        const int first = a.k && weights ? two : two / 2;
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(first_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, first));
+        hipLaunchKernelGGL(first_bins_kernel, pieces, threads, first, st, p);
+        if (a.k) join(0);
+        if (weights) join(1);
         hipLaunchKernelGGL(second_bins_kernel, pieces, threads, two, st, p);
         if (a.k) join(0);
         if (weights) join(1);
