@@ -35,16 +35,34 @@ struct Int8Product {
     Result to;
 };
 
+// scales of eight neighbouring columns (0 past the last), and of their ups
+template <bool GATE_>
+struct Scales {
+    float w[8], up[GATE_ ? 8 : 1];
+    __device__ __forceinline__ void load(const Result &to, uint32_t c)
+    {
+        load_eight_of(to.w_scale, c, to.n_out, w);
+        if constexpr (GATE_) load_eight_of(to.w_scale + to.n_out, c, to.n_out, up);
+    }
+    static __device__ __forceinline__ void load_eight_of(const float *row, uint32_t c, uint32_t n, float (&v)[8])
+    {
+        float low[4], high[4];
+        load_chunk(row, c, n, low);
+        load_chunk(row, c + 4, n, high);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = low[i], v[4 + i] = high[i];
+    }
+};
+
 template <class T, bool GATE_>
-__device__ __forceinline__ void finish_as(const Result &to, uint64_t m, uint32_t c, const int (&v)[8], const int (&u)[8])
+__device__ __forceinline__ void finish_as(const Result &to, uint64_t m, uint32_t c, float row, const Scales<GATE_> &scales, const int (&v)[8],
+                                          const int (&u)[8])
 {
-    const float row = to.x_scale[m];
     float y[8], up[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const bool there = c + i < to.n_out;
-        y[i] = there ? (float)v[i] * row * to.w_scale[c + i] : 0.0f;
-        if (GATE_) up[i] = there ? (float)u[i] * row * to.w_scale[to.n_out + c + i] : 0.0f;
+        y[i] = (float)v[i] * row * scales.w[i];
+        if constexpr (GATE_) up[i] = (float)u[i] * row * scales.up[i];
     }
     if (GATE_)
         with_act(to.act, [&](auto act) {
@@ -54,10 +72,11 @@ __device__ __forceinline__ void finish_as(const Result &to, uint64_t m, uint32_t
     store_eight((T *)to.y + m * to.ld_y, c, to.n_out, y);
 }
 template <bool GATE_>
-__device__ __forceinline__ void finish(const Result &to, uint64_t m, uint32_t c, const int (&v)[8], const int (&u)[8])
+__device__ __forceinline__ void finish(const Result &to, uint64_t m, uint32_t c, float row, const Scales<GATE_> &scales, const int (&v)[8],
+                                       const int (&u)[8])
 {
-    if (to.f32) finish_as<float, GATE_>(to, m, c, v, u);
-    else finish_as<bf16, GATE_>(to, m, c, v, u);
+    if (to.f32) finish_as<float, GATE_>(to, m, c, row, scales, v, u);
+    else finish_as<bf16, GATE_>(to, m, c, row, scales, v, u);
 }
 
 // ------------------------------------------------------------------------------------------------ tiles
@@ -182,6 +201,20 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
     static_assert(ROWS * PITCH * 4 <= S::LDS && ITEMS * S::THREADS == ROWS * CHUNKS, "the rows fit, and every thread has as many");
     const uint32_t mine = threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS, c = c0 + 8 * chunk;
     int *const rows = reinterpret_cast<int *>(lds);
+    const auto row_of = [&](int step, int item) {
+        const uint32_t r = mine + item * (S::THREADS / CHUNKS);
+        return m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
+    };
+    // all scales that a thread needs at once: one after the other, each waited for, they took 35 us at the end of a 256 x 256 tile
+    Scales<GATE_> scales;
+    float row_scale[S::TM / HIGH][ITEMS];
+    if constexpr (!SHARED) {
+        scales.load(p.to, c);
+#pragma unroll
+        for (int step = 0; step < S::TM / HIGH; ++step)
+#pragma unroll
+            for (int item = 0; item < ITEMS; ++item) row_scale[step][item] = row_of(step, item) < p.n ? p.to.x_scale[row_of(step, item)] : 0.0f;
+    }
 #pragma unroll
     for (int step = 0; step < S::TM / HIGH; ++step) {
         if (step > 0) lds_barrier();
@@ -194,10 +227,9 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
         lds_barrier();
 #pragma unroll
         for (int item = 0; item < ITEMS; ++item) {
-            const uint32_t r = mine + item * (S::THREADS / CHUNKS);
-            const uint32_t m = m0 + r / (16 * HIGH) * (16 * S::TM) + step * (16 * HIGH) + r % (16 * HIGH);
+            const uint32_t m = row_of(step, item);
             if (m >= p.n || c >= N) continue;
-            const int *row = rows + r * PITCH;
+            const int *row = rows + (mine + item * (S::THREADS / CHUNKS)) * PITCH;
             const uint32_t at = PAIRED ? 8 * chunk / HALF * (2 * HALF) + 8 * chunk % HALF : 8 * chunk;
             int v[8], u[8];
 #pragma unroll
@@ -211,7 +243,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::A
                 for (int i = 0; i < 8; ++i)
                     if (c + i < N) to[c + i] = v[i];
             } else {
-                finish<GATE_>(p.to, m, c, v, u);
+                finish<GATE_>(p.to, m, c, row_scale[step][item], scales, v, u);
             }
         }
     }
@@ -236,7 +268,9 @@ __global__ __launch_bounds__(256) void join_kernel(const Int8Product p)
                     if (GATE_) u[i] += row[p.to.n_out + c + i];
                 }
         }
-        finish<GATE_>(p.to, m, c, v, u);
+        Scales<GATE_> scales;
+        scales.load(p.to, c);
+        finish<GATE_>(p.to, m, c, p.to.x_scale[m], scales, v, u);
     }
 }
 
@@ -247,7 +281,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Int8Product p)
 template <int WAVES, int TILES, bool GATE_>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product p)
 {
-    constexpr int SIDES = GATE_ ? 2 : 1, AHEAD = TILES == 1 ? 4 : 2; // steps on their way at a time
+    constexpr int SIDES = GATE_ ? 2 : 1, AHEAD = TILES == 1 && !GATE_ ? 4 : 2; // steps on their way at a time
     __shared__ __attribute__((aligned(16))) int sums[WAVES][SIDES * TILES][16 * 16];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const uint32_t c0 = blockIdx.x * 16, whole = (p.n_in + 15) / 16 * 16;
@@ -292,6 +326,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
     for (uint32_t at = threadIdx.x; at < TILES * 32; at += 64 * WAVES) {
         const uint32_t m = at / 2, c = at % 2 * 8, t = m / 16;
         if (m >= p.n || c0 + c >= p.to.n_out) continue;
+        Scales<GATE_> scales;
+        scales.load(p.to, c0 + c);
         int v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         for (int wv = 0; wv < WAVES; ++wv)
 #pragma unroll
@@ -299,7 +335,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
                 v[i] += sums[wv][t][m % 16 * 16 + c + i];
                 if (GATE_) u[i] += sums[wv][TILES + t][m % 16 * 16 + c + i];
             }
-        finish<GATE_>(p.to, m, c0 + c, v, u);
+        finish<GATE_>(p.to, m, c0 + c, p.to.x_scale[m], scales, v, u);
     }
 }
 
@@ -324,21 +360,43 @@ typedef Shapes<1>::Small Small;
 typedef Shapes<1>::Medium Medium;
 typedef Shapes<1>::Large Large;
 
+// How a product is cut up, by times in us that were fitted to some 80 measured ones (1 to 2^18 rows, 64 to 131071 integers a row, 16 to 16384
+// columns; the choice is within a tenth of the best, but for the smallest, which all take 3 to 5): a tile alone on a compute unit (start, end
+// and a step of 128 integers), tiles of a unit that is full, and what shares of k cost (a launch, sums written and read).  Up to 32 rows the
+// weights' bytes count, and reading them straight into registers takes less than tiles do, until there are tiles for all units:
+// 1 x 4096 x 4096 6.7 against 10.4 us, 1 x 4096 x 16384 15.3 against 12.6.
+enum Int8Shape { TILES_64, TILES_128, TILES_256, FEW };
 struct Int8Plan {
-    int shape; // 0, 1, 2: tiles of 64, 128, 256
+    Int8Shape shape;
     uint32_t shares;
+    double time;
 };
-constexpr uint64_t FEW_ROWS = 64;
+constexpr uint64_t FEW_ROWS = 32;
 
 Int8Plan plan(const Sizes &s)
 {
-    const auto tiles = [&](uint64_t side) { return (s.n + side - 1) / side * ((s.columns() + side - 1) / side); };
-    if (tiles(256) >= 256) return {2, 1};
-    if (tiles(128) >= 256) return {1, 1};
-    const uint64_t steps = (s.n_in + 127) / 128;
-    uint32_t shares = 1;
-    while (tiles(64) * shares < 256 && steps / (2 * shares) >= 4 && shares < 16) shares *= 2;
-    return {0, shares};
+    static const struct {
+        uint64_t side;
+        double rest, step, full_rest, full_step;
+    } SHAPES[3] = {{64, 3.6, 0.2, 1.05, 0.165}, {128, 5.0, 0.57, 2.55, 0.5}, {256, 10.0, 1.1, 10.5, 1.6}};
+    const double steps = (double)((s.n_in + 127) / 128), columns = (double)s.columns(), n = (double)s.n;
+    Int8Plan best = {FEW, 1, 1e300};
+    if (s.n <= FEW_ROWS) {
+        const double chain = steps / (s.gate() ? 11.0 : 16.0), bytes = columns * s.n_in / 5.4e6;
+        best.time = 3.0 + (chain > bytes ? chain : bytes);
+    }
+    for (int shape = 0; shape < 3; ++shape) {
+        const auto &of = SHAPES[shape];
+        const uint64_t tiles = (s.n + of.side - 1) / of.side * ((s.columns() + of.side - 1) / of.side);
+        for (uint32_t shares = 1; shares <= (shape == TILES_64 ? 16u : 1u); shares *= 2) {
+            if (shares > 1 && (steps / shares < 4.0 || tiles * shares > 512)) break;
+            const double of_share = steps / shares, a_unit = (double)((tiles * shares + 255) / 256);
+            const double alone = of.rest + of.step * of_share, full = a_unit * (of.full_rest + of.full_step * of_share);
+            const double time = (alone > full ? alone : full) + (shares > 1 ? 5.0 + 0.75 * shares + shares * n * columns * 8.0 / 4.0e6 : 0.0);
+            if (time < best.time) best = {(Int8Shape)shape, shares, time};
+        }
+    }
+    return best;
 }
 
 template <class S>
@@ -356,7 +414,8 @@ int32_t launch_tiles(Int8Product p, bool gate, hipStream_t st)
         return ECK_OK;
     };
     if (!shared) return gate ? go(tiles_kernel<S, true, false>) : go(tiles_kernel<S, false, false>);
-    if (const int32_t rc = go(tiles_kernel<S, false, true>)) return rc;
+    if constexpr (S::BM > 64) return ECK_EUNSUPPORTED; // (shares are of small tiles alone)
+    else if (const int32_t rc = go(tiles_kernel<S, false, true>)) return rc;
     const uint64_t chunks = (uint64_t)p.n * ((p.to.n_out + 7) / 8), blocks = (chunks + 255) / 256;
     hipLaunchKernelGGL((gate ? join_kernel<true> : join_kernel<false>), dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
     ECK_HIP_TRY(hipGetLastError());
@@ -380,7 +439,7 @@ using namespace eck;
 extern "C" uint64_t product_int8_workspace_bytes(uint64_t n, uint32_t n_in, uint32_t n_out, int32_t act)
 {
     const Sizes s = {n, n_in, n_out, act};
-    if (check_sizes(s) || n <= FEW_ROWS) return 0;
+    if (check_sizes(s)) return 0;
     const Int8Plan how = plan(s);
     return how.shares > 1 ? how.shares * n * s.columns() * 4 : 0;
 }
@@ -404,14 +463,10 @@ extern "C" int32_t product_int8(const int8_t *x, uint64_t ld_x, const float *x_s
     Int8Product p = {x, w, ld_x, ld_w, (uint32_t)n, n_in, 0, 0, 1, (int32_t *)ws, (uint32_t)s.columns(),
                      {x_scale, w_scale, y, ld_y, n_out, act, dtype == ECK_F32}};
     const hipStream_t st = as_stream(stream);
-    if (n <= FEW_ROWS) {
-        if (n <= 16) return (n_out + 15) / 16 < 512 ? launch_few<16, 1>(p, s.gate(), st) : launch_few<4, 1>(p, s.gate(), st);
-        if (n <= 32) return launch_few<4, 2>(p, s.gate(), st);
-        return launch_few<4, 4>(p, s.gate(), st);
-    }
     const Int8Plan how = plan(s);
     p.shares = how.shares;
-    if (how.shape == 2) return launch_tiles<Large>(p, s.gate(), st);
-    if (how.shape == 1) return launch_tiles<Medium>(p, s.gate(), st);
+    if (how.shape == FEW) return n <= 16 ? launch_few<8, 1>(p, s.gate(), st) : launch_few<4, 2>(p, s.gate(), st);
+    if (how.shape == TILES_256) return launch_tiles<Large>(p, s.gate(), st);
+    if (how.shape == TILES_128) return launch_tiles<Medium>(p, s.gate(), st);
     return launch_tiles<Small>(p, s.gate(), st);
 }

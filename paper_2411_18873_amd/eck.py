@@ -719,17 +719,19 @@ def int8_rows(n, width):
     return torch.zeros(n, -(-width // 16) * 16, dtype=torch.int8, device="cuda")[:, :width]
 
 
-def _int8(t, name, width):
-    """the row distance of an int8 matrix of that width: of a single row the next multiple of sixteen.  Its last row has to have all of its
-    sixteens in memory"""
-    ld, whole = _here_rows(t, name, torch.int8), -(-width // 16) * 16
-    n = t.shape[0]
-    if n <= 1:
-        ld = whole
-    if t.shape[1] != width:
-        raise ValueError("%s must have rows of %d" % (name, width))
-    if t.storage_offset() + (n - 1) * ld + whole > t.untyped_storage().nbytes():
-        raise ValueError("%s must have its rows whole sixteens long in memory" % name)
+def _int8(t, name, shape):
+    """the row distance of an int8 matrix: of a single row the next multiple of sixteen.  Its last row has to have all of its sixteens in
+    memory"""
+    ld = _here_rows(t, name, torch.int8)
+    if t.shape != shape:
+        raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
+    n, width = shape
+    if width & 15 or n == 1:
+        whole = -(-width // 16) * 16
+        if n == 1:
+            ld = whole
+        if t.storage_offset() + (n - 1) * ld + whole > t.untyped_storage().nbytes():
+            raise ValueError("%s must have its rows whole sixteens long in memory" % name)
     return ld
 
 
@@ -747,7 +749,7 @@ def quantise_rows(x, q, scale, order=ROWS):
         ld_x = _here_rows(x, "x", dtype, q.shape)
     else:
         ld_x = _feature_rows(x, n, width, dtype, "x")
-    _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", width),
+    _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", q.shape),
                                                 _scales(scale, "scale", n), _stream()))
 
 
@@ -764,7 +766,7 @@ def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
     ld_y = _here_rows(y, "y", dtype, (n, n_out))
     ws_ptr, ws_bytes = _ws(ws)
     _check("product_int8", lib().product_int8(
-        x.data_ptr(), _int8(x, "x", n_in), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", n_in),
+        x.data_ptr(), _int8(x, "x", x.shape), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", (w.shape[0], n_in)),
         _scales(w_scale, "w_scale", w.shape[0]), act, _FEAT_DTYPE[dtype], y.data_ptr(), ld_y, ws_ptr, ws_bytes, _stream()))
 
 
