@@ -339,6 +339,94 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
     }
 }
 
+// ------------------------------------------------------------------------------------------------ short rows
+
+// Rows of up to 64 * STEPS integers, many of them: what is written bounds it, or the activations.  A wavefront keeps the weights and scales
+// of 64 columns (GATE: and of their ups) in registers and goes over rows, sixteen at a time, with no LDS and no barrier.  Matrix rows are
+// handed out so that a lane's sums of four matrix instructions are sixteen neighbouring columns of one row: whole cache lines are written
+// from the registers.  2^18 rows of 64, 256 gated columns: 88 us by tiles.
+template <class T, bool GATE_, int STEPS>
+__global__ __launch_bounds__(256) void short_rows_kernel(const Int8Product p, uint32_t groups)
+{
+    constexpr int SIDES = GATE_ ? 2 : 1;
+    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const uint32_t id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), step = gridDim.x * 4 / groups;
+    const uint32_t c0 = id % groups * 64, tiles = (p.n + 15) / 16, whole = (p.n_in + 15) / 16 * 16;
+    uint32_t tile = id / groups;
+    if (tile >= step) return; // (wavefronts that are left over)
+    const i32x4 none = {0, 0, 0, 0};
+    i32x4 w[SIDES][4][STEPS];
+    float scale[SIDES][16];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const uint32_t c = c0 + 16 * (r >> 2) + 4 * t + (r & 3);
+#pragma unroll
+        for (int side = 0; side < SIDES; ++side)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const uint32_t k = s * 64 + g * 16;
+                const int8_t *row = p.w + ((uint64_t)side * p.to.n_out + c) * p.ld_w;
+                w[side][t][s] = c < p.to.n_out && k < whole ? *reinterpret_cast<const i32x4 *>(row + k) : none;
+            }
+    }
+    const uint32_t mine = c0 + 16 * g; // a lane's columns of the result
+#pragma unroll
+    for (int side = 0; side < SIDES; ++side)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) scale[side][i] = mine + i < p.to.n_out ? p.to.w_scale[side * p.to.n_out + mine + i] : 0.0f;
+
+    i32x4 x[STEPS], next[STEPS];
+    float row_scale, next_scale;
+    const auto load = [&](uint32_t of, i32x4(&to)[STEPS], float &s_to) {
+        const uint32_t m = of * 16 + r;
+        const bool there = of < tiles && m < p.n;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const uint32_t k = s * 64 + g * 16;
+            to[s] = there && k < whole ? *reinterpret_cast<const i32x4 *>(p.x + (uint64_t)m * p.ld_x + k) : none;
+        }
+        s_to = there ? p.to.x_scale[m] : 0.0f;
+    };
+    load(tile, x, row_scale);
+    for (; tile < tiles; tile += step) {
+        load(tile + step, next, next_scale);
+        i32x4 sum[SIDES][4];
+#pragma unroll
+        for (int side = 0; side < SIDES; ++side)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                sum[side][t] = none;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) sum[side][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[side][t][s], x[s], sum[side][t], 0, 0, 0);
+            }
+        const uint64_t m = (uint64_t)tile * 16 + r;
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = (float)sum[0][i / 4][i % 4] * row_scale * scale[0][i];
+        if constexpr (GATE_) {
+            with_act(p.to.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    y[i] = gate_as<decltype(act)::value, sizeof(T) == 4>(y[i]).value * ((float)sum[1][i / 4][i % 4] * row_scale * scale[1][i]);
+            });
+        }
+        if (m < p.n) {
+            T *row = (T *)p.to.y + m * p.to.ld_y;
+            constexpr int N = Chunk<T>::N;
+#pragma unroll
+            for (int i = 0; i < 16; i += N) {
+                float some[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) some[j] = y[i + j];
+                if (mine + i < p.to.n_out) store_chunk(row, mine + i, p.to.n_out, some);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) x[s] = next[s];
+        row_scale = next_scale;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ host
 
 struct Sizes {
@@ -365,7 +453,7 @@ typedef Shapes<1>::Large Large;
 // and a step of 128 integers), tiles of a unit that is full, and what shares of k cost (a launch, sums written and read).  Up to 32 rows the
 // weights' bytes count, and reading them straight into registers takes less than tiles do, until there are tiles for all units:
 // 1 x 4096 x 4096 6.7 against 10.4 us, 1 x 4096 x 16384 15.3 against 12.6.
-enum Int8Shape { TILES_64, TILES_128, TILES_256, FEW };
+enum Int8Shape { TILES_64, TILES_128, TILES_256, FEW, SHORT };
 struct Int8Plan {
     Int8Shape shape;
     uint32_t shares;
@@ -384,6 +472,8 @@ Int8Plan plan(const Sizes &s)
     if (s.n <= FEW_ROWS) {
         const double chain = steps / (s.gate() ? 11.0 : 16.0), bytes = columns * s.n_in / 5.4e6;
         best.time = 3.0 + (chain > bytes ? chain : bytes);
+    } else if (s.n_in <= 128) {
+        return {SHORT, 1, 0.0};
     }
     for (int shape = 0; shape < 3; ++shape) {
         const auto &of = SHAPES[shape];
@@ -431,6 +521,24 @@ int32_t launch_few(const Int8Product &p, bool gate, hipStream_t st)
     return ECK_OK;
 }
 
+template <class T, bool GATE_, int STEPS>
+int32_t launch_short(const Int8Product &p, hipStream_t st)
+{
+    // as many wavefronts as the units hold, but no more than there are rows for, and the same number for every group of columns
+    const uint64_t groups = (p.to.n_out + 63) / 64, tiles = (p.n + 15) / 16;
+    uint64_t rows = (256 * 12 + groups - 1) / groups;
+    if (rows > tiles) rows = tiles;
+    hipLaunchKernelGGL((short_rows_kernel<T, GATE_, STEPS>), dim3((uint32_t)((groups * rows + 3) / 4)), dim3(256), 0, st, p, (uint32_t)groups);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+template <class T>
+int32_t launch_short_of(const Int8Product &p, bool gate, hipStream_t st)
+{
+    if (p.n_in <= 64) return gate ? launch_short<T, true, 1>(p, st) : launch_short<T, false, 1>(p, st);
+    return gate ? launch_short<T, true, 2>(p, st) : launch_short<T, false, 2>(p, st);
+}
+
 } // namespace
 } // namespace eck
 
@@ -466,6 +574,7 @@ extern "C" int32_t product_int8(const int8_t *x, uint64_t ld_x, const float *x_s
     const Int8Plan how = plan(s);
     p.shares = how.shares;
     if (how.shape == FEW) return n <= 16 ? launch_few<8, 1>(p, s.gate(), st) : launch_few<4, 2>(p, s.gate(), st);
+    if (how.shape == SHORT) return p.to.f32 ? launch_short_of<float>(p, s.gate(), st) : launch_short_of<bf16>(p, s.gate(), st);
     if (how.shape == TILES_256) return launch_tiles<Large>(p, s.gate(), st);
     if (how.shape == TILES_128) return launch_tiles<Medium>(p, s.gate(), st);
     return launch_tiles<Small>(p, s.gate(), st);
