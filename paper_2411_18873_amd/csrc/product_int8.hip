@@ -346,7 +346,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
 // handed out so that a lane's sums of four matrix instructions are sixteen neighbouring columns of one row: whole cache lines are written
 // from the registers.  2^18 rows of 64, 256 gated columns: 88 us by tiles.
 template <class T, bool GATE_, int STEPS>
-__global__ __launch_bounds__(256) void short_rows_kernel(const Int8Product p, uint32_t groups)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && STEPS > 1 ? 2 : 3))) void short_rows_kernel(const Int8Product p, uint32_t groups)
 {
     constexpr int SIDES = GATE_ ? 2 : 1;
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -472,7 +472,9 @@ Int8Plan plan(const Sizes &s)
     if (s.n <= FEW_ROWS) {
         const double chain = steps / (s.gate() ? 11.0 : 16.0), bytes = columns * s.n_in / 5.4e6;
         best.time = 3.0 + (chain > bytes ? chain : bytes);
-    } else if (s.n_in <= 128) {
+    } else if (s.n_in <= 128 || (s.n_in <= 256 && n * columns >= 33554432.0)) {
+        // (rows of 256, by tiles and this way: 2^18 rows of 256 columns 55 and 47 us, gated 101 and 78; 16384 of 2048 28.4 and 28.5, gated 52 and
+        // 47; 4096 of 4096 16.0 and 19.6; 2048 of 2048 gated 9.9 and 22.9.  Of 128 and less this way is never the slower)
         return {SHORT, 1, 0.0};
     }
     for (int shape = 0; shape < 3; ++shape) {
@@ -536,6 +538,7 @@ template <class T>
 int32_t launch_short_of(const Int8Product &p, bool gate, hipStream_t st)
 {
     if (p.n_in <= 64) return gate ? launch_short<T, true, 1>(p, st) : launch_short<T, false, 1>(p, st);
+    if (p.n_in > 128) return gate ? launch_short<T, true, 4>(p, st) : launch_short<T, false, 4>(p, st);
     return gate ? launch_short<T, true, 2>(p, st) : launch_short<T, false, 2>(p, st);
 }
 

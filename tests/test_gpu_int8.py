@@ -144,7 +144,8 @@ def test_product(n, n_in, n_out, act, kind):
 # few rows of many columns; tiles of 64 undivided and in shares of k, of 128, of 256
 @pytest.mark.parametrize("act", [eck.ACT_NONE, eck.ACT_SILU])
 @pytest.mark.parametrize("n,n_in,n_out", [(3, 700, 9000), (40, 1000, 5000), (100, 8192, 130), (70, 16000, 16), (70, 131071, 200), (500, 2000, 2050),
-                                          (2100, 300, 2060), (4200, 400, 4100), (100000, 64, 70), (1 << 18, 40, 9)])
+                                          (2100, 300, 2060), (4200, 400, 4100), (100000, 64, 70), (1 << 18, 40, 9), (20000, 128, 130),
+                                          (140000, 250, 256), (9000, 130, 4000), (50000, 1, 1)])
 def test_product_by_every_kernel(n, n_in, n_out, act):
     check_product(n, n_in, n_out, act, "bf16", n, extra=1, ld_extra=3)
 
