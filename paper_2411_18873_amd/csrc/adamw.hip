@@ -12,6 +12,7 @@
 // what is missing (16-bit draws of the generator of the genes), which is right on average.  A positive v never becomes 0, since m / eps
 // would be the next step's size.  The step itself is made with m and v before they are rounded.
 #include "activations.h"
+#include "lanes.h"
 #include "splitmix.h"
 
 #include <math.h>
@@ -54,21 +55,27 @@ struct Tensors {
 };
 static_assert(sizeof(Tensors) <= 4096, "arguments of a launch");
 
-// which tensor a block of threads works on
-template <class T>
-__device__ __forceinline__ uint32_t tensor_of(const T *all, uint32_t count, uint32_t block)
+// which tensor a block of threads works on: the last whose first block, first(i), is not behind it
+template <class F>
+__device__ __forceinline__ uint32_t tensor_of(uint32_t count, uint32_t block, F &&first)
 {
     uint32_t lo = 0, hi = count;
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (all[mid].first <= block) lo = mid;
+        if (first(mid) <= block) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 
-// the largest of 32 lanes' values
-__device__ __forceinline__ float half_most(float v);
+// the largest of 32 lanes' values, none of them negative or NaN
+__device__ __forceinline__ float half_most(float v)
+{
+    uint32_t bits = __float_as_uint(v);
+#pragma unroll
+    for (int stride = 1; stride < 32; stride <<= 1) bits = max(bits, lane_exchange(bits, stride));
+    return __uint_as_float(bits);
+}
 
 template <class T>
 __device__ __forceinline__ void fetch(const T *from, uint64_t at, uint64_t n, T (&x)[EACH])
@@ -148,13 +155,6 @@ struct Eight {
     }
 };
 
-__device__ __forceinline__ float half_most(float v)
-{
-#pragma unroll
-    for (int stride = 16; stride; stride >>= 1) v = fmaxf(v, __shfl_xor(v, stride));
-    return v;
-}
-
 // what a thread holds of its tensor
 template <bool EIGHT, class G>
 struct Hold {
@@ -202,7 +202,11 @@ __device__ __forceinline__ void advance(const Tensor &t, uint64_t at, const Hold
             m[i] = fmaf(step.one_beta1, g, m[i] * step.beta1);
             v[i] = fmaf(step.one_beta2, g * g, v[i] * step.beta2);
         }
-        w[i] = fmaf(-rate, m[i] / (sqrtf(v[i] * inverse) + step.eps), had.w[i] * t.keep);
+        // (8 bits: root and quotient as the instructions give them, within a unit of the last place each; full ones are two dozen
+        // instructions, and instructions bound this kernel)
+        const float corrected = v[i] * inverse;
+        const float step_of = EIGHT ? m[i] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(corrected) + step.eps) : m[i] / (sqrtf(corrected) + step.eps);
+        w[i] = fmaf(-rate, step_of, had.w[i] * t.keep);
     }
     put(t.param, at, t.n, w);
     if (t.copy) {
@@ -252,7 +256,7 @@ __device__ __forceinline__ void work(const Tensor &t, uint32_t block, uint32_t r
 template <bool EIGHT>
 __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors a)
 {
-    const Tensor &t = a.one[tensor_of(a.one, a.count, blockIdx.x)];
+    const Tensor &t = a.one[tensor_of(a.count, blockIdx.x, [&](uint32_t i) { return a.one[i].first; })];
     const float scale = a.step.grad_scale ? *a.step.grad_scale : 1.0f;
     if (!(__builtin_fabsf(scale) < __builtin_inff())) return; // gradients that are not finite: nothing changes
     float rate = a.step.rate, inverse = a.step.inverse;
@@ -279,24 +283,21 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors a)
 
 // ------------------------------------------------------------------------------------------------ norm
 
-struct Gradient {
-    const void *grad;
-    uint64_t n;
-    uint32_t first;
-    int32_t grad_bf16;
-};
-constexpr int GRADIENTS_AT_ONCE = 160;
+constexpr int GRADIENTS_AT_ONCE = 200;
 struct GradientList {
-    Gradient one[GRADIENTS_AT_ONCE];
+    const void *grad[GRADIENTS_AT_ONCE];
+    uint64_t n[GRADIENTS_AT_ONCE]; // the highest bit: of bf16
+    uint32_t first[GRADIENTS_AT_ONCE];
     uint32_t count, stretch; // stretch: elements of a block of threads, a multiple of THREADS * 8
     double *sums;
 };
+constexpr uint64_t OF_BF16 = 1ull << 63;
 static_assert(sizeof(GradientList) <= 4096, "arguments of a launch");
 
 __device__ __forceinline__ double block_sum(double x, double *lds)
 {
 #pragma unroll
-    for (int stride = 32; stride; stride >>= 1) x += __shfl_xor(x, stride);
+    for (int stride = 1; stride < 64; stride <<= 1) x += lane_exchange(x, stride);
     const uint32_t waves = blockDim.x / 64;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = x;
     __syncthreads();
@@ -309,23 +310,30 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
 template <class G>
 __device__ __forceinline__ double squares(const G *grad, uint64_t from, uint64_t to)
 {
+    constexpr int AHEAD = 4, N = Chunk<G>::N;
     double sum = 0.0;
-    for (uint64_t at = from + threadIdx.x * 8; at < to; at += THREADS * 8) {
-        float x[8];
-        if (at + 8 <= to) {
-            constexpr int N = 16 / sizeof(G);
+    for (uint64_t at = from + threadIdx.x * 8; at < to; at += THREADS * 8 * AHEAD) {
+        Chunk<G> c[AHEAD][8 / N];
 #pragma unroll
-            for (int i = 0; i < 8; i += N) {
-                const Chunk<G> c = *reinterpret_cast<const Chunk<G> *>(grad + at + i);
+        for (int k = 0; k < AHEAD; ++k) {
+            const uint64_t here = at + (uint64_t)k * (THREADS * 8);
 #pragma unroll
-                for (int j = 0; j < N; ++j) x[i + j] = (float)c.v[j];
+            for (int i = 0; i < 8 / N; ++i) {
+                if (here + (i + 1) * N <= to) c[k][i] = *reinterpret_cast<const Chunk<G> *>(grad + here + i * N);
+                else
+#pragma unroll
+                    for (int j = 0; j < N; ++j) c[k][i].v[j] = here + i * N + j < to ? grad[here + i * N + j] : (G)0.0f;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = at + i < to ? (float)grad[at + i] : 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (double)x[i] * (double)x[i];
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < 8 / N; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const double x = (double)(float)c[k][i].v[j];
+                    sum += x * x;
+                }
     }
     return sum;
 }
@@ -333,9 +341,9 @@ __device__ __forceinline__ double squares(const G *grad, uint64_t from, uint64_t
 __global__ __launch_bounds__(THREADS) void squares_kernel(const GradientList a)
 {
     __shared__ double lds[THREADS / 64];
-    const Gradient &t = a.one[tensor_of(a.one, a.count, blockIdx.x)];
-    const uint64_t from = (uint64_t)(blockIdx.x - t.first) * a.stretch, to = min(t.n, from + a.stretch);
-    const double sum = t.grad_bf16 ? squares((const bf16 *)t.grad, from, to) : squares((const float *)t.grad, from, to);
+    const uint32_t t = tensor_of(a.count, blockIdx.x, [&](uint32_t i) { return a.first[i]; });
+    const uint64_t n = a.n[t] & ~OF_BF16, from = (uint64_t)(blockIdx.x - a.first[t]) * a.stretch, to = min(n, from + a.stretch);
+    const double sum = a.n[t] & OF_BF16 ? squares((const bf16 *)a.grad[t], from, to) : squares((const float *)a.grad[t], from, to);
     const double all = block_sum(sum, lds);
     if (threadIdx.x == 0) a.sums[blockIdx.x] = all;
 }
@@ -473,7 +481,9 @@ extern "C" int32_t gradients_norm(const eck_parameter *parameters, uint32_t coun
         if (p.n == 0) continue;
         if (a.count == GRADIENTS_AT_ONCE)
             if (const int32_t rc = launch()) return rc;
-        a.one[a.count++] = {p.grad, p.n, (uint32_t)blocks, p.grad_dtype == ECK_BF16};
+        a.grad[a.count] = p.grad;
+        a.n[a.count] = p.n | (p.grad_dtype == ECK_BF16 ? OF_BF16 : 0);
+        a.first[a.count++] = (uint32_t)blocks;
         blocks += (p.n + stretch - 1) / stretch;
     }
     if (const int32_t rc = launch()) return rc;

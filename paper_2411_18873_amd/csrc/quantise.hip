@@ -2,6 +2,7 @@
 //
 // One pass where a row (or, of a feature matrix, a column) fits the registers of the threads that share it; the memory bounds it.
 #include "activations.h"
+#include "lanes.h"
 
 namespace eck {
 namespace {
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const T *x, uint64_t ld_x, ui
                 most = max(most, some.most());
             }
 #pragma unroll
-        for (int stride = 1; stride < (LANES < 64 ? LANES : 64); stride <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, stride));
+        for (int stride = 1; stride < (LANES < 64 ? LANES : 64); stride <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, stride)); // (not all lanes go round as often)
         if (LANES == 256) {
             __shared__ uint32_t all[4];
             __syncthreads();
@@ -106,9 +107,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const T *x, uint64_t ld_x, ui
 }
 
 // A matrix with a row of the result in every column.  A block takes 8 * CHUNKS columns; a thread eight of them, four rows at a time, whose
-// bytes are a word of the result; words are exchanged by way of the LDS so that memory sees whole pieces of the result's rows.  The matrix
-// is read a second time, out of the caches.
-template <class T, int CHUNKS>
+// bytes are a word of the result; words are exchanged by way of the LDS so that memory sees whole pieces of the result's rows.  A matrix of
+// more rows than a block takes at a time is read a second time, out of the caches.
+template <class T, int CHUNKS, bool ONCE>
 __global__ __launch_bounds__(256) void columns_kernel(const T *x, uint64_t ld_x, uint64_t n, uint32_t width, int8_t *q, uint64_t ld_q,
                                                       float *scale)
 {
@@ -126,20 +127,21 @@ __global__ __launch_bounds__(256) void columns_kernel(const T *x, uint64_t ld_x,
             for (int i = 0; i < 8; ++i) v[i] = 0.0f;
     };
     uint32_t most[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (uint32_t r = 4 * group; r < width; r += STEP) {
-        float v[4][8];
+    float v[4][8];
+    for (uint32_t r = 4 * group; ONCE || r < width; r += STEP) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) load(r + k, v[k]);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) most[i] = max(most[i], size_bits(v[k][i]));
+        if (ONCE) break;
     }
     // of a wavefront's groups, then of the four wavefronts
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int stride = CHUNKS; stride < 64; stride <<= 1) most[i] = max(most[i], (uint32_t)__shfl_xor((int)most[i], stride));
+        for (int stride = CHUNKS; stride < 64; stride <<= 1) most[i] = max(most[i], lane_exchange(most[i], stride));
         if ((threadIdx.x & 63) < CHUNKS) most_of[threadIdx.x / 64][chunk * 8 + i] = most[i];
     }
     __syncthreads();
@@ -155,9 +157,9 @@ __global__ __launch_bounds__(256) void columns_kernel(const T *x, uint64_t ld_x,
     for (int i = 0; i < 8; ++i) inverse[i] = chunk * 8 + i < columns ? inverse_of[chunk * 8 + i] : 0.0f;
     const uint32_t whole = (width + UNIT - 1) / UNIT * UNIT;
     for (uint32_t r0 = 0; r0 < width; r0 += STEP) {
-        float v[4][8];
+        if (!ONCE)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load(r0 + 4 * group + k, v[k]);
+            for (int k = 0; k < 4; ++k) load(r0 + 4 * group + k, v[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t word = 0;
@@ -199,7 +201,7 @@ int32_t launch_columns(const void *x, uint64_t ld_x, uint64_t n, uint32_t width,
 {
     const uint32_t columns = width <= 64 ? 128 : 64;
     const dim3 grid((uint32_t)((n + columns - 1) / columns));
-    hipLaunchKernelGGL((columns == 128 ? columns_kernel<T, 16> : columns_kernel<T, 8>), grid, dim3(256), 0, st, (const T *)x, ld_x, n, width, q,
+    hipLaunchKernelGGL((columns == 128 ? columns_kernel<T, 16, true> : columns_kernel<T, 8, false>), grid, dim3(256), 0, st, (const T *)x, ld_x, n, width, q,
                        ld_q, scale);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;
