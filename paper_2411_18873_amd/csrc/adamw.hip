@@ -273,7 +273,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors a)
             square2 *= square2;
         }
         rate = (float)(a.step.lr / (1.0 - power1));
-        inverse = 1.0f / (float)(1.0 - power2);
+        inverse = (float)(1.0 / (1.0 - power2));
         state = splitmix_finalise(a.step.seed + kGamma * ((uint64_t)now + 1));
     }
     const uint32_t block = blockIdx.x - t.first;
@@ -422,7 +422,7 @@ extern "C" int32_t adamw_step(const eck_parameter *parameters, uint32_t count, i
               step_more, grad_scale};
     if (!step_more) {
         a.step.rate = (float)(lr / (1.0 - pow(beta1, step)));
-        a.step.inverse = 1.0f / (float)(1.0 - pow(beta2, step));
+        a.step.inverse = (float)(1.0 / (1.0 - pow(beta2, step)));
         a.step.state = stream_state(seed, step);
     }
     uint64_t number = 0, blocks = 0;

@@ -6,10 +6,11 @@ Eq. (1) is the loss of a refit).
     x <- x + dropout(feedforward(layernorm(x)))              `blocks` times, in bf16
     score = feedforward(layernorm(x))                        one output, in fp32
 
-The operators run in the library.  torch holds the memory, and does what lies between them: changes of type before the first block
-and the head (and, in a refit, of their gradients), the sum of the residual's two gradients, the loss on vectors of scores, and
-Adam's arithmetic on the fp32 master parameters.  A model's calls share one workspace, so they belong on one stream.
-`python -m paper_2411_18873_amd.gated` fits one on simulated measurements and picks candidates with it."""
+The operators run in the library, a refit's norm of all gradients and its steps of AdamW on the fp32 master parameters among them (states in
+32 or in 8 bits), and scoring with the blocks' products in 8-bit integers.  torch holds the memory, and does what lies between them:
+changes of type before the first block and the head (and, in a refit, of their rows' gradients), the sum of the residual's two gradients and
+the loss on vectors of scores.  A model's calls share one workspace, so they belong on one stream.
+`python -m paper_2411_18873_amd.gated` fits one on simulated measurements, picks candidates with it and draws parents for the next ones."""
 import numpy as np
 import torch
 
@@ -19,7 +20,9 @@ EPS = 1e-5
 
 
 class GatedModel:
-    def __init__(self, n_feat=64, hidden=256, blocks=2, head=64, p_drop=0.05, seed=1):
+    def __init__(self, n_feat=64, hidden=256, blocks=2, head=64, p_drop=0.05, seed=1, state_bits=32):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
         self.n_feat, self.hidden, self.blocks, self.head = int(n_feat), int(hidden), int(blocks), int(head)
         self.p_drop_q32, self.seed, self.steps = int(p_drop * 2 ** 32), int(seed), 0
         g = torch.Generator().manual_seed(self.seed)
@@ -33,13 +36,41 @@ class GatedModel:
                        "head.gate_up": weights(f, 2 * self.head), "head.down": weights(self.head, 1)}
         for b in range(self.blocks):
             self.params.update({"%d.gamma" % b: ones(), "%d.beta" % b: zeros(), "%d.gate_up" % b: weights(f, 2 * h), "%d.down" % b: weights(h, f)})
-        self.moments = {k: (torch.zeros_like(p), torch.zeros_like(p)) for k, p in self.params.items()}
+        # of each parameter m and v, and, in 8 bits, the powers of two of their blocks
+        if state_bits == 32:
+            self.moments = {k: (torch.zeros_like(p), torch.zeros_like(p)) for k, p in self.params.items()}
+        else:
+            self.moments = {k: tuple(torch.zeros(m, dtype=torch.uint8, device="cuda")
+                                     for m in (p.numel(), p.numel(), *[-(-p.numel() // eck.STATE_BLOCK)] * 2)) for k, p in self.params.items()}
         self._work = {}
         self._copy()
 
     def _copy(self):
         """bf16 copies of the blocks' weights, which their products are made with"""
         self.bf16 = {k: p.bfloat16() for k, p in self.params.items() if k[0].isdigit() and p.dim() == 2}
+        self._int8 = None
+
+    def _quantised(self):
+        """the blocks' weights in 8-bit integers, a row and a scale for each column, laid out when a scoring pass first wants them"""
+        if self._int8 is None:
+            self._int8 = {}
+            for k in self.bf16:
+                w = self.params[k]
+                q, scale = eck.int8_rows(w.shape[1], w.shape[0]), torch.empty(w.shape[1], device="cuda")
+                eck.quantise_rows(w, q, scale, order=eck.COLUMNS)
+                self._int8[k] = q, scale
+        return self._int8
+
+    def _block_int8(self, b, xn, out):
+        """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest"""
+        n, f, h, w = xn.shape[0], self.n_feat, self.hidden, self._quantised()
+        ws = self._ws(max(eck.product_int8_workspace_bytes(n, f, h, eck.ACT_SILU), eck.product_int8_workspace_bytes(n, h, f), 1))
+        q, scale, hidden = eck.int8_rows(n, f), torch.empty(n, device="cuda"), torch.empty(n, h, dtype=torch.bfloat16, device="cuda")
+        eck.quantise_rows(xn, q, scale)
+        eck.product_int8(q, scale, *w["%d.gate_up" % b], hidden, ws, act=eck.ACT_SILU)
+        q = eck.int8_rows(n, h)
+        eck.quantise_rows(hidden, q, scale)
+        eck.product_int8(q, scale, *w["%d.down" % b], out, ws)
 
     def _ws(self, need):
         """one workspace for all calls: they follow each other on one stream"""
@@ -47,8 +78,9 @@ class GatedModel:
             self._work["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda")
         return self._work["ws"]
 
-    def _forward(self, feat, n, train):
-        """scores float [n]; train: with dropout, and what the backward pass needs of every layer, of which a scoring pass keeps none"""
+    def _forward(self, feat, n, train, int8=False):
+        """scores float [n]; train: with dropout, and what the backward pass needs of every layer, of which a scoring pass keeps none;
+        int8: the blocks' products in 8-bit integers (scoring alone)"""
         f, p = self.n_feat, self.params
         kept = {} if train else None
         rows = lambda width=f, dtype=torch.bfloat16: torch.empty(n, width, dtype=dtype, device="cuda")  # noqa: E731
@@ -64,7 +96,10 @@ class GatedModel:
             xn, out, s = rows(), rows(), stats()
             pre = rows(2 * self.hidden, torch.float32) if train else None
             eck.layernorm_forward(x, p["%d.gamma" % b], p["%d.beta" % b], xn, *s, eps=EPS)
-            eck.gatedffn_forward(xn, self.bf16["%d.gate_up" % b], self.bf16["%d.down" % b], out, ws, pre_out=pre)
+            if int8:
+                self._block_int8(b, xn, out)
+            else:
+                eck.gatedffn_forward(xn, self.bf16["%d.gate_up" % b], self.bf16["%d.down" % b], out, ws, pre_out=pre)
             if train:
                 kept[b] = x, xn, pre, s
             nxt = rows()
@@ -72,6 +107,7 @@ class GatedModel:
             x = nxt
         x, xn, s = x.float(), rows(dtype=torch.float32), stats()
         pre = rows(2 * self.head, torch.float32) if train else None
+        ws = self._ws(0)  # (a block in 8-bit integers may have made it larger)
         score = rows(1, torch.float32)
         eck.layernorm_forward(x, p["head.gamma"], p["head.beta"], xn, *s, eps=EPS)
         eck.gatedffn_forward(xn, p["head.gate_up"], p["head.down"], score, ws, pre_out=pre)
@@ -79,9 +115,10 @@ class GatedModel:
             kept["head"] = x, xn, pre, s
         return score.view(n), kept
 
-    def score(self, feat, n, score_out):
-        """predicted scores of candidates 0 .. n - 1 of a feature matrix [n_feat][ld], as costmodel_score writes them"""
-        score_out[:n].copy_(self._forward(feat, n, False)[0])
+    def score(self, feat, n, score_out, int8=False):
+        """predicted scores of candidates 0 .. n - 1 of a feature matrix [n_feat][ld], as costmodel_score writes them; int8: the blocks'
+        products in 8-bit integers"""
+        score_out[:n].copy_(self._forward(feat, n, False, int8)[0])
 
     def _backward(self, feat, n, kept, d_score):
         """gradients of all parameters from dL/d score"""
@@ -93,7 +130,7 @@ class GatedModel:
         def ffn(name, xn, pre, dy, gate_up, down):
             d_xn, d_gate_up, d_down = torch.empty_like(xn), torch.empty_like(gate_up), torch.empty_like(down)
             eck.gatedffn_backward(xn, gate_up, down, pre, dy, d_xn, d_gate_up, d_down, ws)
-            grads[name + ".gate_up"], grads[name + ".down"] = d_gate_up.float(), d_down.float()
+            grads[name + ".gate_up"], grads[name + ".down"] = d_gate_up, d_down
             return d_xn
 
         def norm(name, x, dy, stats, dx, order=eck.ROWS):
@@ -113,10 +150,11 @@ class GatedModel:
         norm("in", feat, dx.to(feat.dtype), kept["in"], None, order=eck.COLUMNS)
         return grads
 
-    def refit(self, feat, energy_measured, n_steps, minibatch, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8):
+    def refit(self, feat, energy_measured, n_steps, minibatch, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, max_norm=None):
         """Adam on Eq. (1) over minibatches of measured kernels, as costmodel_update goes over them; the losses of all steps.  As there,
         minibatches have to divide the pairs, and with an energy that is not positive and finite losses are NaN and the model is left
-        unchanged (which the host waits for, once a refit)."""
+        unchanged (which the host waits for, once a refit).  weight_decay: AdamW's, of the matrices; max_norm: what the norm of all gradients
+        is brought down to (a step whose norm is not finite changes nothing)."""
         n, pairs, losses = int(minibatch), energy_measured.numel(), []
         if n <= 0 or n_steps <= 0 or pairs == 0 or pairs % n:
             raise ValueError("pairs must be a whole number of minibatches, steps one or more")
@@ -125,6 +163,12 @@ class GatedModel:
         if not bool(((energy_measured > 0) & torch.isfinite(energy_measured)).all()):
             return torch.full((n_steps,), float("nan"), device="cuda")
         y_all = energy_measured / energy_measured.max()
+        names = list(self.params)
+        params = [self.params[k] for k in names]
+        states = list(zip(*(self.moments[k] for k in names)))
+        plan = None
+        self._int8 = None  # (of the weights as they were)
+        scale = torch.ones(1, device="cuda") if max_norm is not None else None
         for step in range(n_steps):
             first = step % (pairs // n) * n
             x, y = feat[:, first:first + n], y_all[first:first + n]
@@ -132,16 +176,19 @@ class GatedModel:
             losses.append(((pred - y) ** 2 / y).mean())
             grads = self._backward(x, n, kept, 2.0 * (pred - y) / y / n)
             self.steps += 1
-            for k, param in self.params.items():
-                m, v = self.moments[k]
-                m.mul_(beta1).add_(grads[k], alpha=1 - beta1)
-                v.mul_(beta2).addcmul_(grads[k], grads[k], value=1 - beta2)
-                param.addcdiv_(m, (v / (1 - beta2 ** self.steps)).sqrt_().add_(eps), value=-lr / (1 - beta1 ** self.steps))
-            self._copy()
+            of = [grads[k] for k in names]
+            if plan is None:
+                plan = eck.Parameters(of, params, *states, copies=[self.bf16.get(k) for k in names],
+                                      weight_decay=[weight_decay if p.dim() == 2 else 0.0 for p in params])
+            else:
+                plan.set_grads(of)
+            if max_norm is not None:
+                eck.gradients_norm(plan, None, scale, self._ws(eck.gradients_norm_workspace_bytes(plan)), max_norm=max_norm)
+            eck.adamw_step(plan, lr, self.steps, beta1, beta2, eps, grad_scale=scale, seed=self.seed)
         return torch.stack(losses)
 
 
-def main(pairs=4096, n=1 << 18, steps=200, k=32):
+def main(pairs=4096, n=1 << 18, steps=200, k=32, parents=256):
     cfg = synth.CONFIGS["c2"]
     space = eck.Space(cfg["problem"], eck.SPACE_SPLIT)
     feats = []
@@ -162,6 +209,17 @@ def main(pairs=4096, n=1 << 18, steps=200, k=32):
     ws = torch.empty(eck.topk_select_workspace_bytes(n, 1, k), dtype=torch.uint8, device="cuda")
     eck.topk_select(score, None, legal, 1, k, idx, best, count, ws)
     print("Eq. (1) loss %.4f -> %.4f in %d steps; least of %d predicted scores: %s" % (losses[0], losses[-8:].mean(), steps, n, best[0, :4].tolist()))
+    # the next generation's parents: drawn from the better ones, by scores whose products are made in 8-bit integers
+    quick = torch.empty(n, device="cuda")
+    model.score(feats[1].bfloat16(), n, quick, int8=True)
+    drawn, logprob = torch.zeros((1, parents), dtype=torch.int32, device="cuda"), torch.zeros((1, parents), device="cuda")
+    uniform = torch.rand((1, parents), generator=torch.Generator().manual_seed(model.seed)).cuda()
+    ws = torch.empty(eck.sample_select_workspace_bytes(n, 1, parents), dtype=torch.uint8, device="cuda")
+    eck.sample_select(quick, legal, 1, uniform, drawn, logprob, count, ws, temperature=0.02, k=4096, top_p=0.95)
+    bred = torch.empty((space.n_genes, parents), dtype=torch.int16, device="cuda")
+    eck.candidates_gather(genes, n, drawn.view(-1), parents, bred)
+    print("8-bit scores %.4f off on average; %d parents, %d of them different, drawn from the best %d" % (
+        (quick - score).abs().mean(), parents, bred.unique(dim=1).shape[1], int(count)))
 
 
 if __name__ == "__main__":

@@ -15,7 +15,9 @@ is fitted once on the initial sample (the paper takes it from its host framework
 whose round(k * M) is 0 measures nothing, leaves the model and k alone and still picks parents.
 
 Options that depart from the printed algorithm (off by default): parents="measured" lets the n_parents measured
-kernels of least measured energy over the whole record reproduce; k_min > 0 keeps k from falling below it."""
+kernels of least measured energy over the whole record reproduce; parents="sampled" draws parents among the M fastest
+kernels by exp(-predicted energy / temperature) instead of taking the better half (sample_select; numbers from a host
+generator of (seed, round)); k_min > 0 keeps k from falling below it."""
 import numpy as np
 import torch
 
@@ -25,12 +27,13 @@ from . import eck
 class EnergySearch:
     def __init__(self, problem, kind, measure, population=1 << 14, M=64, n_parents=None, depth=6, init_rounds=40,
                  update_rounds=8, mu=20.0, k_min=0.0, eta=0.3, lam=1.0, p_mut_q32=429496729, seed=1,
-                 max_rounds=64, crossover=False, dedup=False, meter_seconds=0.0, parents="model"):
-        assert parents in ("model", "measured")
+                 max_rounds=64, crossover=False, dedup=False, meter_seconds=0.0, parents="model", temperature=0.02):
+        assert parents in ("model", "measured", "sampled")
         self.space = eck.Space(problem, kind)
         self.measure, self.N, self.M = measure, int(population), int(M)
         self.parent_rule = parents
-        self.P = eck.k_count(0.5, self.M) if parents == "model" else int(n_parents)   # Alg. 1: 0.5 * M
+        self.P = eck.k_count(0.5, self.M) if parents == "model" or n_parents is None else int(n_parents)   # Alg. 1: 0.5 * M
+        self.temperature = float(temperature)
         self.init_rounds, self.update_rounds = int(init_rounds), int(update_rounds)
         self.mu, self.k_min, self.eta, self.lam = float(mu), float(k_min), float(eta), float(lam)
         self.p_mut, self.seed = int(p_mut_q32), int(seed)
@@ -75,6 +78,7 @@ class EnergySearch:
         self.ws_par = torch.empty(max(eck.topk_select_workspace_bytes(N, 1, self.P, m_latency=self.M),
                                       eck.topk_select_workspace_bytes(self.M, 1, min(self.P, self.M))),
                                   dtype=torch.uint8, device=dev)
+        self.uniform = torch.zeros((1, self.P), dtype=torch.float32, device=dev)  # parents="sampled": the numbers drawn with
         # host-side record of the measured kernels (a few hundred rows)
         self.h_genes = np.zeros((G, 0), dtype=np.uint16)
         self.h_energy = np.zeros(0, dtype=np.float32)
@@ -115,6 +119,18 @@ class EnergySearch:
                         self.ws_par, mode=eck.SELECT_RANK, m_latency=self.M)
         eck.candidates_gather(self.genes, self.N, self.par_idx.view(-1), self.P, self.parents)
 
+    def _parents_drawn(self):
+        """option parents="sampled": the M fastest kernels of this generation, rated again by the energy model as it is now, in order of
+        energy (a short pick's padding is of infinite energy, and never drawn); P draws among them"""
+        eck.treemodel_score(self.energy_model, self.feat, self.N, self.e_pred)
+        eck.topk_select(self.e_pred, self.l_pred, self.legal, 1, self.M, self.idx, self.e_sel, self.count, self.ws_topk,
+                        mode=eck.SELECT_RANK, m_latency=self.M)
+        g = torch.Generator().manual_seed(self.seed * 1000003 + self.round)
+        self.uniform.copy_(torch.rand((1, self.P), generator=g))
+        eck.sample_select(self.e_sel.view(-1), None, 1, self.uniform, self.par_idx, None, self.par_count, None, temperature=self.temperature)
+        self.par_idx.copy_(self.idx.view(-1)[self.par_idx.long().clamp_(min=0)])
+        eck.candidates_gather(self.genes, self.N, self.par_idx.view(-1), self.P, self.parents)
+
     def _first_parents(self, m):
         """the better half, by the freshly fitted energy model, of the first training set"""
         eck.treemodel_score(self.energy_model, self.new_feat, m, self.new_pred)
@@ -141,7 +157,7 @@ class EnergySearch:
         lat_dev = torch.from_numpy(latency).cuda()
         self._fit(self.latency_model, self.buf_feat, lat_dev, m, self.init_rounds)
         self._fit(self.energy_model, self.buf_feat, self.buf_energy, m, self.init_rounds)
-        if self.parent_rule == "model":
+        if self.parent_rule in ("model", "sampled"):
             self._first_parents(m)
         else:
             self._parents_from_the_record()
@@ -185,6 +201,9 @@ class EnergySearch:
             n_par = int(self.par_count.item())
             cols = self.par_idx.view(-1)[:n_par].cpu().numpy().astype(np.uint32)
             entry["parents"] = np.concatenate([cols, np.full(self.P - n_par, cols[0], dtype=np.uint32)])
+        elif self.parent_rule == "sampled":
+            self._parents_drawn()
+            entry["parents"] = self.par_idx.view(-1).cpu().numpy().view(np.uint32).copy()
         else:
             self._parents_from_the_record()
         self.history.append(entry)
