@@ -3,8 +3,9 @@
 //   g = s grad,  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g g,
 //   w <- w (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Everything is read and written once, so memory bounds it.  The tensors' addresses travel as kernel arguments, some dozens a launch,
-// so that a step needs no table on the device and a captured one holds its own.  Blocks of threads take stretches of a tensor.
+// Everything is read and written once, so memory bounds it.  The tensors' addresses travel as kernel arguments, so that a step needs no
+// table on the device and a captured one holds its own; a kilobyte of them takes about a microsecond (a launch of 72 bytes 3.3 us, of 4 KB 6.9,
+// of 14 KB 16), so a launch has room for 12, 48 or 200 tensors, whichever does.  Blocks of threads take stretches of a tensor.
 //
 // 8-bit states.  m is held in e4m3 and v in e5m2, each with a power of two for every 128 elements that brings the largest into
 // [2^7, 2^8) and [2^14, 2^15): steps of at most an eighth and a quarter of a number, down to 2^-17 and 2^-31 of the block's largest.
@@ -27,17 +28,32 @@ constexpr uint32_t ROUND = THREADS * EACH;           // of a block of threads at
 constexpr uint64_t MOST_ELEMENTS = 1ull << 40;
 static_assert(ECK_STATE_BLOCK == 32 * EACH, "a block of an 8-bit state is half a wavefront's");
 
-struct Tensor {
+template <bool EIGHT>
+struct Tensor;
+template <>
+struct Tensor<false> {
     float *param;
     const void *grad;
     void *m, *v;
-    uint8_t *m_scale, *v_scale;
     bf16 *copy;
-    uint64_t n, number; // number: of the first element, for the draws
-    uint32_t first;     // block of threads that starts it
-    int32_t grad_bf16;
-    float keep;         // 1 - lr decay
+    uint64_t n;
+    uint32_t first; // block of threads that starts it
+    float keep;     // 1 - lr decay
+    static constexpr uint8_t *m_scale = nullptr, *v_scale = nullptr;
 };
+template <>
+struct Tensor<true> {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    bf16 *copy;
+    uint64_t n;
+    uint32_t first;
+    float keep;
+    uint8_t *m_scale, *v_scale;
+    uint64_t number; // of the first element, for the draws
+};
+constexpr uint64_t OF_BF16 = 1ull << 63; // the highest bit of a number of elements: gradients of bf16
 struct Step {
     float beta1, beta2, one_beta1, one_beta2, eps, rate, inverse; // rate: lr / (1 - b1^t); inverse: 1 / (1 - b2^t)
     double lr, beta1_wide, beta2_wide;
@@ -46,14 +62,13 @@ struct Step {
     const uint32_t *more;    // or NULL: rate, inverse and state are those of t
     const float *grad_scale; // or NULL: 1
 };
-// arguments of one launch, at most 4 KB of them
-constexpr int AT_ONCE = 40;
+// arguments of one launch
+template <bool EIGHT, int ROOM>
 struct Tensors {
-    Tensor one[AT_ONCE];
-    uint32_t count, rounds; // rounds: of a block of threads
     Step step;
+    uint32_t count, rounds; // rounds: of a block of threads
+    Tensor<EIGHT> one[ROOM];
 };
-static_assert(sizeof(Tensors) <= 4096, "arguments of a launch");
 
 // which tensor a block of threads works on: the last whose first block, first(i), is not behind it
 template <class F>
@@ -164,14 +179,14 @@ struct Hold {
     S m[EACH], v[EACH];
     uint8_t m_scale, v_scale;
 
-    __device__ __forceinline__ void load(const Tensor &t, uint64_t at)
+    __device__ __forceinline__ void load(const Tensor<EIGHT> &t, uint64_t n, uint64_t at)
     {
-        fetch(t.param, at, t.n, w);
-        fetch((const G *)t.grad, at, t.n, g);
-        fetch((const S *)t.m, at, t.n, m);
-        fetch((const S *)t.v, at, t.n, v);
-        if (EIGHT) {
-            const bool there = at < t.n;
+        fetch(t.param, at, n, w);
+        fetch((const G *)t.grad, at, n, g);
+        fetch((const S *)t.m, at, n, m);
+        fetch((const S *)t.v, at, n, v);
+        if constexpr (EIGHT) {
+            const bool there = at < n;
             m_scale = there ? t.m_scale[at / ECK_STATE_BLOCK] : 0;
             v_scale = there ? t.v_scale[at / ECK_STATE_BLOCK] : 0;
         }
@@ -179,7 +194,7 @@ struct Hold {
 };
 
 template <bool EIGHT, class G>
-__device__ __forceinline__ void advance(const Tensor &t, uint64_t at, const Hold<EIGHT, G> &had, const Step &step, float rate, float inverse,
+__device__ __forceinline__ void advance(const Tensor<EIGHT> &t, uint64_t n, uint64_t at, const Hold<EIGHT, G> &had, const Step &step, float rate, float inverse,
                                         float scale, uint64_t state)
 {
     float w[EACH], m[EACH], v[EACH];
@@ -208,12 +223,12 @@ __device__ __forceinline__ void advance(const Tensor &t, uint64_t at, const Hold
         const float step_of = EIGHT ? m[i] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(corrected) + step.eps) : m[i] / (sqrtf(corrected) + step.eps);
         w[i] = fmaf(-rate, step_of, had.w[i] * t.keep);
     }
-    put(t.param, at, t.n, w);
+    put(t.param, at, n, w);
     if (t.copy) {
         bf16 c[EACH];
 #pragma unroll
         for (uint32_t i = 0; i < EACH; ++i) c[i] = (bf16)w[i];
-        put(t.copy, at, t.n, c);
+        put(t.copy, at, n, c);
     }
     if constexpr (EIGHT) {
         uint32_t for_m[EACH], for_v[EACH];
@@ -227,36 +242,36 @@ __device__ __forceinline__ void advance(const Tensor &t, uint64_t at, const Hold
         // (elements past the end are zeros with zero gradients: they count nothing)
         uint8_t code_m[EACH], code_v[EACH];
         const uint8_t scale_m = Eight<3>::encode(m, for_m, code_m), scale_v = Eight<2>::encode(v, for_v, code_v);
-        put((uint8_t *)t.m, at, t.n, code_m);
-        put((uint8_t *)t.v, at, t.n, code_v);
-        if (at % ECK_STATE_BLOCK == 0 && at < t.n) {
+        put((uint8_t *)t.m, at, n, code_m);
+        put((uint8_t *)t.v, at, n, code_v);
+        if (at % ECK_STATE_BLOCK == 0 && at < n) {
             t.m_scale[at / ECK_STATE_BLOCK] = scale_m;
             t.v_scale[at / ECK_STATE_BLOCK] = scale_v;
         }
     } else {
-        put((float *)t.m, at, t.n, m);
-        put((float *)t.v, at, t.n, v);
+        put((float *)t.m, at, n, m);
+        put((float *)t.v, at, n, v);
     }
 }
 
 template <bool EIGHT, class G>
-__device__ __forceinline__ void work(const Tensor &t, uint32_t block, uint32_t rounds, const Step &step, float rate, float inverse, float scale,
+__device__ __forceinline__ void work(const Tensor<EIGHT> &t, uint64_t n, uint32_t block, uint32_t rounds, const Step &step, float rate, float inverse, float scale,
                                      uint64_t state)
 {
     const uint64_t first = (uint64_t)block * rounds * ROUND + threadIdx.x * EACH;
     // (whole wavefronts stay together: 8-bit blocks are exchanged between lanes)
-    for (uint32_t r = 0; r < rounds && first - threadIdx.x * EACH + r * ROUND < t.n; ++r) {
+    for (uint32_t r = 0; r < rounds && first - threadIdx.x * EACH + r * ROUND < n; ++r) {
         const uint64_t at = first + r * ROUND;
         Hold<EIGHT, G> had;
-        had.load(t, at);
-        advance<EIGHT, G>(t, at, had, step, rate, inverse, scale, state);
+        had.load(t, n, at);
+        advance<EIGHT, G>(t, n, at, had, step, rate, inverse, scale, state);
     }
 }
 
-template <bool EIGHT>
-__global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors a)
+template <bool EIGHT, int ROOM>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors<EIGHT, ROOM> a)
 {
-    const Tensor &t = a.one[tensor_of(a.count, blockIdx.x, [&](uint32_t i) { return a.one[i].first; })];
+    const Tensor<EIGHT> &t = a.one[tensor_of(a.count, blockIdx.x, [&](uint32_t i) { return a.one[i].first; })];
     const float scale = a.step.grad_scale ? *a.step.grad_scale : 1.0f;
     if (!(__builtin_fabsf(scale) < __builtin_inff())) return; // gradients that are not finite: nothing changes
     float rate = a.step.rate, inverse = a.step.inverse;
@@ -277,22 +292,21 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors a)
         state = splitmix_finalise(a.step.seed + kGamma * ((uint64_t)now + 1));
     }
     const uint32_t block = blockIdx.x - t.first;
-    if (t.grad_bf16) work<EIGHT, bf16>(t, block, a.rounds, a.step, rate, inverse, scale, state);
-    else work<EIGHT, float>(t, block, a.rounds, a.step, rate, inverse, scale, state);
+    const uint64_t n = t.n & ~OF_BF16;
+    if (t.n & OF_BF16) work<EIGHT, bf16>(t, n, block, a.rounds, a.step, rate, inverse, scale, state);
+    else work<EIGHT, float>(t, n, block, a.rounds, a.step, rate, inverse, scale, state);
 }
 
 // ------------------------------------------------------------------------------------------------ norm
 
-constexpr int GRADIENTS_AT_ONCE = 200;
+template <int ROOM>
 struct GradientList {
-    const void *grad[GRADIENTS_AT_ONCE];
-    uint64_t n[GRADIENTS_AT_ONCE]; // the highest bit: of bf16
-    uint32_t first[GRADIENTS_AT_ONCE];
-    uint32_t count, stretch; // stretch: elements of a block of threads, a multiple of THREADS * 8
     double *sums;
+    uint32_t count, stretch; // stretch: elements of a block of threads, a multiple of THREADS * 8
+    const void *grad[ROOM];
+    uint64_t n[ROOM];
+    uint32_t first[ROOM];
 };
-constexpr uint64_t OF_BF16 = 1ull << 63;
-static_assert(sizeof(GradientList) <= 4096, "arguments of a launch");
 
 __device__ __forceinline__ double block_sum(double x, double *lds)
 {
@@ -338,7 +352,8 @@ __device__ __forceinline__ double squares(const G *grad, uint64_t from, uint64_t
     return sum;
 }
 
-__global__ __launch_bounds__(THREADS) void squares_kernel(const GradientList a)
+template <int ROOM>
+__global__ __launch_bounds__(THREADS) void squares_kernel(const GradientList<ROOM> a)
 {
     __shared__ double lds[THREADS / 64];
     const uint32_t t = tensor_of(a.count, blockIdx.x, [&](uint32_t i) { return a.first[i]; });
@@ -394,6 +409,71 @@ uint64_t norm_blocks(const eck_parameter *p, uint32_t count, uint64_t stretch)
     return blocks;
 }
 
+// tensors from `from` on, as many as there is room for, in one launch; advances `from` and the elements' number
+template <bool EIGHT, int ROOM>
+int32_t step_some(const eck_parameter *p, uint32_t count, uint32_t &from, uint64_t &number, const Step &step, hipStream_t st)
+{
+    Tensors<EIGHT, ROOM> a;
+    a.step = step;
+    a.count = 0;
+    a.rounds = 2;
+    uint64_t blocks = 0;
+    for (; from < count && a.count < ROOM; ++from) {
+        const eck_parameter &t = p[from];
+        if (t.n == 0) continue;
+        const uint64_t mine = (t.n + a.rounds * ROUND - 1) / (a.rounds * ROUND);
+        if (blocks + mine > 0x7FFFFFFF) break;
+        Tensor<EIGHT> &to = a.one[a.count++];
+        to.param = t.param, to.grad = t.grad, to.m = t.m, to.v = t.v, to.copy = (bf16 *)t.bf16_out;
+        to.n = t.n | (t.grad_dtype == ECK_BF16 ? OF_BF16 : 0);
+        to.first = (uint32_t)blocks;
+        to.keep = (float)(1.0 - step.lr * t.weight_decay);
+        if constexpr (EIGHT) to.m_scale = t.m_scale, to.v_scale = t.v_scale, to.number = number;
+        blocks += mine;
+        number += (t.n + ECK_STATE_BLOCK - 1) / ECK_STATE_BLOCK * ECK_STATE_BLOCK;
+    }
+    if (a.count == 0) return ECK_OK;
+    hipLaunchKernelGGL((adamw_kernel<EIGHT, ROOM>), dim3((uint32_t)blocks), dim3(THREADS), 0, st, a);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
+template <bool EIGHT>
+int32_t step_all(const eck_parameter *p, uint32_t count, const Step &step, hipStream_t st)
+{
+    uint64_t number = 0;
+    for (uint32_t from = 0; from < count;) {
+        const uint32_t left = count - from;
+        const int32_t rc = left <= 12   ? step_some<EIGHT, 12>(p, count, from, number, step, st)
+                           : left <= 48 ? step_some<EIGHT, 48>(p, count, from, number, step, st)
+                                        : step_some<EIGHT, 200>(p, count, from, number, step, st);
+        if (rc) return rc;
+    }
+    return ECK_OK;
+}
+
+template <int ROOM>
+int32_t squares_of_some(const eck_parameter *p, uint32_t count, uint32_t &from, double *&sums, uint64_t stretch, hipStream_t st)
+{
+    GradientList<ROOM> a;
+    a.sums = sums;
+    a.count = 0;
+    a.stretch = (uint32_t)stretch;
+    uint64_t blocks = 0;
+    for (; from < count && a.count < ROOM; ++from) {
+        const eck_parameter &t = p[from];
+        if (t.n == 0) continue;
+        a.grad[a.count] = t.grad;
+        a.n[a.count] = t.n | (t.grad_dtype == ECK_BF16 ? OF_BF16 : 0);
+        a.first[a.count++] = (uint32_t)blocks;
+        blocks += (t.n + stretch - 1) / stretch;
+    }
+    if (a.count == 0) return ECK_OK;
+    hipLaunchKernelGGL(squares_kernel<ROOM>, dim3((uint32_t)blocks), dim3(THREADS), 0, st, a);
+    ECK_HIP_TRY(hipGetLastError());
+    sums += blocks;
+    return ECK_OK;
+}
+
 } // namespace
 } // namespace eck
 
@@ -415,37 +495,15 @@ extern "C" int32_t adamw_step(const eck_parameter *parameters, uint32_t count, i
     }
     if (!aligned(step_more, 4) || !aligned(grad_scale, 4)) return ECK_EALIGN;
 
-    Tensors a;
-    a.count = 0;
-    a.rounds = 2;
-    a.step = {(float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps, 0.0f, 0.0f, lr, beta1, beta2, seed, 0, step,
-              step_more, grad_scale};
+    Step of = {(float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps, 0.0f, 0.0f, lr, beta1, beta2, seed, 0, step,
+               step_more, grad_scale};
     if (!step_more) {
-        a.step.rate = (float)(lr / (1.0 - pow(beta1, step)));
-        a.step.inverse = (float)(1.0 / (1.0 - pow(beta2, step)));
-        a.step.state = stream_state(seed, step);
+        of.rate = (float)(lr / (1.0 - pow(beta1, step)));
+        of.inverse = (float)(1.0 / (1.0 - pow(beta2, step)));
+        of.state = stream_state(seed, step);
     }
-    uint64_t number = 0, blocks = 0;
-    const auto launch = [&]() -> int32_t {
-        if (a.count == 0) return ECK_OK;
-        hipLaunchKernelGGL(eight ? adamw_kernel<true> : adamw_kernel<false>, dim3((uint32_t)blocks), dim3(THREADS), 0, as_stream(stream), a);
-        ECK_HIP_TRY(hipGetLastError());
-        a.count = 0;
-        blocks = 0;
-        return ECK_OK;
-    };
-    for (uint32_t i = 0; i < count; ++i) {
-        const eck_parameter &p = parameters[i];
-        if (p.n == 0) continue;
-        const uint64_t mine = (p.n + a.rounds * ROUND - 1) / (a.rounds * ROUND);
-        if (a.count == AT_ONCE || blocks + mine > 0x7FFFFFFF)
-            if (const int32_t rc = launch()) return rc;
-        a.one[a.count++] = {p.param, p.grad, p.m, p.v, p.m_scale, p.v_scale, (bf16 *)p.bf16_out, p.n, number, (uint32_t)blocks,
-                            p.grad_dtype == ECK_BF16, (float)(1.0 - lr * p.weight_decay)};
-        blocks += mine;
-        number += (p.n + ECK_STATE_BLOCK - 1) / ECK_STATE_BLOCK * ECK_STATE_BLOCK;
-    }
-    return launch();
+    if (eight) return step_all<true>(parameters, count, of, as_stream(stream));
+    return step_all<false>(parameters, count, of, as_stream(stream));
 }
 
 extern "C" uint64_t gradients_norm_workspace_bytes(const eck_parameter *parameters, uint32_t count)
@@ -463,30 +521,14 @@ extern "C" int32_t gradients_norm(const eck_parameter *parameters, uint32_t coun
     if (stretch > 0x7FFFFFFF || total > 0x7FFFFFFF) return ECK_EUNSUPPORTED;
     if (!ws || ws_bytes < total * sizeof(double)) return ECK_EWORKSPACE;
     if (!aligned(ws, 256) || !aligned(norm_out, 4) || !aligned(scale_out, 4)) return ECK_EALIGN;
-    GradientList a;
-    a.count = 0;
-    a.stretch = (uint32_t)stretch;
-    a.sums = (double *)ws;
-    uint64_t blocks = 0;
-    const auto launch = [&]() -> int32_t {
-        hipLaunchKernelGGL(squares_kernel, dim3((uint32_t)blocks), dim3(THREADS), 0, as_stream(stream), a);
-        ECK_HIP_TRY(hipGetLastError());
-        a.sums += blocks;
-        a.count = 0;
-        blocks = 0;
-        return ECK_OK;
-    };
-    for (uint32_t i = 0; i < count; ++i) {
-        const eck_parameter &p = parameters[i];
-        if (p.n == 0) continue;
-        if (a.count == GRADIENTS_AT_ONCE)
-            if (const int32_t rc = launch()) return rc;
-        a.grad[a.count] = p.grad;
-        a.n[a.count] = p.n | (p.grad_dtype == ECK_BF16 ? OF_BF16 : 0);
-        a.first[a.count++] = (uint32_t)blocks;
-        blocks += (p.n + stretch - 1) / stretch;
+    double *sums = (double *)ws;
+    for (uint32_t from = 0; from < count;) {
+        const uint32_t left = count - from;
+        const int32_t rc = left <= 16   ? squares_of_some<16>(parameters, count, from, sums, stretch, as_stream(stream))
+                           : left <= 64 ? squares_of_some<64>(parameters, count, from, sums, stretch, as_stream(stream))
+                                        : squares_of_some<256>(parameters, count, from, sums, stretch, as_stream(stream));
+        if (rc) return rc;
     }
-    if (const int32_t rc = launch()) return rc;
     hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(1024), 0, as_stream(stream), (const double *)ws, (uint32_t)total, max_norm, norm_out, scale_out);
     ECK_HIP_TRY(hipGetLastError());
     return ECK_OK;

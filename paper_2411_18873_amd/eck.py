@@ -698,20 +698,33 @@ def gatedffn_backward(x, w_gate_up, w_down, pre, dy, dx, dw_gate_up, dw_down, ws
 # ------------------------------------------------------------------------------ scoring in 8-bit integers
 
 
-def _here(t, dtype, name):
-    """a contiguous CUDA tensor of dtype on the current device"""
-    _dev(t, dtype, name)
+# (Small calls wait for the host, and every question that a tensor is asked takes it 0.1 us: the checks below ask each once, and the words
+# of a refusal are looked for when there is one.)
+
+
+def _refuse(t, dtype, name, what):
+    if not t.is_cuda or t.dtype is not dtype:
+        raise TypeError("%s must be %s of %s" % (name, what, dtype))
     if t.get_device() != _device():
         raise ValueError("%s must be on the current device" % name)
+    raise TypeError("%s must be %s" % (name, what))
+
+
+def _here(t, dtype, name):
+    """a contiguous CUDA tensor of dtype on the current device"""
+    if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or t.get_device() != _device():
+        _refuse(t, dtype, name, "a contiguous CUDA tensor")
     return t
 
 
-def _here_rows(t, name, dtype, shape=None):
-    """_rows of a matrix on the current device"""
-    ld = _rows(t, name, dtype, shape)
-    if t.get_device() != _device():
-        raise ValueError("%s must be on the current device" % name)
-    return ld
+def _here_rows(t, name, dtype, shape):
+    """the row distance of a matrix of that shape on the current device, values of a row side by side"""
+    is_shape, stride = t.shape, t.stride()
+    if is_shape != shape:
+        raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
+    if t.dtype is not dtype or not t.is_cuda or t.get_device() != _device() or (stride[1] != 1 and is_shape[1] != 1):
+        _refuse(t, dtype, name, "a CUDA matrix with adjacent columns")
+    return stride[0] if is_shape[0] > 1 else is_shape[1]
 
 
 def int8_rows(n, width):
@@ -722,9 +735,7 @@ def int8_rows(n, width):
 def _int8(t, name, shape):
     """the row distance of an int8 matrix: of a single row the next multiple of sixteen.  Its last row has to have all of its sixteens in
     memory"""
-    ld = _here_rows(t, name, torch.int8)
-    if t.shape != shape:
-        raise ValueError("%s must be of shape %s" % (name, tuple(shape)))
+    ld = _here_rows(t, name, torch.int8, shape)
     n, width = shape
     if width & 15 or n == 1:
         whole = -(-width // 16) * 16
@@ -743,13 +754,17 @@ def _scales(t, name, n):
 
 def quantise_rows(x, q, scale, order=ROWS):
     """q [n][width] (int8) and scale [n]: rows of x [n][width] (ROWS), or its first n columns [width][n or more] (COLUMNS), by their largest"""
-    n, width = q.shape
-    dtype = x.dtype if x.dtype in _FEAT_DTYPE else torch.float32
+    shape, dtype = q.shape, x.dtype
+    n, width = shape
     if order != COLUMNS:
-        ld_x = _here_rows(x, "x", dtype, q.shape)
+        ld_x = _here_rows(x, "x", dtype, shape)
     else:
-        ld_x = _feature_rows(x, n, width, dtype, "x")
-    _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", q.shape),
+        if x.shape[0] != width or x.shape[1] < n:
+            raise ValueError("x must be of shape (%d, %d or more)" % (width, n))
+        ld_x = _here_rows(x, "x", dtype, x.shape)
+    if dtype not in _FEAT_DTYPE:
+        raise TypeError("x must be of float32 or bfloat16")
+    _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", shape),
                                                 _scales(scale, "scale", n), _stream()))
 
 
@@ -759,15 +774,16 @@ def product_int8_workspace_bytes(n, n_in, n_out, act=ACT_NONE):
 
 def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
     """y [n][n_out] = x w^T times both scales, of int8 matrices [n][n_in] and [n_out][n_in]; with an activation, a(g) u of w [2 n_out][n_in]"""
-    (n, n_in), n_out = x.shape, y.shape[1]
-    if w.shape[0] != (n_out if act == ACT_NONE else 2 * n_out):
-        raise ValueError("w must have %d rows" % (n_out if act == ACT_NONE else 2 * n_out))
-    dtype = y.dtype if y.dtype in _FEAT_DTYPE else torch.float32
-    ld_y = _here_rows(y, "y", dtype, (n, n_out))
+    shape, dtype = x.shape, y.dtype
+    n, n_in = shape
+    n_out = y.shape[1]
+    rows = n_out if act == ACT_NONE else 2 * n_out
+    if dtype not in _FEAT_DTYPE:
+        raise TypeError("y must be of float32 or bfloat16")
     ws_ptr, ws_bytes = _ws(ws)
     _check("product_int8", lib().product_int8(
-        x.data_ptr(), _int8(x, "x", x.shape), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", (w.shape[0], n_in)),
-        _scales(w_scale, "w_scale", w.shape[0]), act, _FEAT_DTYPE[dtype], y.data_ptr(), ld_y, ws_ptr, ws_bytes, _stream()))
+        x.data_ptr(), _int8(x, "x", shape), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", (rows, n_in)),
+        _scales(w_scale, "w_scale", rows), act, _FEAT_DTYPE[dtype], y.data_ptr(), _here_rows(y, "y", dtype, (n, n_out)), ws_ptr, ws_bytes, _stream()))
 
 
 # ------------------------------------------------------------------------------ refits of models of many tensors
@@ -859,22 +875,30 @@ def sample_select_workspace_bytes(n, n_segments, draws):
     return int(lib().sample_select_workspace_bytes(n, n_segments, draws))
 
 
+def _drawn(t, dtype, name, n):
+    """the address of a result of n elements of that type on the current device, or None"""
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return _here(t, dtype, name).data_ptr()
+
+
 def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, count_out, ws, temperature=1.0, k=0, top_p=1.0, min_p=0.0):
     """idx_out [n_segments][draws] = candidates drawn by exp(-energy / temperature) with the numbers uniform [n_segments][draws], of the k least
     (0: all) that have the share top_p of the weight and min_p of the best one's or more; logprob_out (as idx_out) and count_out may be None"""
-    if uniform.dim() != 2 or uniform.shape[0] != n_segments:
+    shape = uniform.shape
+    if len(shape) != 2 or shape[0] != n_segments:
         raise ValueError("uniform must be of shape (%d, draws)" % n_segments)
-    _here(energy, torch.float32, "energy")
-    _here(uniform, torch.float32, "uniform")
-    draws = uniform.shape[1]
-    for t, name, n, size in ((legal, "legal", energy.numel(), 1), (idx_out, "idx_out", n_segments * draws, 4),
-                             (logprob_out, "logprob_out", n_segments * draws, 4), (count_out, "count_out", n_segments, 4)):
-        if t is None and name != "idx_out":
-            continue
-        if t.numel() != n or t.element_size() != size:
-            raise ValueError("%s must have %d elements of %d bytes" % (name, n, size))
-        _here(t, torch.float32 if name == "logprob_out" else t.dtype, name)
+    draws, n = shape[1], energy.numel()
+    if idx_out is None:
+        raise ValueError("idx_out must not be None")
+    flags = torch.uint8 if legal is None or legal.element_size() != 1 else legal.dtype
+    whole = lambda t: t.dtype if t is not None and t.element_size() == 4 else torch.int32  # noqa: E731
     ws_ptr, ws_bytes = _ws(ws)
     _check("sample_select", lib().sample_select(
-        energy.data_ptr(), _ptr(legal), energy.numel(), n_segments, uniform.data_ptr(), draws, temperature, k, top_p, min_p, idx_out.data_ptr(),
-        _ptr(logprob_out), _ptr(count_out), ws_ptr, ws_bytes, _stream()))
+        _here(energy, torch.float32, "energy").data_ptr(), _drawn(legal, flags, "legal", n), n, n_segments,
+        _here(uniform, torch.float32, "uniform").data_ptr(), draws, temperature, k, top_p, min_p,
+        _drawn(idx_out, whole(idx_out), "idx_out", n_segments * draws),
+        _drawn(logprob_out, torch.float32, "logprob_out", n_segments * draws),
+        _drawn(count_out, whole(count_out), "count_out", n_segments), ws_ptr, ws_bytes, _stream()))

@@ -93,7 +93,7 @@ def test_step_with_32_bit_states(kind, offset):
     check_step(SIZES, kind, 1 + offset, offset)
 
 
-@pytest.mark.parametrize("count", [1, 39, 40, 41, 200])
+@pytest.mark.parametrize("count", [1, 12, 13, 48, 49, 200, 201, 450])
 def test_as_many_tensors_as_there_are(count):
     check_step([1 + 37 * i % 301 for i in range(count)], "both", count)
 

@@ -127,3 +127,21 @@ def test_sample_select_validates_before_launch():
     assert call(n=(1 << 31) + 1, seg=1) == eck.EUNSUPPORTED
     assert call(energy=FAKE + 2) == call(uniform=FAKE + 1) == call(idx=FAKE + 2) == call(logprob=FAKE + 2) == call(count=FAKE + 1) == eck.EALIGN
     assert W(0, 1, 1) == W(10, 3, 1) == W(10, 0, 1) == W(10, 1, 0) == 0
+
+
+def test_the_binding_refuses_what_it_cannot_pass_on():
+    """tensors that are not on the GPU, of other shapes and types: refused before the library is called"""
+    f, b, q = torch.zeros(4, 16), torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(4, 16, dtype=torch.int8)
+    for call in (lambda: eck.quantise_rows(f, q, torch.zeros(4)), lambda: eck.quantise_rows(f.double(), q, torch.zeros(4)),
+                 lambda: eck.product_int8(q, torch.zeros(4), q, torch.zeros(4), torch.zeros(4, 4), None),
+                 lambda: eck.product_int8(q, torch.zeros(4), q, torch.zeros(4), torch.zeros(4, 4).double(), None),
+                 lambda: eck.sample_select(f.view(-1), None, 1, torch.zeros(1, 2), torch.zeros(2, dtype=torch.int32), None, None, None)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: eck.quantise_rows(f, torch.zeros(4, 15, dtype=torch.int8), torch.zeros(4)),
+                 lambda: eck.quantise_rows(b, torch.zeros(17, 4, dtype=torch.int8), torch.zeros(17), order=eck.COLUMNS),
+                 lambda: eck.sample_select(f.view(-1), None, 2, torch.zeros(1, 2), torch.zeros(2, dtype=torch.int32), None, None, None),
+                 lambda: eck.sample_select(f.view(-1), None, 1, torch.zeros(2), torch.zeros(2, dtype=torch.int32), None, None, None),
+                 lambda: eck.sample_select(f.view(-1), None, 1, torch.zeros(1, 2), None, None, None, None)):
+        with pytest.raises(ValueError):
+            call()
