@@ -161,7 +161,7 @@ struct Eight {
             const bool small = size < least;
             const uint32_t raised = __float_as_uint(small ? size + least : size) + (draw[i] << (DROP - 16));
             uint32_t c = (raised >> DROP) - ((uint32_t)(LOW + (small ? 127 : 126)) << FRACTION);
-            if (FRACTION == 2) c = max(c, y > 0.0f ? 1u : 0u);
+            if (FRACTION == 2) c = max(c, x[i] > 0.0f ? 1u : 0u);
             c = size < __builtin_inff() ? c : 0x7Fu;
             if (FRACTION == 3) c |= __float_as_uint(y) >> 24 & 0x80;
             code[i] = (uint8_t)c;
@@ -255,8 +255,8 @@ __device__ __forceinline__ void advance(const Tensor<EIGHT> &t, uint64_t n, uint
 }
 
 template <bool EIGHT, class G>
-__device__ __forceinline__ void work(const Tensor<EIGHT> &t, uint64_t n, uint32_t block, uint32_t rounds, const Step &step, float rate, float inverse, float scale,
-                                     uint64_t state)
+__device__ __forceinline__ void work(const Tensor<EIGHT> &t, uint64_t n, uint32_t block, uint32_t rounds, const Step &step, float rate,
+                                     float inverse, float scale, uint64_t state)
 {
     const uint64_t first = (uint64_t)block * rounds * ROUND + threadIdx.x * EACH;
     // (whole wavefronts stay together: 8-bit blocks are exchanged between lanes)
@@ -278,6 +278,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors<EIGHT, ROO
     uint64_t state = a.step.state;
     if (a.step.more) {
         const uint32_t now = a.step.t + *a.step.more;
+        if (now == 0) return; // (there is no step before the first)
         double power1 = 1.0, power2 = 1.0, square1 = a.step.beta1_wide, square2 = a.step.beta2_wide;
         for (uint32_t k = now; k; k >>= 1) {
             if (k & 1) {

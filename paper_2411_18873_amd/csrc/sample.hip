@@ -834,21 +834,22 @@ __global__ __launch_bounds__(LONG_THREADS) __attribute__((amdgpu_waves_per_eu(8)
         at[1] = narrow<LONG_THREADS>(s, bins[0], at[1], weight_goal(p.a, limited, at[0], of_range, total), true);
     }
     if (first) of.by_count = at[0], of.by_weight = at[1], of.total = total;
-    clear_bins<LONG_THREADS>(bins[0], weights);
-    clear_bins<LONG_THREADS>(bins[1], weights);
+    // (one histogram where one is wanted: with both in the LDS a compute unit has room for one block, not two)
+    Histogram &of_count = bins[0], &of_weight = bins[p.a.k ? 1 : 0];
+    if (limited) clear_bins<LONG_THREADS>(of_count, weights);
+    if (weights) clear_bins<LONG_THREADS>(of_weight, true);
     const uint32_t shift[2] = {shift_of(at[0]), shift_of(at[1])};
     each_of_piece(p.a, segment, from, to, [&](uint32_t key, uint32_t) {
         const uint32_t place[2] = {key, scale(key)};
         const bool in[2] = {limited && key >= at[0].lo && key <= at[0].hi, weights && place[1] >= at[1].lo && place[1] <= at[1].hi};
         if (!in[0] && !in[1]) return;
         const double w = weights ? weight_of(key, best, p.a.per_temperature) : 0.0;
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-            if (in[r]) add_to_bins(bins[r], (place[r] - at[r].lo) >> shift[r], weights, w);
+        if (in[0]) add_to_bins(of_count, (place[0] - at[0].lo) >> shift[0], weights, w);
+        if (in[1]) add_to_bins(of_weight, (place[1] - at[1].lo) >> shift[1], true, w);
     });
     __syncthreads();
-    if (limited) write_bins(p.parts[blockIdx.x], bins[0], weights); // (the first ones are not needed again)
-    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], bins[1], true);
+    if (limited) write_bins(p.parts[blockIdx.x], of_count, weights); // (the first ones are not needed again)
+    if (weights) write_bins(p.parts[p.segments * p.pieces + blockIdx.x], of_weight, true);
 }
 
 // The ranges again, by the second histograms, and the candidates in them
@@ -1737,14 +1738,14 @@ int32_t launch_long(const Draws &a, uint32_t segments, void *ws, hipStream_t st)
         const auto join = [&](int which) {
             if (p.pieces > 1) hipLaunchKernelGGL(join_bins_kernel, dim3(segments * JOIN_BLOCKS), threads, 0, st, p, which);
         };
-        constexpr int two = 2 * sizeof(Histogram);
-        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(second_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, two));
-        const int first = a.k && weights ? two : two / 2;
-        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(first_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, first));
-        hipLaunchKernelGGL(first_bins_kernel, pieces, threads, first, st, p);
+        constexpr int one = sizeof(Histogram);
+        const int bins = a.k && weights ? 2 * one : one;
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(first_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bins));
+        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(second_bins_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bins));
+        hipLaunchKernelGGL(first_bins_kernel, pieces, threads, bins, st, p);
         if (a.k) join(0);
         if (weights) join(1);
-        hipLaunchKernelGGL(second_bins_kernel, pieces, threads, two, st, p);
+        hipLaunchKernelGGL(second_bins_kernel, pieces, threads, bins, st, p);
         if (a.k) join(0);
         if (weights) join(1);
         hipLaunchKernelGGL(list_kernel, pieces, threads, 0, st, p);

@@ -164,6 +164,20 @@ def test_energies_next_to_each_other_with_outliers(n):
         check(e, None, g.random((2, 20)).astype(np.float32), temperature=3.0, **how)
 
 
+@pytest.mark.parametrize("n", [9000, 60000])
+def test_ends_next_to_zero(n):
+    """more than a list takes on both sides of 0, zeros of both signs among them: ranges of keys end there"""
+    g = np.random.default_rng(n)
+    e = (g.integers(-3, 4, (4, n)) * 1e-45).astype(np.float32)
+    e[0, ::5] = -0.0
+    e[1] = np.where(g.random(n) < 0.5, -0.0, -1e-45).astype(np.float32)
+    e[2] = np.abs(e[2])
+    below = int((e < 0).sum(1).max())
+    for k in (5, below - 1, below, below + 1, below + 40, n - 1):
+        check(e, None, g.random((4, 10)).astype(np.float32), temperature=1e-3, k=k)
+        check(e, None, g.random((4, 10)).astype(np.float32), temperature=1e-3, k=k, top_p=0.7)
+
+
 def test_results_that_are_not_wanted_may_be_left_out():
     e, flags, u = inputs(3, 700, 20, 1)
     put = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
