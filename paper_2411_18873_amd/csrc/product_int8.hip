@@ -343,8 +343,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
 
 // Rows of up to 64 * STEPS integers, many of them: what is written bounds it, or the activations.  A wavefront keeps the weights and scales
 // of 64 columns (GATE: and of their ups) in registers and goes over rows, sixteen at a time, with no LDS and no barrier.  Matrix rows are
-// handed out so that a lane's sums of four matrix instructions are sixteen neighbouring columns of one row: whole cache lines are written
-// from the registers.  2^18 rows of 64, 256 gated columns: 88 us by tiles.
+// handed out so that a lane's sums of four matrix instructions make pieces of sixteen bytes of one row, which lie next to those of the other
+// lanes: results are written from the registers.  2^18 rows of 64, 256 gated columns: 88 us by tiles.
 template <class T, bool GATE_, int STEPS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && STEPS > 1 ? 2 : 3))) void short_rows_kernel(const Int8Product p, uint32_t groups)
 {
@@ -357,9 +357,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
     const i32x4 none = {0, 0, 0, 0};
     i32x4 w[SIDES][4][STEPS];
     float scale[SIDES][16];
+    // the column of sum number i (of sixteen) of the lanes of a quarter of the wavefront
+    constexpr int N = Chunk<T>::N;
+    const auto column = [&](int i, uint32_t quarter) { return c0 + i / N * (4 * N) + N * quarter + i % N; };
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const uint32_t c = c0 + 16 * (r >> 2) + 4 * t + (r & 3);
+        const uint32_t c = column(4 * t, r >> 2) + (r & 3);
 #pragma unroll
         for (int side = 0; side < SIDES; ++side)
 #pragma unroll
@@ -369,11 +372,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
                 w[side][t][s] = c < p.to.n_out && k < whole ? *reinterpret_cast<const i32x4 *>(row + k) : none;
             }
     }
-    const uint32_t mine = c0 + 16 * g; // a lane's columns of the result
 #pragma unroll
     for (int side = 0; side < SIDES; ++side)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) scale[side][i] = mine + i < p.to.n_out ? p.to.w_scale[side * p.to.n_out + mine + i] : 0.0f;
+        for (int i = 0; i < 16; ++i) scale[side][i] = column(i, g) < p.to.n_out ? p.to.w_scale[side * p.to.n_out + column(i, g)] : 0.0f;
 
     i32x4 x[STEPS], next[STEPS];
     float row_scale, next_scale;
@@ -412,13 +414,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
         }
         if (m < p.n) {
             T *row = (T *)p.to.y + m * p.to.ld_y;
-            constexpr int N = Chunk<T>::N;
 #pragma unroll
             for (int i = 0; i < 16; i += N) {
                 float some[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j) some[j] = y[i + j];
-                if (mine + i < p.to.n_out) store_chunk(row, mine + i, p.to.n_out, some);
+                if (column(i, g) < p.to.n_out) store_chunk(row, column(i, g), p.to.n_out, some);
             }
         }
 #pragma unroll
