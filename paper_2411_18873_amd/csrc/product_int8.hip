@@ -377,21 +377,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
 #pragma unroll
         for (int i = 0; i < 16; ++i) scale[side][i] = column(i, g) < p.to.n_out ? p.to.w_scale[side * p.to.n_out + column(i, g)] : 0.0f;
 
+    // Rows past the last are the last one again, k's past the end the first ones (times weights of 0): no load depends on a condition, and in
+    // the loop over whole tiles no store does, so that the wait for the next rows need not be one for all stores before them
+    // (2^18-64-256 gate, results past the last-level cache: 56 us with conditions, 50 without).  Stores that pass the caches take 39, but the
+    // next operator's reads more than that: with quantise_rows behind it 92 us for 82
     i32x4 x[STEPS], next[STEPS];
     float row_scale, next_scale;
     const auto load = [&](uint32_t of, i32x4(&to)[STEPS], float &s_to) {
-        const uint32_t m = of * 16 + r;
-        const bool there = of < tiles && m < p.n;
+        const uint32_t m = min(of * 16 + r, p.n - 1);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const uint32_t k = s * 64 + g * 16;
-            to[s] = there && k < whole ? *reinterpret_cast<const i32x4 *>(p.x + (uint64_t)m * p.ld_x + k) : none;
+            to[s] = *reinterpret_cast<const i32x4 *>(p.x + (uint64_t)m * p.ld_x + (k < whole ? k : 0));
         }
-        s_to = there ? p.to.x_scale[m] : 0.0f;
+        s_to = p.to.x_scale[m];
     };
-    load(tile, x, row_scale);
-    for (; tile < tiles; tile += step) {
-        load(tile + step, next, next_scale);
+    const auto rows_of = [&](uint32_t of, auto all_there) {
+        constexpr bool ALL = decltype(all_there)::value;
+        load(min(of + step, tiles - 1), next, next_scale);
         i32x4 sum[SIDES][4];
 #pragma unroll
         for (int side = 0; side < SIDES; ++side)
@@ -401,7 +404,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) sum[side][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[side][t][s], x[s], sum[side][t], 0, 0, 0);
             }
-        const uint64_t m = (uint64_t)tile * 16 + r;
+        const uint64_t m = (uint64_t)of * 16 + r;
         float y[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[i] = (float)sum[0][i / 4][i % 4] * row_scale * scale[0][i];
@@ -412,20 +415,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && ST
                     y[i] = gate_as<decltype(act)::value, sizeof(T) == 4>(y[i]).value * ((float)sum[1][i / 4][i % 4] * row_scale * scale[1][i]);
             });
         }
-        if (m < p.n) {
-            T *row = (T *)p.to.y + m * p.to.ld_y;
+        T *row = (T *)p.to.y + m * p.to.ld_y;
 #pragma unroll
-            for (int i = 0; i < 16; i += N) {
+        for (int i = 0; i < 16; i += N) {
+            if constexpr (ALL) {
+                Chunk<T> some;
+#pragma unroll
+                for (int j = 0; j < N; ++j) some.v[j] = (T)y[i + j];
+                *reinterpret_cast<Chunk<T> *>(row + column(i, g)) = some;
+            } else if (m < p.n && column(i, g) < p.to.n_out) {
                 float some[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j) some[j] = y[i + j];
-                if (column(i, g) < p.to.n_out) store_chunk(row, column(i, g), p.to.n_out, some);
+                store_chunk(row, column(i, g), p.to.n_out, some);
             }
         }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) x[s] = next[s];
         row_scale = next_scale;
-    }
+    };
+    load(tile, x, row_scale);
+    if (c0 + 64 <= p.to.n_out)
+        for (; tile < p.n / 16; tile += step) rows_of(tile, std::true_type{});
+    for (; tile < tiles; tile += step) rows_of(tile, std::false_type{});
 }
 
 // ------------------------------------------------------------------------------------------------ host

@@ -199,12 +199,18 @@ int32_t launch_rows(const void *x, uint64_t ld_x, uint64_t n, uint32_t width, in
 template <class T>
 int32_t launch_columns(const void *x, uint64_t ld_x, uint64_t n, uint32_t width, int8_t *q, uint64_t ld_q, float *scale, hipStream_t st)
 {
-    const uint32_t columns = width <= 64 ? 128 : 64;
-    const dim3 grid((uint32_t)((n + columns - 1) / columns));
-    hipLaunchKernelGGL((columns == 128 ? columns_kernel<T, 16, true> : columns_kernel<T, 8, false>), grid, dim3(256), 0, st, (const T *)x, ld_x, n, width, q,
-                       ld_q, scale);
-    ECK_HIP_TRY(hipGetLastError());
-    return ECK_OK;
+    const auto go = [&](auto kernel, uint32_t columns) -> int32_t {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)((n + columns - 1) / columns)), dim3(256), 0, st, (const T *)x, ld_x, n, width, q, ld_q, scale);
+        ECK_HIP_TRY(hipGetLastError());
+        return ECK_OK;
+    };
+    if (width <= 64) return go(columns_kernel<T, 16, true>, 128);
+    // as many columns a block as leave a block for every compute unit, and with the fewer more rows at a time (a column of 2920: 60 us where a
+    // block takes 128 rows of 64 columns, 9 where it takes 1024 of 8)
+    if (n >= 256 * 64) return go(columns_kernel<T, 8, false>, 64);
+    if (n >= 256 * 32) return go(columns_kernel<T, 4, false>, 32);
+    if (n >= 256 * 16) return go(columns_kernel<T, 2, false>, 16);
+    return go(columns_kernel<T, 1, false>, 8);
 }
 
 } // namespace
