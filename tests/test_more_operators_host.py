@@ -124,7 +124,11 @@ def test_sample_select_validates_before_launch():
     assert call(t=-0.1) == call(t=nan) == call(t=inf) == call(top_p=0.0) == call(top_p=1.01) == call(top_p=nan) == eck.EINVAL
     assert call(min_p=-0.1) == call(min_p=1.01) == call(min_p=nan) == eck.EINVAL
     assert call(seg=3) == eck.ESHAPE
-    assert call(n=(1 << 31) + 1, seg=1) == eck.EUNSUPPORTED
+    assert call(n=(1 << 31) + 1, seg=1) == call(n=(1 << 21) + 2, seg=(1 << 20) + 1) == eck.EUNSUPPORTED
+    need = W(1 << 18, 1, 8)
+    assert need > 0 == W(1 << 14, 1, 8) == W(1 << 20, 64, 8) and W((1 << 31) + 1, 1, 8) == W((1 << 21) + 2, (1 << 20) + 1, 8) == 0
+    assert call(n=1 << 18, seg=1, ws=None) == call(n=1 << 18, seg=1, ws_bytes=need - 1) == eck.EWORKSPACE
+    assert call(n=1 << 18, seg=1, ws=FAKE + 16) == eck.EALIGN
     assert call(energy=FAKE + 2) == call(uniform=FAKE + 1) == call(idx=FAKE + 2) == call(logprob=FAKE + 2) == call(count=FAKE + 1) == eck.EALIGN
     assert W(0, 1, 1) == W(10, 3, 1) == W(10, 0, 1) == W(10, 1, 0) == 0
 
