@@ -667,7 +667,7 @@ typedef struct {
  * 8BIT states: m in the float8 format e4m3, v in e5m2 (all bytes 0: a state of
  * zeros), times 2^(scale - 127) of the block of ECK_STATE_BLOCK elements, which
  * brings its largest finite one into [2^7, 2^8) or [2^14, 2^15) (scales of 27 to
- * 227).  They are rounded up or down to the format's next number by 16-bit
+ * 247).  They are rounded up or down to the format's next number by 16-bit
  * draws d: up iff d / 2^16 + (the way to the next lower one, in steps) >= 1; a v
  * that is not 0 does not become 0, what is not finite becomes NaN.  Elements are
  * numbered over the list, every tensor from a multiple of ECK_STATE_BLOCK on;

@@ -152,7 +152,7 @@ struct Eight {
         }
         most = half_most(most);
         const int exponent = (int)(__float_as_uint(most) >> 23) - 127;
-        const int power = min(max(exponent - TOP, -100), 100);
+        const int power = max(exponent - TOP, -100);
         const float down = power_of_two(-power), least = power_of_two(LOW);
 #pragma unroll
         for (uint32_t i = 0; i < EACH; ++i) {

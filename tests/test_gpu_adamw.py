@@ -216,6 +216,27 @@ def test_states_of_zero_bytes_are_zeros_and_no_v_becomes_zero():
     assert torch.isfinite(param).all()
 
 
+@pytest.mark.parametrize("size", [1e15, 1e17, 1e18, 1e20, 2e20])
+def test_8_bit_states_of_the_largest_gradients(size):
+    """squares up to the end of fp32: a state is the format's number below or above, a quarter (v) or an eighth (m) off at most"""
+    n = 300
+    g = torch.linspace(0.3, 1.0, n).double() * size
+    grads = torch.where(torch.arange(n) % 3 == 0, -g, g).float().cuda()
+    param = torch.zeros(n, device="cuda")
+    m, v = [torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(-(-n // eck.STATE_BLOCK), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    p = eck.Parameters([grads], [param], [m], [v], [scales[0]], [scales[1]])
+    for step in range(1, 4):
+        eck.adamw_step(p, lr=1e-3, step=step, seed=5)
+        got_m, got_v = [t.view(kind).double() * torch.exp2(s.double() - 127).repeat_interleave(eck.STATE_BLOCK)[:n]
+                        for t, kind, s in ((m, torch.float8_e4m3fn, scales[0]), (v, torch.float8_e5m2, scales[1]))]
+        # (each step's rounding is part of the next one's state)
+        want_m, want_v = (1 - 0.9 ** step) * grads.double(), (1 - 0.999 ** step) * grads.double() ** 2
+        assert ((got_m - want_m).abs() <= step * 0.126 * want_m.abs()).all()
+        assert ((got_v - want_v).abs() <= step * 0.251 * want_v).all()
+        assert (param * grads <= 0).all() and torch.isfinite(param).all()  # (0 where v / (1 - beta2^t) passes fp32's range)
+
+
 def test_8_bit_roundings_are_right_on_average():
     """the same step from the same state under 4000 seeds: the mean of the new states is the state in 32 bits.  A rounding is off by f(1 - f)
     of a step squared at most a quarter, so the mean of k of them by half a step over root k, and six times that is not seen"""
