@@ -678,7 +678,7 @@ typedef struct {
  * launch takes some dozens of tensors.
  * Errors: EINVAL (nulls, no element at all, a bad dtype or state, lr, eps or a
  * decay negative or not finite, a beta outside [0, 1), step 0 without
- * step_more), EUNSUPPORTED (n > 2^40), EALIGN. */
+ * step_more), EUNSUPPORTED (n > 2^34), EALIGN. */
 int32_t adamw_step(const eck_parameter *parameters, uint32_t count, int32_t state, double lr, double beta1, double beta2,
                    double eps, uint32_t step, const uint32_t *step_more, const float *grad_scale, uint64_t seed, void *stream);
 
@@ -689,7 +689,7 @@ int32_t adamw_step(const eck_parameter *parameters, uint32_t count, int32_t stat
  *   is not finite (device float; one may be NULL).
  * The query says 0 for lists that are refused.
  * Errors: EINVAL (nulls, no element at all, a bad dtype, max_norm not above 0),
- * EUNSUPPORTED (n > 2^40), EWORKSPACE, EALIGN (ws: 256 bytes). */
+ * EUNSUPPORTED (n > 2^34), EWORKSPACE, EALIGN (ws: 256 bytes). */
 uint64_t gradients_norm_workspace_bytes(const eck_parameter *parameters, uint32_t count);
 int32_t gradients_norm(const eck_parameter *parameters, uint32_t count, float max_norm, float *norm_out, float *scale_out,
                        void *ws, uint64_t ws_bytes, void *stream);

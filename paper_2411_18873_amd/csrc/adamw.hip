@@ -25,7 +25,7 @@ namespace {
 
 constexpr uint32_t THREADS = 256, EACH = 4;          // elements of a thread at a time: 32 lanes share an 8-bit block
 constexpr uint32_t ROUND = THREADS * EACH;           // of a block of threads at a time
-constexpr uint64_t MOST_ELEMENTS = 1ull << 40;
+constexpr uint64_t MOST_ELEMENTS = 1ull << 34, MOST_BLOCKS = (1u << 24) - 1; // (a launch has less than 2^32 threads)
 static_assert(ECK_STATE_BLOCK == 32 * EACH, "a block of an 8-bit state is half a wavefront's");
 
 template <bool EIGHT>
@@ -423,7 +423,7 @@ int32_t step_some(const eck_parameter *p, uint32_t count, uint32_t &from, uint64
         const eck_parameter &t = p[from];
         if (t.n == 0) continue;
         const uint64_t mine = (t.n + a.rounds * ROUND - 1) / (a.rounds * ROUND);
-        if (blocks + mine > 0x7FFFFFFF) break;
+        if (blocks + mine > MOST_BLOCKS) break;
         Tensor<EIGHT> &to = a.one[a.count++];
         to.param = t.param, to.grad = t.grad, to.m = t.m, to.v = t.v, to.copy = (bf16 *)t.bf16_out;
         to.n = t.n | (t.grad_dtype == ECK_BF16 ? OF_BF16 : 0);
@@ -519,7 +519,7 @@ extern "C" int32_t gradients_norm(const eck_parameter *parameters, uint32_t coun
     if ((!norm_out && !scale_out) || !(max_norm > 0.0f)) return ECK_EINVAL;
     if (const int32_t rc = check_list(parameters, count, true)) return rc;
     const uint64_t stretch = norm_stretch(parameters, count), total = norm_blocks(parameters, count, stretch);
-    if (stretch > 0x7FFFFFFF || total > 0x7FFFFFFF) return ECK_EUNSUPPORTED;
+    if (stretch > 0x7FFFFFFF || total > MOST_BLOCKS) return ECK_EUNSUPPORTED;
     if (!ws || ws_bytes < total * sizeof(double)) return ECK_EWORKSPACE;
     if (!aligned(ws, 256) || !aligned(norm_out, 4) || !aligned(scale_out, 4)) return ECK_EALIGN;
     double *sums = (double *)ws;

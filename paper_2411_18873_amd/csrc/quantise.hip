@@ -200,8 +200,13 @@ template <class T>
 int32_t launch_columns(const void *x, uint64_t ld_x, uint64_t n, uint32_t width, int8_t *q, uint64_t ld_q, float *scale, hipStream_t st)
 {
     const auto go = [&](auto kernel, uint32_t columns) -> int32_t {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)((n + columns - 1) / columns)), dim3(256), 0, st, (const T *)x, ld_x, n, width, q, ld_q, scale);
-        ECK_HIP_TRY(hipGetLastError());
+        const uint64_t most = (uint64_t)columns << 22; // (a launch has less than 2^32 threads)
+        for (uint64_t from = 0; from < n; from += most) {
+            const uint64_t some = n - from < most ? n - from : most;
+            hipLaunchKernelGGL(kernel, dim3((uint32_t)((some + columns - 1) / columns)), dim3(256), 0, st, (const T *)x + from, ld_x, some, width,
+                               q + from * ld_q, ld_q, scale + from);
+            ECK_HIP_TRY(hipGetLastError());
+        }
         return ECK_OK;
     };
     if (width <= 64) return go(columns_kernel<T, 16, true>, 128);

@@ -235,3 +235,17 @@ def test_a_gated_block_in_8_bits_on_a_stream_and_as_a_graph(n):
         gate, up = (x.double() @ weights[0].double()).chunk(2, 1)
         want = (gate * torch.sigmoid(gate) * up) @ weights[1].double()
         assert (eager["y"].double() - want).norm() <= 0.03 * want.norm()
+
+
+def test_candidates_past_2e29_columns():
+    """more columns than one launch takes: the last ones, those at the border of two launches, and offsets past 2^32 bytes"""
+    n = (1 << 29) + 1000
+    x = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+    some = torch.tensor([0, 1, 127, 128, (1 << 29) - 1, 1 << 29, (1 << 29) + 1, n - 1], device="cuda")
+    values = torch.tensor([1.0, -2.0, 0.5, 3.0, -4.0, 5.0, -0.25, 6.0], device="cuda")
+    x[0, some] = values.bfloat16()
+    q, scale = torch.full((n, 16), 7, dtype=torch.int8, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    eck.quantise_rows(x, q[:, :1], scale, order=eck.COLUMNS)
+    assert torch.equal(q[some, 0].float(), 127 * values.sign()) and torch.allclose(scale[some], values.abs() / 127, rtol=2.0 ** -23, atol=0)
+    assert (q[some, 1:] == 0).all()
+    assert torch.count_nonzero(scale) == some.numel() and torch.count_nonzero(q[:, 0]) == some.numel()

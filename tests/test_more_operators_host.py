@@ -35,7 +35,7 @@ def test_adamw_validates_before_launch():
     assert call(entry(n=0, param=None)) == eck.EINVAL           # no element at all
     assert call(entry(n=0), entry(grad_dtype=2)) == call(entry(weight_decay=-1.0)) == call(entry(weight_decay=nan)) == eck.EINVAL
     assert call(entry(m_scale=None), state=1) == call(entry(v_scale=None), state=1) == eck.EINVAL
-    assert call(entry(n=(1 << 40) + 1)) == eck.EUNSUPPORTED
+    assert call(entry(n=(1 << 40) + 1)) == call(entry(n=(1 << 34) + 1)) == eck.EUNSUPPORTED
     assert call(entry(param=FAKE + 2)) == call(entry(grad=FAKE + 2)) == call(entry(grad=FAKE + 1, grad_dtype=1)) == eck.EALIGN
     assert call(entry(m=FAKE + 1)) == call(entry(v=FAKE + 2)) == call(entry(bf16_out=FAKE + 1)) == eck.EALIGN
     assert call(more=C.c_void_p(FAKE + 2)) == call(scale=C.c_void_p(FAKE + 1)) == eck.EALIGN
@@ -54,7 +54,7 @@ def test_gradients_norm_validates_before_launch():
     assert 0 < need <= 8 * 16500
     assert call(norm=None, scale=None) == call(most=0.0) == call(most=-1.0) == call(most=float("nan")) == call(count=0) == eck.EINVAL
     assert call(entry(grad=None)) == call(entry(n=0)) == call(entry(grad_dtype=7)) == eck.EINVAL
-    assert call(entry(n=(1 << 40) + 1)) == eck.EUNSUPPORTED
+    assert call(entry(n=(1 << 40) + 1)) == call(entry(n=(1 << 34) + 1)) == eck.EUNSUPPORTED
     assert call(ws=None) == call(ws_bytes=7) == eck.EWORKSPACE
     assert call(ws=FAKE + 16) == call(norm=FAKE + 2) == call(scale=FAKE + 2) == call(entry(grad=FAKE + 2)) == eck.EALIGN
 
