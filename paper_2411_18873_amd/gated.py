@@ -48,18 +48,22 @@ class GatedModel:
     def _copy(self):
         """bf16 copies of the blocks' weights, which their products are made with"""
         self.bf16 = {k: p.bfloat16() for k, p in self.params.items() if k[0].isdigit() and p.dim() == 2}
-        self._int8 = None
+        self._int8, self._int8_steps = None, None  # (of which step they are)
 
     def _quantised(self):
         """the blocks' weights in 8-bit integers, a row and a scale for each column, laid out when a scoring pass first wants them"""
         if self._int8 is None:
-            self._int8 = {}
-            for k in self.bf16:
-                w = self.params[k]
-                q, scale = eck.int8_rows(w.shape[1], w.shape[0]), torch.empty(w.shape[1], device="cuda")
-                eck.quantise_rows(w, q, scale, order=eck.COLUMNS)
-                self._int8[k] = q, scale
+            self._int8 = {k: (eck.int8_rows(w.shape[1], w.shape[0]), torch.empty(w.shape[1], device="cuda"))
+                          for k, w in self.params.items() if k in self.bf16}
+        if self._int8_steps != self.steps:
+            self._lay_out_int8()
         return self._int8
+
+    def _lay_out_int8(self):
+        """the 8-bit weights of the parameters as they are, where they have lain before: a captured scoring pass reads them there"""
+        for k, (q, scale) in (self._int8 or {}).items():
+            eck.quantise_rows(self.params[k], q, scale, order=eck.COLUMNS)
+        self._int8_steps = self.steps
 
     def _block_int8(self, b, xn, out):
         """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest"""
@@ -167,7 +171,6 @@ class GatedModel:
         params = [self.params[k] for k in names]
         states = list(zip(*(self.moments[k] for k in names)))
         plan = None
-        self._int8 = None  # (of the weights as they were)
         scale = torch.ones(1, device="cuda") if max_norm is not None else None
         for step in range(n_steps):
             first = step % (pairs // n) * n
@@ -185,6 +188,7 @@ class GatedModel:
             if max_norm is not None:
                 eck.gradients_norm(plan, None, scale, self._ws(eck.gradients_norm_workspace_bytes(plan)), max_norm=max_norm)
             eck.adamw_step(plan, lr, self.steps, beta1, beta2, eps, grad_scale=scale, seed=self.seed)
+        self._lay_out_int8()
         return torch.stack(losses)
 
 

@@ -98,6 +98,25 @@ def test_scores_in_8_bit_integers(n, refit):
     assert (got[:n].double() - want).abs().max().item() <= 8 * 0.02
 
 
+def test_a_captured_score_in_8_bit_integers_follows_refits():
+    feat = features(64, 512, 5, torch.float32)
+    model = gated.GatedModel(hidden=96, blocks=2, head=40, seed=3)
+    model.refit(feat, labels(feat), 2, 128)  # (the workspace has its size)
+    got, want = torch.zeros(512, device="cuda"), torch.zeros(512, device="cuda")
+    model.score(feat, 512, got, int8=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.score(feat, 512, got, int8=True)
+    for _ in range(3):
+        model.refit(feat, labels(feat), 4, 128, lr=1e-2)
+        got.zero_()
+        graph.replay()
+        model.score(feat, 512, want, int8=True)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_parents_drawn_from_a_refitted_models_scores():
     """the whole round: refit, lay out, score, draw; and each draw is a launchable candidate among the best"""
     n, k = 30000, 512
