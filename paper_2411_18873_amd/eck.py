@@ -826,6 +826,9 @@ class Parameters:
                 if _here(tensors[i], dtype, field).numel() != n:
                     raise ValueError("%s of tensor %d must have %d elements" % (field, i, n))
                 setattr(entry, field, tensors[i].data_ptr())
+        written = [p for e in self._array if e.n for p in (e.param, e.m, e.v, e.m_scale, e.v_scale, e.bf16_out) if p]
+        if len(set(written)) != len(written):
+            raise ValueError("parameters, states and copies must be tensors of their own")
         self.set_grads(grads)
 
     def set_grads(self, grads):

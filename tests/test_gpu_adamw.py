@@ -359,3 +359,14 @@ def test_a_clipped_step_on_a_stream_and_as_a_graph(eight):
         for a, b in zip(sides[0]["params"], sides[1]["params"]):
             assert (a.t - b.t).abs().max().item() <= 8 * E * (1 + 1e-2)
             b.t.copy_(a.t)
+
+
+def test_a_tensor_in_two_places_is_refused():
+    a = [torch.zeros(8, device="cuda") for _ in range(6)]
+    eck.Parameters(a[:2], a[:2], a[2:4], a[4:6])  # (gradients are only read)
+    for params, m, v in (([a[0], a[0]], a[2:4], a[4:6]), (a[:2], [a[2], a[2]], a[4:6]), (a[:2], a[2:4], [a[4], a[2]])):
+        with pytest.raises(ValueError, match="of their own"):
+            eck.Parameters(a[:2], params, m, v)
+    copy = torch.zeros(8, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="of their own"):
+        eck.Parameters(a[:2], a[:2], a[2:4], a[4:6], copies=[copy, copy])
