@@ -61,9 +61,10 @@ class GatedModel:
 
     def _lay_out_int8(self):
         """the 8-bit weights of the parameters as they are, where they have lain before: a captured scoring pass reads them there"""
-        for k, (q, scale) in (self._int8 or {}).items():
-            eck.quantise_rows(self.params[k], q, scale, order=eck.COLUMNS)
-        self._int8_steps = self.steps
+        if self._int8 is not None:
+            for k, (q, scale) in self._int8.items():
+                eck.quantise_rows(self.params[k], q, scale, order=eck.COLUMNS)
+            self._int8_steps = self.steps
 
     def _block_int8(self, b, xn, out):
         """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest"""

@@ -98,6 +98,22 @@ def test_scores_in_8_bit_integers(n, refit):
     assert (got[:n].double() - want).abs().max().item() <= 8 * 0.02
 
 
+@pytest.mark.parametrize("before", [False, True])
+def test_8_bit_weights_are_those_of_the_parameters(before):
+    """whether a scoring pass has laid them out before the refit or not"""
+    feat, got = features(64, 512, 5, torch.float32), torch.empty(512, device="cuda")
+    model = gated.GatedModel(hidden=96, blocks=2, head=40, seed=3)
+    for _ in range(2):
+        if before:
+            model.score(feat, 512, got, int8=True)
+        model.refit(feat, labels(feat), 2, 128, lr=1e-2)
+        model.score(feat, 512, got, int8=True)
+        for k, (q, scale) in model._int8.items():
+            w = model.params[k].t()
+            most = w.abs().amax(1)
+            assert torch.equal(scale, most / 127) and torch.equal(q.float(), torch.round(w * (127 / most)[:, None])), k
+
+
 def test_a_captured_score_in_8_bit_integers_follows_refits():
     feat = features(64, 512, 5, torch.float32)
     model = gated.GatedModel(hidden=96, blocks=2, head=40, seed=3)
