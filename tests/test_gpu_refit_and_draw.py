@@ -111,7 +111,8 @@ def test_8_bit_weights_are_those_of_the_parameters(before):
         for k, (q, scale) in model._int8.items():
             w = model.params[k].t()
             most = w.abs().amax(1)
-            assert torch.equal(scale, most / 127) and torch.equal(q.float(), torch.round(w * (127 / most)[:, None])), k
+            all127 = torch.full_like(most, 127.0)  # (quotients by a number are products with its reciprocal in torch)
+            assert torch.equal(scale, most / all127) and torch.equal(q.float(), torch.round(w * (all127 / most)[:, None])), k
 
 
 def test_a_captured_score_in_8_bit_integers_follows_refits():
