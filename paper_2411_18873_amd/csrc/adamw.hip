@@ -3,7 +3,9 @@
 //   g = s grad,  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g g,
 //   w <- w (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Everything is read and written once, so memory bounds it.  The tensors' addresses travel as kernel arguments, so that a step needs no
+// Everything is read and written once, so memory bounds it: 100.7 million parameters with bf16 gradients and copies, 2.82 GB, take 533 us
+// (5.3 TB/s; a copy of 1 GiB 5.1), 96 million with 8-bit states, 1.54 GB, 312 (4.9 TB/s; the states' arithmetic takes nearly as long as their
+// way).  The tensors' addresses travel as kernel arguments, so that a step needs no
 // table on the device and a captured one holds its own; a kilobyte of them takes about a microsecond (a launch of 72 bytes 3.3 us, of 4 KB 6.9,
 // of 14 KB 16), so a launch has room for 12, 48 or 200 tensors, whichever does.  Blocks of threads take stretches of a tensor.
 //
@@ -300,6 +302,8 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Tensors<EIGHT, ROO
 
 // ------------------------------------------------------------------------------------------------ norm
 
+// Sums of squares of stretches of tensors, a block of threads each, then one block adds them up in a fixed order.  Memory bounds the first
+// (37.3 million bf16 gradients in 194 tensors: 16 us for 74.6 MB), the launches themselves small lists (18 us for these, 9 for 99 thousand in ten)
 template <int ROOM>
 struct GradientList {
     double *sums;
