@@ -307,6 +307,14 @@ def test_norm(sizes, kind, offset):
     assert all_untouched(t)
 
 
+@pytest.mark.parametrize("kind,offset", [("both", 0), ("f32", 1), ("bf16", 3)])
+@pytest.mark.parametrize("sizes", [[2048], [2047, 2049, 1], [0, 4096, 0, 5, 2048 * 17 + 3], [131072], [131073], [100] * 16, [100] * 17, [1] * 64,
+                                   [1] * 65, [0] * 30 + [777] * 64 + [0] * 9, [262144], [262145], [5000] * 40])
+def test_norm_of_short_lists(sizes, kind, offset):
+    """lists of a few blocks of threads, of as many tensors as a launch takes and one more, and of empty ones between"""
+    test_norm(sizes, kind, offset)
+
+
 def test_norm_of_the_largest_the_smallest_and_none():
     norm, scale = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
     ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
