@@ -12,8 +12,8 @@
 //
 // Segments of up to 16 384 candidates: a block each, keys in registers, one launch.  Longer ones: blocks by the piece, a launch for each
 // time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws; where few are kept,
-// range, histogram, list, draws).  Short ones are bound by a block's chain of phases between barriers (6400 candidates, all three limits:
-// 18 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 84 us in four launches, one
+// range, histogram, list, draws).  Short ones are bound by a block's chain of phases between barriers (6400 candidates, k = 64, all
+// limits: 9.8 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 84 us in four launches, one
 // reading of the 84 MB is 16.5; 16 of 2^20 by share alone: 180 us in nine).
 #include "activations.h"
 #include "lanes.h"
@@ -434,7 +434,121 @@ struct Short {
     uint32_t least[THREADS / 64], most[THREADS / 64], number[THREADS / 64];
 };
 
-template <int THREADS, int EACH>
+// The least of a short segment, where so few are kept that a list takes all up to the end's bin: put in order once, after which one wavefront
+// has all ends and sums without a barrier.  False (and nothing written) where the bin holds too many for that.  6400 candidates, k = 64, all
+// limits: 9.8 us by this, 18.3 by the ends one after the other.
+template <int THREADS, int EACH, class S, class W>
+__device__ __forceinline__ bool draw_from_few(const Draws &a, S &s, Histogram &bins, const uint32_t (&key)[EACH], uint32_t least, uint32_t most,
+                                              uint32_t number, W &&weight)
+{
+    constexpr int OF_LANE = S::LIST / 64;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t segment = blockIdx.x;
+    const Linear linear(least, most);
+    clear_bins<THREADS>(bins, false);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (key[i] != NO_KEY) atomicAdd(&bins.count[linear.bin(energy_of(key[i]))], 1u);
+    if (threadIdx.x == 0) s.listed = 0;
+    __syncthreads();
+    const Range end = narrow<THREADS>(s, bins, {0, BINS - 1, number, 0, {0, 0}}, {false, a.k, {0.0, 0.0}}, false); // (one bin)
+    const uint32_t listed = end.before + end.number;
+    if (listed > (uint32_t)S::LIST) return false;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (key[i] != NO_KEY && linear.bin(energy_of(key[i])) <= end.lo) s.list[atomicAdd(&s.listed, 1u)] = (u64)key[i] << 32 | (threadIdx.x * EACH + i);
+    sort_list<THREADS>(s, listed);
+
+    u64 *const w_of = bins.high, *const sum_to = bins.low; // (by index; bits of fp64)
+    if (threadIdx.x < 64) {
+        const auto meet = [] { // what the wavefront has written is there for all its lanes
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        u64 one[OF_LANE];
+        double w[OF_LANE];
+        uint32_t kept = a.k;
+#pragma unroll
+        for (int i = 0; i < OF_LANE; ++i) {
+            const uint32_t e = lane * OF_LANE + i;
+            one[i] = e < kept ? s.sorted[e] : 0;
+            w[i] = e < kept ? weight((uint32_t)(one[i] >> 32)) : 0.0;
+        }
+        if (a.top_p < 1.0) {
+            Mass sum = {0, 0};
+#pragma unroll
+            for (int i = 0; i < OF_LANE; ++i) sum = sum + mass_of(w[i]);
+            Mass to = {wave_sums((u64)sum.high), wave_sums((u64)sum.low)};
+            const double target = a.top_p * Mass{of_lane((u64)to.high, 63), of_lane((u64)to.low, 63)}.value();
+            to = {to.high - sum.high, to.low - sum.low};
+            uint32_t before = 0; // how many leave the sum below the target
+#pragma unroll
+            for (int i = 0; i < OF_LANE; ++i) {
+                to = to + mass_of(w[i]);
+                before += lane * OF_LANE + i < kept && to.value() < target;
+            }
+            kept = min(kept, of_lane(wave_sums(before), 63) + 1);
+        }
+        uint32_t mine[OF_LANE], rank[OF_LANE];
+#pragma unroll
+        for (int i = 0; i < OF_LANE; ++i) {
+            const bool stays = lane * OF_LANE + i < kept && w[i] >= a.min_p;
+            mine[i] = stays ? (uint32_t)one[i] : NOBODY;
+            rank[i] = 0;
+            s.list[lane * OF_LANE + i] = mine[i];
+        }
+        meet();
+#pragma unroll 4
+        for (uint32_t j = 0; j < kept; ++j) {
+            const uint32_t other = (uint32_t)s.list[j];
+#pragma unroll
+            for (int i = 0; i < OF_LANE; ++i) rank[i] += other < mine[i];
+        }
+        uint32_t number_kept = 0;
+#pragma unroll
+        for (int i = 0; i < OF_LANE; ++i) {
+            number_kept += __builtin_popcountll(__ballot(mine[i] != NOBODY));
+            if (mine[i] == NOBODY) continue;
+            s.sorted[rank[i]] = mine[i];
+            w_of[rank[i]] = __builtin_bit_cast(u64, w[i]);
+        }
+        meet();
+        double up_to[OF_LANE], sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < OF_LANE; ++i) {
+            sum += lane * OF_LANE + i < number_kept ? __builtin_bit_cast(double, w_of[lane * OF_LANE + i]) : 0.0;
+            up_to[i] = sum;
+        }
+        const double before = wave_sums(sum) - sum;
+#pragma unroll
+        for (int i = 0; i < OF_LANE; ++i) sum_to[lane * OF_LANE + i] = __builtin_bit_cast(u64, before + up_to[i]);
+        if (lane == 0) {
+            s.listed = number_kept;
+            if (a.count) a.count[segment] = number_kept;
+        }
+    }
+    __syncthreads();
+    const uint32_t kept = s.listed;
+    const auto sum_of = [&](uint32_t i) { return __builtin_bit_cast(double, sum_to[i]); };
+    const auto weight_at = [&](uint32_t i) { return __builtin_bit_cast(double, w_of[i]); };
+    const double all = sum_of(kept - 1);
+    for (uint32_t d = threadIdx.x; d < a.draws; d += THREADS) {
+        const double target = fmax((double)a.uniform[segment * a.draws + d] * all, 0.0);
+        uint32_t lo = 0, hi = kept - 1;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (sum_of(mid) > target) hi = mid;
+            else lo = mid + 1;
+        }
+        while (!(weight_at(lo) > 0.0) && lo + 1 < kept && all > target) ++lo;
+        while (!(weight_at(lo) > 0.0) && lo > 0) --lo;
+        a.idx[segment * a.draws + d] = (uint32_t)s.sorted[lo];
+        if (a.logprob) a.logprob[segment * a.draws + d] = (float)log(weight_at(lo) / all);
+    }
+    return true;
+}
+
+template <int THREADS, int EACH, bool FEWEST>
 __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -482,6 +596,12 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
     const double best = (double)energy_of(least);
     const auto weight = [&](uint32_t k) { return weight_of(k, best, a.per_temperature); };
 
+    if constexpr (FEWEST) {
+        if (a.k < number) {
+            if (draw_from_few<THREADS, EACH>(a, s.ends.s, s.ends.bins[0], key, least, most, number, weight)) return;
+            __syncthreads();
+        }
+    }
     Cut cut = {most, n};
     {
         typename Lds::S &sc = s.ends.s;
@@ -1697,15 +1817,28 @@ uint64_t lay_out_few(Few &p, void *ws)
     return (uint64_t)(at - (char *)ws);
 }
 
+// Whether the least of a segment are put in order first: not so many that a list would seldom take the end's bin too, and, where nothing but k
+// limits them, few of many (k = 64 of 16 384 in 512 segments 59 us by this, 66 otherwise, of 4096 in 2000 45 and 49, of 1000 in 4096 51 and 40; k
+// = 192 63 and 45; with a share of their weight k = 192 of 16 384 67 and 104, of 1000 65 and 84).  A kernel of its own: both in one take more
+// registers than there are (16 384 by share alone 43 us, 84); so does this one where it has to go the other way, for bins of many equal ones.
+bool is_fewest(const Draws &a) { return a.k > 1 && a.n > 256 && (a.top_p < 1.0 ? a.k <= 192 : a.k <= 64 && a.n > 1024); }
+
+template <int THREADS, int EACH, bool FEWEST>
+int32_t launch_short_of(const Draws &a, uint32_t segments, hipStream_t st)
+{
+    constexpr int bytes = sizeof(Short<THREADS, EACH>);
+    const auto kernel = short_kernel<THREADS, EACH, FEWEST>;
+    if (bytes > 65536) ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    hipLaunchKernelGGL(kernel, dim3(segments), dim3(THREADS), bytes, st, a);
+    ECK_HIP_TRY(hipGetLastError());
+    return ECK_OK;
+}
 template <int THREADS, int EACH>
 int32_t launch_short(const Draws &a, uint32_t segments, hipStream_t st)
 {
-    constexpr int bytes = sizeof(Short<THREADS, EACH>);
-    if (bytes > 65536)
-        ECK_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(short_kernel<THREADS, EACH>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    hipLaunchKernelGGL((short_kernel<THREADS, EACH>), dim3(segments), dim3(THREADS), bytes, st, a);
-    ECK_HIP_TRY(hipGetLastError());
-    return ECK_OK;
+    if constexpr (Short<THREADS, EACH>::BINNED)
+        if (is_fewest(a)) return launch_short_of<THREADS, EACH, true>(a, segments, st);
+    return launch_short_of<THREADS, EACH, false>(a, segments, st);
 }
 
 int32_t launch_few(const Draws &a, uint32_t segments, void *ws, hipStream_t st)

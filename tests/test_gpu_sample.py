@@ -112,6 +112,15 @@ def test_equal_energies(seg, n, steps, how):
     check(*inputs(seg, n, 40, steps + n, steps=steps), temperature=0.07, **how)
 
 
+@pytest.mark.parametrize("n", [257, 1024, 1025, 6400, 12001, 16384])
+@pytest.mark.parametrize("k", [2, 63, 64, 65, 191, 192, 193, 256])
+@pytest.mark.parametrize("how", [dict(), dict(top_p=0.6), dict(min_p=0.3), dict(top_p=0.9, min_p=0.02)], ids=str)
+@pytest.mark.parametrize("steps", [0, 48])
+def test_few_of_short_segments(n, k, how, steps):
+    """lists that take all up to the end's bin, and bins of so many equal ones that none does"""
+    check(*inputs(3, n, 70, n + k, steps=steps), temperature=0.3, k=k, **how)
+
+
 @pytest.mark.parametrize("n", [9, 5000, 20000, 500000])
 def test_all_energies_equal(n):
     """weights of one: every border is a whole number, and sums are exact"""
