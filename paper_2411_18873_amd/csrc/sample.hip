@@ -1821,10 +1821,10 @@ uint64_t lay_out_few(Few &p, void *ws)
 }
 
 // Whether the least of a segment are put in order first: not so many that a list would seldom take the end's bin too, and, where nothing but k
-// limits them, few of many (k = 64 of 16 384 in 512 segments 59 us by this, 66 otherwise, of 4096 in 2000 45 and 49, of 1000 in 4096 51 and 40; k
-// = 192 63 and 45; with a share of their weight k = 192 of 16 384 67 and 104, of 1000 65 and 84).  A kernel of its own: both in one take more
-// registers than there are (16 384 by share alone 43 us, 84); so does this one where it has to go the other way, for bins of many equal ones.
-bool is_fewest(const Draws &a) { return a.k > 1 && a.n > 256 && (a.top_p < 1.0 ? a.k <= 192 : a.k <= 64 && a.n > 1024); }
+// limits them, few of not too many (1024 segments of 6400: k = 16 32 us by this, 39 otherwise, k = 64 41 and 39; 512 of 16 384, k = 64, 59 and 42;
+// 4096 of 1000 51 and 40; with a share of their weight, k = 192, 56 and 76, 67 and 74, 65 and 80).  A kernel of its own: both in one take more
+// registers than there are (16 384 by share alone 43 us, 84).
+bool is_fewest(const Draws &a) { return a.k > 1 && a.n > 256 && (a.top_p < 1.0 ? a.k <= 192 : a.k <= 48 && a.n > 1024 && a.n <= 8192); }
 
 template <int THREADS, int EACH, bool FEWEST>
 int32_t launch_short_of(const Draws &a, uint32_t segments, hipStream_t st)

@@ -112,8 +112,8 @@ def test_equal_energies(seg, n, steps, how):
     check(*inputs(seg, n, 40, steps + n, steps=steps), temperature=0.07, **how)
 
 
-@pytest.mark.parametrize("n", [257, 1024, 1025, 6400, 12001, 16384])
-@pytest.mark.parametrize("k", [2, 63, 64, 65, 191, 192, 193, 256])
+@pytest.mark.parametrize("n", [257, 1024, 1025, 6400, 8192, 8193, 16384])
+@pytest.mark.parametrize("k", [2, 47, 48, 49, 64, 65, 191, 192, 193, 256])
 @pytest.mark.parametrize("how", [dict(), dict(top_p=0.6), dict(min_p=0.3), dict(top_p=0.9, min_p=0.02)], ids=str)
 @pytest.mark.parametrize("steps", [0, 48])
 def test_few_of_short_segments(n, k, how, steps):
