@@ -13,7 +13,7 @@
 // Segments of up to 16 384 candidates: a block each, keys in registers, one launch.  Longer ones: blocks by the piece, a launch for each
 // time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws; where few are kept,
 // range, histogram, list, draws).  Short ones are bound by a block's chain of phases between barriers (6400 candidates, k = 64, all
-// limits: 9.8 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 84 us in four launches, one
+// limits: 9.8 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 83 us in four launches, one
 // reading of the 84 MB is 16.5; 16 of 2^20 by share alone: 180 us in nine).
 #include "activations.h"
 #include "lanes.h"
@@ -148,11 +148,23 @@ struct Scratch { // of a block that looks for ends
     uint32_t listed;
 };
 
+// of all threads
+template <int THREADS, class S>
+__device__ __forceinline__ Mass block_total(S &s, const Mass &mine)
+{
+    const u64 high = block_prefix<THREADS>((u64)mine.high, s.wide[0]), low = block_prefix<THREADS>((u64)mine.low, s.wide[1]);
+    __syncthreads();
+    if (threadIdx.x == THREADS - 1) s.total = {high, low};
+    __syncthreads();
+    return s.total;
+}
+
 // which prefix: the `need` least candidates, or the fewest of a weight of `target` (from and up to, while that is not known)
 struct Goal {
     bool by_weight;
     uint32_t need;
     double target[2];
+    double share = 0.0; // above 0: the targets are this share of all weight, which find_cut_of takes from its first histogram
     __device__ __forceinline__ bool reached(int which, uint32_t count, const Mass &mass) const
     {
         return by_weight ? mass.value() >= target[which] : count >= need;
@@ -352,14 +364,20 @@ __device__ void find_cut(S &s, Histogram &bins, Range at, const Goal &goal, bool
 // The same over all keys from..to of the source, `number` candidates, most of them far from each other: a first histogram linear in energy has
 // few of them in a bin, and none that all threads add to at once
 template <int THREADS, class S, class Source, class W>
-__device__ void find_cut_of(S &s, Histogram &bins, uint32_t from, uint32_t to, uint32_t number, const Goal &goal, bool weights, const Source &source,
-                            W &&weight)
+__device__ void find_cut_of(S &s, Histogram &bins, uint32_t from, uint32_t to, uint32_t number, Goal goal, bool weights, const Source &source, W &&weight)
 {
     if (!Source::FITS && number > (uint32_t)S::LIST) {
         const Linear linear(from, to);
         clear_bins<THREADS>(bins, weights);
         source.each([&](uint32_t key, uint32_t) { add_to_bins(bins, linear.bin(energy_of(key)), weights, weights ? weight(key) : 0.0); });
         __syncthreads();
+        if (goal.share > 0.0) {
+            constexpr uint32_t EACH = BINS / THREADS;
+            Mass sum = {0, 0};
+#pragma unroll
+            for (uint32_t i = 0; i < EACH; ++i) sum = sum + Mass{bins.high[threadIdx.x * EACH + i], bins.low[threadIdx.x * EACH + i]};
+            goal.target[0] = goal.target[1] = goal.share * block_total<THREADS>(s, sum).value();
+        }
         const Range bin = narrow<THREADS>(s, bins, {0, BINS - 1, number, 0, {0, 0}}, goal, weights);
         if (bin.number <= (uint32_t)S::LIST && bin.lo == bin.hi) {
             if (threadIdx.x == 0) s.listed = 0;
@@ -429,7 +447,7 @@ struct Short {
     union {
         Ends ends;
         // sums of weights up to and including each candidate; a place between threads' keeps their lanes off each other's banks (16 384 by a least
-        // weight alone: 25 us without it)
+        // weight alone: 14 us, 25 without it)
         double to[THREADS * (EACH + 1)];
     };
     static __device__ __forceinline__ uint32_t place(uint32_t i) { return i + i / EACH; }
@@ -624,19 +642,13 @@ __global__ __launch_bounds__(THREADS) void short_kernel(const Draws a)
             kept = a.k;
         }
         if (a.top_p < 1.0 && kept > 1) {
-            u64 high = 0, low = 0;
-            held.each([&](uint32_t k, uint32_t) {
-                const Mass m = mass_of(weight(k));
-                high += m.high;
-                low += m.low;
-            });
-            high = block_prefix<THREADS>(high, sc.wide[0]);
-            low = block_prefix<THREADS>(low, sc.wide[1]);
-            __syncthreads();
-            if (threadIdx.x == THREADS - 1) sc.total = {high, low};
-            __syncthreads();
-            const double target = a.top_p * sc.total.value();
-            find_cut_of<THREADS>(sc, bins, least, cut.key, kept, {true, 0, {target, target}}, true, held, weight);
+            Goal goal = {true, 0, {0.0, 0.0}, a.top_p};
+            if (decltype(held)::FITS || kept <= (uint32_t)Lds::S::LIST) { // (no histogram will be made)
+                Mass mine = {0, 0};
+                held.each([&](uint32_t k, uint32_t) { mine = mine + mass_of(weight(k)); });
+                goal.target[0] = goal.target[1] = a.top_p * block_total<THREADS>(sc, mine).value();
+            }
+            find_cut_of<THREADS>(sc, bins, least, cut.key, kept, goal, true, held, weight);
             cut = sc.cut;
         }
     }
@@ -1634,15 +1646,14 @@ __global__ __launch_bounds__(LONG_THREADS) void few_draws_kernel(const Few p)
 
     // a share of their weight
     if (a.top_p < 1.0 && entries > 1) {
-        Mass mine = {0, 0};
-        for (uint32_t i = threadIdx.x; i < entries; i += LONG_THREADS) mine = mine + mass_of(weight((uint32_t)(l.kept[i] >> 32)));
-        const u64 high = block_prefix<LONG_THREADS>((u64)mine.high, s.wide[0]), low = block_prefix<LONG_THREADS>((u64)mine.low, s.wide[1]);
-        __syncthreads();
-        if (threadIdx.x == LONG_THREADS - 1) s.total = {high, low};
-        __syncthreads();
-        const double target = a.top_p * s.total.value();
+        Goal goal = {true, 0, {0.0, 0.0}, a.top_p};
+        if (entries <= (uint32_t)LongScratch::LIST) { // (no histogram will be made)
+            Mass mine = {0, 0};
+            for (uint32_t i = threadIdx.x; i < entries; i += LONG_THREADS) mine = mine + mass_of(weight((uint32_t)(l.kept[i] >> 32)));
+            goal.target[0] = goal.target[1] = a.top_p * block_total<LONG_THREADS>(s, mine).value();
+        }
         const Listed listed = {l.kept, entries, s.listed};
-        find_cut_of<LONG_THREADS>(s, l.bins, of.least, cut.key, entries, {true, 0, {target, target}}, true, listed, weight);
+        find_cut_of<LONG_THREADS>(s, l.bins, of.least, cut.key, entries, goal, true, listed, weight);
         cut = s.cut;
         __syncthreads();
     }
@@ -1820,11 +1831,16 @@ uint64_t lay_out_few(Few &p, void *ws)
     return (uint64_t)(at - (char *)ws);
 }
 
-// Whether the least of a segment are put in order first: not so many that a list would seldom take the end's bin too, and, where nothing but k
-// limits them, few of not too many (1024 segments of 6400: k = 16 32 us by this, 39 otherwise, k = 64 41 and 39; 512 of 16 384, k = 64, 59 and 42;
-// 4096 of 1000 51 and 40; with a share of their weight, k = 192, 56 and 76, 67 and 74, 65 and 80).  A kernel of its own: both in one take more
-// registers than there are (16 384 by share alone 43 us, 84).
-bool is_fewest(const Draws &a) { return a.k > 1 && a.n > 256 && (a.top_p < 1.0 ? a.k <= 192 : a.k <= 48 && a.n > 1024 && a.n <= 8192); }
+// Whether the least of a segment are put in order first: not so many that a list would seldom take the end's bin too, and few where the other way
+// is short, for k alone (1024 segments of 6400: k = 16 32 us by this, 36 otherwise, k = 64 41 and 36; 512 of 16 384, k = 64, 59 and 39; 4096 of
+// 1000 51 and 40) and long segments (with a share 512 of 16 384, k = 64, 59 us by this, k = 192 67; k = 300, the other way, 64).  Of others with a
+// share k = 192 takes 56 (1024 of 6400) and 65 (4096 of 1000), k = 300 the other way 75 and 86.  A kernel of its own: both in one take more
+// registers than there are (16 384 by share alone twice the time).
+bool is_fewest(const Draws &a)
+{
+    const uint32_t most = a.top_p < 1.0 ? (a.n <= 8192 ? 192 : 64) : a.n > 1024 && a.n <= 8192 ? 48 : 0;
+    return a.n > 256 && a.k > 1 && a.k <= most;
+}
 
 template <int THREADS, int EACH, bool FEWEST>
 int32_t launch_short_of(const Draws &a, uint32_t segments, hipStream_t st)
