@@ -249,3 +249,21 @@ def test_candidates_past_2e29_columns():
     assert torch.equal(q[some, 0].float(), 127 * values.sign()) and torch.allclose(scale[some], values.abs() / 127, rtol=2.0 ** -23, atol=0)
     assert (q[some, 1:] == 0).all()
     assert torch.count_nonzero(scale) == some.numel() and torch.count_nonzero(q[:, 0]) == some.numel()
+
+
+@pytest.mark.parametrize("n,n_in,n_out", [(1, 15, 40), (20, 100, 40), (300, 33, 70), (300, 100, 64), (300, 300, 70), (40, 4099, 33), (1, 4099, 9000)])
+@pytest.mark.parametrize("act", [eck.ACT_NONE, eck.ACT_SILU])
+def test_what_lies_behind_the_width_counts_nothing_where_one_side_is_zero(n, n_in, n_out, act):
+    g = torch.Generator(device="cuda").manual_seed(n + n_in)
+    rows, whole, got = n_out * (1 if act == eck.ACT_NONE else 2), -(-n_in // 16) * 16, []
+    full = [torch.randint(-128, 128, (count, whole), generator=g, device="cuda").to(torch.int8) for count in (n, rows)]
+    scales = [torch.rand(count, generator=g, device="cuda") for count in (n, rows)]
+    ws = torch.empty(max(1, eck.product_int8_workspace_bytes(n, n_in, n_out, act)), dtype=torch.uint8, device="cuda")
+    for zeros in ((True, True), (True, False), (False, True)):
+        x, w = [m.clone() for m in full]
+        for m, zero in zip((x, w), zeros):
+            if zero:
+                m[:, n_in:] = 0
+        got.append(torch.empty(n, n_out, device="cuda"))
+        eck.product_int8(x[:, :n_in], scales[0], w[:, :n_in], scales[1], got[-1], ws, act=act)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
