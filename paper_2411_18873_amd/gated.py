@@ -66,10 +66,9 @@ class GatedModel:
                 eck.quantise_rows(self.params[k], q, scale, order=eck.COLUMNS)
             self._int8_steps = self.steps
 
-    def _block_int8(self, b, xn, out):
+    def _block_int8(self, b, xn, out, ws):
         """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest"""
         n, f, h, w = xn.shape[0], self.n_feat, self.hidden, self._quantised()
-        ws = self._ws(max(eck.product_int8_workspace_bytes(n, f, h, eck.ACT_SILU), eck.product_int8_workspace_bytes(n, h, f), 1))
         q, scale, hidden = eck.int8_rows(n, f), torch.empty(n, device="cuda"), torch.empty(n, h, dtype=torch.bfloat16, device="cuda")
         eck.quantise_rows(xn, q, scale)
         eck.product_int8(q, scale, *w["%d.gate_up" % b], hidden, ws, act=eck.ACT_SILU)
@@ -78,7 +77,10 @@ class GatedModel:
         eck.product_int8(q, scale, *w["%d.down" % b], out, ws)
 
     def _ws(self, need):
-        """one workspace for all calls: they follow each other on one stream"""
+        """one workspace for all calls, which follow each other on one stream; for one that is captured its own, out of the graph's memory: the
+        shared one goes back to the allocator when a later call wants a larger one, and replays would still write there"""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device="cuda")
         if self._work.get("ws") is None or self._work["ws"].numel() < need:
             self._work["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda")
         return self._work["ws"]
@@ -95,14 +97,16 @@ class GatedModel:
         if train:
             kept["in"] = s
         x = x.bfloat16()
-        ws = self._ws(max(eck.gatedffn_forward_workspace_bytes(n, f, self.hidden, f, eck.BF16),
-                          eck.gatedffn_forward_workspace_bytes(n, f, self.head, 1, eck.F32)))
+        need = max(eck.gatedffn_forward_workspace_bytes(n, f, self.hidden, f, eck.BF16), eck.gatedffn_forward_workspace_bytes(n, f, self.head, 1, eck.F32))
+        if int8:
+            need = max(need, eck.product_int8_workspace_bytes(n, f, self.hidden, eck.ACT_SILU), eck.product_int8_workspace_bytes(n, self.hidden, f))
+        ws = self._ws(need)
         for b in range(self.blocks):
             xn, out, s = rows(), rows(), stats()
             pre = rows(2 * self.hidden, torch.float32) if train else None
             eck.layernorm_forward(x, p["%d.gamma" % b], p["%d.beta" % b], xn, *s, eps=EPS)
             if int8:
-                self._block_int8(b, xn, out)
+                self._block_int8(b, xn, out, ws)
             else:
                 eck.gatedffn_forward(xn, self.bf16["%d.gate_up" % b], self.bf16["%d.down" % b], out, ws, pre_out=pre)
             if train:
@@ -112,7 +116,6 @@ class GatedModel:
             x = nxt
         x, xn, s = x.float(), rows(dtype=torch.float32), stats()
         pre = rows(2 * self.head, torch.float32) if train else None
-        ws = self._ws(0)  # (a block in 8-bit integers may have made it larger)
         score = rows(1, torch.float32)
         eck.layernorm_forward(x, p["head.gamma"], p["head.beta"], xn, *s, eps=EPS)
         eck.gatedffn_forward(xn, p["head.gate_up"], p["head.down"], score, ws, pre_out=pre)

@@ -162,3 +162,29 @@ def test_a_search_that_draws_its_parents(temperature):
     for a, b in zip(*runs):
         assert a["parents"].size == 16 and (a["parents"] < 4096).all() and np.array_equal(a["parents"], b["parents"]) and a["best"] == b["best"]
         assert len(np.unique(a["parents"])) == 1 if temperature == 0 else len(np.unique(a["parents"])) > 1
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_captured_score_outlives_calls_that_want_more_memory(int8):
+    """captured after a small pass; then a refit and a score whose workspace is larger, memory that they gave up handed out again, and replays
+    that neither write there nor read it"""
+    small, feat = features(64, 512, 5, torch.float32), features(64, 70000, 6, torch.float32)
+    model = gated.GatedModel(hidden=96, blocks=2, head=40, seed=3)
+    got, want, many = torch.zeros(512, device="cuda"), torch.zeros(512, device="cuda"), torch.zeros(70000, device="cuda")
+    model.score(small, 512, got, int8=int8)
+    before = model._work["ws"].numel()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.score(small, 512, got, int8=int8)
+    for step in range(3):
+        model.refit(small, labels(small), 4, 256, lr=1e-2)
+        model.score(feat, 70000, many, int8=int8)
+        assert model._work["ws"].numel() > before
+        others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for size in (before, before // 2, 2 * before) for _ in range(20)]
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(bool((t == 0x5A).all()) for t in others)
+        model.score(small, 512, want, int8=int8)
+        assert torch.equal(got, want)

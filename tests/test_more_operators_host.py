@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
-from paper_2411_18873_amd import eck
+from paper_2411_18873_amd import eck, gated
 
 FAKE = 0x1000   # never dereferenced: every call below must fail validation first
 
@@ -149,3 +149,21 @@ def test_the_binding_refuses_what_it_cannot_pass_on():
                  lambda: eck.sample_select(f.view(-1), None, 1, torch.zeros(1, 2), None, None, None, None)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_captured_pass_of_a_gated_model_has_a_workspace_of_its_own(monkeypatch):
+    """what a graph writes to is neither lent to other calls nor given up when one of them wants more"""
+    empty, capturing = torch.empty, [False]
+    monkeypatch.setattr(torch, "empty", lambda *size, device=None, **kw: empty(*size, **kw))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    model = object.__new__(gated.GatedModel)
+    model._work = {}
+    first = model._ws(100)
+    assert model._ws(60) is first
+    capturing[0] = True
+    captured = [model._ws(100), model._ws(100), model._ws(500)]
+    capturing[0] = False
+    assert captured[2].numel() == 500 and model._ws(70) is first
+    larger = model._ws(1000)
+    assert larger.numel() == 1000 and model._ws(1) is larger
+    assert len({t.data_ptr() for t in captured + [first, larger]}) == 5
