@@ -51,7 +51,10 @@ class GatedModel:
         self._int8, self._int8_steps = None, None  # (of which step they are)
 
     def _quantised(self):
-        """the blocks' weights in 8-bit integers, a row and a scale for each column, laid out when a scoring pass first wants them"""
+        """the blocks' weights in 8-bit integers, a row and a scale for each column, laid out when a scoring pass first wants them.  Not by one that
+        is captured, which would only record it: other passes would take what has not been written yet for the weights"""
+        if (self._int8 is None or self._int8_steps != self.steps) and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the weights in 8-bit integers have to be laid out before a pass is captured: score(int8=True) once")
         if self._int8 is None:
             self._int8 = {k: (eck.int8_rows(w.shape[1], w.shape[0]), torch.empty(w.shape[1], device="cuda"))
                           for k, w in self.params.items() if k in self.bf16}
@@ -66,9 +69,9 @@ class GatedModel:
                 eck.quantise_rows(self.params[k], q, scale, order=eck.COLUMNS)
             self._int8_steps = self.steps
 
-    def _block_int8(self, b, xn, out, ws):
-        """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest"""
-        n, f, h, w = xn.shape[0], self.n_feat, self.hidden, self._quantised()
+    def _block_int8(self, b, w, xn, out, ws):
+        """out = feedforward(xn) of block b in 8-bit integers: rows of xn and of h by their largest; w: _quantised()"""
+        n, f, h = xn.shape[0], self.n_feat, self.hidden
         q, scale, hidden = eck.int8_rows(n, f), torch.empty(n, device="cuda"), torch.empty(n, h, dtype=torch.bfloat16, device="cuda")
         eck.quantise_rows(xn, q, scale)
         eck.product_int8(q, scale, *w["%d.gate_up" % b], hidden, ws, act=eck.ACT_SILU)
@@ -89,6 +92,7 @@ class GatedModel:
         """scores float [n]; train: with dropout, and what the backward pass needs of every layer, of which a scoring pass keeps none;
         int8: the blocks' products in 8-bit integers (scoring alone)"""
         f, p = self.n_feat, self.params
+        w = self._quantised() if int8 else None
         kept = {} if train else None
         rows = lambda width=f, dtype=torch.bfloat16: torch.empty(n, width, dtype=dtype, device="cuda")  # noqa: E731
         stats = lambda: [torch.empty(n, device="cuda") for _ in range(2)] if train else [None, None]  # noqa: E731
@@ -106,7 +110,7 @@ class GatedModel:
             pre = rows(2 * self.hidden, torch.float32) if train else None
             eck.layernorm_forward(x, p["%d.gamma" % b], p["%d.beta" % b], xn, *s, eps=EPS)
             if int8:
-                self._block_int8(b, xn, out, ws)
+                self._block_int8(b, w, xn, out, ws)
             else:
                 eck.gatedffn_forward(xn, self.bf16["%d.gate_up" % b], self.bf16["%d.down" % b], out, ws, pre_out=pre)
             if train:
@@ -125,7 +129,7 @@ class GatedModel:
 
     def score(self, feat, n, score_out, int8=False):
         """predicted scores of candidates 0 .. n - 1 of a feature matrix [n_feat][ld], as costmodel_score writes them; int8: the blocks'
-        products in 8-bit integers"""
+        products in 8-bit integers (which has to have been called once before it is captured)"""
         score_out[:n].copy_(self._forward(feat, n, False, int8)[0])
 
     def _backward(self, feat, n, kept, d_score):

@@ -188,3 +188,28 @@ def test_a_captured_score_outlives_calls_that_want_more_memory(int8):
         assert all(bool((t == 0x5A).all()) for t in others)
         model.score(small, 512, want, int8=int8)
         assert torch.equal(got, want)
+
+
+def test_a_first_score_in_8_bit_integers_is_not_captured():
+    feat = features(64, 512, 5, torch.float32)
+    model, other = [gated.GatedModel(hidden=96, blocks=2, head=40, seed=3) for _ in range(2)]
+    got, want = torch.zeros(512, device="cuda"), torch.zeros(512, device="cuda")
+    other.score(feat, 512, want, int8=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="laid out"):
+        with torch.cuda.graph(graph):
+            got.add_(1.0)
+            model.score(feat, 512, got, int8=True)
+    for _ in range(2):  # eager ones, before any replay
+        model.score(feat, 512, got.zero_(), int8=True)
+        assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.score(feat, 512, got, int8=True)
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        other.score(feat, 512, want, int8=True)

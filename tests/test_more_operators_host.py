@@ -167,3 +167,21 @@ def test_a_captured_pass_of_a_gated_model_has_a_workspace_of_its_own(monkeypatch
     larger = model._ws(1000)
     assert larger.numel() == 1000 and model._ws(1) is larger
     assert len({t.data_ptr() for t in captured + [first, larger]}) == 5
+
+
+def test_8_bit_weights_are_not_laid_out_by_a_pass_that_is_only_recorded(monkeypatch):
+    capturing = [True]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    model = object.__new__(gated.GatedModel)
+    model.params, model.bf16, model.steps, model._int8, model._int8_steps = {}, {}, 3, None, None
+    with pytest.raises(RuntimeError, match="laid out"):
+        model._quantised()
+    assert model._int8 is None
+    capturing[0] = False
+    model._quantised()
+    capturing[0] = True
+    model._quantised()
+    model.steps = 4
+    with pytest.raises(RuntimeError, match="laid out"):
+        model._quantised()
+    assert model._int8_steps == 3
