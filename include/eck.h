@@ -661,9 +661,11 @@ typedef struct {
  * tensors, number t = step (the first is 1):
  *   g = s grad,  m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
  *   w <- w (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32.  step_more: device uint32 or NULL, added to step (a captured step
- * that is replayed counts there; where t is 0, the call changes nothing).  grad_scale: device float s or NULL (1), as
- * gradients_norm writes it; where it is not finite, the call changes nothing.
+ * in fp32.  step_more: device uint32 or NULL, added to step modulo 2^32 (a
+ * captured step that is replayed counts there, or steps that were left out are
+ * taken off; where t is 0, the call changes nothing).  grad_scale: device float
+ * s or NULL (1), as gradients_norm writes it; where it is not finite, the call
+ * changes nothing.
  * 8BIT states: m in the float8 format e4m3, v in e5m2 (all bytes 0: a state of
  * zeros), times 2^(scale - 127) of the block of ECK_STATE_BLOCK elements, which
  * brings its largest finite one into [2^7, 2^8) or [2^14, 2^15) (scales of 27 to

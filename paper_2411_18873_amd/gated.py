@@ -42,7 +42,7 @@ class GatedModel:
         else:
             self.moments = {k: tuple(torch.zeros(m, dtype=torch.uint8, device="cuda")
                                      for m in (p.numel(), p.numel(), *[-(-p.numel() // eck.STATE_BLOCK)] * 2)) for k, p in self.params.items()}
-        self._work = {}
+        self._work, self._left_out = {}, None  # (minus the number of steps that a norm that is not finite left out, on the device; None: none can be)
         self._copy()
 
     def _copy(self):
@@ -166,7 +166,8 @@ class GatedModel:
         """Adam on Eq. (1) over minibatches of measured kernels, as costmodel_update goes over them; the losses of all steps.  As there,
         minibatches have to divide the pairs, and with an energy that is not positive and finite losses are NaN and the model is left
         unchanged (which the host waits for, once a refit).  weight_decay: AdamW's, of the matrices; max_norm: what the norm of all gradients
-        is brought down to (a step whose norm is not finite changes nothing)."""
+        is brought down to (a step whose norm is not finite changes nothing, and Adam does not count it; `steps`, which numbers the masks of the
+        dropout, does)."""
         n, pairs, losses = int(minibatch), energy_measured.numel(), []
         if n <= 0 or n_steps <= 0 or pairs == 0 or pairs % n:
             raise ValueError("pairs must be a whole number of minibatches, steps one or more")
@@ -180,6 +181,8 @@ class GatedModel:
         states = list(zip(*(self.moments[k] for k in names)))
         plan = None
         scale = torch.ones(1, device="cuda") if max_norm is not None else None
+        if max_norm is not None and self._left_out is None:
+            self._left_out = torch.zeros(1, dtype=torch.int32, device="cuda")
         for step in range(n_steps):
             first = step % (pairs // n) * n
             x, y = feat[:, first:first + n], y_all[first:first + n]
@@ -195,7 +198,8 @@ class GatedModel:
                 plan.set_grads(of)
             if max_norm is not None:
                 eck.gradients_norm(plan, None, scale, self._ws(eck.gradients_norm_workspace_bytes(plan)), max_norm=max_norm)
-            eck.adamw_step(plan, lr, self.steps, beta1, beta2, eps, grad_scale=scale, seed=self.seed)
+                self._left_out.add_(scale != scale, alpha=-1)  # (a norm that is not finite: NaN)
+            eck.adamw_step(plan, lr, self.steps, beta1, beta2, eps, grad_scale=scale, seed=self.seed, step_more=self._left_out)
         self._lay_out_int8()
         return torch.stack(losses)
 

@@ -213,3 +213,34 @@ def test_a_first_score_in_8_bit_integers_is_not_captured():
         torch.cuda.synchronize()
         assert torch.equal(got, want)
         other.score(feat, 512, want, int8=True)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_that_is_left_out_does_not_count(bits):
+    """two poisoned minibatches, then good ones with and without a bound: as the good ones alone"""
+    feat = features(64, 512, 5, torch.float32)
+    poisoned, y = feat.clone(), labels(feat)
+    poisoned[5, 7] = float("nan")
+    models = [gated.GatedModel(hidden=96, blocks=2, head=40, p_drop=0.0, seed=4, state_bits=bits) for _ in range(2)]
+    models[0].refit(poisoned[:, :128], y[:128], 2, 128, max_norm=1.0)
+    assert models[0].steps == 2
+    losses = [[m.refit(feat, y, 3, 128, lr=1e-2, max_norm=1.0) for m in models]]
+    models[0].refit(poisoned[:, :128], y[:128], 1, 128, max_norm=1.0)
+    losses += [[m.refit(feat, y, 3, 128, lr=1e-2, max_norm=1.0) for m in models], [m.refit(feat, y, 3, 128, lr=1e-2) for m in models]]
+    assert all(torch.equal(*two) and torch.isfinite(two[0]).all() for two in losses)
+    for k, p in models[0].params.items():
+        assert torch.equal(p, models[1].params[k]), k
+        assert all(torch.equal(a, b) for a, b in zip(models[0].moments[k], models[1].moments[k])), k
+
+
+def test_a_bound_that_is_never_reached_changes_no_refit():
+    """but by Adam's corrections, whose powers are made by squaring on the device: within a unit of their last place, so a step's size within two"""
+    feat = features(64, 512, 5, torch.float32)
+    models = [gated.GatedModel(hidden=96, blocks=2, head=40, p_drop=0.0, seed=4) for _ in range(2)]
+    start = {k: p.clone() for k, p in models[0].params.items()}
+    for model, most in zip(models, (None, 1e30)):
+        model.refit(feat, labels(feat), 1, 128, lr=1e-3, max_norm=most)
+    for k, p in models[0].params.items():
+        # (w is rounded once more: by half a unit of its own last place on either side)
+        bound = 3 * 2.0 ** -24 * (p - start[k]).abs() + 2 * 2.0 ** -24 * torch.maximum(p.abs(), start[k].abs())
+        assert ((p - models[1].params[k]).abs() <= bound).all(), k
