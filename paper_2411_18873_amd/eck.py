@@ -790,7 +790,8 @@ def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
 
 
 class Parameters:
-    """The tensors of a model as gradients_norm (grads alone) and adamw_step take them, checked once and kept: lists of contiguous CUDA tensors.
+    """The tensors of a model as gradients_norm (grads alone) and adamw_step take them, checked once and kept: lists of contiguous CUDA tensors,
+    none of which is given other memory (its `data` another's, a resize) while the plan is used.
     m, v: float32, or uint8 with m_scale, v_scale (uint8, one for each STATE_BLOCK elements); copies (bfloat16, or None in the list's or a
     tensor's place) receive the new parameters.  weight_decay: one for all, or a list."""
 
@@ -798,6 +799,8 @@ class Parameters:
         count = len(grads)
         self.count, self.state = count, STATE_F32
         self._array = (Parameter * count)()
+        params, m, v, m_scale, v_scale, copies = [t if t is None else tuple(t) for t in (params, m, v, m_scale, v_scale, copies)]
+        # (tuples of its own: tensors live as long as their addresses are here, whatever becomes of the caller's lists)
         self._kept = {"params": params, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies}
         for name, tensors in self._kept.items():
             if tensors is not None and len(tensors) != count:
@@ -840,7 +843,7 @@ class Parameters:
                 raise ValueError("a gradient must have as many elements as its parameter")
             _here(t, t.dtype if t.dtype in _FEAT_DTYPE else torch.float32, "a gradient")
             entry.grad, entry.grad_dtype = t.data_ptr(), _FEAT_DTYPE[t.dtype]
-        self._kept["grads"] = list(grads)
+        self._kept["grads"] = tuple(grads)
 
 
 def _one(t, dtype, name):

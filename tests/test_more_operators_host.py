@@ -1,5 +1,7 @@
 """Host-side checks that need no GPU: refits' and scoring's operators refuse bad arguments before anything is launched."""
 import ctypes as C
+import gc
+import weakref
 
 import pytest
 import torch
@@ -185,3 +187,38 @@ def test_8_bit_weights_are_not_laid_out_by_a_pass_that_is_only_recorded(monkeypa
     with pytest.raises(RuntimeError, match="laid out"):
         model._quantised()
     assert model._int8_steps == 3
+
+
+@pytest.fixture
+def on_the_cpu(monkeypatch):
+    """plans of CPU tensors, which the library never sees"""
+    def here(t, dtype, name):
+        if t.dtype is not dtype or not t.is_contiguous():
+            eck._refuse(t, dtype, name, "a contiguous CUDA tensor")
+        return t
+
+    monkeypatch.setattr(eck, "_here", here)
+    monkeypatch.setattr(eck, "_device", lambda: 0)
+
+
+def lists_of(count, n, eight=False):
+    state = (lambda: torch.zeros(n, dtype=torch.uint8)) if eight else (lambda: torch.zeros(n))
+    make = {"grads": lambda: torch.zeros(n), "params": lambda: torch.zeros(n), "m": state, "v": state, "copies": lambda: torch.zeros(n, dtype=torch.bfloat16)}
+    if eight:
+        make["m_scale"] = make["v_scale"] = lambda: torch.zeros(-(-n // eck.STATE_BLOCK), dtype=torch.uint8)
+    return {name: [one() for _ in range(count)] for name, one in make.items()}
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_plan_holds_its_tensors_whatever_becomes_of_the_lists(on_the_cpu, eight):
+    lists = lists_of(3, 200, eight)
+    seen = [weakref.ref(t) for tensors in lists.values() for t in tensors]
+    plan = eck.Parameters(**lists)
+    lists["m"][1] = None
+    for tensors in lists.values():
+        tensors.clear()
+    gc.collect()
+    assert all(r() is not None for r in seen)
+    del plan
+    gc.collect()
+    assert all(r() is None for r in seen)
