@@ -838,11 +838,14 @@ class Parameters:
         """other gradients of the same sizes, float32 or bfloat16"""
         if len(grads) != self.count:
             raise ValueError("there must be %d gradients" % self.count)
+        new = []
         for entry, t in zip(self._array, grads):
             if t.numel() != entry.n:
                 raise ValueError("a gradient must have as many elements as its parameter")
             _here(t, t.dtype if t.dtype in _FEAT_DTYPE else torch.float32, "a gradient")
-            entry.grad, entry.grad_dtype = t.data_ptr(), _FEAT_DTYPE[t.dtype]
+            new.append((t.data_ptr(), _FEAT_DTYPE[t.dtype]))
+        for entry, (address, dtype) in zip(self._array, new):  # (all of them or, where one is refused, none)
+            entry.grad, entry.grad_dtype = address, dtype
         self._kept["grads"] = tuple(grads)
 
 

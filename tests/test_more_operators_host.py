@@ -222,3 +222,17 @@ def test_a_plan_holds_its_tensors_whatever_becomes_of_the_lists(on_the_cpu, eigh
     del plan
     gc.collect()
     assert all(r() is None for r in seen)
+
+
+def test_gradients_that_are_refused_leave_a_plan_as_it_is(on_the_cpu):
+    lists = lists_of(3, 50)
+    plan = eck.Parameters(**lists)
+    had = [(e.grad, e.grad_dtype, e.n) for e in plan._array]
+    for bad in (torch.zeros(49), torch.zeros(50, dtype=torch.float64), torch.zeros(100)[::2]):
+        with pytest.raises((ValueError, TypeError)):
+            plan.set_grads([torch.zeros(50, dtype=torch.bfloat16), torch.zeros(50), bad])
+        assert [(e.grad, e.grad_dtype, e.n) for e in plan._array] == had
+        assert [t.data_ptr() for t in plan._kept["grads"]] == [address for address, _, _ in had]
+    new = [torch.zeros(50, dtype=torch.bfloat16) for _ in range(3)]
+    plan.set_grads(new)
+    assert [(e.grad, e.grad_dtype) for e in plan._array] == [(t.data_ptr(), eck.BF16) for t in new]
