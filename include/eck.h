@@ -676,8 +676,9 @@ typedef struct {
  * those of 2j and 2j + 1 have the low and the high half of output number j + 1 of
  * a SplitMix64 generator whose state starts at mix(seed + gamma*(t+1)), as in
  * candidate_enumerate: the low half of that m's draw, the high half v's.
- * parameters: host, read during the call.  No two tensors may overlap.  A
- * launch takes some dozens of tensors.
+ * parameters: host, read during the call.  No tensor that is written may
+ * overlap another, or a gradient, unless that is of the same entry and, element
+ * for element, the same memory.  A launch takes up to 200 tensors.
  * Errors: EINVAL (nulls, no element at all, a bad dtype or state, lr, eps or a
  * decay negative or not finite, a beta outside [0, 1), step 0 without
  * step_more), EUNSUPPORTED (n > 2^34), EALIGN. */

@@ -6,6 +6,7 @@ include/eck.h and raises EckError on a non-zero return code.  No arithmetic of
 the method happens here, and there is no fallback: if the library is missing
 the import of the library handle fails loudly.
 """
+import bisect
 import ctypes as C
 import os
 
@@ -829,13 +830,26 @@ class Parameters:
                 if _here(tensors[i], dtype, field).numel() != n:
                     raise ValueError("%s of tensor %d must have %d elements" % (field, i, n))
                 setattr(entry, field, tensors[i].data_ptr())
-        written = [p for e in self._array if e.n for p in (e.param, e.m, e.v, e.m_scale, e.v_scale, e.bf16_out) if p]
-        if len(set(written)) != len(written):
+        # what a step writes, in order of address: (first byte, one past the last)
+        each = 4 if self.state == STATE_F32 else 1
+        self._written = sorted((p, p + size) for e in self._array if e.n for p, size in (
+            (e.param, 4 * e.n), (e.m, each * e.n), (e.v, each * e.n), (e.m_scale, -(-e.n // STATE_BLOCK)), (e.v_scale, -(-e.n // STATE_BLOCK)),
+            (e.bf16_out, 2 * e.n)) if p)
+        if any(end > begin for (_, end), (begin, _) in zip(self._written, self._written[1:])):
             raise ValueError("parameters, states and copies must be tensors of their own")
         self.set_grads(grads)
 
+    def _check_apart(self, entry, address, size):
+        written, end = self._written, address + size * entry.n
+        at = bisect.bisect_left(written, (address,))  # the first that begins with the gradient or behind it
+        if (at and written[at - 1][1] > address) or (at < len(written) and written[at][0] < end):
+            own = (entry.bf16_out,) if size == 2 else (entry.param, entry.m, entry.v) if self.state == STATE_F32 else (entry.param,)
+            if entry.n and address not in own:
+                raise ValueError("a gradient must not lie in what a step writes")
+
     def set_grads(self, grads):
-        """other gradients of the same sizes, float32 or bfloat16"""
+        """other gradients of the same sizes, float32 or bfloat16, in memory that a step does not write (or, element for element, a tensor that it
+        writes of the same parameter: a thread reads its elements before it writes them)"""
         if len(grads) != self.count:
             raise ValueError("there must be %d gradients" % self.count)
         new = []
@@ -843,7 +857,9 @@ class Parameters:
             if t.numel() != entry.n:
                 raise ValueError("a gradient must have as many elements as its parameter")
             _here(t, t.dtype if t.dtype in _FEAT_DTYPE else torch.float32, "a gradient")
-            new.append((t.data_ptr(), _FEAT_DTYPE[t.dtype]))
+            address, dtype = t.data_ptr(), _FEAT_DTYPE[t.dtype]
+            self._check_apart(entry, address, 4 if dtype == F32 else 2)
+            new.append((address, dtype))
         for entry, (address, dtype) in zip(self._array, new):  # (all of them or, where one is refused, none)
             entry.grad, entry.grad_dtype = address, dtype
         self._kept["grads"] = tuple(grads)

@@ -236,3 +236,47 @@ def test_gradients_that_are_refused_leave_a_plan_as_it_is(on_the_cpu):
     new = [torch.zeros(50, dtype=torch.bfloat16) for _ in range(3)]
     plan.set_grads(new)
     assert [(e.grad, e.grad_dtype) for e in plan._array] == [(t.data_ptr(), eck.BF16) for t in new]
+
+
+def test_tensors_that_share_memory_are_refused(on_the_cpu):
+    n = 64
+    apart = lambda: torch.zeros(n)  # noqa: E731
+    memory, bytes_ = torch.zeros(4 * n), torch.zeros(8 * n, dtype=torch.uint8)
+
+    def written(*tensors, **kw):
+        with pytest.raises(ValueError, match="of their own"):
+            eck.Parameters([apart()], *[[t] for t in tensors], **{k: [t] for k, t in kw.items()})
+
+    at = lambda first: memory[first:first + n]  # noqa: E731
+    eck.Parameters([apart()], [at(0)], [at(n)], [at(2 * n)], copies=[at(3 * n).view(torch.bfloat16)[:n]])  # (neighbours)
+    for first in (0, 1, n - 1):
+        written(at(n), at(n + first), apart())
+        written(apart(), at(n), at(n - first))
+        written(at(n + first), apart(), at(n))
+    written(apart(), apart(), at(n), copies=at(n + 5).view(torch.bfloat16)[n:])
+    written(at(0), apart(), apart(), copies=at(0).view(torch.bfloat16)[:n])
+    state = lambda first, size=n: bytes_[first:first + size]  # noqa: E731
+    eck.Parameters([apart()], [apart()], [state(0)], [state(n)], [state(2 * n, 1)], [state(2 * n + 1, 1)])
+    written(apart(), state(0), state(n - 1), state(2 * n, 1), state(2 * n + 1, 1))
+    written(apart(), state(0), state(n), state(2 * n, 1), state(2 * n, 1))
+    written(apart(), state(0), state(n), state(2 * n - 1, 1), state(2 * n, 1))
+
+    # gradients: in memory of their own or, element for element, where their parameter or its states lie
+    def grads(*of, **how):
+        plan = eck.Parameters([apart(), apart()], [at(0), at(n)], [apart(), at(2 * n)], [apart(), apart()], **how)
+        plan.set_grads([apart() if g is None else g for g in of])
+
+    copy = torch.zeros(2 * n, dtype=torch.bfloat16)
+    grads(at(0), at(n))
+    grads(None, at(2 * n))
+    grads(copy[:n], None, copies=[copy[:n], None])
+    grads(at(3 * n), at(3 * n))  # (both the same, but only read)
+    for first, second in ((at(1), None), (at(n), None), (None, at(n - 1)), (at(2 * n), None), (None, at(3 * n - 1)), (at(0).view(torch.bfloat16)[:n], None),
+                          (None, at(n).view(torch.bfloat16)[n:])):
+        with pytest.raises(ValueError, match="must not lie"):
+            grads(first, second)
+    for first, second in ((copy[1:n + 1], None), (None, copy[:n])):
+        with pytest.raises(ValueError, match="must not lie"):
+            grads(first, second, copies=[copy[:n], None])
+    with pytest.raises(ValueError, match="must not lie"):  # (a state of bytes is no gradient's memory)
+        eck.Parameters([memory[:n // 4]], [apart()[:n // 4]], [memory[:n // 4].view(torch.uint8)[:n // 4]], [state(0, n // 4)], [state(n, 1)], [state(n + 1, 1)])
