@@ -728,6 +728,13 @@ def _here_rows(t, name, dtype, shape):
     return stride[0] if is_shape[0] > 1 else is_shape[1]
 
 
+def _ws_here(ws):
+    """_ws, of the current device"""
+    if ws is not None and ws.is_cuda and ws.get_device() != _device():
+        raise ValueError("ws must be on the current device")
+    return _ws(ws)
+
+
 def int8_rows(n, width):
     """an int8 matrix [n][width] whose rows lie the next multiple of sixteen apart, as quantise_rows writes and product_int8 reads them"""
     return torch.zeros(n, -(-width // 16) * 16, dtype=torch.int8, device="cuda")[:, :width]
@@ -781,7 +788,7 @@ def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
     rows = n_out if act == ACT_NONE else 2 * n_out
     if dtype not in _FEAT_DTYPE:
         raise TypeError("y must be of float32 or bfloat16")
-    ws_ptr, ws_bytes = _ws(ws)
+    ws_ptr, ws_bytes = _ws_here(ws)
     _check("product_int8", lib().product_int8(
         x.data_ptr(), _int8(x, "x", shape), _scales(x_scale, "x_scale", n), n, n_in, n_out, w.data_ptr(), _int8(w, "w", (rows, n_in)),
         _scales(w_scale, "w_scale", rows), act, _FEAT_DTYPE[dtype], y.data_ptr(), _here_rows(y, "y", dtype, (n, n_out)), ws_ptr, ws_bytes, _stream()))
@@ -798,7 +805,7 @@ class Parameters:
 
     def __init__(self, grads, params=None, m=None, v=None, m_scale=None, v_scale=None, copies=None, weight_decay=0.0):
         count = len(grads)
-        self.count, self.state = count, STATE_F32
+        self.count, self.state, self.device = count, STATE_F32, None
         self._array = (Parameter * count)()
         params, m, v, m_scale, v_scale, copies = [t if t is None else tuple(t) for t in (params, m, v, m_scale, v_scale, copies)]
         # (tuples of its own: tensors live as long as their addresses are here, whatever becomes of the caller's lists)
@@ -839,6 +846,10 @@ class Parameters:
             raise ValueError("parameters, states and copies must be tensors of their own")
         self.set_grads(grads)
 
+    def check_device(self):
+        if self.device is not None and self.device != _device():
+            raise ValueError("parameters must be on the current device")
+
     def _check_apart(self, entry, address, size):
         written, end = self._written, address + size * entry.n
         at = bisect.bisect_left(written, (address,))  # the first that begins with the gradient or behind it
@@ -848,10 +859,11 @@ class Parameters:
                 raise ValueError("a gradient must not lie in what a step writes")
 
     def set_grads(self, grads):
-        """other gradients of the same sizes, float32 or bfloat16, in memory that a step does not write (or, element for element, a tensor that it
+        """other gradients of the same sizes and device, float32 or bfloat16, in memory that a step does not write (or, element for element, a tensor that it
         writes of the same parameter: a thread reads its elements before it writes them)"""
         if len(grads) != self.count:
             raise ValueError("there must be %d gradients" % self.count)
+        self.check_device()
         new = []
         for entry, t in zip(self._array, grads):
             if t.numel() != entry.n:
@@ -863,6 +875,8 @@ class Parameters:
         for entry, (address, dtype) in zip(self._array, new):  # (all of them or, where one is refused, none)
             entry.grad, entry.grad_dtype = address, dtype
         self._kept["grads"] = tuple(grads)
+        if new:
+            self.device = _device()  # (all tensors are on it)
 
 
 def _one(t, dtype, name):
@@ -878,6 +892,7 @@ def adamw_step(parameters, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scal
     """step number `step` (+ *step_more, an int32 tensor) over all of a Parameters; gradients times *grad_scale; seed: of 8-bit states' roundings"""
     if not 0 <= step < 1 << 32:
         raise ValueError("step must be a whole number of 32 bits")
+    parameters.check_device()
     _check("adamw_step", lib().adamw_step(parameters._array, parameters.count, parameters.state, lr, beta1, beta2, eps, step,
                                           _one(step_more, torch.int32, "step_more"), _one(grad_scale, torch.float32, "grad_scale"), seed, _stream()))
 
@@ -888,7 +903,8 @@ def gradients_norm_workspace_bytes(parameters):
 
 def gradients_norm(parameters, norm_out, scale_out, ws, max_norm=float("inf")):
     """norm_out = the norm of all gradients, scale_out = what brings it to max_norm or less (one of them may be None)"""
-    ws_ptr, ws_bytes = _ws(ws)
+    parameters.check_device()
+    ws_ptr, ws_bytes = _ws_here(ws)
     _check("gradients_norm", lib().gradients_norm(parameters._array, parameters.count, max_norm, _one(norm_out, torch.float32, "norm_out"),
                                                   _one(scale_out, torch.float32, "scale_out"), ws_ptr, ws_bytes, _stream()))
 
@@ -920,7 +936,7 @@ def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, coun
         raise ValueError("idx_out must not be None")
     flags = torch.uint8 if legal is None or legal.element_size() != 1 else legal.dtype
     whole = lambda t: t.dtype if t is not None and t.element_size() == 4 else torch.int32  # noqa: E731
-    ws_ptr, ws_bytes = _ws(ws)
+    ws_ptr, ws_bytes = _ws_here(ws)
     _check("sample_select", lib().sample_select(
         _here(energy, torch.float32, "energy").data_ptr(), _drawn(legal, flags, "legal", n), n, n_segments,
         _here(uniform, torch.float32, "uniform").data_ptr(), draws, temperature, k, top_p, min_p,

@@ -280,3 +280,39 @@ def test_tensors_that_share_memory_are_refused(on_the_cpu):
             grads(first, second, copies=[copy[:n], None])
     with pytest.raises(ValueError, match="must not lie"):  # (a state of bytes is no gradient's memory)
         eck.Parameters([memory[:n // 4]], [apart()[:n // 4]], [memory[:n // 4].view(torch.uint8)[:n // 4]], [state(0, n // 4)], [state(n, 1)], [state(n + 1, 1)])
+
+
+class ElsewhereOnTheGPU:
+    is_cuda = True
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return 1
+
+    def data_ptr(self):
+        return FAKE
+
+    def numel(self):
+        return 1 << 30
+
+    def element_size(self):
+        return 1
+
+
+def test_plans_and_workspaces_of_another_device_are_refused(on_the_cpu, monkeypatch):
+    lists = lists_of(2, 50)
+    plan, one = eck.Parameters(**lists), torch.zeros(1)
+    need = eck.gradients_norm_workspace_bytes(plan)
+    assert need > 0
+    monkeypatch.setattr(eck, "lib", lambda: pytest.fail("the library was called"))
+    q, f = torch.zeros(4, 16, dtype=torch.int8), torch.zeros(4)
+    for call in (lambda ws: eck.gradients_norm(plan, one, one, ws), lambda ws: eck.product_int8(q, f, q, f, torch.zeros(4, 4), ws),
+                 lambda ws: eck.sample_select(torch.zeros(64), None, 1, torch.zeros(1, 2), torch.zeros(2, dtype=torch.int32), None, None, ws)):
+        with pytest.raises(ValueError, match="current device"):
+            call(ElsewhereOnTheGPU())
+    monkeypatch.setattr(eck, "_device", lambda: 1)
+    for call in (lambda: eck.adamw_step(plan, 1e-3, 1), lambda: eck.gradients_norm(plan, one, one, None), lambda: plan.set_grads(lists["grads"])):
+        with pytest.raises(ValueError, match="current device"):
+            call()
