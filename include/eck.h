@@ -382,7 +382,8 @@ int32_t topk_select_static(const float *energy, const float *latency, const uint
  * The result does not depend on the order of execution.
  * Errors: EINVAL (nulls, a zero size, temperature negative or not finite, top_p
  * outside (0, 1], min_p outside [0, 1]), ESHAPE (n % n_segments), EUNSUPPORTED
- * (a segment longer than 2^31, more than 2^20 segments), EWORKSPACE, EALIGN. */
+ * (a segment longer than 2^31, more than 2^20 segments, more than 2^31 draws of
+ * a segment), EWORKSPACE, EALIGN. */
 uint64_t sample_select_workspace_bytes(uint64_t n, uint32_t n_segments, uint32_t draws);
 int32_t sample_select(const float *energy, const uint8_t *legal, uint64_t n, uint32_t n_segments, const float *uniform,
                       uint32_t draws, float temperature, uint32_t k, float top_p, float min_p, uint32_t *idx_out,

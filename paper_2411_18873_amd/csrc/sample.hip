@@ -23,7 +23,7 @@ namespace {
 
 constexpr uint32_t BINS = 2048, BIN_BITS = 11, NO_KEY = 0xFFFFFFFFu, NOBODY = 0xFFFFFFFFu;
 constexpr uint64_t MOST_CANDIDATES = 1ull << 31;
-constexpr uint32_t MOST_SEGMENTS = 1u << 20;
+constexpr uint32_t MOST_SEGMENTS = 1u << 20, MOST_DRAWS = 1u << 31; // (draws are counted in 32 bits, a launch's threads at a time)
 
 struct Draws {
     const float *energy;
@@ -1924,7 +1924,8 @@ using namespace eck;
 
 extern "C" uint64_t sample_select_workspace_bytes(uint64_t n, uint32_t n_segments, uint32_t draws)
 {
-    if (n == 0 || n_segments == 0 || draws == 0 || n % n_segments || n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS) return 0;
+    if (n == 0 || n_segments == 0 || draws == 0 || n % n_segments || n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS || draws > MOST_DRAWS)
+        return 0;
     if (n / n_segments <= SHORT) return 0;
     Long p; // (the query does not know k: room for either way)
     p.a.n = n / n_segments;
@@ -1943,7 +1944,7 @@ extern "C" int32_t sample_select(const float *energy, const uint8_t *legal, uint
     if (!energy || !uniform || !idx_out || n == 0 || n_segments == 0 || draws == 0) return ECK_EINVAL;
     if (!(temperature >= 0.0f && temperature < __builtin_inff()) || !(top_p > 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f)) return ECK_EINVAL;
     if (n % n_segments) return ECK_ESHAPE;
-    if (n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS) return ECK_EUNSUPPORTED;
+    if (n / n_segments > MOST_CANDIDATES || n_segments > MOST_SEGMENTS || draws > MOST_DRAWS) return ECK_EUNSUPPORTED;
     if (!aligned(energy, 4) || !aligned(uniform, 4) || !aligned(idx_out, 4) || !aligned(logprob_out, 4) || !aligned(count_out, 4)) return ECK_EALIGN;
     const uint64_t need = sample_select_workspace_bytes(n, n_segments, draws);
     if (need && (!ws || ws_bytes < need)) return ECK_EWORKSPACE;

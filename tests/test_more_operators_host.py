@@ -316,3 +316,14 @@ def test_plans_and_workspaces_of_another_device_are_refused(on_the_cpu, monkeypa
     for call in (lambda: eck.adamw_step(plan, 1e-3, 1), lambda: eck.gradients_norm(plan, one, one, None), lambda: plan.set_grads(lists["grads"])):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+@pytest.mark.parametrize("n", [1 << 12, 1 << 18])
+@pytest.mark.parametrize("k,t", [(0, 0.5), (1, 0.5), (100, 0.5), (5000, 0.5), (0, 0.0)])
+def test_more_draws_than_are_counted_are_refused(n, k, t):
+    F, W = eck.lib().sample_select, eck.lib().sample_select_workspace_bytes
+    vp = C.c_void_p
+    assert W(1 << 18, 1, 1 << 31) == W(1 << 18, 1, 8)
+    for draws in ((1 << 31) + 1, (1 << 32) - 1):
+        assert W(n, 1, draws) == 0
+        assert F(vp(FAKE), None, n, 1, vp(FAKE), draws, t, k, 0.9, 0.1, vp(FAKE), vp(FAKE), vp(FAKE), vp(FAKE), 1 << 40, None) == eck.EUNSUPPORTED
