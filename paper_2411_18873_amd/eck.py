@@ -711,6 +711,11 @@ def _refuse(t, dtype, name, what):
     raise TypeError("%s must be %s" % (name, what))
 
 
+def _no_size(name):
+    """(ctypes cuts whole numbers off: 2^32 + 5 draws would be five)"""
+    raise ValueError("%s must be whole numbers of 32 bits" % name)
+
+
 def _here(t, dtype, name):
     """a contiguous CUDA tensor of dtype on the current device"""
     if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or t.get_device() != _device():
@@ -772,11 +777,15 @@ def quantise_rows(x, q, scale, order=ROWS):
         ld_x = _here_rows(x, "x", dtype, x.shape)
     if dtype not in _FEAT_DTYPE:
         raise TypeError("x must be of float32 or bfloat16")
+    if width >> 32:
+        _no_size("widths")
     _check("quantise_rows", lib().quantise_rows(x.data_ptr(), order, _FEAT_DTYPE[dtype], ld_x, n, width, q.data_ptr(), _int8(q, "q", shape),
                                                 _scales(scale, "scale", n), _stream()))
 
 
 def product_int8_workspace_bytes(n, n_in, n_out, act=ACT_NONE):
+    if (n_in | n_out) >> 32:
+        _no_size("widths")
     return int(lib().product_int8_workspace_bytes(n, n_in, n_out, act))
 
 
@@ -786,6 +795,8 @@ def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
     n, n_in = shape
     n_out = y.shape[1]
     rows = n_out if act == ACT_NONE else 2 * n_out
+    if (n_in | n_out) >> 32:
+        _no_size("widths")
     if dtype not in _FEAT_DTYPE:
         raise TypeError("y must be of float32 or bfloat16")
     ws_ptr, ws_bytes = _ws_here(ws)
@@ -913,6 +924,8 @@ def gradients_norm(parameters, norm_out, scale_out, ws, max_norm=float("inf")):
 
 
 def sample_select_workspace_bytes(n, n_segments, draws):
+    if (n_segments | draws) >> 32:
+        _no_size("segments and draws")
     return int(lib().sample_select_workspace_bytes(n, n_segments, draws))
 
 
@@ -932,6 +945,8 @@ def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, coun
     if len(shape) != 2 or shape[0] != n_segments:
         raise ValueError("uniform must be of shape (%d, draws)" % n_segments)
     draws, n = shape[1], energy.numel()
+    if (n_segments | draws | k) >> 32:
+        _no_size("segments, draws and k")
     if idx_out is None:
         raise ValueError("idx_out must not be None")
     flags = torch.uint8 if legal is None or legal.element_size() != 1 else legal.dtype

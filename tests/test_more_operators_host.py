@@ -327,3 +327,22 @@ def test_more_draws_than_are_counted_are_refused(n, k, t):
     for draws in ((1 << 31) + 1, (1 << 32) - 1):
         assert W(n, 1, draws) == 0
         assert F(vp(FAKE), None, n, 1, vp(FAKE), draws, t, k, 0.9, 0.1, vp(FAKE), vp(FAKE), vp(FAKE), vp(FAKE), 1 << 40, None) == eck.EUNSUPPORTED
+
+
+def test_sizes_past_32_bits_are_refused_and_not_cut_off(on_the_cpu, monkeypatch):
+    monkeypatch.setattr(eck, "lib", lambda: pytest.fail("the library was called"))
+    monkeypatch.setattr(eck, "_here_rows", lambda t, name, dtype, shape: t.stride(0))
+    monkeypatch.setattr(eck, "_int8", lambda t, name, shape: t.stride(0))
+    monkeypatch.setattr(eck, "_stream", lambda: None)
+    empty = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="meta")  # noqa: E731
+    past, i8 = (1 << 32) + 16, torch.int8
+    few = dict(energy=empty(64), legal=None, n_segments=1, uniform=empty(1, 2), idx_out=empty(2, dtype=torch.int32), logprob_out=None, count_out=None, ws=None)
+    for call in (lambda: eck.quantise_rows(empty(2, past), empty(2, past, dtype=i8), empty(2)),
+                 lambda: eck.product_int8(empty(2, past, dtype=i8), empty(2), empty(3, past, dtype=i8), empty(3), empty(2, 3), None),
+                 lambda: eck.product_int8(empty(2, 16, dtype=i8), empty(2), empty(past, 16, dtype=i8), empty(past), empty(2, past), None),
+                 lambda: eck.product_int8_workspace_bytes(2, past, 3), lambda: eck.product_int8_workspace_bytes(2, 3, -1),
+                 lambda: eck.sample_select(**dict(few, uniform=empty(1, past), idx_out=empty(past, dtype=torch.int32))),
+                 lambda: eck.sample_select(**few, k=past), lambda: eck.sample_select(**few, k=-1),
+                 lambda: eck.sample_select_workspace_bytes(64, 1, past), lambda: eck.sample_select_workspace_bytes(64, past, 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
