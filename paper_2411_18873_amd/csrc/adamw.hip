@@ -4,7 +4,7 @@
 //   w <- w (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Everything is read and written once, so memory bounds it: 100.7 million parameters with bf16 gradients and copies, 2.82 GB, take 533 us
-// (5.3 TB/s; a copy of 1 GiB 5.1), 96 million with 8-bit states, 1.54 GB, 312 (4.9 TB/s; the states' arithmetic takes nearly as long as their
+// (5.3 TB/s; a copy of 1 GiB 5.1), 96 million with 8-bit states, 1.54 GB, 315 (4.9 TB/s; the states' arithmetic takes nearly as long as their
 // way).  The tensors' addresses travel as kernel arguments, so that a step needs no
 // table on the device and a captured one holds its own; a kilobyte of them takes about a microsecond (a launch of 72 bytes 3.3 us, of 4 KB 6.9,
 // of 14 KB 16), so a launch has room for 12, 48 or 200 tensors, whichever does.  Blocks of threads take stretches of a tensor.
@@ -219,11 +219,17 @@ __device__ __forceinline__ void advance(const Tensor<EIGHT> &t, uint64_t n, uint
             m[i] = fmaf(step.one_beta1, g, m[i] * step.beta1);
             v[i] = fmaf(step.one_beta2, g * g, v[i] * step.beta2);
         }
+    }
+    if (EIGHT && step.eps >= 0x1p-39f) {
         // (8 bits: root and quotient as the instructions give them, within a unit of the last place each; full ones are two dozen
-        // instructions, and instructions bound this kernel)
-        const float corrected = v[i] * inverse;
-        const float step_of = EIGHT ? m[i] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(corrected) + step.eps) : m[i] / (sqrtf(corrected) + step.eps);
-        w[i] = fmaf(-rate, step_of, had.w[i] * t.keep);
+        // instructions, and instructions bound this kernel.  They take numbers below 2^-126 for 0: of roots, which are below 2^-63, that is within a
+        // rounding beside such an eps, but not beside a smaller one, with which the smallest gradients' steps would be infinite)
+#pragma unroll
+        for (uint32_t i = 0; i < EACH; ++i)
+            w[i] = fmaf(-rate, m[i] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inverse) + step.eps), had.w[i] * t.keep);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < EACH; ++i) w[i] = fmaf(-rate, m[i] / (sqrtf(v[i] * inverse) + step.eps), had.w[i] * t.keep);
     }
     put(t.param, at, n, w);
     if (t.copy) {

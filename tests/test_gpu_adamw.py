@@ -378,3 +378,25 @@ def test_a_tensor_in_two_places_is_refused():
     copy = torch.zeros(8, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(ValueError, match="of their own"):
         eck.Parameters(a[:2], a[:2], a[2:4], a[4:6], copies=[copy, copy])
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-18, 1e-13, 2e-12, 1e-8])
+@pytest.mark.parametrize("step", [1, 5])
+def test_8_bit_steps_of_the_smallest_gradients(eps, step):
+    """down to those whose square is a denormal number: from states of zeros, as the formula has them.  Errors in relative terms: g and 1 - beta1 of m,
+    g twice and 1 - beta2 of v, each product of v (of which those below 2^-126 are rounded to 2^-149: by half of that), the correction's factor
+    and product, halved by the root; root and quotient by instructions of a unit each, eps, their sum, rate, its product with the step: 20 e"""
+    n = 400
+    grads = torch.exp2(torch.linspace(-73.0, -40.0, n)).cuda()
+    grads[::2] *= -1
+    param = torch.zeros(n, device="cuda")
+    m, v = [torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(-(-n // eck.STATE_BLOCK), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    eck.adamw_step(eck.Parameters([grads], [param], [m], [v], [scales[0]], [scales[1]]), lr=1e-3, beta1=0.5, beta2=0.5, step=step, eps=eps)
+    g = grads.double()
+    wide = 0.5 * g * g
+    den = torch.sqrt(wide / (1 - 0.5 ** step)) + eps
+    want = -1e-3 / (1 - 0.5 ** step) * 0.5 * g / den
+    off = 20 * E + 0.5 * 1.5 * 2.0 ** -149 / wide  # (two products of v and the corrected one; half for the root)
+    assert torch.isfinite(param).all()
+    assert ((param.double() - want).abs() <= off * want.abs() * 1.01).all()
