@@ -940,7 +940,8 @@ def _drawn(t, dtype, name, n):
 
 def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, count_out, ws, temperature=1.0, k=0, top_p=1.0, min_p=0.0):
     """idx_out [n_segments][draws] = candidates drawn by exp(-energy / temperature) with the numbers uniform [n_segments][draws], of the k least
-    (0: all) that have the share top_p of the weight and min_p of the best one's or more; logprob_out (as idx_out) and count_out may be None"""
+    (0: all) that have the share top_p of the weight and min_p of the best one's or more; logprob_out (as idx_out) and count_out may be None.
+    idx_out and count_out: int32 or uint32"""
     shape = uniform.shape
     if len(shape) != 2 or shape[0] != n_segments:
         raise ValueError("uniform must be of shape (%d, draws)" % n_segments)
@@ -950,7 +951,7 @@ def sample_select(energy, legal, n_segments, uniform, idx_out, logprob_out, coun
     if idx_out is None:
         raise ValueError("idx_out must not be None")
     flags = torch.uint8 if legal is None or legal.element_size() != 1 else legal.dtype
-    whole = lambda t: t.dtype if t is not None and t.element_size() == 4 else torch.int32  # noqa: E731
+    whole = lambda t: torch.uint32 if t is not None and t.dtype is torch.uint32 else torch.int32  # noqa: E731
     ws_ptr, ws_bytes = _ws_here(ws)
     _check("sample_select", lib().sample_select(
         _here(energy, torch.float32, "energy").data_ptr(), _drawn(legal, flags, "legal", n), n, n_segments,

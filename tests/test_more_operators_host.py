@@ -346,3 +346,26 @@ def test_sizes_past_32_bits_are_refused_and_not_cut_off(on_the_cpu, monkeypatch)
                  lambda: eck.sample_select_workspace_bytes(64, 1, past), lambda: eck.sample_select_workspace_bytes(64, past, 1)):
         with pytest.raises(ValueError, match="32 bits"):
             call()
+
+
+def test_indices_and_counts_are_whole_numbers(on_the_cpu, monkeypatch):
+    monkeypatch.setattr(eck, "_stream", lambda: None)
+    called = []
+    library = type("Library", (), {"sample_select": staticmethod(lambda *args: called.append(args) or eck.OK)})
+    monkeypatch.setattr(eck, "lib", lambda: library)
+
+    def call(idx, count):
+        eck.sample_select(torch.zeros(64), None, 1, torch.zeros(1, 2), idx, None, count, None)
+
+    whole = (torch.int32, torch.uint32)
+    for idx in whole:
+        call(torch.zeros(2, dtype=idx), None)
+        for count in whole:
+            call(torch.zeros(2, dtype=idx), torch.zeros(1, dtype=count))
+    assert len(called) == 6
+    for wrong in (torch.float32, torch.int64, torch.int16):
+        with pytest.raises(TypeError):
+            call(torch.zeros(2, dtype=wrong), None)
+        with pytest.raises(TypeError):
+            call(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=wrong))
+    assert len(called) == 6
