@@ -850,24 +850,19 @@ class Parameters:
                 setattr(entry, field, tensors[i].data_ptr())
         # what a step writes, in order of address: (first byte, one past the last)
         each = 4 if self.state == STATE_F32 else 1
-        self._written = sorted((p, p + size) for e in self._array if e.n for p, size in (
+        written = sorted((p, p + size) for e in self._array if e.n for p, size in (
             (e.param, 4 * e.n), (e.m, each * e.n), (e.v, each * e.n), (e.m_scale, -(-e.n // STATE_BLOCK)), (e.v_scale, -(-e.n // STATE_BLOCK)),
             (e.bf16_out, 2 * e.n)) if p)
-        if any(end > begin for (_, end), (begin, _) in zip(self._written, self._written[1:])):
+        if any(end > begin for (_, end), (begin, _) in zip(written, written[1:])):
             raise ValueError("parameters, states and copies must be tensors of their own")
+        # (a sentinel behind the last one; and what of each gradient's check does not change)
+        self._begins, self._ends = [begin for begin, _ in written] + [1 << 64], [end for _, end in written]
+        self._each = [(e.n, (e.bf16_out,), (e.param, e.m, e.v) if self.state == STATE_F32 else (e.param,)) for e in self._array]
         self.set_grads(grads)
 
     def check_device(self):
         if self.device is not None and self.device != _device():
             raise ValueError("parameters must be on the current device")
-
-    def _check_apart(self, entry, address, size):
-        written, end = self._written, address + size * entry.n
-        at = bisect.bisect_left(written, (address,))  # the first that begins with the gradient or behind it
-        if (at and written[at - 1][1] > address) or (at < len(written) and written[at][0] < end):
-            own = (entry.bf16_out,) if size == 2 else (entry.param, entry.m, entry.v) if self.state == STATE_F32 else (entry.param,)
-            if entry.n and address not in own:
-                raise ValueError("a gradient must not lie in what a step writes")
 
     def set_grads(self, grads):
         """other gradients of the same sizes and device, float32 or bfloat16, in memory that a step does not write (or, element for element, a tensor that it
@@ -875,14 +870,19 @@ class Parameters:
         if len(grads) != self.count:
             raise ValueError("there must be %d gradients" % self.count)
         self.check_device()
-        new = []
-        for entry, t in zip(self._array, grads):
-            if t.numel() != entry.n:
+        new, begins, ends = [], self._begins, self._ends
+        for (n, bf16_own, f32_own), t in zip(self._each, grads):
+            dtype = t.dtype
+            if t.numel() != n:
                 raise ValueError("a gradient must have as many elements as its parameter")
-            _here(t, t.dtype if t.dtype in _FEAT_DTYPE else torch.float32, "a gradient")
-            address, dtype = t.data_ptr(), _FEAT_DTYPE[t.dtype]
-            self._check_apart(entry, address, 4 if dtype == F32 else 2)
-            new.append((address, dtype))
+            if dtype is not torch.bfloat16:
+                dtype = torch.float32
+            address = _here(t, dtype, "a gradient").data_ptr()
+            size, own, code = (4, f32_own, F32) if dtype is torch.float32 else (2, bf16_own, BF16)
+            at = bisect.bisect_left(begins, address)  # the first written tensor that begins with the gradient or behind it
+            if (begins[at] < address + size * n or (at and ends[at - 1] > address)) and n and address not in own:
+                raise ValueError("a gradient must not lie in what a step writes")
+            new.append((address, code))
         for entry, (address, dtype) in zip(self._array, new):  # (all of them or, where one is refused, none)
             entry.grad, entry.grad_dtype = address, dtype
         self._kept["grads"] = tuple(grads)

@@ -181,6 +181,7 @@ class GatedModel:
         states = list(zip(*(self.moments[k] for k in names)))
         plan = None
         scale = torch.ones(1, device="cuda") if max_norm is not None else None
+        left_out = torch.zeros(1, dtype=torch.bool, device="cuda") if max_norm is not None else None
         if max_norm is not None and self._left_out is None:
             self._left_out = torch.zeros(1, dtype=torch.int32, device="cuda")
         for step in range(n_steps):
@@ -198,7 +199,7 @@ class GatedModel:
                 plan.set_grads(of)
             if max_norm is not None:
                 eck.gradients_norm(plan, None, scale, self._ws(eck.gradients_norm_workspace_bytes(plan)), max_norm=max_norm)
-                self._left_out.add_(scale != scale, alpha=-1)  # (a norm that is not finite: NaN)
+                self._left_out.add_(torch.ne(scale, scale, out=left_out), alpha=-1)  # (a norm that is not finite: NaN)
             eck.adamw_step(plan, lr, self.steps, beta1, beta2, eps, grad_scale=scale, seed=self.seed, step_more=self._left_out)
         self._lay_out_int8()
         return torch.stack(losses)
