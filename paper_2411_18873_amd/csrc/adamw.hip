@@ -3,11 +3,12 @@
 //   g = s grad,  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g g,
 //   w <- w (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Everything is read and written once, so memory bounds it: 100.7 million parameters with bf16 gradients and copies, 2.82 GB, take 533 us
+// Everything is read and written once, so memory bounds it: 100.7 million parameters with bf16 gradients and copies, 2.82 GB, take 534 us
 // (5.3 TB/s; a copy of 1 GiB 5.1), 96 million with 8-bit states, 1.54 GB, 315 (4.9 TB/s; the states' arithmetic takes nearly as long as their
 // way).  The tensors' addresses travel as kernel arguments, so that a step needs no
-// table on the device and a captured one holds its own; a kilobyte of them takes about a microsecond (a launch of 72 bytes 3.3 us, of 4 KB 6.9,
-// of 14 KB 16), so a launch has room for 12, 48 or 200 tensors, whichever does.  Blocks of threads take stretches of a tensor.
+// table on the device and a captured one holds its own; arguments are not free, so a launch has room for 12, 48 or 200 tensors, whichever does
+// (steps of 12, 48, 49 and 200 tensors of 1024 elements: 5.1, 5.5, 5.7 and 6.1 us; of 16 384 elements 5.2, 7.4, 7.6 and 15.5).  Blocks of
+// threads take stretches of a tensor.
 //
 // 8-bit states.  m is held in e4m3 and v in e5m2, each with a power of two for every 128 elements that brings the largest into
 // [2^7, 2^8) and [2^14, 2^15): steps of at most an eighth and a quarter of a number, down to 2^-17 and 2^-31 of the block's largest.
@@ -41,7 +42,6 @@ struct Tensor<false> {
     uint64_t n;
     uint32_t first; // block of threads that starts it
     float keep;     // 1 - lr decay
-    static constexpr uint8_t *m_scale = nullptr, *v_scale = nullptr;
 };
 template <>
 struct Tensor<true> {

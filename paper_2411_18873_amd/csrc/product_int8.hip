@@ -343,11 +343,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const Int8Product 
 
 // ------------------------------------------------------------------------------------------------ short rows
 
-// Rows of up to 64 * STEPS integers, many of them: what is written bounds it, or the activations.  A wavefront keeps the weights and scales
+// Rows of up to 64 * STEPS integers, many of them: what is written bounds it, and then the activations.  A wavefront keeps the weights and scales
 // of 64 columns (GATE: and of their ups) in registers and goes over rows, sixteen at a time, with no LDS and no barrier.  Matrix rows are
 // handed out so that a lane's sums of four matrix instructions make pieces of sixteen bytes of one row, which lie next to those of the other
-// lanes: results are written from the registers.  2^18 rows of 64, 256 gated columns: 50 us (88 by tiles), 152 MB at 3 TB/s; the exponentials,
-// quotients and products of 67 million activations alone take 40.
+// lanes: results are written from the registers.  2^18 rows of 64, 256 columns, 152 MB in three sets of buffers in turn: 44 us (3.4 TB/s);
+// gated by ReLU 48, by SiLU 50, by GELU, whose erfc is a function's length, 105; of 128 integers by SiLU 75, of 256 101.  (The gated block of
+// bf16 values that is one kernel does as many SiLUs and both products in 36, and writes a quarter of the bytes.)
 template <class T, bool GATE_, int STEPS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(GATE_ && STEPS > 1 ? 2 : 3))) void short_rows_kernel(const Int8Product p, uint32_t groups)
 {

@@ -7,14 +7,16 @@
 // Nothing is sorted but a few.  The end of a prefix is looked for in a histogram of the energies' order keys over the range in question,
 // count and weight of every bin, then in the bin where it lies, until that holds so few candidates that they can be put in order, or equal
 // ones alone, which are counted by index.  (Keys are close to logarithms of energies, so a range over both signs, or one outlier, leaves
-// most candidates in a few bins: a second histogram is what that costs.)  Weights are 64-bit floating point, and in histograms whole
-// multiples of 2^-60, held as two numbers of thirty bits, whose sums do not depend on the order in which the atomics come.
+// most candidates in a few bins: a second histogram is what that costs.)  Weights are 64-bit floating point, and in histograms, which find the
+// ends of shares, whole multiples of 2^-60 (of a largest weight of 1; rounded down), held as two numbers of thirty bits, whose sums do not
+// depend on the order in which the atomics come.
 //
 // Segments of up to 16 384 candidates: a block each, keys in registers, one launch.  Longer ones: blocks by the piece, a launch for each
 // time that all of a segment has to be known (range, histogram, histogram, candidates at the ends, ends, sums, draws; where few are kept,
 // range, histogram, list, draws).  Short ones are bound by a block's chain of phases between barriers (6400 candidates, k = 64, all
-// limits: 9.8 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 83 us in four launches, one
-// reading of the 84 MB is 16.5; 16 of 2^20 by share alone: 180 us in nine).
+// limits: 10 us), long ones by the passes over their candidates (64 segments of 2^18, k = 4096, all three limits: 83 us in four launches, one
+// reading of the 84 MB is 16.5; 16 of 2^20 by share alone: 179 us in nine, of which the first histogram, an exponential and three LDS atomics a
+// candidate, takes 49; 122 of 92 987, k = 4345 and a share 297 in eleven; 16 of 2^20 without limits 66 in four, the sums 41 of them).
 #include "activations.h"
 #include "lanes.h"
 
@@ -1052,7 +1054,6 @@ struct Stream {
     static constexpr bool FITS = false;
     const Draws &a;
     uint64_t segment;
-    Bounds *of_waves;
     template <class F>
     __device__ __forceinline__ void each(F &&f) const { each_of_piece(a, segment, 0, a.n, f); }
     // by index, a block's threads at a time
@@ -1108,7 +1109,7 @@ __global__ __launch_bounds__(LONG_THREADS) void ends_kernel(const Long p)
     const bool limited = by_count(p, number);
     const double best = (double)energy_of(of.least);
     const auto weight = [&](uint32_t key) { return weight_of(key, best, p.a.per_temperature); };
-    const Stream stream = {p.a, segment, of_waves};
+    const Stream stream = {p.a, segment};
     const Segment &ranges = p.segment[p.segments + segment];
     const Scale scale(p.a, of.least, of.most);
 
@@ -1593,7 +1594,7 @@ __global__ __launch_bounds__(LONG_THREADS) void few_draws_kernel(const Few p)
     const uint32_t need = of.need, at_end = of.at_end, below = of.before;
     const double best = (double)energy_of(of.least);
     const auto weight = [&](uint32_t key) { return weight_of(key, best, a.per_temperature); };
-    const Stream stream = {a, segment, l.of_waves};
+    const Stream stream = {a, segment};
 
     // the k least
     const u64 *list = p.at + segment * FEW;
@@ -1621,7 +1622,9 @@ __global__ __launch_bounds__(LONG_THREADS) void few_draws_kernel(const Few p)
             const uint64_t from = l.which_piece * p.piece;
             const uint32_t index = stream.nth_from(from, min(a.n, from + p.piece), b.least, l.left_there);
             if (threadIdx.x == 0) s.cut = {b.least, index};
-        } else { // so many next to each other, or one candidate far below all others
+        } else {
+            // so many next to each other, or one candidate so far below all others that these share a bin: this block goes over the segment again
+            // (64 segments of 2^18, k = 4096, with such a candidate in each: 333 us, 84 without; one of 2^24 10.9 ms, 83 us without)
             find_cut<LONG_THREADS>(s, l.bins, {of.least, of.most, of.number, 0, {0, 0}}, {false, need, {0.0, 0.0}}, false, stream, weight);
         }
     }
