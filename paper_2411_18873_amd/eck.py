@@ -766,7 +766,8 @@ def _scales(t, name, n):
 
 
 def quantise_rows(x, q, scale, order=ROWS):
-    """q [n][width] (int8) and scale [n]: rows of x [n][width] (ROWS), or its first n columns [width][n or more] (COLUMNS), by their largest"""
+    """q [n][width] (int8) and scale [n]: rows of x [n][width] (ROWS), or its first n columns [width][n or more] (COLUMNS), by their largest.
+    A row of q ends with a whole sixteen in memory: up to fifteen bytes behind the width belong to it, and become zeros"""
     shape, dtype = q.shape, x.dtype
     n, width = shape
     if order != COLUMNS:
@@ -790,7 +791,8 @@ def product_int8_workspace_bytes(n, n_in, n_out, act=ACT_NONE):
 
 
 def product_int8(x, x_scale, w, w_scale, y, ws, act=ACT_NONE):
-    """y [n][n_out] = x w^T times both scales, of int8 matrices [n][n_in] and [n_out][n_in]; with an activation, a(g) u of w [2 n_out][n_in]"""
+    """y [n][n_out] = x w^T times both scales, of int8 matrices [n][n_in] and [n_out][n_in]; with an activation, a(g) u of w [2 n_out][n_in].
+    Up to fifteen bytes behind the width of x and w, to the next sixteen, are read too, and have to be zeros in one of them"""
     shape, dtype = x.shape, y.dtype
     n, n_in = shape
     n_out = y.shape[1]

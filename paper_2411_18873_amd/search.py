@@ -12,7 +12,8 @@ eck_k_count, eck_k_step).  What stays on the host is what the paper does on the 
 Both cost models are boosted trees, the paper's model form (Sec. 5.4).  The energy model is refitted every round
 on all kernels measured so far, labels normalised by the largest energy measured so far; the latency model
 is fitted once on the initial sample (the paper takes it from its host framework) and then left alone.  A round
-whose round(k * M) is 0 measures nothing, leaves the model and k alone and still picks parents.
+whose round(k * M) is 0 measures nothing, leaves the model and k alone and still picks parents.  n_parents belongs to the
+options below; left out, or with parents="model", it is half of M as well.
 
 Options that depart from the printed algorithm (off by default): parents="measured" lets the n_parents measured
 kernels of least measured energy over the whole record reproduce; parents="sampled" draws parents among the M fastest
