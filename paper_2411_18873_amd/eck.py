@@ -735,9 +735,14 @@ def _here_rows(t, name, dtype, shape):
 
 def _ws_here(ws):
     """_ws, of the current device"""
-    if ws is not None and ws.is_cuda and ws.get_device() != _device():
+    if ws is None:
+        return None, 0
+    device = ws.get_device()
+    if device < 0 or not ws.is_contiguous():
+        raise TypeError("ws must be a contiguous CUDA tensor")
+    if device != _device():
         raise ValueError("ws must be on the current device")
-    return _ws(ws)
+    return ws.data_ptr(), ws.nbytes
 
 
 def int8_rows(n, width):
@@ -905,7 +910,8 @@ def adamw_step(parameters, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scal
     """step number `step` (+ *step_more, an int32 tensor) over all of a Parameters; gradients times *grad_scale; seed: of 8-bit states' roundings"""
     if not 0 <= step < 1 << 32:
         raise ValueError("step must be a whole number of 32 bits")
-    parameters.check_device()
+    if parameters.device != _device():
+        parameters.check_device()
     _check("adamw_step", lib().adamw_step(parameters._array, parameters.count, parameters.state, lr, beta1, beta2, eps, step,
                                           _one(step_more, torch.int32, "step_more"), _one(grad_scale, torch.float32, "grad_scale"), seed, _stream()))
 
@@ -916,7 +922,8 @@ def gradients_norm_workspace_bytes(parameters):
 
 def gradients_norm(parameters, norm_out, scale_out, ws, max_norm=float("inf")):
     """norm_out = the norm of all gradients, scale_out = what brings it to max_norm or less (one of them may be None)"""
-    parameters.check_device()
+    if parameters.device != _device():
+        parameters.check_device()
     ws_ptr, ws_bytes = _ws_here(ws)
     _check("gradients_norm", lib().gradients_norm(parameters._array, parameters.count, max_norm, _one(norm_out, torch.float32, "norm_out"),
                                                   _one(scale_out, torch.float32, "scale_out"), ws_ptr, ws_bytes, _stream()))
