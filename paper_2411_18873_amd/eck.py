@@ -872,8 +872,8 @@ class Parameters:
             raise ValueError("parameters must be on the current device")
 
     def set_grads(self, grads):
-        """other gradients of the same sizes and device, float32 or bfloat16, in memory that a step does not write (or, element for element, a tensor that it
-        writes of the same parameter: a thread reads its elements before it writes them)"""
+        """other gradients of the same sizes and device, float32 or bfloat16, in memory that a step does not write (or, element for element, where
+        a tensor lies that it writes of the same parameter: a thread reads its elements before it writes them)"""
         if len(grads) != self.count:
             raise ValueError("there must be %d gradients" % self.count)
         self.check_device()

@@ -101,7 +101,8 @@ class GatedModel:
         if train:
             kept["in"] = s
         x = x.bfloat16()
-        need = max(eck.gatedffn_forward_workspace_bytes(n, f, self.hidden, f, eck.BF16), eck.gatedffn_forward_workspace_bytes(n, f, self.head, 1, eck.F32))
+        need = max(eck.gatedffn_forward_workspace_bytes(n, f, self.hidden, f, eck.BF16),
+                   eck.gatedffn_forward_workspace_bytes(n, f, self.head, 1, eck.F32))
         if int8:
             need = max(need, eck.product_int8_workspace_bytes(n, f, self.hidden, eck.ACT_SILU), eck.product_int8_workspace_bytes(n, self.hidden, f))
         ws = self._ws(need)
